@@ -54,6 +54,8 @@ typedef enum tq_result {
 #define TQ_STATUS_BAD_LEN 4    /* seq_lens[b] outside [0, S_cap]; treated as clamped to that range */
 #define TQ_STATUS_TIMEOUT 8    /* a bounded wait for an asynchronous copy ran out; that call's results are not valid */
 #define TQ_STATUS_BAD_PAGE 16  /* a page-table entry outside [0, num_pages) was met */
+#define TQ_STATUS_POOL_EMPTY 32 /* tq_pages_assign: too few free pages; that sequence was refused */
+#define TQ_STATUS_BAD_SLOT 64   /* tq_kv8_append, tq_kv8_gather: a slot outside the cache or out of order; that row was skipped */
 
 #define TQ_GROUP 32         /* quantisation group size g (fixed) */
 #define TQ_SPLIT_QUANTUM 16 /* split boundaries fall on multiples of this many tokens */
@@ -387,6 +389,155 @@ int tq_sdpa_mixed_precision_attend(const tq_kv_cache* cache /* host */, const vo
 #define TQ_STATIC_SCRATCH_BYTES (8u << 20)
 int tq_sdpa_int4_attend_static(const tq_kv_cache* cache /* host */, const void* q, int32_t H_q, float attn_scale,
                                void* out, int32_t out_is_fp32, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Serving ragged batches: pages and slots on the device, a cache in 8 bits, attention over it and over whole prompts.
+ * The paper stops at one sequence and a 4-bit cache; these entry points are what a server needs around them:
+ *   tq_pages_release, tq_pages_assign   once per step, for all layers: pages, lengths, packed offsets and slots
+ *   tq_sdpa_prompt                      per layer: attention of the prompts' own tokens
+ *   tq_kv8_append                       per layer: the new tokens into the 8-bit cache, through the slots
+ *   tq_sdpa_int8_decode                 per layer: one query token per sequence over that cache
+ *   tq_kv8_gather                       cached tokens back as 16-bit values (the past of a chunked prompt)
+ * All rules at the top of this file hold.  Unlike the paper's kernels these take fp16 and bf16.
+ */
+typedef enum tq_dtype { TQ_FP16 = 0, TQ_FP32 = 1, TQ_BF16 = 2 } tq_dtype;
+
+/*
+ * Pages of finished sequences go back to the pool.  free_pages[0 .. *free_count) is a stack of the pool's unused pages
+ * (device memory with room for num_pages entries, all of them distinct and in [0, num_pages)); the pages of every
+ * sequence with finished[b] != 0 -- ceil(seq_lens[b] / page_tokens) entries of its row -- are pushed onto it, sequences
+ * and pages in ascending order, and its length becomes 0.
+ *   page_table     : device [B][max_pages] int32, read (rows of finished sequences are left as they are); NULL for a
+ *                    contiguous cache: only the lengths change, the pool's arguments are ignored
+ *   seq_lens       : device [B] int32;  seq_lens_out [B] the lengths after it (may be the same array)
+ *   finished       : device [B] bytes
+ *   free_count     : device int32;  free_count_out: the stack's size after it (may be the same)
+ * More pages than the pool can hold (a page that was free already) set TQ_STATUS_BAD_PAGE and release nothing;
+ * a table entry outside the pool sets it too.  A length outside [0, max_pages * page_tokens] sets TQ_STATUS_BAD_LEN
+ * and is clamped.  Requirements: B in 1..65535, page_tokens a power of two of at least 16 (contiguous: a multiple of
+ * 16), max_pages >= 1, page_tokens * max_pages < 2^31, num_pages >= 1.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_CUDA.
+ */
+int tq_pages_release(const int32_t* page_table, const int32_t* seq_lens, const uint8_t* finished, int32_t B,
+                     int32_t page_tokens, int32_t max_pages, int32_t num_pages, int32_t* free_pages,
+                     const int32_t* free_count, int32_t* seq_lens_out, int32_t* free_count_out, int32_t* status,
+                     void* stream);
+
+/*
+ * Room for new_lens[b] more tokens of every sequence (0: none; a prompt, a chunk of one, or 1 for a decode step): fresh
+ * pages come off the stack in sequence order -- the i-th fresh page of the call is free_pages[*free_count - 1 - i] --
+ * and are entered into page_table.  The new tokens are packed: sequence b owns the rows token_offsets[b] ..
+ * token_offsets[b + 1] - 1 of the step's q, k and v, and row n goes to slots[n] of every layer's cache.
+ *   slots          : device [n_slots] int64, n_slots >= the number of new tokens; rows behind the last token get -1.
+ *                    A slot is page * page_tokens + position in the page; without a page table it is
+ *                    b * page_tokens * max_pages + position.
+ *   token_offsets  : device [B + 1] int32, the sums of new_lens
+ *   seq_lens_out, free_count_out : as in tq_pages_release
+ *   free_pages     : read only
+ *   workspace      : tq_pages_workspace_bytes(B) bytes, 16-byte aligned, contents destroyed
+ * A sequence is refused -- length and pages stay, the slots of its rows are -1 -- if it would not fit its table
+ * (TQ_STATUS_CACHE_FULL), if the pages wanted by it and the sequences before it exceed the stack
+ * (TQ_STATUS_POOL_EMPTY), if its rows do not fit n_slots or a length is out of range (TQ_STATUS_BAD_LEN).  A sequence
+ * that needs no fresh page is never refused for the pool's sake.  An entry of the stack or of the table outside
+ * the pool sets TQ_STATUS_BAD_PAGE and its tokens get slot -1.  Requirements as tq_pages_release; n_slots in 1..2^31 - 1.
+ */
+size_t tq_pages_workspace_bytes(int32_t B);
+int tq_pages_assign(int32_t* page_table, const int32_t* seq_lens, const int32_t* new_lens, int32_t B, int32_t page_tokens,
+                    int32_t max_pages, int32_t num_pages, const int32_t* free_pages, const int32_t* free_count,
+                    int32_t* seq_lens_out, int32_t* free_count_out, int32_t* token_offsets, int64_t* slots,
+                    int64_t n_slots, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * The 8-bit KV cache of ONE layer: the fields of tq_kv_cache (contiguous or paged alike) over blocks of
+ * TQ_BLOCK8_BYTES(d) = 32 d + 16 bytes (4112 at d = 128).  A block holds 16 tokens of one KV head with one range for its
+ * K and one for its V:
+ *     range a = max |x| over the tokens appended so far (fp32),  code = round_half_even(127 x / a),  x^ = code * a / 127
+ * (all codes 0 where a = 0).  When an appended token raises the range, the block's older codes c become
+ * round_half_even(c * a_old / a_new).  Every code is the exact rounding of the true quotient.  A NaN is stored as 0,
+ * an infinity as the largest finite value of its type.  Layout of a block:
+ *     K codes | V codes | K range (fp32) | V range (fp32) | 8 bytes unused
+ *   a code is stored as code + 128 in one byte; (token t, channel c) at
+ *     K: 512 (c / 32) + 64 (t % 8) + 16 (c % 32 / 8) + 8 (t / 8) + c % 8
+ *     V: 512 (c / 32) + 64 (c % 8) + 16 (t % 8 / 2) + 4 (c % 32 / 8) + 2 (t / 8) + t % 2   (after the K codes)
+ *   -- the operand order of the decode kernel's matrix instructions.  tq_cache8_code_offset addresses single codes.
+ * 2.5 % more than half the bytes of an fp16 cache, 1.6 times those of the 4-bit one.
+ * Rows of a block behind the last token, and of blocks that no token was appended to, are unspecified.
+ */
+#define TQ_BLOCK8_BYTES(d) (32 * (d) + 16)
+typedef struct tq_kv8_cache {
+  uint8_t* blocks;    /* [B][H_kv][S_cap/16][TQ_BLOCK8_BYTES(d)]; with paging [num_pages][H_kv][page_tokens/16][...] */
+  int32_t* seq_lens;  /* [B]; read by tq_sdpa_int8_decode, not advanced by tq_kv8_append (tq_pages_assign does that) */
+  int32_t B, H_kv, S_cap, d;
+  const int32_t* page_table;
+  int32_t page_tokens, max_pages, num_pages;
+} tq_kv8_cache;
+/* Byte offset inside a block of the code of token t (0 .. 15), channel c; which = 0 for K, 1 for V. */
+size_t tq_cache8_code_offset(int32_t d, int32_t which, int32_t t, int32_t c);
+size_t tq_cache8_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d);
+
+/*
+ * Append n packed tokens through their slots.
+ *   k_new, v_new : device, fp16 or bf16 (dtype): row i, KV head h at i * stride + h * d elements, e.g. slices of a fused
+ *                  projection's output [n][H_q + 2 H_kv][d] (stride (H_q + 2 H_kv) d); strides multiples of 8 elements
+ *                  and at least H_kv * d
+ *   slots        : device [n] int64, one per row, as tq_pages_assign writes them: the rows of a block stand together in
+ *                  ascending order without gaps; -1 skips a row.  The tokens of a block before the first one appended are taken
+ *                  as present.  A slot outside the cache, or a row that is out of order inside its block, sets TQ_STATUS_BAD_SLOT and
+ *                  is skipped with the rest of its run.  A block that is met in two places of one call is the caller's mistake: its contents
+ *                  are then unspecified (nothing outside it is touched).
+ * seq_lens is not read.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (cache requirements as tq_kv_cache, n < 1, strides, dtype
+ * TQ_FP32), TQ_ERR_ALIGN, TQ_ERR_CUDA.
+ */
+int tq_kv8_append(const tq_kv8_cache* cache /* host */, const void* k_new, const void* v_new, int32_t dtype,
+                  int64_t k_stride, int64_t v_stride, const int64_t* slots, int64_t n, int32_t* status, void* stream);
+
+/*
+ * Values of n slots, in any order and as often as asked: k_out, v_out device [n][H_kv][d] of dtype (fp16, bf16 or
+ * fp32).  Rows of negative slots are zero; a slot beyond the cache sets TQ_STATUS_BAD_SLOT and its rows are zero.
+ */
+int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, int64_t n, void* k_out, void* v_out,
+                  int32_t dtype, int32_t* status, void* stream);
+
+/*
+ * softmax(attn_scale q . K^T) V over the 8-bit cache in one launch: query token b attends the cached tokens
+ * [max(0, seq_lens[b] - window), seq_lens[b]) of its sequence (window = 0: all of them).
+ *   q            : device, fp16 or bf16 (q_dtype): sequence b, head h at b * q_stride + h * d elements (q_stride a
+ *                  multiple of 8, at least H_q * d)
+ *   max_seq_len  : 0, or an upper bound on the lengths that the host knows; it only limits the launch
+ *   workspace    : tq_int8_workspace_bytes(B, H_kv, H_q, d) bytes, 16-byte aligned: counters, then the partial results
+ *                  of sequences that several thread blocks share.  ZERO the first tq_int8_counter_bytes(B, H_kv, H_q)
+ *                  bytes once before the first use; every call leaves them zero.  Calls that may overlap on the GPU
+ *                  (other streams, graphs replayed side by side) need workspaces of their own.
+ *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype)
+ * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,
+ * TQ_STATUS_BAD_PAGE, TQ_STATUS_TIMEOUT (zero the counters again after it).
+ */
+size_t tq_int8_counter_bytes(int32_t B, int32_t H_kv, int32_t H_q);
+size_t tq_int8_workspace_bytes(int32_t B, int32_t H_kv, int32_t H_q, int32_t d);
+int tq_sdpa_int8_decode(const tq_kv8_cache* cache /* host */, const void* q, int32_t q_dtype, int64_t q_stride, int32_t H_q,
+                        float attn_scale, int32_t window, int32_t max_seq_len, void* workspace, size_t workspace_bytes,
+                        void* out, int32_t out_dtype, int32_t* status, void* stream);
+
+/*
+ * Attention of whole prompts: packed sequences, grouped heads.  Sequence b has the query rows q_offsets[b] ..
+ * q_offsets[b + 1] - 1 and the key rows kv_offsets[b] .. kv_offsets[b + 1] - 1.  With lq queries and lk keys, query i
+ * (0 = oldest) attends, for causal = 1, the keys j <= i + lk - lq -- the queries are the newest lq of the lk tokens --
+ * and with window > 0 of those only j > i + lk - lq - window; for causal = 0 all lk keys.  A query that attends
+ * nothing gives zeros.
+ *   q, k, v      : device, fp16 or bf16 (dtype): row i, head h at i * stride + h * d elements (slices of a fused
+ *                  projection's output are fine); strides multiples of 8 elements and at least heads * d
+ *   n_q, n_kv    : rows of q and of k, v; offsets are clamped to them (TQ_STATUS_BAD_LEN)
+ *   q_offsets, kv_offsets : device [B + 1] int32, ascending; the same array where the keys are the queries' own tokens
+ *   out          : device [n_q][H_q][d], of dtype or fp32 (out_dtype).  Rows of no sequence are left as they were.
+ * d in {64, 128, 256, 512}; H_q a multiple of H_kv, H_q / H_kv <= 64; causal = 0 with a window is TQ_ERR_SHAPE.
+ * A NaN or an infinity in k or v reaches only the queries that attend its token.
+ * Status: TQ_STATUS_BAD_LEN, TQ_STATUS_EMPTY_SEQ (queries of a sequence without keys), TQ_STATUS_TIMEOUT.
+ */
+int tq_sdpa_prompt(const void* q, const void* k, const void* v, int32_t dtype, int64_t q_stride, int64_t k_stride,
+                   int64_t v_stride, int32_t n_q, int32_t n_kv, const int32_t* q_offsets, const int32_t* kv_offsets,
+                   int32_t B, int32_t H_q, int32_t H_kv, int32_t d, float attn_scale, int32_t causal, int32_t window,
+                   void* out, int32_t out_dtype, int32_t* status, void* stream);
 
 /* Bytes of one layer's cache arrays (packed + scales + zeros, K and V), i.e. Eq. 1 with the int4 format. */
 size_t tq_cache_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d);

@@ -11,6 +11,8 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -42,8 +44,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-I", INCLUDE, "-I", CSRC, "-o", LIB] + sources()
-    subprocess.run(cmd, check=True)
+    extra = ["-Xptxas", "-v"] if verbose else []
+    with tempfile.TemporaryDirectory() as tmp:  # one nvcc per source file, side by side
+        def compile_one(src):
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            subprocess.run([nvcc] + NVCC_FLAGS[:-3] + extra + ["-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj], check=True)
+            return obj
+
+        with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as pool:
+            objects = list(pool.map(compile_one, sources()))
+        subprocess.run([nvcc] + NVCC_FLAGS + ["-o", LIB] + objects, check=True)
     return LIB
 
 

@@ -1,0 +1,604 @@
+// Decode attention over the 8-bit cache: one query token per sequence, softmax(alpha q . K^T) V over its cached tokens
+// (or the last `window` of them), in one launch.
+//
+//   Scores:  alpha q . k^ = (alpha a_K / 127) sum_c q_c code_c -- the range of a block is one number per KV head and 16
+//            tokens, so it multiplies the fp32 accumulator and the tensor cores see exact integer codes in fp16.
+//   Output:  o = sum_j 2^(s_j) a_V(j) code_j / (127 sum_j 2^(s_j)).  The weight that enters the second MMA in fp16 is
+//            w_j = 2^(s_j + log2 a_V(j) - M'), with M' the running maximum of the whole exponent: a block whose values
+//            are small is weighed against the largest contribution, not against the largest score, so its rounding
+//            (2^-11 relative) never exceeds what it contributes.  The denominator has a maximum M of its own, and the
+//            factor 2^(M' - M) joins them at the end.
+//   Both maxima are raised only when a score exceeds them by more than 2^8 (weights stay below 256).
+//
+// What bounds it: HBM.  2 d + 0.5 bytes per token and KV head; per 16-token block a warp issues 2 x d / 16 MMAs, 3 d / 8
+// integer and half-precision instructions that widen the codes, and 8 exponentials per lane (2 per score): a quarter
+// of what an SM could do in the time that the block takes to arrive.
+//
+// Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
+// block i of N takes the blocks [i W / N, (i + 1) W / N) of the W in all, whatever the lengths: ragged batches load
+// every SM alike, one short sequence still spreads.  A unit that lies in one thread block is finished there; the parts
+// of a cut one go to the workspace (at most two per thread block), and the last to arrive (a counter per unit) joins
+// them.  A thread block is 16 warps (8 and 4 at d = 256 and 512: registers); each warp owns a ring of three to six
+// stages of one 16-token block each, filled by one bulk copy per block (K codes, V codes and ranges are contiguous) --
+// 200 KB in flight per SM, no barrier in the main loop, and the copies run on into the thread block's next unit.
+#include "tq_async.cuh"
+#include "tq_kv8.cuh"
+
+namespace tq {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoMax = -1.0e30f;
+constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running maxima
+
+template <int D>
+struct Cfg {
+  static constexpr int NW = D <= 128 ? 16 : (D == 256 ? 8 : 4);  // warps
+  static constexpr int NST = D == 64 ? 6 : 3;                    // stages of a warp's ring
+  static constexpr int STAGE = block8_bytes(D);
+  static constexpr int THREADS = 32 * NW;
+  static constexpr int RING = NW * NST * STAGE;
+  // the merge arrays lie behind the rings (copies for the next unit are in flight while a unit is merged); the outputs
+  // of the warps go through them MQ query heads at a time
+  static constexpr int ROW = D + 4;  // floats of one query's row: 8 rows x 2 words apart hit different banks
+  static constexpr int MQ = 2;
+  static constexpr int MERGE = NW * MQ * ROW * 4;
+  static constexpr int STATS = RING + MERGE;             // [NW][8] x {M, M', l} and the factors of them
+  static constexpr int BARS = STATS + NW * 8 * 3 * 4 + 8 * 4 * 4;
+  static constexpr int QS = BARS + NW * NST * 8;         // d = 512: the query's B fragments, 8 bytes per lane and step
+  static constexpr int QBYTES = D == 512 ? (D / 16) * 32 * 8 : 0;
+  static constexpr int SMEM = QS + QBYTES;
+  static_assert(BARS % 8 == 0 && QS % 8 == 0 && STAGE % 16 == 0 && SMEM <= 232448, "shared memory");
+};
+
+struct Args {
+  tq_kv8_cache c;
+  const uint16_t* q;
+  long long q_stride;
+  int H_q, G, tiles, window;
+  float scale_log2;  // alpha * log2(e) / 127
+  int units;         // H_kv * tiles
+  int grid;          // thread blocks launched
+  int min_blocks;    // fewest cache blocks worth a thread block
+  int32_t* counters;
+  float* parts;      // [2 grid][8][D + 2]
+  void* out;
+  int32_t* status;
+};
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+// stored bytes (code + 128) of a word -> two words of exact fp16 codes
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const __half2 bias = __half2half2(__ushort_as_half(0x6480));  // 1152
+  uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+  const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+
+// Tokens [lo, hi) that a sequence attends.
+struct Span {
+  int lo, hi;
+  __device__ int first() const { return lo >> 4; }
+  __device__ int blocks() const { return hi > lo ? ((hi + 15) >> 4) - (lo >> 4) : 0; }
+};
+__device__ __forceinline__ Span span_of(const Args& a, int b) {
+  int len = a.c.seq_lens[b];
+  len = len < 0 ? 0 : (len > a.c.S_cap ? a.c.S_cap : len);
+  return {window_begin(len, a.window), len};
+}
+
+// A walk over a thread block's share of the line: units, and in a unit the blocks [j0, j1).
+struct Walk {
+  long long g, g1;  // position on the line and end of the share
+  int b, u;         // sequence, unit in it
+  int j0, j1, n;    // blocks of this visit, blocks of the unit
+  Span span;
+  __device__ void open(const Args& a, int j) {
+    span = span_of(a, b);
+    n = span.blocks();
+    j0 = j;
+    const long long left = g1 - g;
+    j1 = n - j0 < left ? n : j0 + static_cast<int>(left);
+  }
+  __device__ bool next(const Args& a) {
+    g += j1 - j0;
+    if (g >= g1) return false;
+    if (++u == a.units) {
+      u = 0;
+      do {
+        if (++b >= a.c.B) {  // lengths that change while the kernel runs break the caller's promise: stop
+          g = g1;
+          return false;
+        }
+      } while (span_of(a, b).blocks() == 0);
+    }
+    open(a, 0);
+    return true;
+  }
+};
+
+__device__ __forceinline__ const uint8_t* block_at(const Args& a, int b, int h, int j) {
+  if (a.c.page_table == nullptr)
+    return a.c.blocks + ((static_cast<long long>(b) * a.c.H_kv + h) * (a.c.S_cap >> 4) + j) * block8_bytes(a.c.d);
+  const int shift = __ffs(a.c.page_tokens) - 5;  // log2 of the blocks of a page
+  int p = a.c.page_table[static_cast<long long>(b) * a.c.max_pages + (j >> shift)];
+  if (p < 0 || p >= a.c.num_pages) {
+    if (a.status) atomicOr(a.status, TQ_STATUS_BAD_PAGE);
+    p = 0;
+  }
+  return a.c.blocks + (((static_cast<long long>(p) * a.c.H_kv + h) << shift) + (j & ((1 << shift) - 1))) * block8_bytes(a.c.d);
+}
+
+template <int OT>
+__device__ __forceinline__ void store_out(void* out, long long at, float x) {
+  if (OT == TQ_FP32) static_cast<float*>(out)[at] = x;
+  else if (OT == TQ_BF16) static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(x);
+  else static_cast<__half*>(out)[at] = __float2half_rn(x);
+}
+
+// position of thread block i's share on the line
+__device__ __forceinline__ long long share(long long W, int N, int i) { return W * i / N; }
+__device__ __forceinline__ int owner(long long W, int N, long long g) {
+  int i = static_cast<int>(g * N / W);
+  while (i + 1 < N && share(W, N, i + 1) <= g) ++i;
+  while (i > 0 && share(W, N, i) > g) --i;
+  return i;
+}
+
+template <int D, int QT, int OT>
+__global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args a) {
+  using C = Cfg<D>;
+  constexpr int KK = D / 32;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ long long s_start;
+  __shared__ int s_b, s_warp[C::NW], s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int gid = lane >> 2, t4 = lane & 3;
+  float* const merge = reinterpret_cast<float*>(smem + C::RING);
+  float* const stats = reinterpret_cast<float*>(smem + C::STATS);  // [3][NW][8]
+  float* const sums = stats + 3 * C::NW * 8;                       // [8] x {M, M', l, factor}
+  uint32_t ring, bars;
+  {
+    uint32_t base;
+    asm("{ .reg .u64 p; cvta.to.shared.u64 p, %1; cvt.u32.u64 %0, p; }\n" : "=r"(base) : "l"(smem));
+    ring = base + warp * C::NST * C::STAGE;
+    bars = base + C::BARS + warp * C::NST * 8;
+  }
+  if (lane == 0) {
+    for (int s = 0; s < C::NST; ++s) mbar_init(bars + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  pdl_launch_dependents();
+  pdl_wait();
+
+  // ---- where this thread block's share starts: blocks of all sequences, then the sequence that holds the start
+  auto scan = [&](int v, int& before) {  // inclusive sum over the threads; returns it, `before` = the sum of all
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int add = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < C::NW; ++w) {
+      const int y = s_warp[w];
+      if (w < warp) add += y;
+      all += y;
+    }
+    __syncthreads();
+    before = all;
+    return x + add;
+  };
+  long long W = 0;
+  for (int base = 0; base < a.c.B; base += C::THREADS) {
+    const int b = base + tid;
+    int n = 0;
+    if (b < a.c.B) {
+      n = span_of(a, b).blocks();
+      const int len = a.c.seq_lens[b];
+      if (blockIdx.x == 0 && a.status && (len <= 0 || len > a.c.S_cap))
+        atomicOr(a.status, (len < 0 || len > a.c.S_cap ? TQ_STATUS_BAD_LEN : 0) | (len <= 0 ? TQ_STATUS_EMPTY_SEQ : 0));
+    }
+    int all;
+    scan(n, all);
+    W += all;
+  }
+  W *= a.units;
+  const long long worth = (W + a.min_blocks - 1) / a.min_blocks;
+  const int N = static_cast<int>(worth < 1 ? 1 : (worth < a.grid ? worth : a.grid));
+
+  // sequences without a token: their rows are zero
+  for (int b = blockIdx.x; b < a.c.B; b += gridDim.x)
+    if (span_of(a, b).blocks() == 0)
+      for (int i = tid; i < a.H_q * D; i += C::THREADS) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
+  if (static_cast<int>(blockIdx.x) >= N || W == 0) return;
+
+  const long long g0 = share(W, N, blockIdx.x);
+  {
+    long long carry = 0;
+    for (int base = 0; base < a.c.B; base += C::THREADS) {
+      const int b = base + tid;
+      const int n = b < a.c.B ? span_of(a, b).blocks() : 0;
+      int all;
+      const long long upto = (carry + scan(n, all)) * a.units;
+      if (n > 0 && upto > g0 && upto - static_cast<long long>(n) * a.units <= g0) {
+        s_b = b;
+        s_start = upto - static_cast<long long>(n) * a.units;
+      }
+      carry += all;
+    }
+    __syncthreads();
+  }
+  Walk use;
+  use.g = g0;
+  use.g1 = share(W, N, blockIdx.x + 1);
+  use.b = s_b;
+  {
+    const int n = span_of(a, use.b).blocks();
+    const long long r = g0 - s_start;
+    use.u = static_cast<int>(r / n);
+    use.open(a, static_cast<int>(r % n));
+  }
+
+  // ---- the ring: lane 0 runs ahead of the arithmetic with a walk of its own
+  Walk ahead = use;
+  int ja = ahead.j0 + warp;
+  bool more = true;
+  auto settle = [&]() {  // the warp's next block may lie in a later unit
+    while (more && ja >= ahead.j1) {
+      more = ahead.next(a);
+      ja = ahead.j0 + warp;
+    }
+  };
+  auto fetch = [&](int s) {
+    settle();
+    if (!more) return;
+    const uint8_t* src = block_at(a, ahead.b, ahead.u / a.tiles, ahead.span.first() + ja);
+    mbar_expect_tx(bars + 8 * s, C::STAGE);
+    bulk_g2s(ring + s * C::STAGE, src, C::STAGE, bars + 8 * s);
+    ja += C::NW;
+  };
+  if (lane == 0)
+    for (int s = 0; s < C::NST; ++s) fetch(s);
+
+  int stage = 0;
+  uint32_t phase = 0;
+  bool dead = false;
+
+  for (bool go = true; go; go = use.next(a)) {
+    const int h = use.u / a.tiles, tile = use.u - h * a.tiles;
+    const int head0 = h * a.G + tile * 8;
+    const int heads = a.G - tile * 8 < 8 ? a.G - tile * 8 : 8;
+
+    // ---- B fragments of the scores: query gid, channels 32 kk + 8 t4 .. + 7 (both k = 16 steps).  bf16 queries are
+    // scaled by a power of two per query into the range of fp16: exact down to 2^-28 of the query's largest value.
+    uint32_t qf[D == 512 ? 1 : KK][4];
+    float back = 1.0f;  // undoes that scale
+    {
+      const bool real = gid < heads;
+      const uint16_t* src = a.q + static_cast<long long>(use.b) * a.q_stride + static_cast<long long>(head0 + gid) * D + 8 * t4;
+      float mul = 1.0f;
+      if (QT == TQ_BF16) {
+        float top = 0.0f;
+        for (int kk = 0; kk < KK; ++kk) {
+          const uint4 x = real ? __ldg(reinterpret_cast<const uint4*>(src + 32 * kk)) : make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = unpack2<QT>(w[e]);
+            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;  // exponent; 128: infinite
+        if (top > 0.0f && e < 128) {
+          int by = 13 - e;
+          by = by > 126 ? 126 : by;
+          mul = __uint_as_float(static_cast<uint32_t>(127 + by) << 23);
+          back = __uint_as_float(static_cast<uint32_t>(127 - by) << 23);
+        }
+      }
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint4 x = real ? __ldg(reinterpret_cast<const uint4*>(src + 32 * kk)) : make_uint4(0, 0, 0, 0);
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        if (QT == TQ_BF16) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = unpack2<QT>(w[e]);
+            w[e] = pack2<TQ_FP16>(f.x * mul, f.y * mul);
+          }
+        }
+        if (D == 512) {
+          uint2* to = reinterpret_cast<uint2*>(smem + C::QS);
+          if (warp == 0) {
+            to[(2 * kk) * 32 + lane] = make_uint2(w[0], w[1]);
+            to[(2 * kk + 1) * 32 + lane] = make_uint2(w[2], w[3]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qf[D == 512 ? 0 : kk][e] = w[e];
+        }
+      }
+      if (D == 512) __syncthreads();
+    }
+    const float back0 = __shfl_sync(0xffffffffu, back, 8 * t4), back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
+
+    float o[2 * KK][4];  // channels 16 m + gid (+ 8), queries 2 t4 (+ 1)
+#pragma unroll
+    for (int m = 0; m < 2 * KK; ++m) o[m][0] = o[m][1] = o[m][2] = o[m][3] = 0.0f;
+    float M0 = kNoMax, M1 = kNoMax, P0 = kNoMax, P1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
+
+    for (int j = use.j0 + warp; j < use.j1; j += C::NW) {
+      const uint32_t bar = bars + 8 * stage;
+      if (!dead && !wait_stage(bar, phase)) {
+        dead = true;
+        if (a.status && lane == 0) atomicOr(a.status, TQ_STATUS_TIMEOUT);
+      }
+      dead = __any_sync(0xffffffffu, dead);
+      if (dead) break;
+      const uint8_t* blk = smem + (warp * C::NST + stage) * C::STAGE;
+      float s[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint4 x = *reinterpret_cast<const uint4*>(blk + 512 * kk + 16 * lane);
+        uint32_t f0[4], f1[4];  // rows gid: words x, y; rows gid + 8: words z, w; x and z are the first k = 16 step
+        widen(x.x, f0[0], f0[2]);
+        widen(x.z, f0[1], f0[3]);
+        widen(x.y, f1[0], f1[2]);
+        widen(x.w, f1[1], f1[3]);
+        if (D == 512) {
+          const uint2* from = reinterpret_cast<const uint2*>(smem + C::QS);
+          const uint2 b0 = from[(2 * kk) * 32 + lane], b1 = from[(2 * kk + 1) * 32 + lane];
+          mma16816(s[0], f0, b0.x, b0.y);
+          mma16816(s[1], f1, b1.x, b1.y);
+        } else {
+          mma16816(s[0], f0, qf[kk][0], qf[kk][1]);
+          mma16816(s[1], f1, qf[kk][2], qf[kk][3]);
+        }
+      }
+      const float2 range = *reinterpret_cast<const float2*>(blk + 32 * D);
+      const float f = range.x * a.scale_log2;
+      const float f0 = f * back0, f1 = f * back1;
+      float s0 = (s[0][0] + s[1][0]) * f0, s1 = (s[0][1] + s[1][1]) * f1;  // token gid
+      float s2 = (s[0][2] + s[1][2]) * f0, s3 = (s[0][3] + s[1][3]) * f1;  // token gid + 8
+      const int tok = (use.span.first() + j) * 16 + gid;
+      if (tok < use.span.lo || tok >= use.span.hi) s0 = s1 = -INFINITY;
+      if (tok + 8 < use.span.lo || tok + 8 >= use.span.hi) s2 = s3 = -INFINITY;
+      float lg;  // log2 of the value range; -inf for a block of zeros
+      asm("lg2.approx.f32 %0, %1;\n" : "=f"(lg) : "f"(range.y));
+      const float b0 = fmaxf(s0, s2), b1 = fmaxf(s1, s3);
+      if (__any_sync(0xffffffffu, b0 > M0 + kSlack || b1 > M1 + kSlack || b0 + lg > P0 + kSlack || b1 + lg > P1 + kSlack)) {
+        float m0 = b0, m1 = b1;
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) {
+          m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
+          m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
+        }
+        const float n0 = fmaxf(M0, m0), n1 = fmaxf(M1, m1), p0 = fmaxf(P0, m0 + lg), p1 = fmaxf(P1, m1 + lg);
+        l0 *= ex2(M0 - n0);
+        l1 *= ex2(M1 - n1);
+        const float c0 = ex2(P0 - p0), c1 = ex2(P1 - p1);
+        M0 = n0;
+        M1 = n1;
+        P0 = p0;
+        P1 = p1;
+#pragma unroll
+        for (int m = 0; m < 2 * KK; ++m) {
+          o[m][0] *= c0;
+          o[m][1] *= c1;
+          o[m][2] *= c0;
+          o[m][3] *= c1;
+        }
+      }
+      l0 += ex2(s0 - M0) + ex2(s2 - M0);
+      l1 += ex2(s1 - M1) + ex2(s3 - M1);
+      const float w0 = lg - P0, w1 = lg - P1;
+      const uint32_t v0 = transpose8x8(pack2<TQ_FP16>(ex2(s0 + w0), ex2(s1 + w1)));  // tokens 2 t4, + 1 of query gid
+      const uint32_t v1 = transpose8x8(pack2<TQ_FP16>(ex2(s2 + w0), ex2(s3 + w1)));  // tokens 2 t4 + 8, + 9
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint4 x = *reinterpret_cast<const uint4*>(blk + 16 * D + 512 * kk + 16 * lane);
+        uint32_t e[4];
+        widen(x.x, e[0], e[2]);
+        widen(x.y, e[1], e[3]);
+        mma16816(o[2 * kk], e, v0, v1);
+        widen(x.z, e[0], e[2]);
+        widen(x.w, e[1], e[3]);
+        mma16816(o[2 * kk + 1], e, v0, v1);
+      }
+      __syncwarp();
+      if (lane == 0) fetch(stage);
+      if (++stage == C::NST) {
+        stage = 0;
+        phase ^= 1;
+      }
+    }
+
+    // ---- join the warps: maxima and sums first, then the outputs, MQ query heads at a time
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, x);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+    }
+    if (gid == 0) {
+      float* st = stats + warp * 8 + 2 * t4;
+      st[0] = M0;
+      st[1] = M1;
+      st[C::NW * 8] = P0;
+      st[C::NW * 8 + 1] = P1;
+      st[2 * C::NW * 8] = l0;
+      st[2 * C::NW * 8 + 1] = l1;
+    }
+    __syncthreads();
+    if (tid < 8) {
+      float m = kNoMax, p = kNoMax, l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < C::NW; ++w) {
+        m = fmaxf(m, stats[w * 8 + tid]);
+        p = fmaxf(p, stats[(C::NW + w) * 8 + tid]);
+      }
+#pragma unroll
+      for (int w = 0; w < C::NW; ++w) l += stats[(2 * C::NW + w) * 8 + tid] * ex2(stats[w * 8 + tid] - m);
+      sums[tid] = m;
+      sums[8 + tid] = p;
+      sums[16 + tid] = l;
+      sums[24 + tid] = ex2(p - m) / (127.0f * l);
+    }
+    __syncthreads();
+    const bool whole = use.j0 == 0 && use.j1 == use.n;
+    const long long part = 2LL * blockIdx.x + (use.g == g0 ? 0 : 1);
+    float* const mine = a.parts + part * 8 * (D + 2);
+    const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
+    for (int q0 = 0; q0 < heads; q0 += C::MQ) {
+      // lanes with the queries q0 .. q0 + MQ - 1 (MQ = 2: one t4) put their channels down
+      if (2 * t4 == q0) {
+        float* row = merge + warp * C::MQ * C::ROW;
+#pragma unroll
+        for (int m = 0; m < 2 * KK; ++m) {
+          row[16 * m + gid] = o[m][0] * c0;
+          row[16 * m + gid + 8] = o[m][2] * c0;
+          row[C::ROW + 16 * m + gid] = o[m][1] * c1;
+          row[C::ROW + 16 * m + gid + 8] = o[m][3] * c1;
+        }
+      }
+      __syncthreads();
+      for (int i = tid; i < C::MQ * D; i += C::THREADS) {
+        const int q = i / D, ch = i - q * D;
+        float x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < C::NW; ++w) x += merge[(w * C::MQ + q) * C::ROW + ch];
+        if (q0 + q < heads) {
+          x *= sums[24 + q0 + q];
+          if (whole) store_out<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q0 + q) * D + ch, x);
+          else mine[(q0 + q) * D + ch] = x;
+        }
+      }
+      __syncthreads();
+    }
+    if (!whole) {
+      if (tid < 8) {
+        mine[8 * D + tid] = sums[tid];
+        mine[8 * D + 8 + tid] = sums[16 + tid];
+      }
+      __threadfence();
+      __syncthreads();
+      const long long unit = static_cast<long long>(use.b) * a.units + use.u;
+      const long long u0 = use.g - use.j0, u1 = u0 + use.n;  // the unit on the line
+      const int from = owner(W, N, u0), to = owner(W, N, u1 - 1);
+      if (tid == 0) {
+        const int got = atomicAdd(a.counters + unit, 1);
+        s_last = got == to - from;
+        if (s_last) a.counters[unit] = 0;  // left as it was found
+      }
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        const int skip = share(W, N, from) == u0 ? 0 : 1;  // the first part is its thread block's second one
+        for (int i = tid; i < heads * D; i += C::THREADS) {
+          const int q = i / D, ch = i - q * D;
+          float m = kNoMax, l = 0.0f, x = 0.0f;
+          for (int p = from; p <= to; ++p) {
+            const float* src = a.parts + (2LL * p + (p == from ? skip : 0)) * 8 * (D + 2);
+            const float pm = __ldcg(src + 8 * D + q), pl = __ldcg(src + 8 * D + 8 + q), px = __ldcg(src + q * D + ch);
+            const float nm = fmaxf(m, pm), was = ex2(m - nm), now = pl * ex2(pm - nm);
+            l = l * was + now;
+            x = x * was + px * now;
+            m = nm;
+          }
+          store_out<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch, x / l);
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  // copies that are still on their way after a timeout land before the block ends (bounded again)
+  if (dead && lane == 0)
+    for (int s = 0; s < C::NST; ++s) {
+      const int at = (stage + s) % C::NST;
+      wait_stage(bars + 8 * at, at >= stage ? phase : phase ^ 1);
+    }
+}
+
+template <int D, int QT, int OT>
+cudaError_t launch_dqo(const Args& a, cudaStream_t st) {
+  using C = Cfg<D>;
+  auto* kernel = decode8_kernel<D, QT, OT>;
+  static std::atomic<uint64_t> ready{0};  // devices on which the shared-memory limit has been raised
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit) || !bit) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM)) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  Args x = a;
+  x.min_blocks = C::NW;
+  return launch_kernel(kernel, dim3(static_cast<unsigned>(a.grid)), dim3(C::THREADS), C::SMEM, st, x);
+}
+
+template <int D>
+cudaError_t launch_d(const Args& a, int q_type, int out_type, cudaStream_t st) {
+  if (q_type == TQ_BF16) return out_type == TQ_FP32 ? launch_dqo<D, TQ_BF16, TQ_FP32>(a, st) : launch_dqo<D, TQ_BF16, TQ_BF16>(a, st);
+  return out_type == TQ_FP32 ? launch_dqo<D, TQ_FP16, TQ_FP32>(a, st) : launch_dqo<D, TQ_FP16, TQ_FP16>(a, st);
+}
+
+}  // namespace
+
+// Thread blocks of a launch: one per SM, or as many as the longest sequences could give work to.
+int decode8_grid(int B, int H_kv, int G, int d, int max_len) {
+  const long long warps = d <= 128 ? 16 : (d == 256 ? 8 : 4);
+  const long long blocks = static_cast<long long>(B) * H_kv * ((G + 7) / 8) * ((max_len + 15LL) / 16 + 1);
+  const long long worth = (blocks + warps - 1) / warps, most = device_sm_count();
+  return static_cast<int>(worth < most ? worth : most);
+}
+
+cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,
+                           int window, int grid, int32_t* counters, float* parts, void* out, int out_type, int32_t* status,
+                           cudaStream_t st) {
+  Args a = {};
+  a.c = c;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_stride = q_stride;
+  a.H_q = H_q;
+  a.G = H_q / c.H_kv;
+  a.tiles = (a.G + 7) / 8;
+  a.window = window;
+  a.scale_log2 = attn_scale * kLog2e / 127.0f;
+  a.units = c.H_kv * a.tiles;
+  a.grid = grid;
+  a.counters = counters;
+  a.parts = parts;
+  a.out = out;
+  a.status = status;
+  switch (c.d) {
+    case 64: return launch_d<64>(a, q_type, out_type, st);
+    case 128: return launch_d<128>(a, q_type, out_type, st);
+    case 256: return launch_d<256>(a, q_type, out_type, st);
+    default: return launch_d<512>(a, q_type, out_type, st);
+  }
+}
+
+}  // namespace tq

@@ -164,6 +164,42 @@ cudaError_t launch_attend_materialized(const tq_kv_cache& c, const void* k_mat, 
 cudaError_t launch_attend_mixed(const tq_kv_cache& c, const __half* k_fp16, const __half* v_fp16, const __half* q, int H_q,
                                 float attn_scale, int C, float* o_part, float* m_part, float* l_part, int32_t* status,
                                 cudaStream_t st);
+// Serving operators (tq_pages.cu, tq_kv8.cu, tq_decode8.cu, tq_prompt.cu)
+struct PageArgs {
+  int32_t* page_table;  // NULL: contiguous
+  const int32_t *seq_lens, *new_lens;
+  int B, page_tokens, max_pages, num_pages;
+  const int32_t *free_pages, *free_count;
+  int32_t *seq_lens_out, *free_count_out, *token_offsets;
+  int64_t* slots;
+  long long n_slots;
+};
+cudaError_t launch_pages_assign(const PageArgs& a, int32_t* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_release(const PageArgs& a, const uint8_t* finished, int32_t* free_pages, int32_t* status,
+                                 cudaStream_t st);
+cudaError_t launch_kv8_append(const tq_kv8_cache& c, const void* k, const void* v, int dtype, long long k_stride,
+                              long long v_stride, const int64_t* slots, long long n, int32_t* status, cudaStream_t st);
+cudaError_t launch_kv8_gather(const tq_kv8_cache& c, const int64_t* slots, long long n, void* k, void* v, int dtype,
+                              int32_t* status, cudaStream_t st);
+int decode8_grid(int B, int H_kv, int G, int d, int max_len);
+cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,
+                           int window, int grid, int32_t* counters, float* parts, void* out, int out_type, int32_t* status,
+                           cudaStream_t st);
+struct PromptArgs {
+  const void *q, *k, *v;
+  int dtype;
+  long long q_stride, k_stride, v_stride;
+  int n_q, n_kv;
+  const int32_t *q_offsets, *kv_offsets;
+  int B, H_q, H_kv, d;
+  float attn_scale;
+  int causal, window;
+  void* out;
+  int out_dtype;
+  int32_t* status;
+};
+cudaError_t launch_prompt(const PromptArgs& a, cudaStream_t st);
+
 // Knobs for the library's own tests, set through tq_internal_test_hook (exported from the shared object for
 // the test suite but not declared in tq.h: not part of the ABI).  Read with relaxed loads on the call path.
 struct TestHooks {

@@ -1,0 +1,251 @@
+// Page bookkeeping of a serving step: the pages of finished sequences go back to the pool, new tokens get pages and
+// slots.  Everything is computed from device-side lengths, so a step needs no host round trip and can be replayed
+// from a CUDA graph.
+//
+// The free list is a stack free_pages[0 .. count).  With len_b cached and new_b new tokens, pages of P tokens and
+//   need_b = ceil((len_b + new_b) / P) - ceil(len_b / P),   N_b = sum of need over the sequences before b,
+// the i-th fresh page of sequence b is free_pages[count - 1 - N_b - i]: two prefix sums (tokens and pages) over
+// the batch and one table look-up per token, nothing sequential.
+//
+// These launches are made of latencies (17 bytes per sequence, 8 per page and per slot): one thread block scans the
+// batch, 1024 sequences a round, warp shuffles and one exchange through shared memory.  The slots of many tokens
+// (8 bytes each) are written by a second launch over the whole GPU; up to kOneLaunchSlots of them the scanning block
+// writes them itself, which saves the hand-over.  Measured on a B200: see kOneLaunchSlots.
+#include "tq_internal.cuh"
+
+namespace tq {
+namespace {
+
+constexpr int kScan = 1024;                    // threads of the scanning block = sequences per round
+constexpr int kFill = 256;                     // threads of a block of the slot launch
+constexpr long long kOneLaunchSlots = 8192;    // most slots that the scanning block writes itself
+
+struct Sums {
+  long long tokens, pages;
+};
+
+// Inclusive sums over the block's threads (thread order).  `warp_sums` holds 32 entries; all threads call it.
+__device__ __forceinline__ Sums block_inclusive(Sums v, Sums* warp_sums, Sums& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long t = __shfl_up_sync(0xffffffffu, v.tokens, o), p = __shfl_up_sync(0xffffffffu, v.pages, o);
+    if (lane >= o) {
+      v.tokens += t;
+      v.pages += p;
+    }
+  }
+  if (lane == 31) warp_sums[warp] = v;
+  __syncthreads();
+  Sums before = {0, 0}, all = {0, 0};
+#pragma unroll
+  for (int w = 0; w < kScan / 32; ++w) {
+    const Sums s = warp_sums[w];
+    if (w < warp) {
+      before.tokens += s.tokens;
+      before.pages += s.pages;
+    }
+    all.tokens += s.tokens;
+    all.pages += s.pages;
+  }
+  __syncthreads();  // warp_sums may be written again
+  total = all;
+  v.tokens += before.tokens;
+  v.pages += before.pages;
+  return v;
+}
+
+__device__ __forceinline__ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// What the slot launch needs of a sequence: its old length (-1: refused) and the pages taken before it.
+struct Row {
+  int32_t old, pages_before;
+};
+
+__device__ __forceinline__ int read_count(const int32_t* free_count, int num_pages, int32_t* status) {
+  int count = *free_count;
+  if (count < 0 || count > num_pages) {
+    if (status && threadIdx.x == 0) atomicOr(status, TQ_STATUS_BAD_PAGE);
+    count = count < 0 ? 0 : num_pages;
+  }
+  return count;
+}
+
+// Slot of packed token n, and the table entry of a page that token is the first of.
+__device__ __forceinline__ long long slot_of(const PageArgs& a, const Row* rows, int count, long long n, int32_t* status) {
+  if (n >= a.token_offsets[a.B]) return -1;  // padding behind the last token
+  int lo = 0, hi = a.B;                      // the sequence with offsets[lo] <= n < offsets[lo + 1]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.token_offsets[mid] <= n) lo = mid;
+    else hi = mid;
+  }
+  const Row r = rows[lo];
+  if (r.old < 0) return -1;  // refused
+  const int pos = r.old + static_cast<int>(n - a.token_offsets[lo]);  // below the capacity, which fits 31 bits
+  if (a.page_table == nullptr) return static_cast<long long>(lo) * a.page_tokens * a.max_pages + pos;
+  const int shift = __ffs(a.page_tokens) - 1;  // a power of two
+  const int logical = pos >> shift, within = pos & (a.page_tokens - 1);
+  const int first = static_cast<int>((static_cast<unsigned>(r.old) + a.page_tokens - 1) >> shift);
+  int page;
+  if (logical >= first) {
+    page = a.free_pages[count - 1 - r.pages_before - (logical - first)];
+    if (within == 0) a.page_table[static_cast<long long>(lo) * a.max_pages + logical] = page;
+  } else {
+    page = a.page_table[static_cast<long long>(lo) * a.max_pages + logical];
+  }
+  if (page < 0 || page >= a.num_pages) {
+    if (status) atomicOr(status, TQ_STATUS_BAD_PAGE);
+    return -1;
+  }
+  return static_cast<long long>(page) * a.page_tokens + within;
+}
+
+__global__ void __launch_bounds__(kScan) assign_scan_kernel(PageArgs a, int32_t* ws, bool fill, int32_t* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ Sums warp_sums[kScan / 32];
+  __shared__ int granted;
+  Row* rows = reinterpret_cast<Row*>(ws + 2);
+  const bool paged = a.page_table != nullptr;
+  const int count = paged ? read_count(a.free_count, a.num_pages, status) : 0;
+  const long long cap = static_cast<long long>(a.page_tokens) * a.max_pages;
+  if (threadIdx.x == 0) {
+    granted = 0;
+    ws[0] = count;  // the slot launch reads it here: free_count_out may be free_count
+  }
+  Sums carry = {0, 0};
+  for (int base = 0; base < a.B; base += kScan) {
+    const int b = base + threadIdx.x;
+    long long old = 0, fresh = 0, need = 0;
+    bool fits = false;
+    int bad = 0;
+    if (b < a.B) {
+      old = a.seq_lens[b];
+      fresh = a.new_lens[b];
+      if (fresh < 0 || old < 0 || old > cap) bad |= TQ_STATUS_BAD_LEN;
+      if (fresh < 0) fresh = 0;
+      fits = bad == 0 && old + fresh <= cap;
+      if (paged && fits) need = ceil_div(old + fresh, a.page_tokens) - ceil_div(old, a.page_tokens);
+    }
+    // A refused sequence still owns its rows of the packed tokens (their slots are -1), but no pages.  Sums of
+    // tokens are kept in 64 bits and cut at n_slots on the way out.
+    Sums total;
+    const Sums upto0 = block_inclusive({fresh, need}, warp_sums, total);
+    const Sums upto = {upto0.tokens + carry.tokens, upto0.pages + carry.pages};
+    if (b < a.B) {
+      bool ok = fits;
+      if (!fits && bad == 0) bad |= TQ_STATUS_CACHE_FULL;
+      if (upto.tokens > a.n_slots) {
+        if (fresh > 0) bad |= TQ_STATUS_BAD_LEN;
+        ok = ok && fresh == 0;
+      }
+      if (ok && need > 0 && upto.pages > count) {
+        bad |= TQ_STATUS_POOL_EMPTY;
+        ok = false;
+      }
+      if (bad && status) atomicOr(status, bad);
+      const long long end = upto.tokens < a.n_slots ? upto.tokens : a.n_slots;
+      a.token_offsets[b + 1] = static_cast<int32_t>(end);
+      a.seq_lens_out[b] = static_cast<int32_t>(ok ? old + fresh : old);
+      const long long before = upto.pages - need;
+      rows[b] = {ok ? static_cast<int32_t>(old) : -1, static_cast<int32_t>(before < 0x7fffffff ? before : 0x7fffffff)};
+      if (ok && need > 0) atomicMax(&granted, static_cast<int>(upto.pages));
+    }
+    carry.tokens += total.tokens;
+    carry.pages += total.pages;
+  }
+  if (threadIdx.x == 0) a.token_offsets[0] = 0;
+  __syncthreads();
+  if (threadIdx.x == 0 && paged) *a.free_count_out = count - granted;
+  if (!fill) return;
+  for (long long n = threadIdx.x; n < a.n_slots; n += kScan) a.slots[n] = slot_of(a, rows, count, n, status);
+}
+
+__global__ void __launch_bounds__(kFill) assign_fill_kernel(PageArgs a, const int32_t* ws, int32_t* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const Row* rows = reinterpret_cast<const Row*>(ws + 2);
+  const int count = ws[0];
+  const long long step = static_cast<long long>(gridDim.x) * kFill;
+  for (long long n = static_cast<long long>(blockIdx.x) * kFill + threadIdx.x; n < a.n_slots; n += step)
+    a.slots[n] = slot_of(a, rows, count, n, status);
+}
+
+// Pages of finished sequences, sequences and pages in ascending order, are pushed onto the stack.
+__global__ void __launch_bounds__(kScan) release_kernel(PageArgs a, const uint8_t* finished, int32_t* free_pages,
+                                                        int32_t* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ Sums warp_sums[kScan / 32];
+  __shared__ int s_pages[kScan], s_at[kScan];
+  const bool paged = a.page_table != nullptr;
+  const int count = paged ? read_count(a.free_count, a.num_pages, status) : 0;
+  const long long cap = static_cast<long long>(a.page_tokens) * a.max_pages;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // More than 1024 sequences: the total is needed before anything is written, so the lengths are read twice.
+  long long all = 0;
+  for (int round = (a.B > kScan ? 0 : 1); round < 2; ++round) {
+    long long carry = 0;
+    for (int base = 0; base < a.B; base += kScan) {
+      const int b = base + threadIdx.x;
+      long long len = 0, pages = 0;
+      bool gone = false;
+      if (b < a.B) {
+        len = a.seq_lens[b];
+        gone = finished[b] != 0;
+        if (len < 0 || len > cap) {
+          if (status) atomicOr(status, TQ_STATUS_BAD_LEN);
+          len = len < 0 ? 0 : cap;
+        }
+        if (gone && paged) pages = ceil_div(len, a.page_tokens);
+      }
+      Sums total;
+      const Sums upto = block_inclusive({0, pages}, warp_sums, total);
+      if (round == 1) {
+        if (a.B <= kScan) all = total.pages;
+        // more pages than the pool has: the table or the stack is not what it should be, and nothing is released
+        const bool refuse = count + all > a.num_pages && paged;
+        if (refuse && status && threadIdx.x == 0) atomicOr(status, TQ_STATUS_BAD_PAGE);
+        if (b < a.B) a.seq_lens_out[b] = static_cast<int32_t>(gone && !refuse ? 0 : len);
+        if (paged) {
+          s_pages[threadIdx.x] = refuse ? 0 : static_cast<int>(pages);
+          s_at[threadIdx.x] = static_cast<int>(count + carry + upto.pages - pages);
+          __syncthreads();
+          const int here = a.B - base < kScan ? a.B - base : kScan;
+          for (int r = warp; r < here; r += kScan / 32) {
+            const int n = s_pages[r], at = s_at[r];
+            const int32_t* row = a.page_table + static_cast<long long>(base + r) * a.max_pages;
+            for (int i = lane; i < n; i += 32) {
+              const int page = row[i];
+              if ((page < 0 || page >= a.num_pages) && status) atomicOr(status, TQ_STATUS_BAD_PAGE);
+              free_pages[at + i] = page;
+            }
+          }
+          __syncthreads();
+        }
+      }
+      carry += total.pages;
+    }
+    if (round == 0) all = carry;
+  }
+  if (threadIdx.x == 0 && paged) *a.free_count_out = static_cast<int32_t>(count + all > a.num_pages ? count : count + all);
+}
+
+}  // namespace
+
+cudaError_t launch_pages_assign(const PageArgs& a, int32_t* ws, int32_t* status, cudaStream_t st) {
+  const bool fill = a.n_slots <= kOneLaunchSlots;
+  cudaError_t e = launch_kernel(assign_scan_kernel, dim3(1), dim3(kScan), 0, st, a, ws, fill, status);
+  if (e != cudaSuccess || fill) return e;
+  const long long want = (a.n_slots + kFill - 1) / kFill, most = 8LL * device_sm_count();
+  return launch_kernel(assign_fill_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(kFill), 0, st, a,
+                       const_cast<const int32_t*>(ws), status);
+}
+
+cudaError_t launch_pages_release(const PageArgs& a, const uint8_t* finished, int32_t* free_pages, int32_t* status,
+                                 cudaStream_t st) {
+  return launch_kernel(release_kernel, dim3(1), dim3(kScan), 0, st, a, finished, free_pages, status);
+}
+
+}  // namespace tq
