@@ -532,7 +532,8 @@ int tq_sdpa_int8_decode(const tq_kv8_cache* cache /* host */, const void* q, int
  *   out          : device [n_q][H_q][d], of dtype or fp32 (out_dtype).  Rows of no sequence are left as they were.
  * d in {64, 128, 256, 512}; H_q a multiple of H_kv, H_q / H_kv <= 64; causal = 0 with a window is TQ_ERR_SHAPE.
  * A NaN or an infinity in k or v reaches only the queries that attend its token.
- * Status: TQ_STATUS_BAD_LEN, TQ_STATUS_EMPTY_SEQ (queries of a sequence without keys), TQ_STATUS_TIMEOUT.
+ * Status: TQ_STATUS_BAD_LEN, TQ_STATUS_EMPTY_SEQ (queries of a sequence without keys), TQ_STATUS_TIMEOUT; the first two
+ * are set for sequences that have queries.
  */
 int tq_sdpa_prompt(const void* q, const void* k, const void* v, int32_t dtype, int64_t q_stride, int64_t k_stride,
                    int64_t v_stride, int32_t n_q, int32_t n_kv, const int32_t* q_offsets, const int32_t* kv_offsets,

@@ -1,4 +1,4 @@
-// What the kernels of tq_sdpa_prompt share: a sequence's rows and the keys that a query sees.
+// A packed sequence's rows and the keys that a query sees (tq_sdpa_prompt).
 #pragma once
 #include "tq_internal.cuh"
 
@@ -35,7 +35,5 @@ __device__ __forceinline__ void prompt_keys(const PromptArgs& a, const PromptSeq
     if (a.window > 0 && up > a.window) lo = up - a.window;
   }
 }
-
-cudaError_t launch_prompt_simple(const PromptArgs& a, cudaStream_t st);  // tq_prompt_simple.cu
 
 }  // namespace tq
