@@ -18,6 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libtq.so")
+BIND = os.path.join(HERE, "_tq_bind.so")  # native binding of the serving operators (a CPython extension)
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -40,7 +41,28 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def build_binding(force: bool = False) -> str:
+    """The CPython extension that hands torch tensors to libtq; needs torch's headers, no CUDA compiler."""
+    src = os.path.join(CSRC, "binding", "tq_bind.cpp")
+    if not force and os.path.exists(BIND) and all(os.path.getmtime(p) <= os.path.getmtime(BIND)
+                                                  for p in [src] + glob.glob(os.path.join(INCLUDE, "*.h"))):
+        return BIND
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    for path in cpp_extension.include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]:
+        cmd += ["-isystem", path]
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd += ["-I", INCLUDE, src, "-o", BIND, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    subprocess.run(cmd, check=True)
+    return BIND
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_binding(force)
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -1,4 +1,5 @@
-"""ctypes binding of libtq.so -- same names as include/tq.h, argument marshalling only.
+"""Binding of libtq.so -- same names as include/tq.h, argument marshalling only: through ctypes, and for the serving
+operators, whose kernels can be shorter than that, through a small extension module (csrc/binding).
 
 Tensors are torch CUDA tensors (torch supplies device memory and streams, nothing else); every
 function forwards data pointers and sizes to the C entry point and raises TqError on a non-zero
@@ -6,6 +7,7 @@ result.  There is no CPU fallback: importing this module fails if the library ha
 built (python -m paper_2604_16957_b200.build), and calls fail without a CUDA device.
 """
 import ctypes as C
+import importlib.util
 import os
 
 import torch
@@ -424,7 +426,12 @@ def alloc_partials(B, H_q, d, num_splits, device="cuda"):
 
 # ---- serving: pages and slots, the 8-bit cache, attention over it and over whole prompts (see tq.h)
 
-_DTYPES = {torch.float16: TQ_FP16, torch.float32: TQ_FP32, torch.bfloat16: TQ_BF16}
+_BIND_PATH = os.path.join(_HERE, "_tq_bind.so")
+if not os.path.exists(_BIND_PATH):
+    raise ImportError(f"{_BIND_PATH} is missing: build it with `python -m paper_2604_16957_b200.build`")
+_spec = importlib.util.spec_from_file_location("_tq_bind", _BIND_PATH)
+_bind = importlib.util.module_from_spec(_spec)
+_spec.loader.exec_module(_bind)
 
 
 def _refuse(where, why):
@@ -433,57 +440,47 @@ def _refuse(where, why):
     raise e
 
 
-def _ints_of(t, where, name, dtype, n=None):
-    """Device address of a contiguous integer tensor (of n elements)."""
-    if t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
-        _refuse(where, f"{name} must be a contiguous {dtype} tensor" + ("" if n is None else f" of {n} elements"))
-    return t.data_ptr()
-
-
-def _one_device(where, stream, *tensors):
-    """All tensors live on one CUDA device, and that is the current one; returns the stream to launch on."""
-    dev = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != dev:
-            _refuse(where, "tensors on different devices")
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        _refuse(where, f"tensors on {dev}, which is not the current CUDA device")
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+_bind.attach(_refuse, _check, *(C.cast(f, _vp).value for f in (
+    _lib.tq_pages_release, _lib.tq_pages_assign, _lib.tq_kv8_append, _lib.tq_kv8_gather, _lib.tq_sdpa_int8_decode,
+    _lib.tq_sdpa_prompt)))
 
 
 class KV8Cache:
     """Device buffer of one layer's 8-bit KV cache, contiguous: `blocks` [B][H_kv][S_cap/16][block bytes]."""
 
+    __slots__ = ("blocks", "seq_lens", "page_table", "_handle")
+
     def __init__(self, B, H_kv, S_cap, d, device="cuda"):
         if S_cap % 16 or d not in (64, 128, 256, 512):
             _refuse("KV8Cache", "S_cap must be a multiple of 16 and d one of 64, 128, 256, 512")
         self._hold(torch.zeros((B, H_kv, S_cap // 16, TQ_BLOCK8_BYTES(d)), dtype=torch.uint8, device=device),
-                   torch.zeros((B,), dtype=torch.int32, device=device))
+                   torch.zeros((B,), dtype=torch.int32, device=device), None)
 
     @classmethod
     def over(cls, blocks, seq_lens):
         """The cache in tensors of the caller: blocks as above, seq_lens [B] int32 (shared by the layers, if need be)."""
         self = cls.__new__(cls)
-        self._hold(blocks, seq_lens)
+        self._hold(blocks, seq_lens, None)
         return self
 
-    def _hold(self, blocks, seq_lens):
-        self.B, self.H_kv, n, row = blocks.shape
-        self.S_cap, self.d = 16 * n, (row - 16) // 32
-        if blocks.dtype != torch.uint8 or not blocks.is_contiguous() or row != TQ_BLOCK8_BYTES(self.d):
-            _refuse("KV8Cache", "blocks must be a contiguous uint8 tensor [B][H_kv][S_cap/16][32 d + 16]")
-        self.blocks, self.seq_lens, self.page_table = blocks, seq_lens, None
-        self._struct = tq_kv8_cache(blocks.data_ptr(), _ints_of(seq_lens, "KV8Cache", "seq_lens", torch.int32, self.B), self.B,
-                                    self.H_kv, self.S_cap, self.d, None, 0, 0, 0)
-        self._ref = C.byref(self._struct)
+    def _hold(self, blocks, seq_lens, page_table):
+        self._handle = _bind.cache8(blocks, seq_lens, page_table)
+        self.blocks, self.seq_lens, self.page_table = blocks, seq_lens, page_table
+
+    B = property(lambda self: _bind.sizes(self._handle)[0])
+    H_kv = property(lambda self: _bind.sizes(self._handle)[1])
+    S_cap = property(lambda self: _bind.sizes(self._handle)[2])
+    d = property(lambda self: _bind.sizes(self._handle)[3])
 
     def struct(self):
-        return self._struct
+        return tq_kv8_cache.from_address(_bind.address(self._handle))
 
 
 class PagedKV8Cache(KV8Cache):
     """The same served from a pool of pages: `blocks` [num_pages][H_kv][page_tokens/16][block bytes], `page_table`
     [B][max_pages] int32 (shared by the layers, if need be)."""
+
+    __slots__ = ()
 
     def __init__(self, B, H_kv, page_tokens, max_pages, num_pages, d, device="cuda"):
         if page_tokens < 16 or page_tokens & (page_tokens - 1) or d not in (64, 128, 256, 512):
@@ -498,18 +495,9 @@ class PagedKV8Cache(KV8Cache):
         self._hold(blocks, seq_lens, page_table)
         return self
 
-    def _hold(self, blocks, seq_lens, page_table):
-        self.num_pages, self.H_kv, n, row = blocks.shape
-        self.B, self.max_pages = page_table.shape
-        self.page_tokens, self.d = 16 * n, (row - 16) // 32
-        self.S_cap = self.page_tokens * self.max_pages
-        if blocks.dtype != torch.uint8 or not blocks.is_contiguous() or row != TQ_BLOCK8_BYTES(self.d):
-            _refuse("PagedKV8Cache", "blocks must be a contiguous uint8 tensor [num_pages][H_kv][page_tokens/16][32 d + 16]")
-        self.blocks, self.seq_lens, self.page_table = blocks, seq_lens, page_table
-        self._struct = tq_kv8_cache(blocks.data_ptr(), _ints_of(seq_lens, "PagedKV8Cache", "seq_lens", torch.int32, self.B), self.B,
-                                    self.H_kv, self.S_cap, self.d, _ints_of(page_table, "PagedKV8Cache", "page_table", torch.int32),
-                                    self.page_tokens, self.max_pages, self.num_pages)
-        self._ref = C.byref(self._struct)
+    page_tokens = property(lambda self: _bind.sizes(self._handle)[4])
+    max_pages = property(lambda self: _bind.sizes(self._handle)[5])
+    num_pages = property(lambda self: _bind.sizes(self._handle)[6])
 
 
 def alloc_pages_workspace(B, device="cuda"):
@@ -520,90 +508,31 @@ def tq_pages_release(page_table, seq_lens, finished, page_tokens, num_pages, fre
                      free_count_out, status=None, stream=None, max_pages=None):
     """Push the pages of finished sequences (finished: [B] uint8 or bool) onto the stack free_pages[0 .. free_count).
     page_table [B][max_pages] int32, or None for contiguous caches (then page_tokens * max_pages is their capacity)."""
-    w = "tq_pages_release"
-    st = _one_device(w, stream, seq_lens, page_table, finished, free_pages, free_count, seq_lens_out, free_count_out, status)
-    B = seq_lens.numel()
-    if page_table is not None:
-        if page_table.dim() != 2 or page_table.shape[0] != B or free_pages.numel() < num_pages:
-            _refuse(w, "page_table must be [B][max_pages] and free_pages hold num_pages entries")
-        max_pages = page_table.shape[1]
-    if finished.dtype not in (torch.uint8, torch.bool) or finished.numel() != B or not finished.is_contiguous():
-        _refuse(w, "finished must be a contiguous uint8 or bool tensor [B]")
-    i32 = torch.int32
-    _check(_lib.tq_pages_release(
-        None if page_table is None else _ints_of(page_table, w, "page_table", i32), _ints_of(seq_lens, w, "seq_lens", i32),
-        finished.data_ptr(), B, page_tokens, max_pages or 1, num_pages,
-        None if page_table is None else _ints_of(free_pages, w, "free_pages", i32),
-        None if page_table is None else _ints_of(free_count, w, "free_count", i32, 1),
-        _ints_of(seq_lens_out, w, "seq_lens_out", i32, B),
-        None if page_table is None else _ints_of(free_count_out, w, "free_count_out", i32, 1),
-        None if status is None else status.data_ptr(), st), w)
+    _bind.pages_release(page_table, seq_lens, finished, page_tokens, num_pages, free_pages, free_count, seq_lens_out,
+                        free_count_out, status, stream, max_pages)
 
 
 def tq_pages_assign(page_table, seq_lens, new_lens, page_tokens, num_pages, free_pages, free_count, seq_lens_out,
                     free_count_out, token_offsets, slots, workspace, status=None, stream=None, max_pages=None):
     """Room for new_lens[b] more tokens of every sequence: pages, lengths, packed offsets [B + 1] int32 and slots [n] int64
     (n: at least the number of new tokens).  page_table None: contiguous caches of page_tokens * max_pages tokens."""
-    w = "tq_pages_assign"
-    st = _one_device(w, stream, seq_lens, page_table, new_lens, free_pages, free_count, seq_lens_out, free_count_out,
-                     token_offsets, slots, workspace, status)
-    B = seq_lens.numel()
-    if page_table is not None:
-        if page_table.dim() != 2 or page_table.shape[0] != B or free_pages.numel() < num_pages:
-            _refuse(w, "page_table must be [B][max_pages] and free_pages hold num_pages entries")
-        max_pages = page_table.shape[1]
-    i32 = torch.int32
-    _check(_lib.tq_pages_assign(
-        None if page_table is None else _ints_of(page_table, w, "page_table", i32), _ints_of(seq_lens, w, "seq_lens", i32),
-        _ints_of(new_lens, w, "new_lens", i32, B), B, page_tokens, max_pages or 1, num_pages,
-        None if page_table is None else _ints_of(free_pages, w, "free_pages", i32),
-        None if page_table is None else _ints_of(free_count, w, "free_count", i32, 1),
-        _ints_of(seq_lens_out, w, "seq_lens_out", i32, B),
-        None if page_table is None else _ints_of(free_count_out, w, "free_count_out", i32, 1),
-        _ints_of(token_offsets, w, "token_offsets", i32, B + 1), _ints_of(slots, w, "slots", torch.int64), slots.numel(),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), None if status is None else status.data_ptr(), st), w)
+    _bind.pages_assign(page_table, seq_lens, new_lens, page_tokens, num_pages, free_pages, free_count, seq_lens_out,
+                       free_count_out, token_offsets, slots, workspace, status, stream, max_pages)
 
 
-def _packed_rows(t, where, name, heads, d):
-    """Row stride (elements) of a packed [n][heads][d] tensor whose heads stand side by side (a slice of a fused projection
-    will do)."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
-        _refuse(where, f"{name} must be [n][{heads}][{d}] with its heads side by side")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+def _handle_of(cache):
+    return cache._handle if isinstance(cache, KV8Cache) else None
 
 
 def tq_kv8_append(cache, k_new, v_new, slots, status=None, stream=None):
-    """k_new, v_new: packed [n][H_kv][d], fp16 or bf16 (slices of a fused projection will do); slots [n] int64."""
-    w = "tq_kv8_append"
-    if not isinstance(cache, KV8Cache):
-        _refuse(w, "cache must be a KV8Cache or a PagedKV8Cache")
-    st = _one_device(w, stream, cache.blocks, k_new, v_new, slots, status)
-    n = slots.numel()
-    if k_new.dtype != v_new.dtype or k_new.dtype not in _DTYPES or k_new.shape[0] != n or v_new.shape[0] != n:
-        _refuse(w, "k_new, v_new must be fp16 or bf16 with one row per slot")
-    if n == 0:
-        return
-    _check(_lib.tq_kv8_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), _DTYPES[k_new.dtype],
-                              _packed_rows(k_new, w, "k_new", cache.H_kv, cache.d),
-                              _packed_rows(v_new, w, "v_new", cache.H_kv, cache.d), _ints_of(slots, w, "slots", torch.int64), n,
-                              None if status is None else status.data_ptr(), st), w)
+    """k_new, v_new: packed [n][H_kv][d], fp16 or bf16, heads side by side (slices of a fused projection will do); slots
+    [n] int64."""
+    _bind.kv8_append(_handle_of(cache), k_new, v_new, slots, status, stream)
 
 
 def tq_kv8_gather(cache, slots, k_out, v_out, status=None, stream=None):
     """Values of the slots into k_out, v_out: contiguous [n][H_kv][d], fp16, bf16 or fp32."""
-    w = "tq_kv8_gather"
-    if not isinstance(cache, KV8Cache):
-        _refuse(w, "cache must be a KV8Cache or a PagedKV8Cache")
-    st = _one_device(w, stream, cache.blocks, slots, k_out, v_out, status)
-    n = slots.numel()
-    shape = (n, cache.H_kv, cache.d)
-    if k_out.shape != shape or v_out.shape != shape or k_out.dtype != v_out.dtype or k_out.dtype not in _DTYPES or \
-            not k_out.is_contiguous() or not v_out.is_contiguous():
-        _refuse(w, f"k_out, v_out must be contiguous {list(shape)} tensors of one type (fp16, bf16, fp32)")
-    if n == 0:
-        return
-    _check(_lib.tq_kv8_gather(cache._ref, _ints_of(slots, w, "slots", torch.int64), n, k_out.data_ptr(), v_out.data_ptr(),
-                              _DTYPES[k_out.dtype], None if status is None else status.data_ptr(), st), w)
+    _bind.kv8_gather(_handle_of(cache), slots, k_out, v_out, status, stream)
 
 
 def alloc_int8_workspace(B, H_kv, H_q, d, device="cuda"):
@@ -614,34 +543,10 @@ def alloc_int8_workspace(B, H_kv, H_q, d, device="cuda"):
 def tq_sdpa_int8_decode(cache, q, attn_scale, window, max_seq_len, workspace, out, status=None, stream=None):
     """q: [B][H_q][d] fp16 or bf16, heads side by side; out: contiguous [B][H_q][d] of q's type or fp32.  window = 0: all
     cached tokens; max_seq_len = 0: no bound known."""
-    w = "tq_sdpa_int8_decode"
-    if not isinstance(cache, KV8Cache):
-        _refuse(w, "cache must be a KV8Cache or a PagedKV8Cache")
-    st = _one_device(w, stream, cache.blocks, cache.seq_lens, q, workspace, out, status)
-    if q.dim() != 3 or q.shape[0] != cache.B or out.shape != q.shape or not out.is_contiguous() or q.dtype not in _DTYPES or \
-            out.dtype not in _DTYPES:
-        _refuse(w, "q must be [B][H_q][d], fp16 or bf16, and out a contiguous tensor of the same shape")
-    _check(_lib.tq_sdpa_int8_decode(cache._ref, q.data_ptr(), _DTYPES[q.dtype], _packed_rows(q, w, "q", q.shape[1], cache.d),
-                                    q.shape[1], attn_scale, window, max_seq_len, workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), out.data_ptr(), _DTYPES[out.dtype],
-                                    None if status is None else status.data_ptr(), st), w)
+    _bind.int8_decode(_handle_of(cache), q, attn_scale, window, max_seq_len, workspace, out, status, stream)
 
 
 def tq_sdpa_prompt(q, k, v, q_offsets, kv_offsets, attn_scale, out, causal=True, window=0, status=None, stream=None):
     """Attention of packed sequences: q [n_q][H_q][d], k and v [n_kv][H_kv][d], fp16 or bf16, heads side by side; offsets
     [B + 1] int32 on the device; out: contiguous [n_q][H_q][d] of q's type or fp32."""
-    w = "tq_sdpa_prompt"
-    st = _one_device(w, stream, q, k, v, q_offsets, kv_offsets, out, status)
-    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or not (q.dtype == k.dtype == v.dtype) or q.dtype not in _DTYPES or \
-            out.dtype not in _DTYPES or out.shape != q.shape or not out.is_contiguous():
-        _refuse(w, "q, k, v must be packed [n][heads][d] tensors of one type, and out a contiguous tensor of q's shape")
-    n_q, H_q, d = q.shape
-    n_kv, H_kv, _ = k.shape
-    if n_q == 0:
-        return
-    B = q_offsets.numel() - 1
-    _check(_lib.tq_sdpa_prompt(q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[q.dtype], _packed_rows(q, w, "q", H_q, d),
-                               _packed_rows(k, w, "k", H_kv, d), _packed_rows(v, w, "v", H_kv, d), n_q, n_kv,
-                               _ints_of(q_offsets, w, "q_offsets", torch.int32), _ints_of(kv_offsets, w, "kv_offsets", torch.int32, B + 1),
-                               B, H_q, H_kv, d, attn_scale, int(causal), window, out.data_ptr(), _DTYPES[out.dtype],
-                               None if status is None else status.data_ptr(), st), w)
+    _bind.prompt(q, k, v, q_offsets, kv_offsets, attn_scale, out, causal, window, status, stream)

@@ -140,9 +140,14 @@ def test_the_binding_refuses_tensors_it_cannot_use(tq):
     import torch
     z = lambda *s, t=torch.float16: torch.zeros(s, dtype=t)  # noqa: E731
     cache = tq.KV8Cache(1, 2, 32, 64, device="cpu")
-    with pytest.raises(tq.TqError) as e:
-        tq.tq_kv8_append(cache, z(3, 2, 64), z(3, 2, 64), z(3, t=torch.int64))
-    assert e.value.code == tq.TQ_ERR_SHAPE and "CUDA" in str(e.value)
+    if not torch.cuda.is_available():
+        calls = (lambda: tq.tq_kv8_append(cache, z(3, 2, 64), z(3, 2, 64), z(3, t=torch.int64)),
+                 lambda: tq.tq_sdpa_prompt(z(3, 2, 64), z(3, 2, 64), z(3, 2, 64), z(2, t=torch.int32), z(2, t=torch.int32), 1.0, z(3, 2, 64)),
+                 lambda: tq.tq_pages_release(None, z(3, t=torch.int32), z(3, t=torch.uint8), 16, 0, None, None, z(3, t=torch.int32), None))
+        for call in calls:
+            with pytest.raises(tq.TqError) as e:
+                call()
+            assert e.value.code == tq.TQ_ERR_SHAPE and "CUDA" in str(e.value)
     for bad in (lambda: tq.KV8Cache.over(z(1, 2, 2, 100, t=torch.uint8), z(1, t=torch.int32)),
                 lambda: tq.KV8Cache.over(cache.blocks, z(2, t=torch.int32)),
                 lambda: tq.KV8Cache.over(cache.blocks, z(1, t=torch.int64)),
@@ -152,7 +157,8 @@ def test_the_binding_refuses_tensors_it_cannot_use(tq):
         with pytest.raises(tq.TqError):
             bad()
     with pytest.raises((C.ArgumentError, TypeError)):
-        tq._lib.tq_sdpa_int4_decode(cache._ref, F, 8, 1.0, 1, F, F, F, None, None)
-    with pytest.raises(tq.TqError):
-        tq._packed_rows(z(3, 4, 64)[:, ::2], "x", "q", 2, 64)
-    assert tq._packed_rows(z(3, 6, 64)[:, 1:3], "x", "q", 2, 64) == 6 * 64
+        tq._lib.tq_sdpa_int4_decode(C.byref(cache.struct()), F, 8, 1.0, 1, F, F, F, None, None)
+    paged = tq.PagedKV8Cache(3, 2, 32, 4, 9, 128, device="cpu")
+    assert (paged.B, paged.H_kv, paged.S_cap, paged.d, paged.page_tokens, paged.max_pages, paged.num_pages) == (3, 2, 128, 128, 32, 4, 9)
+    c = paged.struct()
+    assert (c.blocks, c.seq_lens, c.page_table) == (paged.blocks.data_ptr(), paged.seq_lens.data_ptr(), paged.page_table.data_ptr())
