@@ -18,9 +18,13 @@
 // block i of N takes the blocks [i W / N, (i + 1) W / N) of the W in all, whatever the lengths: ragged batches load
 // every SM alike, one short sequence still spreads.  A unit that lies in one thread block is finished there; the parts
 // of a cut one go to the workspace (at most two per thread block), and the last to arrive (a counter per unit) joins
-// them.  A thread block is 16 warps (8 and 4 at d = 256 and 512: registers); each warp owns a ring of three to six
-// stages of one 16-token block each, filled by one bulk copy per block (K codes, V codes and ranges are contiguous) --
-// 200 KB in flight per SM, no barrier in the main loop, and the copies run on into the thread block's next unit.
+// them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512: registers), each with a ring of three to
+// six stages of one 16-token block, and one warp that fills the rings, one bulk copy per block (K codes, V codes and
+// ranges are contiguous): 200 KB in flight per SM, no barrier in the main loop, and the copies run on into the thread
+// block's next unit while this one is merged.
+#include <algorithm>
+#include <type_traits>
+
 #include "tq_async.cuh"
 #include "tq_kv8.cuh"
 
@@ -30,22 +34,25 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1.0e30f;
 constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running maxima
+constexpr int kMaxGrid = 160;   // thread blocks of a launch (one per SM)
 
 template <int D>
 struct Cfg {
-  static constexpr int NW = D <= 128 ? 16 : (D == 256 ? 8 : 4);  // warps
+  static constexpr int NW = D <= 128 ? 15 : (D == 256 ? 7 : 4);  // warps of the arithmetic (registers: 16, 8, 8 warps fit)
   static constexpr int NST = D == 64 ? 6 : 3;                    // stages of a warp's ring
   static constexpr int STAGE = block8_bytes(D);
-  static constexpr int THREADS = 32 * NW;
+  static constexpr int THREADS = 32 * NW;                        // ... of the arithmetic; one more warp issues the copies
+  static constexpr int LAUNCH = THREADS + 32;
   static constexpr int RING = NW * NST * STAGE;
   // the merge arrays lie behind the rings (copies for the next unit are in flight while a unit is merged); the outputs
   // of the warps go through them MQ query heads at a time
   static constexpr int ROW = D + 4;  // floats of one query's row: 8 rows x 2 words apart hit different banks
   static constexpr int MQ = 2;
-  static constexpr int MERGE = NW * MQ * ROW * 4;
+  static constexpr int WTS = 2 * 8 * kMaxGrid * 4;  // the last to arrive keeps the weights of a unit's parts there
+  static constexpr int MERGE = NW * MQ * ROW * 4 > WTS ? NW * MQ * ROW * 4 : WTS;
   static constexpr int STATS = RING + MERGE;             // [NW][8] x {M, M', l} and the factors of them
   static constexpr int BARS = STATS + NW * 8 * 3 * 4 + 8 * 4 * 4;
-  static constexpr int QS = BARS + NW * NST * 8;         // d = 512: the query's B fragments, 8 bytes per lane and step
+  static constexpr int QS = BARS + 2 * NW * NST * 8;         // d = 512: the query's B fragments, 8 bytes per lane and step
   static constexpr int QBYTES = D == 512 ? (D / 16) * 32 * 8 : 0;
   static constexpr int SMEM = QS + QBYTES;
   static_assert(BARS % 8 == 0 && QS % 8 == 0 && STAGE % 16 == 0 && SMEM <= 232448, "shared memory");
@@ -106,11 +113,12 @@ __device__ __forceinline__ Span span_of(const Args& a, int b) {
 // A walk over a thread block's share of the line: units, and in a unit the blocks [j0, j1).
 struct Walk {
   long long g, g1;  // position on the line and end of the share
-  int b, u;         // sequence, unit in it
+  int b, u, h;      // sequence, unit in it, its KV head
   int j0, j1, n;    // blocks of this visit, blocks of the unit
   Span span;
   __device__ void open(const Args& a, int j) {
     span = span_of(a, b);
+    h = a.tiles == 1 ? u : u / a.tiles;
     n = span.blocks();
     j0 = j;
     const long long left = g1 - g;
@@ -152,140 +160,211 @@ __device__ __forceinline__ void store_out(void* out, long long at, float x) {
   else static_cast<__half*>(out)[at] = __float2half_rn(x);
 }
 
-// position of thread block i's share on the line
-__device__ __forceinline__ long long share(long long W, int N, int i) { return W * i / N; }
-__device__ __forceinline__ int owner(long long W, int N, long long g) {
-  int i = static_cast<int>(g * N / W);
-  while (i + 1 < N && share(W, N, i + 1) <= g) ++i;
-  while (i > 0 && share(W, N, i) > g) --i;
-  return i;
+template <int OT>
+__device__ __forceinline__ void store_out2(void* out, long long at, float x, float y) {
+  if (OT == TQ_FP32) *reinterpret_cast<float2*>(static_cast<float*>(out) + at) = make_float2(x, y);
+  else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + at) = pack2<OT>(x, y);
 }
 
+// The line of W blocks cut into N shares: share i starts at floor(i W / N).
+// (64-bit divisions cost half a microsecond of latency apiece; lines beyond 31 bits are rare enough to take them.)
+__device__ __forceinline__ long long divide(long long a, long long b) {
+  return ((a | b) >> 31) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+struct Shares {
+  long long each;
+  int rest, N;
+  float per;
+  __device__ Shares(long long W, int n) : each(divide(W, n)), rest(static_cast<int>(W - each * n)), N(n) {
+    per = static_cast<float>(n) / static_cast<float>(W);
+  }
+  __device__ long long start(int i) const { return each * i + i * rest / N; }
+  __device__ int owner(long long g) const {
+    int i = static_cast<int>(static_cast<float>(g) * per);  // off by one at most
+    i = i < N ? i : N - 1;
+    if (start(i) > g) --i;
+    else if (i + 1 < N && start(i + 1) <= g) ++i;
+    return i;
+  }
+};
+
 template <int D, int QT, int OT>
-__global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args a) {
+__global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a) {
   using C = Cfg<D>;
   constexpr int KK = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long s_start;
-  __shared__ int s_b, s_warp[C::NW], s_last;
+  __shared__ long long s_warp[C::NW + 1];
+  __shared__ int s_b, s_last, s_dead;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t4 = lane & 3;
   float* const merge = reinterpret_cast<float*>(smem + C::RING);
   float* const stats = reinterpret_cast<float*>(smem + C::STATS);  // [3][NW][8]
   float* const sums = stats + 3 * C::NW * 8;                       // [8] x {M, M', l, factor}
-  uint32_t ring, bars;
-  {
-    uint32_t base;
-    asm("{ .reg .u64 p; cvta.to.shared.u64 p, %1; cvt.u32.u64 %0, p; }\n" : "=r"(base) : "l"(smem));
-    ring = base + warp * C::NST * C::STAGE;
-    bars = base + C::BARS + warp * C::NST * 8;
-  }
-  if (lane == 0) {
-    for (int s = 0; s < C::NST; ++s) mbar_init(bars + 8 * s, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-  }
+  // warp w's ring of NST stages, and the barriers "stage s is full" and "stage s may be filled" behind all rings
+  uint32_t base;
+  asm("{ .reg .u64 p; cvta.to.shared.u64 p, %1; cvt.u32.u64 %0, p; }\n" : "=r"(base) : "l"(smem));
+  auto full = [&](int w, int s) { return base + C::BARS + (w * C::NST + s) * 8; };
+  auto empty = [&](int w, int s) { return base + C::BARS + (C::NW * C::NST + w * C::NST + s) * 8; };
+  if (tid == 0) s_dead = 0;
+  for (int i = tid; i < 2 * C::NW * C::NST; i += C::LAUNCH) mbar_init(base + C::BARS + 8 * i, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
 
+  const bool few = a.c.B <= 32;  // a warp sums the lengths up by itself: every warp does, and no barrier is needed
+
   // ---- where this thread block's share starts: blocks of all sequences, then the sequence that holds the start
-  auto scan = [&](int v, int& before) {  // inclusive sum over the threads; returns it, `before` = the sum of all
-    int x = v;
+  auto scan = [&](long long v, long long& sum) {  // inclusive sum over the threads; `sum`: that of all
+    long long x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
+    }
+    if (few) {
+      sum = __shfl_sync(0xffffffffu, x, 31);
+      return x;
     }
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    int add = 0, all = 0;
+    long long add = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < C::NW; ++w) {
-      const int y = s_warp[w];
+    for (int w = 0; w <= C::NW; ++w) {
+      const long long y = s_warp[w];
       if (w < warp) add += y;
       all += y;
     }
     __syncthreads();
-    before = all;
+    sum = all;
     return x + add;
   };
   long long W = 0;
-  for (int base = 0; base < a.c.B; base += C::THREADS) {
-    const int b = base + tid;
-    int n = 0;
+  int own_n = 0;  // blocks of the thread's sequence and of all up to it, in the last round
+  long long own_upto = 0;
+  for (int round = 0; round < a.c.B; round += C::LAUNCH) {
+    const int b = few ? lane : round + tid;
+    own_n = 0;
     if (b < a.c.B) {
-      n = span_of(a, b).blocks();
+      own_n = span_of(a, b).blocks();
       const int len = a.c.seq_lens[b];
-      if (blockIdx.x == 0 && a.status && (len <= 0 || len > a.c.S_cap))
+      if (blockIdx.x == 0 && a.status && (!few || warp == 0) && (len <= 0 || len > a.c.S_cap))
         atomicOr(a.status, (len < 0 || len > a.c.S_cap ? TQ_STATUS_BAD_LEN : 0) | (len <= 0 ? TQ_STATUS_EMPTY_SEQ : 0));
     }
-    int all;
-    scan(n, all);
+    long long all;
+    own_upto = scan(own_n, all);
     W += all;
   }
   W *= a.units;
-  const long long worth = (W + a.min_blocks - 1) / a.min_blocks;
-  const int N = static_cast<int>(worth < 1 ? 1 : (worth < a.grid ? worth : a.grid));
+  const long long worth = divide(W + a.min_blocks - 1, a.min_blocks);
+  int N = static_cast<int>(worth < 1 ? 1 : (worth < a.grid ? worth : a.grid));
+  // One sequence: its units are equally long.  Shares that end where units do save the thread blocks in between a second
+  // query and merge (5 us); giving up N % units thread blocks for that lengthens the others by each (N % units) / N
+  // blocks of 0.09 us (128K tokens, 8 KV heads: 144 shares instead of 148).
+  if (a.c.B == 1 && N > a.units) {
+    const int spare = N % a.units;
+    if (spare * divide(W, N) <= 32LL * N) N -= spare;
+  }
 
   // sequences without a token: their rows are zero
   for (int b = blockIdx.x; b < a.c.B; b += gridDim.x)
     if (span_of(a, b).blocks() == 0)
-      for (int i = tid; i < a.H_q * D; i += C::THREADS) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
+      for (int i = tid; i < a.H_q * D; i += C::LAUNCH) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
   if (static_cast<int>(blockIdx.x) >= N || W == 0) return;
 
-  const long long g0 = share(W, N, blockIdx.x);
-  {
+  const Shares shares(W, N);
+  const long long g0 = shares.start(blockIdx.x);
+  int first_b;
+  long long first_at;
+  auto claim = [&](int b, int n, long long upto) {  // the sequence that holds the start of the share
+    if (n > 0 && upto * a.units > g0 && (upto - n) * a.units <= g0) {
+      s_b = b;
+      s_start = (upto - n) * a.units;
+    }
+  };
+  if (few) {
+    // the owner's lane tells its warp
+    const bool holds = own_n > 0 && own_upto * a.units > g0 && (own_upto - own_n) * a.units <= g0;
+    const int from = __ffs(static_cast<int>(__ballot_sync(0xffffffffu, holds))) - 1;
+    first_b = from;
+    first_at = __shfl_sync(0xffffffffu, (own_upto - own_n) * a.units, from);
+  } else if (a.c.B <= C::LAUNCH) {
+    claim(tid, own_n, own_upto);
+  } else {
     long long carry = 0;
-    for (int base = 0; base < a.c.B; base += C::THREADS) {
-      const int b = base + tid;
+    for (int round = 0; round < a.c.B; round += C::LAUNCH) {
+      const int b = round + tid;
       const int n = b < a.c.B ? span_of(a, b).blocks() : 0;
-      int all;
-      const long long upto = (carry + scan(n, all)) * a.units;
-      if (n > 0 && upto > g0 && upto - static_cast<long long>(n) * a.units <= g0) {
-        s_b = b;
-        s_start = upto - static_cast<long long>(n) * a.units;
-      }
+      long long all;
+      const long long upto = scan(n, all);
+      claim(b, n, carry + upto);
       carry += all;
     }
+  }
+  if (!few) {
     __syncthreads();
+    first_b = s_b;
+    first_at = s_start;
   }
   Walk use;
   use.g = g0;
-  use.g1 = share(W, N, blockIdx.x + 1);
-  use.b = s_b;
+  use.g1 = shares.start(blockIdx.x + 1);
+  use.b = first_b;
   {
     const int n = span_of(a, use.b).blocks();
-    const long long r = g0 - s_start;
-    use.u = static_cast<int>(r / n);
-    use.open(a, static_cast<int>(r % n));
+    const long long r = g0 - first_at;
+    use.u = static_cast<int>(divide(r, n));
+    use.open(a, static_cast<int>(r - static_cast<long long>(use.u) * n));
   }
 
-  // ---- the ring: lane 0 runs ahead of the arithmetic with a walk of its own
-  Walk ahead = use;
-  int ja = ahead.j0 + warp;
-  bool more = true;
-  auto settle = [&]() {  // the warp's next block may lie in a later unit
-    while (more && ja >= ahead.j1) {
-      more = ahead.next(a);
-      ja = ahead.j0 + warp;
+  if (warp == C::NW) {
+    // ---- copies: lane w fills warp w's ring, ahead of its arithmetic and on into the next units
+    bool more = lane < C::NW;
+    int j = use.j0 + lane, stage = 0;
+    uint32_t phase = 1;  // the first pass over a ring finds every stage free
+    long long since = clock64();
+    while (true) {
+      while (more && j >= use.j1) {  // the warp's next block may lie in a later unit
+        more = use.next(a);
+        j = use.j0 + lane;
+      }
+      if (!__any_sync(0xffffffffu, more)) break;
+      bool sent = false;
+      if (more && mbar_test_wait(empty(lane, stage), phase)) {
+        const uint8_t* src = block_at(a, use.b, use.h, use.span.first() + j);
+        mbar_expect_tx(full(lane, stage), C::STAGE);
+        bulk_g2s(base + (lane * C::NST + stage) * C::STAGE, src, C::STAGE, full(lane, stage));
+        j += C::NW;
+        if (++stage == C::NST) {
+          stage = 0;
+          phase ^= 1;
+        }
+        sent = true;
+      }
+      if (__any_sync(0xffffffffu, sent)) {
+        since = clock64();
+      } else {
+        if (clock64() - since > 4 * kMaxWaitCycles) break;  // its readers have given up (they report it)
+        __nanosleep(64);
+      }
     }
-  };
-  auto fetch = [&](int s) {
-    settle();
-    if (!more) return;
-    const uint8_t* src = block_at(a, ahead.b, ahead.u / a.tiles, ahead.span.first() + ja);
-    mbar_expect_tx(bars + 8 * s, C::STAGE);
-    bulk_g2s(ring + s * C::STAGE, src, C::STAGE, bars + 8 * s);
-    ja += C::NW;
-  };
-  if (lane == 0)
-    for (int s = 0; s < C::NST; ++s) fetch(s);
+    // whatever is still on its way after that lands before the warp ends (bounded)
+    if (more)
+      for (int s = 0; s < C::NST; ++s) {
+        const int at = (stage + s) % C::NST;
+        wait_stage(full(lane, at), at >= stage ? phase : phase ^ 1);
+      }
+    return;
+  }
+  auto join_warps = [&]() { asm volatile("bar.sync 1, %0;\n" ::"n"(C::THREADS) : "memory"); };
 
   int stage = 0;
   uint32_t phase = 0;
   bool dead = false;
 
   for (bool go = true; go; go = use.next(a)) {
-    const int h = use.u / a.tiles, tile = use.u - h * a.tiles;
+    const int h = use.h, tile = use.u - h * a.tiles;
     const int head0 = h * a.G + tile * 8;
     const int heads = a.G - tile * 8 < 8 ? a.G - tile * 8 : 8;
 
@@ -339,7 +418,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args 
           for (int e = 0; e < 4; ++e) qf[D == 512 ? 0 : kk][e] = w[e];
         }
       }
-      if (D == 512) __syncthreads();
+      if (D == 512) join_warps();
     }
     const float back0 = __shfl_sync(0xffffffffu, back, 8 * t4), back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
 
@@ -349,9 +428,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args 
     float M0 = kNoMax, M1 = kNoMax, P0 = kNoMax, P1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
 
     for (int j = use.j0 + warp; j < use.j1; j += C::NW) {
-      const uint32_t bar = bars + 8 * stage;
-      if (!dead && !wait_stage(bar, phase)) {
+      if (!dead && !wait_stage(full(warp, stage), phase)) {
         dead = true;
+        s_dead = 1;
         if (a.status && lane == 0) atomicOr(a.status, TQ_STATUS_TIMEOUT);
       }
       dead = __any_sync(0xffffffffu, dead);
@@ -429,7 +508,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args 
         mma16816(o[2 * kk + 1], e, v0, v1);
       }
       __syncwarp();
-      if (lane == 0) fetch(stage);
+      if (lane == 0) mbar_arrive(empty(warp, stage));
       if (++stage == C::NST) {
         stage = 0;
         phase ^= 1;
@@ -451,30 +530,42 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args 
       st[2 * C::NW * 8] = l0;
       st[2 * C::NW * 8 + 1] = l1;
     }
-    __syncthreads();
-    if (tid < 8) {
-      float m = kNoMax, p = kNoMax, l = 0.0f;
+    join_warps();
+    for (int q = warp; q < 8; q += C::NW) {
+      const bool has = lane < C::NW;
+      const float wm = has ? stats[lane * 8 + q] : kNoMax, wp = has ? stats[(C::NW + lane) * 8 + q] : kNoMax;
+      float m = wm, p = wp;
 #pragma unroll
-      for (int w = 0; w < C::NW; ++w) {
-        m = fmaxf(m, stats[w * 8 + tid]);
-        p = fmaxf(p, stats[(C::NW + w) * 8 + tid]);
+      for (int x = 1; x < 16; x <<= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+        p = fmaxf(p, __shfl_xor_sync(0xffffffffu, p, x));
       }
+      float l = has ? stats[(2 * C::NW + lane) * 8 + q] * ex2(wm - m) : 0.0f;
 #pragma unroll
-      for (int w = 0; w < C::NW; ++w) l += stats[(2 * C::NW + w) * 8 + tid] * ex2(stats[w * 8 + tid] - m);
-      sums[tid] = m;
-      sums[8 + tid] = p;
-      sums[16 + tid] = l;
-      sums[24 + tid] = ex2(p - m) / (127.0f * l);
+      for (int x = 1; x < 16; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+      if (lane == 0) {
+        sums[q] = m;
+        sums[8 + q] = p;
+        sums[16 + q] = l;
+        sums[24 + q] = ex2(p - m) / (127.0f * l);
+      }
     }
-    __syncthreads();
+    join_warps();
     const bool whole = use.j0 == 0 && use.j1 == use.n;
     const long long part = 2LL * blockIdx.x + (use.g == g0 ? 0 : 1);
     float* const mine = a.parts + part * 8 * (D + 2);
     const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
-    for (int q0 = 0; q0 < heads; q0 += C::MQ) {
-      // lanes with the queries q0 .. q0 + MQ - 1 (MQ = 2: one t4) put their channels down
-      if (2 * t4 == q0) {
-        float* row = merge + warp * C::MQ * C::ROW;
+    auto emit = [&](int q, int ch, float x, float y) {
+      x *= sums[24 + q];
+      y *= sums[24 + q];
+      if (whole) store_out2<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch, x, y);
+      else *reinterpret_cast<float2*>(mine + q * D + ch) = make_float2(x, y);
+    };
+    // rows of the warps' queries q0 .. q0 + MQ - 1 in `area`, summed over the warps
+    auto join = [&](float* area, int q0, auto mq) {
+      constexpr int MQ = decltype(mq)::value;
+      if (MQ == 8 || 2 * t4 == q0) {
+        float* row = area + (warp * MQ + (MQ == 8 ? 2 * t4 : 0)) * C::ROW;
 #pragma unroll
         for (int m = 0; m < 2 * KK; ++m) {
           row[16 * m + gid] = o[m][0] * c0;
@@ -483,63 +574,104 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) decode8_kernel(const Args 
           row[C::ROW + 16 * m + gid + 8] = o[m][3] * c1;
         }
       }
-      __syncthreads();
-      for (int i = tid; i < C::MQ * D; i += C::THREADS) {
-        const int q = i / D, ch = i - q * D;
-        float x = 0.0f;
+      join_warps();
+      for (int i = tid; i < MQ * (D / 2); i += C::THREADS) {
+        const int q = i / (D / 2), ch = 2 * (i - q * (D / 2));
+        float2 x = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < C::NW; ++w) x += merge[(w * C::MQ + q) * C::ROW + ch];
-        if (q0 + q < heads) {
-          x *= sums[24 + q0 + q];
-          if (whole) store_out<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q0 + q) * D + ch, x);
-          else mine[(q0 + q) * D + ch] = x;
+        for (int w = 0; w < C::NW; ++w) {
+          const float2 y = *reinterpret_cast<const float2*>(area + (w * MQ + q) * C::ROW + ch);
+          x.x += y.x;
+          x.y += y.y;
         }
+        if (q0 + q < heads) emit(q0 + q, ch, x.x, x.y);
       }
-      __syncthreads();
+      join_warps();
+    };
+    // On the thread block's last visit nothing is on its way into the rings any more (every warp has used what it asked
+    // for, and the barriers above are behind that): all eight rows at once through the rings' memory.
+    if (use.g + (use.j1 - use.j0) >= use.g1 && !s_dead) {
+      join(reinterpret_cast<float*>(smem), 0, std::integral_constant<int, 8>{});
+    } else {
+      for (int q0 = 0; q0 < heads; q0 += C::MQ) join(merge, q0, std::integral_constant<int, C::MQ>{});
     }
     if (!whole) {
       if (tid < 8) {
         mine[8 * D + tid] = sums[tid];
         mine[8 * D + 8 + tid] = sums[16 + tid];
       }
-      __threadfence();
-      __syncthreads();
       const long long unit = static_cast<long long>(use.b) * a.units + use.u;
       const long long u0 = use.g - use.j0, u1 = u0 + use.n;  // the unit on the line
-      const int from = owner(W, N, u0), to = owner(W, N, u1 - 1);
+      const int from = shares.owner(u0), to = shares.owner(u1 - 1);
+      join_warps();
       if (tid == 0) {
+        __threadfence();  // the block's writes, ordered before it by the barrier
         const int got = atomicAdd(a.counters + unit, 1);
         s_last = got == to - from;
         if (s_last) a.counters[unit] = 0;  // left as it was found
-      }
-      __syncthreads();
-      if (s_last) {
         __threadfence();
-        const int skip = share(W, N, from) == u0 ? 0 : 1;  // the first part is its thread block's second one
-        for (int i = tid; i < heads * D; i += C::THREADS) {
-          const int q = i / D, ch = i - q * D;
-          float m = kNoMax, l = 0.0f, x = 0.0f;
-          for (int p = from; p <= to; ++p) {
-            const float* src = a.parts + (2LL * p + (p == from ? skip : 0)) * 8 * (D + 2);
-            const float pm = __ldcg(src + 8 * D + q), pl = __ldcg(src + 8 * D + 8 + q), px = __ldcg(src + q * D + ch);
-            const float nm = fmaxf(m, pm), was = ex2(m - nm), now = pl * ex2(pm - nm);
-            l = l * was + now;
-            x = x * was + px * now;
-            m = nm;
+      }
+      join_warps();
+      if (s_last) {
+        const int skip = shares.start(from) == u0 ? 0 : 1;  // the first part is its thread block's second one
+        const int np = to - from + 1;
+        auto part_of = [&](int p) { return a.parts + (2LL * (from + p) + (p == 0 ? skip : 0)) * 8 * (D + 2); };
+        // The maxima and sums of all parts at once, one query head per warp for the weights; then the rows.  The loads are
+        // independent of each other, and the first CH rows are on their way while the weights are made (a running maximum
+        // would wait for a round trip to L2 per part: 17 us of a 64 us launch).
+        constexpr int CH = 16;
+        float* const wts = merge;  // [2][8][np]
+        float2 rows[CH];
+        const int items = heads * (D / 2);
+        const int q1 = tid / (D / 2), c1st = 2 * (tid - q1 * (D / 2));
+        if (tid < items) {
+#pragma unroll
+          for (int p = 0; p < CH; ++p)
+            if (p < np) rows[p] = __ldcg(reinterpret_cast<const float2*>(part_of(p) + q1 * D + c1st));
+        }
+        for (int i = tid; i < 8 * np; i += C::THREADS) {
+          const float* src = part_of(i >> 3) + 8 * D + (i & 7);
+          wts[(i & 7) * np + (i >> 3)] = __ldcg(src);
+          wts[8 * np + (i & 7) * np + (i >> 3)] = __ldcg(src + 8);
+        }
+        join_warps();
+        for (int q = warp; q < heads; q += C::NW) {
+          float m = kNoMax, l = 0.0f;
+          for (int p = lane; p < np; p += 32) m = fmaxf(m, wts[q * np + p]);
+#pragma unroll
+          for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+          for (int p = lane; p < np; p += 32) {
+            const float w = wts[(8 + q) * np + p] * ex2(wts[q * np + p] - m);
+            wts[q * np + p] = w;
+            l += w;
           }
-          store_out<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch, x / l);
+#pragma unroll
+          for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+          if (lane == 0) sums[q] = 1.0f / l;
+        }
+        join_warps();
+        for (int i = tid; i < items; i += C::THREADS) {
+          const int q = i / (D / 2), ch = 2 * (i - q * (D / 2));
+          float2 x = make_float2(0.0f, 0.0f);
+          for (int p0 = 0; p0 < np; p0 += CH) {
+            if (i != tid || p0 > 0) {
+#pragma unroll
+              for (int p = 0; p < CH; ++p)
+                if (p0 + p < np) rows[p] = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + p) + q * D + ch));
+            }
+#pragma unroll
+            for (int p = 0; p < CH; ++p)
+              if (p0 + p < np) {
+                x.x += wts[q * np + p0 + p] * rows[p].x;
+                x.y += wts[q * np + p0 + p] * rows[p].y;
+              }
+          }
+          store_out2<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch, x.x * sums[q], x.y * sums[q]);
         }
       }
-      __syncthreads();
+      join_warps();
     }
   }
-
-  // copies that are still on their way after a timeout land before the block ends (bounded again)
-  if (dead && lane == 0)
-    for (int s = 0; s < C::NST; ++s) {
-      const int at = (stage + s) % C::NST;
-      wait_stage(bars + 8 * at, at >= stage ? phase : phase ^ 1);
-    }
 }
 
 template <int D, int QT, int OT>
@@ -555,8 +687,9 @@ cudaError_t launch_dqo(const Args& a, cudaStream_t st) {
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
   Args x = a;
-  x.min_blocks = C::NW;
-  return launch_kernel(kernel, dim3(static_cast<unsigned>(a.grid)), dim3(C::THREADS), C::SMEM, st, x);
+  // a thread block's fixed costs are those of some four blocks per warp
+  x.min_blocks = 4 * C::NW;
+  return launch_kernel(kernel, dim3(static_cast<unsigned>(a.grid)), dim3(C::LAUNCH), C::SMEM, st, x);
 }
 
 template <int D>
@@ -569,10 +702,10 @@ cudaError_t launch_d(const Args& a, int q_type, int out_type, cudaStream_t st) {
 
 // Thread blocks of a launch: one per SM, or as many as the longest sequences could give work to.
 int decode8_grid(int B, int H_kv, int G, int d, int max_len) {
-  const long long warps = d <= 128 ? 16 : (d == 256 ? 8 : 4);
+  const long long warps = d <= 128 ? Cfg<128>::NW : (d == 256 ? Cfg<256>::NW : Cfg<512>::NW);
   const long long blocks = static_cast<long long>(B) * H_kv * ((G + 7) / 8) * ((max_len + 15LL) / 16 + 1);
-  const long long worth = (blocks + warps - 1) / warps, most = device_sm_count();
-  return static_cast<int>(worth < most ? worth : most);
+  const long long worth = (blocks + warps - 1) / warps, most = std::min(device_sm_count(), kMaxGrid);
+  return static_cast<int>(std::min(worth, most));
 }
 
 cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,

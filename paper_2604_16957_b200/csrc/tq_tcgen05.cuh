@@ -17,9 +17,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
-}
 
 // ---- tensor memory: 128 lanes x 512 columns of 32 bits.  Address: column in the low half, lane in the high half.
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t columns) {  // whole warp
