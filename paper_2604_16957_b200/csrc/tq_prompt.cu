@@ -26,6 +26,9 @@
 #include "tq_prompt.cuh"
 #include "tq_tcgen05.cuh"
 
+#ifndef TQ_POLY
+#define TQ_POLY 0
+#endif
 namespace tq {
 namespace {
 
@@ -39,6 +42,7 @@ struct Cfg {
   static constexpr int DV = D <= 256 ? D : 256;       // output channels of a thread block
   static constexpr int NSB = NQ == 2 ? 1 : 2;         // S buffers of a tile
   static constexpr int SOFT = 4 * NQ;                 // softmax warps
+  static constexpr int POLY = NQ == 2 ? TQ_POLY : 0;  // pairs in 16 whose exponentials the FMA units compute
   static constexpr int SCRUB = 2;
   static constexpr int WARPS = SOFT + 2 + SCRUB;      // softmax | TMA | MMA | scrub
   static constexpr int THREADS = 32 * WARPS;
@@ -71,10 +75,11 @@ struct Bars {
   static_assert(COUNT * 8 <= 512, "room for the barriers");
 };
 
-// Bounded wait that also gives up when another warp of the thread block has: false, and the block winds down.
+// Bounded wait that also gives up when another warp of the thread block has: false, and the block winds down.  (Inline:
+// registers cannot be moved between warps, as the kernel does, around a function call.)
 constexpr long long kTileWait = 16 * kMaxWaitCycles;  // 35 ms: a wait may span some other role's work on a few tiles
 constexpr long long kBlockWait = 1LL << 34;           // 9 s: a wait for the first tile that needs mending may span them all
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
     if (*stop) return false;
@@ -98,6 +103,61 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
   return y;
+}
+
+// ---- two fp32 values in a 64-bit register: one instruction for both
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t r) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(v.x), "=f"(v.y) : "l"(r));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if one of them is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// 2^y for two y <= 2^7 on the FMA units: y = n + f with n an integer and |f| <= 1/2, 2^f by a polynomial that is minimax
+// in the relative error on that interval (fitted by linear programming: 7.5e-5 at degree 3, 2.6e-6 at degree 4, against
+// the 2^-9 and 2^-12 of the rounding to bf16 and fp16 that follows), n added to the exponent.  The exponential unit does
+// 16 values per cycle and SM; taking a share of them off it is what lets it keep up with the tensor cores.
+template <int DT>
+__device__ __forceinline__ float2 exp2_pair(uint64_t y) {
+  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
+  const float2 v = unpair(y);
+  y = pair(fmaxf(v.x, -126.0f), fmaxf(v.y, -126.0f));
+  const uint64_t t = add2(y, pair(kMagic, kMagic));
+  const uint64_t f = fma2(add2(t, pair(-kMagic, -kMagic)), pair(-1.0f, -1.0f), y);
+  auto both = [](float x) { return pair(x, x); };
+  uint64_t p;
+  if (DT == TQ_BF16) {
+    p = fma2(both(0.05517132207751274f), f, both(0.2426113337278366f));
+    p = fma2(p, f, both(0.6932610869407654f));
+    p = fma2(p, f, both(0.9999280571937561f));
+  } else {
+    p = fma2(both(0.00957053154706955f), f, both(0.05591866374015808f));
+    p = fma2(p, f, both(0.24024735391139984f));
+    p = fma2(p, f, both(0.6931216716766357f));
+    p = fma2(p, f, both(0.9999992847442627f));
+  }
+  const float2 q = unpair(p), n = unpair(t);
+  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(n.x) << 23)),
+                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // nonzero if one of the two 16-bit values of a word is an infinity or a NaN
@@ -225,6 +285,13 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
   // not 0: a hidden key's score is -inf, and has to stay that
   const float c = fmaxf(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f);
 
+  // With two tiles the softmax threads hold a row of 128 scores each: 208 registers for them, 80 for the other warps
+  // (256 x 208 + 128 x 80 = 63488 of the 384 x 168 = 64512 that the block is launched with).
+  if (C::NQ == 2) {
+    static_assert(C::NQ == 1 || (C::THREADS == 384 && 256 * 208 + 128 * 80 <= 384 * 168), "register split");
+    if (warp < C::SOFT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
+  }
   if (mine && warp < C::SOFT) {
     // =========================================================================================== softmax, epilogue
     const int i = warp >> 2;  // query tile
@@ -260,9 +327,20 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
 #pragma unroll
         for (int x = 0; x < C::BN; ++x) s[x] = x >= from && x < to ? s[x] : -INFINITY;
       }
-      float mx = s[0];
+      float mx;
+      {
+        float m0 = max3(s[0], s[1], s[0]), m1 = max3(s[2], s[3], s[2]), m2 = max3(s[4], s[5], s[4]), m3 = max3(s[6], s[7], s[6]);
 #pragma unroll
-      for (int x = 1; x < C::BN; ++x) mx = fmaxf(mx, s[x]);
+        for (int x = 8; x < C::BN; x += 8) {
+          m0 = max3(m0, s[x], s[x + 1]);
+          m1 = max3(m1, s[x + 2], s[x + 3]);
+          m2 = max3(m2, s[x + 4], s[x + 5]);
+          m3 = max3(m3, s[x + 6], s[x + 7]);
+        }
+        mx = max3(max3(m0, m1, m2), m3, m3);
+      }
+      // a score that is no number makes the whole row none, through its sum (the polynomial below would lose it)
+      if (mx != mx) l = mx;
       const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > kSlack;
       float scale = 1.0f;
       if (raise) {
@@ -275,29 +353,42 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
         ok = warp_wait_on(bar(B::O + i), (n - 1) & 1, stop);
         if (!ok) break;
         tc_fence_after();
-        for (int x = 0; x < C::DV; x += 32) {
-          uint32_t o[32];
-          tmem_ld32(o_addr + x, o);
+#pragma unroll 1
+        for (int x = 0; x < C::DV; x += 16) {
+          uint32_t o[16];
+          tmem_ld16(o_addr + x, o);
           tmem_wait_ld();
 #pragma unroll
-          for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
-          tmem_st32(o_addr + x, o);
+          for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
+          tmem_st16(o_addr + x, o);
         }
       }
       const float mc = m == -INFINITY ? 0.0f : m * c;
-      float sum = 0.0f;
+      uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
+      const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
 #pragma unroll
       for (int x = 0; x < C::BN; x += 32) {
         uint32_t p[16];
 #pragma unroll
         for (int y = 0; y < 32; y += 2) {
-          const float p0 = ex2(fmaf(s[x + y], c, -mc)), p1 = ex2(fmaf(s[x + y + 1], c, -mc));
-          sum += p0 + p1;
-          p[y >> 1] = pack2<DT>(p0, p1);
+          const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
+          float2 e;
+          if ((y >> 1) % 16 < 16 - C::POLY) {
+            const float2 v = unpair(z);
+            e = make_float2(ex2(v.x), ex2(v.y));
+          } else {
+            e = exp2_pair<DT>(z);
+          }
+          if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
+          else sum0 = add2(sum0, pair(e.x, e.y));
+          p[y >> 1] = pack2<DT>(e.x, e.y);
         }
         tmem_st16(s_addr + (x >> 1), p);
       }
-      l += sum;
+      {
+        const float2 v = unpair(add2(sum0, sum1));
+        l = v.x + v.y;
+      }
       // The epilogue's wait for the last output MMA must find the one before it complete (a barrier tells a phase from the
       // one before, not from the one before that).  With one S buffer the scores were issued behind it.
       if (C::NSB == 2 && n > 0 && j + 1 == my1) {
@@ -410,6 +501,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     int slot = 0, scrubs = 0, n[C::NQ];
     uint32_t phase = 0;
     for (int i = 0; i < C::NQ; ++i) n[i] = 0;
+    const uint32_t q_lo = desc_lo(base, 0), ring_lo = desc_lo(base + C::RING, 0);
     bool ok = wait_on(bar(B::Q), 0, stop);
     int issued[C::NQ];  // S tiles
     for (int i = 0; i < C::NQ; ++i) issued[i] = 0;
@@ -424,12 +516,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       const int buf = C::NSB == 2 ? (issued[i] & 1) : i;
       const uint32_t d = tmem + C::S_COL + buf * C::S_STEP;
 #pragma unroll
-      for (int x = 0; x < D / 16; ++x) {
-        const uint32_t in_chunk = (x & 3) * 32;
-        const uint64_t qd = smem_desc(base + i * C::QTILE + (x >> 2) * C::QCHUNK + in_chunk, 16);
-        const uint64_t kd = smem_desc(k_at + (x >> 2) * C::KCHUNK + in_chunk, 16);
-        mma_ss(d, qd, kd, id_s, x > 0);
-      }
+      for (int x = 0; x < D / 16; ++x)
+        mma_ss(d, q_lo + i * (C::QTILE >> 4) + (((x >> 2) * C::QCHUNK + (x & 3) * 32) >> 4),
+               k_at + (((x >> 2) * C::KCHUNK + (x & 3) * 32) >> 4), kDescHi, id_s, x > 0);
       mma_commit(bar(B::S + buf));
       ++issued[i];
     };
@@ -440,17 +529,16 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       tc_fence_after();
       const uint32_t p = tmem + C::S_COL + buf * C::S_STEP, d = tmem + C::O_COL + i * C::DV;
 #pragma unroll
-      for (int x = 0; x < C::BN / 16; ++x)
-        mma_ts(d, p + 8 * x, smem_desc(v_at + 2048 * x, C::KCHUNK), id_o, n[i] > 0 || x > 0);
+      for (int x = 0; x < C::BN / 16; ++x) mma_ts(d, p + 8 * x, v_at + (2048 >> 4) * x, kDescHi, id_o, x > 0 || n[i] > 0);
       mma_commit(bar(B::O + i));
       ++n[i];
     };
     auto take = [&]() {  // the next slot's tile has landed
       ok = ok && wait_on(bar(B::FULL + slot), phase, stop);
-      return base + C::RING + slot * C::SLOT;
+      return ring_lo + slot * (C::SLOT >> 4);
     };
     auto take_v = [&](int j) {
-      const uint32_t x = take();
+      const uint32_t x = take() + ((C::KCHUNK >> 4) << 16);
       if (ok && partly(j)) {
         mbar_arrive(bar(B::ASK));
         ok = wait_on(bar(B::SCRUB), scrubs++ & 1, stop);

@@ -42,6 +42,13 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
       : "r"(addr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      : TQ_R8(r, 0), TQ_R8(r, 8)
+      : "r"(addr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
@@ -60,10 +67,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
 // Shared-memory operand in 128-byte rows, 128-byte swizzle (what a tensor map with that swizzle writes): groups of 8
 // rows are 1024 bytes apart.  K-major (rows along M or N): `lead` is not used.  MN-major (rows along K, 64 elements of
 // M or N per row): `lead` is the distance in bytes from one 64-element column of rows to the next.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
-  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | (static_cast<uint64_t>((lead & 0x3ffff) >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// Low word (advances by bytes / 16) and high word.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) { return ((addr & 0x3ffff) >> 4) | ((lead >> 4) << 16); }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+
 // kind::f16, fp32 accumulators; `bf16`: type of both operands; `mn_major_b`: rows of B run along K; `negate_a`
 __host__ __device__ constexpr uint32_t instr_desc(bool bf16, int m, int n, bool mn_major_b) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((mn_major_b ? 1u : 0u) << 16) |
@@ -71,20 +78,22 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, int m, int n, bool 
 }
 constexpr uint32_t kNegateA = 1u << 13;
 
-// D (tensor memory) = A B or D + A B; one thread issues, the operation is asynchronous
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// D (tensor memory) = A B or D + A B; one thread issues, the operation is asynchronous.  The issuing thread feeds the
+// tensor cores an instruction every 64 cycles, so little may stand between two of them: descriptors come as their
+// constant high word and a low word that is a sum of a register and a constant.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add))
+      "{\n.reg .pred p;\n.reg .b64 x, y;\nsetp.ne.u32 p, %5, 0;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add))
       : "memory");
 }
 // the same with A in tensor memory (two 16-bit elements of K per column)
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add))
+      "{\n.reg .pred p;\n.reg .b64 y;\nsetp.ne.u32 p, %5, 0;\nmov.b64 y, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add))
       : "memory");
 }
 // arrives on the mbarrier once every tcgen05.mma that this thread issued before has completed
