@@ -47,18 +47,15 @@ __device__ __forceinline__ void load_codes(const uint8_t* blk, int lane, int i, 
   } else {
     const int c = Part<D, V>::channel(lane, i);
     const uint8_t* p = blk + 16 * D + 512 * (c >> 5) + 16 * (lane & 3) + 4 * ((c & 31) >> 3);
-    uint32_t t[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = *reinterpret_cast<const uint32_t*>(p + 64 * e);
+    for (int hf = 0; hf < 2; ++hf) {
+      uint32_t t[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+      for (int e = 0; e < 4; ++e) t[e] = *reinterpret_cast<const uint32_t*>(p + 64 * (4 * hf + e));
+      turn4(t);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        uint32_t v = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v |= ((t[4 * hf + e] >> (8 * r)) & 0xffu) << (8 * e);
-        w[r][hf] = v;
-      }
+      for (int r = 0; r < 4; ++r) w[r % Part<D, V>::ROWS][hf] = t[r];
+    }
   }
 }
 
@@ -70,11 +67,13 @@ __device__ __forceinline__ void store_codes(uint8_t* blk, int lane, int i, const
     const int c = Part<D, V>::channel(lane, i);
     uint8_t* p = blk + 16 * D + 512 * (c >> 5) + 16 * (lane & 3) + 4 * ((c & 31) >> 3);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint32_t v = 0;
+    for (int hf = 0; hf < 2; ++hf) {
+      uint32_t t[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v |= ((w[r][e >> 2] >> (8 * (e & 3))) & 0xffu) << (8 * r);
-      *reinterpret_cast<uint32_t*>(p + 64 * e) = v;
+      for (int r = 0; r < 4; ++r) t[r] = w[r % Part<D, V>::ROWS][hf];
+      turn4(t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(p + 64 * (4 * hf + e)) = t[e];
     }
   }
 }
@@ -113,23 +112,37 @@ __device__ __forceinline__ void append_run(uint8_t* blk, const uint16_t* src, lo
   }
   float* range = reinterpret_cast<float*>(blk + range8_offset(D, V));
   const float a_old = off > 0 ? *range : 0.0f;
-  float top = 0.0f;
+  // magnitudes as integers, two to a word; an infinity or a NaN is above every finite one
+  uint32_t top = 0;
 #pragma unroll
   for (int r = 0; r < P::ROWS; ++r)
 #pragma unroll(kHold ? P::VECS : 4)
     for (int i = 0; i < P::VECS; ++i) {
       const uint4 y = kHold ? x[r][kHold ? i : 0] : load(r, i);
-      const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2<DT>(w[e]);
-        top = fmaxf(top, fmaxf(fabsf(finite8<DT>(f.x)), fabsf(finite8<DT>(f.y))));
-      }
+      top = __vmaxu2(__vmaxu2(top, __vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu)), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu));
     }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const float a_new = fmaxf(a_old, top);
-  const Div8 q = div8(a_new);
+  top = max(top & 0xffffu, top >> 16);
+  constexpr uint32_t kInf = DT == TQ_BF16 ? 0x7f80u : 0x7c00u;
+  const bool odd = __any_sync(0xffffffffu, top >= kInf);
+  if (odd) {
+    top = 0;
+#pragma unroll 1
+    for (int r = 0; r < P::ROWS; ++r)
+#pragma unroll 1
+      for (int i = 0; i < P::VECS; ++i) {
+        const uint4 y = load(r, i);
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t z = finite8<DT>(w[e]) & 0x7fff7fffu;
+          top = max(top, max(z & 0xffffu, z >> 16));
+        }
+      }
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  const float a_new = fmaxf(a_old, unpack2<DT>(top).x);
+  const Div8 q(a_new);
+  const float m127 = __fmul_rn(q.scale, 127.0f);
+  const uint64_t fresh_mul = pair(m127, m127), older_mul = pair(__fmul_rn(a_old, q.scale), __fmul_rn(a_old, q.scale));
 #pragma unroll(kHold ? P::VECS : 1)
   for (int i = 0; i < P::VECS; ++i) {
     uint32_t w[P::ROWS][2];
@@ -143,28 +156,20 @@ __device__ __forceinline__ void append_run(uint8_t* blk, const uint16_t* src, lo
     for (int r = 0; r < P::ROWS; ++r) {
       if (fresh[r]) {
         const uint4 y = kHold ? x[r][kHold ? i : 0] : load(r, i);
-        const uint32_t v[4] = {y.x, y.y, y.z, y.w};
-        uint32_t out[2] = {0, 0};
+        uint32_t v[4] = {y.x, y.y, y.z, y.w};
+        if (odd) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = unpack2<DT>(v[e]);
-          const uint32_t lo = static_cast<uint32_t>(code8(finite8<DT>(f.x), q) + 128) & 0xffu;
-          const uint32_t hi = static_cast<uint32_t>(code8(finite8<DT>(f.y), q) + 128) & 0xffu;
-          out[e >> 1] |= (lo | hi << 8) << (16 * (e & 1));
+          for (int e = 0; e < 4; ++e) v[e] = finite8<DT>(v[e]);
         }
-        w[r][0] = out[0];
-        w[r][1] = out[1];
-      } else if (older[r] && a_new != a_old) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          uint32_t v = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int c = static_cast<int>((w[r][hf] >> (8 * e)) & 0xffu) - 128;
-            v |= (static_cast<uint32_t>(recode8(c, a_old, q) + 128) & 0xffu) << (8 * e);
-          }
-          w[r][hf] = v;
+          const float2 f = unpack2<DT>(v[2 * hf]), g = unpack2<DT>(v[2 * hf + 1]);
+          w[r][hf] = low_bytes(q.codes(mul2(pair(f.x, f.y), fresh_mul)), q.codes(mul2(pair(g.x, g.y), fresh_mul)));
         }
+      } else if (older[r] && a_new != a_old) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+          w[r][hf] = low_bytes(q.codes(mul2(codes_of(w[r][hf], 0), older_mul)), q.codes(mul2(codes_of(w[r][hf], 1), older_mul)));
       } else if (!older[r]) {
         w[r][0] = w[r][1] = 0x80808080u;
       }
@@ -184,11 +189,13 @@ __global__ void __launch_bounds__(32 * kWarps) append_kernel(tq_kv8_cache c, Slo
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31;
-  const int unit = blockIdx.y * kWarps + (threadIdx.x >> 5);  // (KV head, K or V)
+  // the units (KV head, K or V) of a chunk of rows are neighbours in the grid: their rows lie side by side in memory
+  const int groups = (2 * c.H_kv + kWarps - 1) / kWarps;
+  const int unit = static_cast<int>(blockIdx.x % groups) * kWarps + (threadIdx.x >> 5);
   if (unit >= 2 * c.H_kv) return;
   const int h = unit >> 1;
   const bool is_v = unit & 1;
-  const long long base = static_cast<long long>(blockIdx.x) * chunk;
+  const long long base = static_cast<long long>(blockIdx.x / groups) * chunk;
   const long long n = base + lane;
   int64_t s = -1, prev = -1;
   if (lane < chunk && n < a.n) {
@@ -235,8 +242,11 @@ __device__ __forceinline__ void gather_run(const uint8_t* blk, void* dst, long l
       if (t < 0 || t >= len) continue;
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        f[e] = __fmul_rn(__int2float_rn(static_cast<int>((w[r][e >> 2] >> (8 * (e & 3))) & 0xffu) - 128), scale);
+      for (int e = 0; e < 4; ++e) {
+        const float2 v = unpair(mul2(codes_of(w[r][e >> 1], e & 1), pair(scale, scale)));
+        f[2 * e] = v.x;
+        f[2 * e + 1] = v.y;
+      }
       const long long at = t * stride + P::channel(lane, i);
       if (DT == TQ_FP32) {
         float4* o = reinterpret_cast<float4*>(static_cast<float*>(dst) + at);
@@ -256,12 +266,13 @@ __global__ void __launch_bounds__(32 * kWarps) gather_kernel(tq_kv8_cache c, Slo
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31;
-  const int unit = blockIdx.y * kWarps + (threadIdx.x >> 5);
+  const int groups = (2 * c.H_kv + kWarps - 1) / kWarps;
+  const int unit = static_cast<int>(blockIdx.x % groups) * kWarps + (threadIdx.x >> 5);
   if (unit >= 2 * c.H_kv) return;
   const int h = unit >> 1;
   const bool is_v = unit & 1;
   constexpr int kBytes = DT == TQ_FP32 ? 4 : 2;
-  const long long base = static_cast<long long>(blockIdx.x) * chunk;
+  const long long base = static_cast<long long>(blockIdx.x / groups) * chunk;
   const long long n = base + lane;
   const bool mine = lane < chunk && n < a.n;
   int64_t s = -1, prev = -1;
@@ -303,7 +314,9 @@ template <int D>
 cudaError_t append_d(const tq_kv8_cache& c, const Slots8& a, const void* k, const void* v, int dtype, long long k_stride,
                      long long v_stride, int32_t* status, cudaStream_t st) {
   const int chunk = chunk_of(c, a.n);
-  const dim3 grid(static_cast<unsigned>((a.n + chunk - 1) / chunk), (2 * c.H_kv + kWarps - 1) / kWarps);
+  const long long blocks = (a.n + chunk - 1) / chunk * ((2 * c.H_kv + kWarps - 1) / kWarps);
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  const dim3 grid(static_cast<unsigned>(blocks));
   auto kp = static_cast<const uint16_t*>(k), vp = static_cast<const uint16_t*>(v);
   if (dtype == TQ_BF16)
     return launch_kernel(append_kernel<D, TQ_BF16>, grid, dim3(32 * kWarps), 0, st, c, a, kp, vp, k_stride, v_stride, chunk, status);
@@ -313,7 +326,9 @@ cudaError_t append_d(const tq_kv8_cache& c, const Slots8& a, const void* k, cons
 template <int D>
 cudaError_t gather_d(const tq_kv8_cache& c, const Slots8& a, void* k, void* v, int dtype, int32_t* status, cudaStream_t st) {
   const int chunk = chunk_of(c, a.n);
-  const dim3 grid(static_cast<unsigned>((a.n + chunk - 1) / chunk), (2 * c.H_kv + kWarps - 1) / kWarps);
+  const long long blocks = (a.n + chunk - 1) / chunk * ((2 * c.H_kv + kWarps - 1) / kWarps);
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  const dim3 grid(static_cast<unsigned>(blocks));
   if (dtype == TQ_BF16) return launch_kernel(gather_kernel<D, TQ_BF16>, grid, dim3(32 * kWarps), 0, st, c, a, k, v, chunk, status);
   if (dtype == TQ_FP32) return launch_kernel(gather_kernel<D, TQ_FP32>, grid, dim3(32 * kWarps), 0, st, c, a, k, v, chunk, status);
   return launch_kernel(gather_kernel<D, TQ_FP16>, grid, dim3(32 * kWarps), 0, st, c, a, k, v, chunk, status);

@@ -12,7 +12,9 @@
 // products 127 x and c a_old are exact in binary32, and of such a quotient u / a one correctly rounded division cannot
 // land on the other side of a half: u / a = k + 1/2 exactly is computed exactly, and otherwise |u / a - (k + 1/2)| >=
 // ulp(x) / (2 a) >= (u / a) / 127 / 2^12 -- 1.9e-6 of the quotient, against 6e-8 of rounding.  So every code is
-// round_half_even of the true quotient.
+// round_half_even of the true quotient.  The division is Markstein's: with r the rounded reciprocal of a, q = u r and
+// the exact remainder u - q a (one fused operation), q + r (u - q a) is the correctly rounded quotient; three packed
+// instructions for two values instead of a division sequence for each.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -48,27 +50,84 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 // What the quantiser makes of a value that is no number or no finite one: 0, or the largest finite value of the type.
 template <int DT>
-__device__ __forceinline__ float finite8(float x) {
-  constexpr float top = DT == TQ_BF16 ? 3.38953139e38f : 65504.0f;
-  if (x != x) return 0.0f;
-  return fminf(fmaxf(x, -top), top);
+__device__ __forceinline__ uint32_t finite8(uint32_t w) {
+  constexpr uint32_t inf = DT == TQ_BF16 ? 0x7f80u : 0x7c00u;
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t x = (w >> (16 * i)) & 0xffffu, mag = x & 0x7fffu;
+    out |= (mag > inf ? 0u : (mag == inf ? x - 1 : x)) << (16 * i);
+  }
+  return out;
 }
 
-// The divisor and the factor that make a code of a value: round(x * mul / div).  127 * x would leave binary32 for
-// ranges near its top; both sides are scaled by 2^-32 there, exactly for every x that is not 0 after it anyway.
+// ---- two fp32 values in a 64-bit register: one instruction for both
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t r) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(v.x), "=f"(v.y) : "l"(r));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Division by the range a.  Everything is scaled by a power of two that brings a into [1, 4) -- 2^-126 to 2^120, which
+// leaves the smallest ranges of bf16 at 2^-13 --, so that nothing overflows or loses digits; a value that this makes
+// subnormal has the code 0 anyway.
 struct Div8 {
-  float div, mul;
+  float scale;  // that power of two
+  uint64_t div, rcp;  // a * scale and its rounded reciprocal, twice each
+  __device__ explicit Div8(float a) {
+    const int e = static_cast<int>(__float_as_uint(a) >> 23);  // biased exponent; 0 for 0 and subnormals
+    scale = __uint_as_float(static_cast<uint32_t>(a > 0.0f ? min(max(254 - e, 1), 247) : 127) << 23);
+    const float d = a > 0.0f ? __fmul_rn(a, scale) : 1.0f;
+    const float r = __fdiv_rn(1.0f, d);
+    div = pair(-d, -d);
+    rcp = pair(r, r);
+  }
+  // stored codes (low bytes of the two words) of two exact products u (already scaled)
+  __device__ __forceinline__ uint64_t codes(uint64_t u) const {
+    constexpr float kMagic = 12582912.0f + 128.0f;  // 1.5 * 2^23 rounds to an integer, half to even; + 128 as stored
+    const uint64_t q = mul2(u, rcp);
+    const uint64_t exact = fma2(fma2(q, div, u), rcp, q);
+    return add2(exact, pair(kMagic, kMagic));
+  }
 };
-__device__ __forceinline__ Div8 div8(float a) {
-  if (a > 1.0e30f) return {a * 2.3283064365386963e-10f, 2.3283064365386963e-10f};
-  return {a > 0.0f ? a : 1.0f, 1.0f};
+__device__ __forceinline__ uint32_t low_bytes(uint64_t a, uint64_t b) {  // of four fp32 words
+  const float2 x = unpair(a), y = unpair(b);
+  return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
+                     __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
-__device__ __forceinline__ int code8(float x, Div8 q) {
-  return __float2int_rn(__fdiv_rn(__fmul_rn(__fmul_rn(x, q.mul), 127.0f), q.div));
+// bytes 2i, 2i + 1 of a word of stored codes as two exact fp32 codes
+__device__ __forceinline__ uint64_t codes_of(uint32_t w, int i) {
+  const uint32_t lo = __byte_perm(w, 0x4b000000u, i ? 0x7442 : 0x7440), hi = __byte_perm(w, 0x4b000000u, i ? 0x7443 : 0x7441);
+  return add2(pair(__uint_as_float(lo), __uint_as_float(hi)), pair(-8388736.0f, -8388736.0f));  // 2^23 + 128
 }
-// an older code under the range a_old, under the new one
-__device__ __forceinline__ int recode8(int c, float a_old, Div8 q) {
-  return __float2int_rn(__fdiv_rn(__fmul_rn(__int2float_rn(c), __fmul_rn(a_old, q.mul)), q.div));
+// 4 x 4 bytes turned around: byte i of out[j] = byte j of w[i]
+__device__ __forceinline__ void turn4(uint32_t (&w)[4]) {
+  const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[0], w[1], 0x7362);
+  const uint32_t c = __byte_perm(w[2], w[3], 0x5140), d = __byte_perm(w[2], w[3], 0x7362);
+  w[0] = __byte_perm(a, c, 0x5410);
+  w[1] = __byte_perm(a, c, 0x7632);
+  w[2] = __byte_perm(b, d, 0x5410);
+  w[3] = __byte_perm(b, d, 0x7632);
 }
 
 // Slots of one call (append and gather).  A slot is page * page_tokens + position in the page (contiguous: sequence *

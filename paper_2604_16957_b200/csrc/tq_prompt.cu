@@ -12,10 +12,16 @@
 // d = 512 the accumulator of a row does not fit TMEM: a thread block computes 256 of the 512 output channels, and S is
 // computed twice.
 //
-// Roles: one warpgroup of softmax threads per tile; a warp that issues TMA loads; a warp that issues the MMAs; two
-// warps that look through the V tiles which some row sees in part.  Those may hold tokens of a neighbouring sequence
-// or of the row's future, whose weight is 0, and 0 * inf is not 0: a value there that is no finite number is
-// replaced by 0 in shared memory, and the rows that do see it get it added back in the epilogue from global memory.
+// Roles: one warpgroup of softmax threads per tile; a warp that finds the work and issues the TMA loads; a warp per tile
+// that issues its MMAs (one issuing thread could not keep the tensor cores busy over its waits: 1.09 ms for the 8K
+// prompt); one or two warps that look through the V tiles which some row sees in part.  Those may hold tokens of a
+// neighbouring sequence or of the row's future, whose weight is 0, and 0 * inf is not 0: a value there that is no finite
+// number is replaced by 0 in shared memory, and the rows that do see it get it added back in the epilogue from global
+// memory.
+//
+// A thread block starts with the tile of its own index and then takes over thread blocks of the grid that have not
+// started (cluster launch control), so the loads and the first scores of the next tile run under the last softmax and the
+// epilogue of this one, and tiles of very different cost (causal masks, ragged lengths) even out.
 //
 // What bounds it: at d = 128 a 128 x 128 tile costs the tensor cores 1024 cycles and the exponential unit 1024 cycles (16
 // per cycle and SM).
@@ -43,8 +49,8 @@ struct Cfg {
   static constexpr int NSB = NQ == 2 ? 1 : 2;         // S buffers of a tile
   static constexpr int SOFT = 4 * NQ;                 // softmax warps
   static constexpr int POLY = NQ == 2 ? TQ_POLY : 0;  // pairs in 16 whose exponentials the FMA units compute
-  static constexpr int SCRUB = 2;
-  static constexpr int WARPS = SOFT + 2 + SCRUB;      // softmax | TMA | MMA | scrub
+  static constexpr int SCRUB = NQ == 2 ? 1 : 2;
+  static constexpr int WARPS = SOFT + 1 + NQ + SCRUB;  // softmax | work and TMA | MMA | scrub
   static constexpr int THREADS = 32 * WARPS;
   static constexpr int QCHUNK = 128 * 128;            // bytes of 128 rows x 64 channels
   static constexpr int QTILE = (D / 64) * QCHUNK;
@@ -69,16 +75,19 @@ struct Maps {
 template <int D>
 struct Bars {
   using C = Cfg<D>;
-  static constexpr int FULL = 0, EMPTY = FULL + C::NS, Q = EMPTY + C::NS, S = Q + 1, P = S + C::NQ * C::NSB,
-                       O = P + C::NQ * C::NSB, ASK = O + C::NQ, SCRUB = ASK + 1, DRAIN = SCRUB + 1,
-                       COUNT = DRAIN + 1;
+  static constexpr int FULL = 0, EMPTY = FULL + C::NS, READY = EMPTY + C::NS;  // K / V slots: landed, free, looked through
+  static constexpr int Q = READY + C::NS, Q_FREE = Q + 1;
+  static constexpr int S = Q_FREE + 1, P = S + C::NQ * C::NSB, P2 = P + C::NQ * C::NSB;  // scores, weights (two halves)
+  static constexpr int O = P2 + C::NQ * C::NSB;                                          // outputs
+  static constexpr int WORK = O + C::NQ, WORK_FREE = WORK + 2, STEAL = WORK_FREE + 2, TURN = STEAL + 1,
+                       DRAIN = TURN + 2, COUNT = DRAIN + 1;
   static_assert(COUNT * 8 <= 512, "room for the barriers");
 };
 
 // Bounded wait that also gives up when another warp of the thread block has: false, and the block winds down.  (Inline:
 // registers cannot be moved between warps, as the kernel does, around a function call.)
 constexpr long long kTileWait = 16 * kMaxWaitCycles;  // 35 ms: a wait may span some other role's work on a few tiles
-constexpr long long kBlockWait = 1LL << 34;           // 9 s: a wait for the first tile that needs mending may span them all
+constexpr long long kBlockWait = 1LL << 34;           // 9 s: a wait for the next piece of work may span a whole sequence
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
@@ -94,6 +103,22 @@ __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile 
   if (mbar_try_wait(bar, parity)) return true;
   return wait_slow(bar, parity, stop, limit);
 }
+#ifndef TQ_SPIN
+#define TQ_SPIN 3
+#endif
+// the same, polled: sooner awake than a wait that lets the hardware suspend the thread
+__device__ __forceinline__ bool poll_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
+#pragma unroll 1
+  for (int i = 0; i < 256; ++i)
+    if (mbar_test_wait(bar, parity)) return true;
+  return wait_slow(bar, parity, stop, limit);
+}
+__device__ __forceinline__ bool wait_stage_inline(uint32_t bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > limit) return false;
+  return true;
+}
 // the same for a whole warp: all its lanes go on, or none
 __device__ __forceinline__ bool warp_wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
   return __all_sync(0xffffffffu, wait_on(bar, parity, stop, limit));
@@ -105,27 +130,6 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// ---- two fp32 values in a 64-bit register: one instruction for both
-__device__ __forceinline__ uint64_t pair(float x, float y) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t r) {
-  float2 v;
-  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(v.x), "=f"(v.y) : "l"(r));
-  return v;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if one of them is
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -166,28 +170,42 @@ __device__ __forceinline__ uint32_t not_finite2(uint32_t w) {
   return ((w & 0x7fff7fffu) + (DT == TQ_BF16 ? 0x00800080u : 0x04000400u)) & 0x80008000u;
 }
 
-// What a thread block works on, the same for all its warps.
+// One piece of work, the same for all warps: NQ tiles of a sequence and a KV head.
 struct Work {
   PromptSeq s;
-  int h;           // KV head
-  int tok0;        // first query token of tile 0
-  int T;           // tokens of a tile
-  int lo_all, up_all;    // keys that some row sees
-  int lo_every, up_every;  // keys that every row sees
+  int h, half;  // KV head; half of the output channels (d = 512)
+  int tok0;     // first query token of tile 0
+  int more;     // 0: there is none
 };
 
-// Key tiles [j0, j1) of query tile i (empty: j0 >= j1).
-template <int BN>
-__device__ __forceinline__ void tile_range(const PromptArgs& a, const Work& w, int i, int& j0, int& j1) {
-  const int first = w.tok0 + i * w.T, last = min(first + w.T, w.s.lq) - 1;
-  j0 = j1 = 0;
-  if (last < first) return;
-  int lo, up, lo2, up2;
-  prompt_keys(a, w.s, first, lo, up);
-  prompt_keys(a, w.s, last, lo2, up2);
-  j0 = lo / BN;
-  j1 = (up2 + BN - 1) / BN;
-}
+// Key tiles of a piece of work: [j0, j1) of each query tile, [J0, J1) of all; the keys that every query sees are
+// [lo, up).
+template <int D>
+struct Span {
+  using C = Cfg<D>;
+  int j0[C::NQ], j1[C::NQ], J0, J1, lo, up;
+  __device__ Span(const PromptArgs& a, const Work& w, int T) : J0(0), J1(0) {
+    int x, y;
+#pragma unroll
+    for (int i = 0; i < C::NQ; ++i) {
+      const int first = w.tok0 + i * T, last = min(first + T, w.s.lq) - 1;
+      j0[i] = j1[i] = 0;
+      if (last < first) continue;
+      int lo1, up1;
+      prompt_keys(a, w.s, first, x, y);
+      prompt_keys(a, w.s, last, lo1, up1);
+      j0[i] = x / C::BN;
+      j1[i] = (up1 + C::BN - 1) / C::BN;
+      if (j1[i] <= j0[i]) continue;
+      J0 = J1 == J0 ? j0[i] : min(J0, j0[i]);
+      J1 = max(J1, j1[i]);
+    }
+    prompt_keys(a, w.s, w.tok0, x, up);
+    prompt_keys(a, w.s, min(w.tok0 + C::NQ * T, w.s.lq) - 1, lo, y);
+  }
+  __device__ bool in(int i, int j) const { return j >= j0[i] && j < j1[i]; }
+  __device__ bool partly(int j) const { return j * C::BN < lo || (j + 1) * C::BN > up; }
+};
 
 template <int D, int DT, int OT>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps maps, const PromptArgs a,
@@ -195,8 +213,10 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
   using C = Cfg<D>;
   using B = Bars<D>;
   extern __shared__ uint8_t raw[];
+  __shared__ __align__(16) uint4 s_answer;
+  __shared__ Work s_work[2];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_stop, s_scrubbed, s_seq;
+  __shared__ int s_stop, s_scrubbed[4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
   uint8_t* const smem = raw + (base - smem_addr(raw));
@@ -208,82 +228,33 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
   if (tid == 0) {
     for (int i = 0; i < C::NS; ++i) {
       mbar_init(bar(B::FULL + i), 1);
-      mbar_init(bar(B::EMPTY + i), 1);
+      mbar_init(bar(B::EMPTY + i), C::NQ + C::SCRUB);
+      mbar_init(bar(B::READY + i), C::SCRUB);
     }
     mbar_init(bar(B::Q), 1);
+    mbar_init(bar(B::Q_FREE), C::NQ);
     for (int i = 0; i < C::NQ * C::NSB; ++i) {
       mbar_init(bar(B::S + i), 1);
       mbar_init(bar(B::P + i), 4);
+      mbar_init(bar(B::P2 + i), 4);
     }
     for (int i = 0; i < C::NQ; ++i) mbar_init(bar(B::O + i), 1);
-    mbar_init(bar(B::ASK), 1);
-    mbar_init(bar(B::SCRUB), C::SCRUB);
-    mbar_init(bar(B::DRAIN), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(B::WORK + i), 1);
+      mbar_init(bar(B::WORK_FREE + i), C::WARPS - 1);
+    }
+    mbar_init(bar(B::STEAL), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(bar(B::TURN + i), 1);
+    mbar_init(bar(B::DRAIN), C::NQ);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     s_stop = 0;
-    s_scrubbed = 0;
-  }
-  pdl_launch_dependents();
-  pdl_wait();
-
-  // ---- which tile: sequence b starts at tile q_offsets[b] / TT + b, which leaves room for its ceil(lq / TT) tiles.  The
-  // late tiles of a sequence see the most keys under the causal mask and go first.
-  const int TT = C::NQ * T;
-  const int halves = D / C::DV;
-  int at = blockIdx.x;
-  const int half = at % halves;
-  at /= halves;
-  Work w;
-  w.T = T;
-  w.h = at % a.H_kv;
-  const int tile = a.n_q / TT + a.B - 1 - at / a.H_kv;
-  if (tid == 0) {
-    int b = 0, hi = a.B;
-    while (hi - b > 1) {
-      const int mid = (b + hi) >> 1;
-      if (min(max(a.q_offsets[mid], 0), a.n_q) / TT + mid <= tile) b = mid;
-      else hi = mid;
-    }
-    s_seq = b;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const int b = s_seq;
   const uint32_t tmem = s_tmem;
-  w.s = prompt_seq(a, b, false);
-  w.tok0 = (tile - (w.s.q0 / TT + b)) * TT;
-  const bool mine = w.tok0 >= 0 && w.tok0 < w.s.lq;
-  if (mine && w.tok0 == 0 && w.h == 0 && tid == 0) (void)prompt_seq(a, b, true);  // one reports for the sequence
-
-  int J0 = 0, J1 = 0, j0[C::NQ], j1[C::NQ];
-#pragma unroll
-  for (int i = 0; i < C::NQ; ++i) {
-    j0[i] = j1[i] = 0;
-    if (mine) tile_range<C::BN>(a, w, i, j0[i], j1[i]);
-    if (j1[i] > j0[i]) {
-      if (J1 == J0) {
-        J0 = j0[i];
-        J1 = j1[i];
-      } else {
-        J0 = min(J0, j0[i]);
-        J1 = max(J1, j1[i]);
-      }
-    }
-  }
-  {
-    // what every valid row sees: from the last token's first key to the first token's last one
-    const int last = min(w.tok0 + TT, w.s.lq) - 1;
-    int x, y;
-    prompt_keys(a, w.s, w.tok0, w.lo_all, w.up_every);
-    prompt_keys(a, w.s, last, x, y);
-    w.lo_every = x;
-    w.up_all = y;
-  }
-  auto in = [&](int i, int j) { return j >= j0[i] && j < j1[i]; };
-  auto partly = [&](int j) { return j * C::BN < w.lo_every || (j + 1) * C::BN > w.up_every; };
-  // not 0: a hidden key's score is -inf, and has to stay that
-  const float c = fmaxf(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f);
+  pdl_launch_dependents();
+  pdl_wait();
 
   // With two tiles the softmax threads hold a row of 128 scores each: 208 registers for them, 80 for the other warps
   // (256 x 208 + 128 x 80 = 63488 of the 384 x 168 = 64512 that the block is launched with).
@@ -292,343 +263,453 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     if (warp < C::SOFT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
   }
-  if (mine && warp < C::SOFT) {
+
+  // the it-th piece of work, for every warp but the one that finds it; false: none, or the block winds down
+  auto next_work = [&](int it, Work& w) {
+    if (!warp_wait_on(bar(B::WORK + (it & 1)), (it >> 1) & 1, stop, kBlockWait)) return false;
+    w = s_work[it & 1];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B::WORK_FREE + (it & 1)));
+    return w.more != 0;
+  };
+
+  if (warp < C::SOFT) {
     // =========================================================================================== softmax, epilogue
     const int i = warp >> 2;  // query tile
     const int row = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t o_addr = tmem + C::O_COL + i * C::DV + lanes;
     const int t = row / G;
-    const int tok = w.tok0 + i * T + t;
-    const bool real = row < T * G && tok < w.s.lq;
-    int lo = 0, up = 0;
-    if (real) prompt_keys(a, w.s, tok, lo, up);
-    float m = -INFINITY, l = 0.0f;
+    // not 0: a hidden key's score is -inf, and has to stay that
+    const float c = fmaxf(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f);
     bool ok = true;
-    int n = 0;  // K / V tiles of this query tile so far
-    int my0 = j0[0], my1 = j1[0];
-    if (C::NQ == 2 && i == 1) {
-      my0 = j0[C::NQ - 1];
-      my1 = j1[C::NQ - 1];
-    }
-    for (int j = my0; j < my1 && ok; ++j, ++n) {
-      const int buf = C::NSB == 2 ? (n & 1) : i;
-      const uint32_t s_addr = tmem + C::S_COL + buf * C::S_STEP + lanes;
-      ok = warp_wait_on(bar(B::S + buf), (C::NSB == 2 ? n >> 1 : n) & 1, stop);
-      if (!ok) break;
-      tc_fence_after();
-      float s[C::BN];
-#pragma unroll
-      for (int x = 0; x < C::BN; x += 32) tmem_ld32(s_addr + x, reinterpret_cast<uint32_t*>(s) + x);
-      tmem_wait_ld();
-      const int k0 = j * C::BN;
-      if (__any_sync(0xffffffffu, lo > k0 || up < k0 + C::BN)) {
-        const int from = lo - k0, to = up - k0;
-#pragma unroll
-        for (int x = 0; x < C::BN; ++x) s[x] = x >= from && x < to ? s[x] : -INFINITY;
-      }
-      float mx;
-      {
-        float m0 = max3(s[0], s[1], s[0]), m1 = max3(s[2], s[3], s[2]), m2 = max3(s[4], s[5], s[4]), m3 = max3(s[6], s[7], s[6]);
-#pragma unroll
-        for (int x = 8; x < C::BN; x += 8) {
-          m0 = max3(m0, s[x], s[x + 1]);
-          m1 = max3(m1, s[x + 2], s[x + 3]);
-          m2 = max3(m2, s[x + 4], s[x + 5]);
-          m3 = max3(m3, s[x + 6], s[x + 7]);
-        }
-        mx = max3(max3(m0, m1, m2), m3, m3);
-      }
-      // a score that is no number makes the whole row none, through its sum (the polynomial below would lose it)
-      if (mx != mx) l = mx;
-      const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > kSlack;
-      float scale = 1.0f;
-      if (raise) {
-        scale = m == -INFINITY ? 0.0f : ex2((m - mx) * c);
-        m = mx;
-        l *= scale;
-      }
-      if (n > 0 && __any_sync(0xffffffffu, raise)) {
-        // O of the tiles before is complete once its MMA has arrived on O
-        ok = warp_wait_on(bar(B::O + i), (n - 1) & 1, stop);
+    uint32_t total = 0;  // K / V tiles of this query tile in all work so far
+    Work w;
+    for (int it = 0; ok && next_work(it, w); ++it) {
+      const Span<D> r(a, w, T);
+      const int tok = w.tok0 + i * T + t;
+      const bool real = row < T * G && tok < w.s.lq;
+      int lo = 0, up = 0;
+      if (real) prompt_keys(a, w.s, tok, lo, up);
+      float m = -INFINITY, l = 0.0f;
+      int n = 0;  // K / V tiles of this work
+      const int my0 = i == 0 ? r.j0[0] : r.j0[C::NQ - 1], my1 = i == 0 ? r.j1[0] : r.j1[C::NQ - 1];
+      for (int j = my0; j < my1 && ok; ++j, ++n) {
+        const uint32_t use = total + n;
+        const int buf = C::NSB == 2 ? (use & 1) : i;
+        const uint32_t s_addr = tmem + C::S_COL + buf * C::S_STEP + lanes;
+        ok = __all_sync(0xffffffffu, (TQ_SPIN & 2) ? poll_on(bar(B::S + buf), (C::NSB == 2 ? use >> 1 : use) & 1, stop) : wait_on(bar(B::S + buf), (C::NSB == 2 ? use >> 1 : use) & 1, stop));
         if (!ok) break;
         tc_fence_after();
-#pragma unroll 1
-        for (int x = 0; x < C::DV; x += 16) {
-          uint32_t o[16];
-          tmem_ld16(o_addr + x, o);
-          tmem_wait_ld();
+        float s[C::BN];
 #pragma unroll
-          for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
-          tmem_st16(o_addr + x, o);
+        for (int x = 0; x < C::BN; x += 32) tmem_ld32(s_addr + x, reinterpret_cast<uint32_t*>(s) + x);
+        tmem_wait_ld();
+        const int k0 = j * C::BN;
+        if (__any_sync(0xffffffffu, lo > k0 || up < k0 + C::BN)) {
+          const int from = lo - k0, to = up - k0;
+#pragma unroll
+          for (int x = 0; x < C::BN; ++x) s[x] = x >= from && x < to ? s[x] : -INFINITY;
         }
-      }
-      const float mc = m == -INFINITY ? 0.0f : m * c;
-      uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
-      const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
+        float mx;
+        {
+          float m0 = max3(s[0], s[1], s[0]), m1 = max3(s[2], s[3], s[2]), m2 = max3(s[4], s[5], s[4]), m3 = max3(s[6], s[7], s[6]);
 #pragma unroll
-      for (int x = 0; x < C::BN; x += 32) {
-        uint32_t p[16];
-#pragma unroll
-        for (int y = 0; y < 32; y += 2) {
-          const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
-          float2 e;
-          if ((y >> 1) % 16 < 16 - C::POLY) {
-            const float2 v = unpair(z);
-            e = make_float2(ex2(v.x), ex2(v.y));
-          } else {
-            e = exp2_pair<DT>(z);
+          for (int x = 8; x < C::BN; x += 8) {
+            m0 = max3(m0, s[x], s[x + 1]);
+            m1 = max3(m1, s[x + 2], s[x + 3]);
+            m2 = max3(m2, s[x + 4], s[x + 5]);
+            m3 = max3(m3, s[x + 6], s[x + 7]);
           }
-          if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
-          else sum0 = add2(sum0, pair(e.x, e.y));
-          p[y >> 1] = pack2<DT>(e.x, e.y);
+          mx = max3(max3(m0, m1, m2), m3, m3);
         }
-        tmem_st16(s_addr + (x >> 1), p);
-      }
-      {
-        const float2 v = unpair(add2(sum0, sum1));
-        l = v.x + v.y;
-      }
-      // The epilogue's wait for the last output MMA must find the one before it complete (a barrier tells a phase from the
-      // one before, not from the one before that).  With one S buffer the scores were issued behind it.
-      if (C::NSB == 2 && n > 0 && j + 1 == my1) {
-        ok = warp_wait_on(bar(B::O + i), (n - 1) & 1, stop);
-        if (!ok) break;
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B::P + buf));
-    }
-    // ---- epilogue: the thread's row of O
-    if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), (n - 1) & 1, stop);
-    if (ok) {
-      tc_fence_after();
-      const float inv = up > lo ? 1.0f / l : 0.0f;
-      const bool mend = s_scrubbed != 0;
-      const int head = w.h * G + (row - t * G);
-      const long long to = (static_cast<long long>(w.s.q0 + tok) * a.H_q + head) * D + half * C::DV;
+        // a score that is no number makes the whole row none, through its sum (the polynomial below would lose it)
+        if (mx != mx) l = mx;
+        const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > kSlack;
+        float scale = 1.0f;
+        if (raise) {
+          scale = m == -INFINITY ? 0.0f : ex2((m - mx) * c);
+          m = mx;
+          l *= scale;
+        }
+        if (n > 0 && __any_sync(0xffffffffu, raise)) {
+          // O of the tiles before is complete once its MMA has arrived on O
+          ok = warp_wait_on(bar(B::O + i), (total + n - 1) & 1, stop);
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll 1
-      for (int x = 0; x < C::DV; x += 32) {
-        uint32_t o[32];
-        if (n > 0) {
-          tmem_ld32(o_addr + x, o);
-          tmem_wait_ld();
-        } else {
+          for (int x = 0; x < C::DV; x += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_addr + x, o);
+            tmem_wait_ld();
 #pragma unroll
-          for (int y = 0; y < 32; ++y) o[y] = 0;
+            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
+            tmem_st16(o_addr + x, o);
+          }
         }
-        if (!real) continue;
-        float f[32];
+        const float mc = m == -INFINITY ? 0.0f : m * c;
+        // The weights go out in two halves: the output MMAs of the first run while the second is made.
+        uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
+        const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
+        auto weights = [&](int x) {
+          uint32_t p[16];
 #pragma unroll
-        for (int y = 0; y < 32; ++y) f[y] = up > lo ? __uint_as_float(o[y]) * inv : 0.0f;
-        if (mend) {
-          // infinities and NaN of tokens that this row sees, in tiles where they were taken out
-          for (int key = lo; key < up; ++key) {
-            if (!partly(key / C::BN)) {
-              key = (key / C::BN + 1) * C::BN - 1;
-              continue;
+          for (int y = 0; y < 32; y += 2) {
+            const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
+            float2 e;
+            if (y / 2 < 16 - C::POLY) {
+              const float2 v = unpair(z);
+              e = make_float2(ex2(v.x), ex2(v.y));
+            } else {
+              e = exp2_pair<DT>(z);
             }
-            const uint32_t* src = reinterpret_cast<const uint32_t*>(
-                static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * D + half * C::DV + x);
+            if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
+            else sum0 = add2(sum0, pair(e.x, e.y));
+            p[y >> 1] = pack2<DT>(e.x, e.y);
+          }
+          tmem_st16(s_addr + (x >> 1), p);
+        };
+        auto hand_over = [&](int which) {
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(which + buf));
+        };
+        constexpr int kHalf = C::BN >= 64 ? C::BN / 2 : C::BN;
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-              const uint32_t v = __ldg(src + (y >> 1));
-              if (not_finite2<DT>(v)) {
-                const float2 g = unpack2<DT>(v);
-                f[y] += g.x - g.x != 0.0f || g.x != g.x ? g.x : 0.0f;
-                f[y + 1] += g.y - g.y != 0.0f || g.y != g.y ? g.y : 0.0f;
+        for (int x = 0; x < kHalf; x += 32) weights(x);
+        // The epilogue's wait for the last output MMA must find the one before it complete (a barrier tells a phase from
+        // the one before, not from the one before that).  With one S buffer the scores were issued behind it.
+        if (C::NSB == 2 && n > 0 && j + 1 == my1) {
+          ok = warp_wait_on(bar(B::O + i), (use - 1) & 1, stop);
+          if (!ok) break;
+        }
+        hand_over(B::P);
+#pragma unroll
+        for (int x = kHalf; x < C::BN; x += 32) weights(x);
+        if (kHalf < C::BN) hand_over(B::P2);
+        {
+          const float2 v = unpair(add2(sum0, sum1));
+          l = v.x + v.y;
+        }
+      }
+      total += n;
+      // ---- epilogue: the thread's row of O
+      if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), (total - 1) & 1, stop);
+      if (ok) {
+        tc_fence_after();
+        const float inv = up > lo ? 1.0f / l : 0.0f;
+        const bool mend = s_scrubbed[it & 3] != 0;
+        const int head = w.h * G + (row - t * G);
+        const long long to = (static_cast<long long>(w.s.q0 + tok) * a.H_q + head) * D + w.half * C::DV;
+#pragma unroll 1
+        for (int x = 0; x < C::DV; x += 32) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(o_addr + x, o);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0;
+          }
+          if (!real) continue;
+          float f[32];
+#pragma unroll
+          for (int y = 0; y < 32; ++y) f[y] = up > lo ? __uint_as_float(o[y]) * inv : 0.0f;
+          if (mend) {
+            // infinities and NaN of tokens that this row sees, in tiles where they were taken out
+            for (int key = lo; key < up; ++key) {
+              if (!r.partly(key / C::BN)) {
+                key = (key / C::BN + 1) * C::BN - 1;
+                continue;
+              }
+              const uint32_t* src = reinterpret_cast<const uint32_t*>(
+                  static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * D + w.half * C::DV + x);
+#pragma unroll
+              for (int y = 0; y < 32; y += 2) {
+                const uint32_t v = __ldg(src + (y >> 1));
+                if (not_finite2<DT>(v)) {
+                  const float2 g = unpack2<DT>(v);
+                  f[y] += g.x - g.x != 0.0f || g.x != g.x ? g.x : 0.0f;
+                  f[y + 1] += g.y - g.y != 0.0f || g.y != g.y ? g.y : 0.0f;
+                }
               }
             }
           }
-        }
-        if (OT == TQ_FP32) {
-          float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to + x);
+          if (OT == TQ_FP32) {
+            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to + x);
 #pragma unroll
-          for (int y = 0; y < 8; ++y) dst[y] = make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to + x);
+            for (int y = 0; y < 8; ++y) dst[y] = make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
+          } else {
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to + x);
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            dst[y] = make_uint4(pack2<DT>(f[8 * y], f[8 * y + 1]), pack2<DT>(f[8 * y + 2], f[8 * y + 3]),
-                                pack2<DT>(f[8 * y + 4], f[8 * y + 5]), pack2<DT>(f[8 * y + 6], f[8 * y + 7]));
+            for (int y = 0; y < 4; ++y)
+              dst[y] = make_uint4(pack2<DT>(f[8 * y], f[8 * y + 1]), pack2<DT>(f[8 * y + 2], f[8 * y + 3]),
+                                  pack2<DT>(f[8 * y + 4], f[8 * y + 5]), pack2<DT>(f[8 * y + 6], f[8 * y + 7]));
+          }
+        }
+        tc_fence_before();
+      }
+    }
+  } else if (warp == C::SOFT) {
+    // ====================================================================================== the work, and TMA loads
+    if (lane == 0) {
+      const int TT = C::NQ * T, halves = D / C::DV;
+      // Tiles of a sequence: b starts at tile q_offsets[b] / TT + b, which leaves room for its ceil(lq / TT) tiles.  The late
+      // tiles of a sequence see the most keys under the causal mask and go first.
+      auto start_of = [&](int b) { return min(max(a.q_offsets[b], 0), a.n_q) / TT + b; };
+      int id = blockIdx.x, b = -1, it = 0, slot = 0, q_uses = 0;
+      uint32_t phase = 1, issued = 0;  // the first pass over the ring finds every slot empty
+      bool ok = true;
+      auto load = [&](const CUtensorMap* map, const Work& w, int j, int chunk0, int chunks) {
+        ok = ok && wait_on(bar(B::EMPTY + slot), phase, stop);
+        if (!ok) return;
+        mbar_expect_tx(bar(B::FULL + slot), chunks * C::KCHUNK);
+        for (int x = 0; x < chunks; ++x)
+          tma_load_3d(base + C::RING + slot * C::SLOT + x * C::KCHUNK, map, 64 * (chunk0 + x), w.h, w.s.k0 + j * C::BN, bar(B::FULL + slot));
+        ++issued;
+        if (++slot == C::NS) {
+          slot = 0;
+          phase ^= 1;
+        }
+      };
+      for (int asked = 0; ok; ++asked) {
+        Work w = {};
+        if (id >= 0) {
+          int at = id;
+          w.half = at % halves;
+          at /= halves;
+          w.h = at % a.H_kv;
+          const int tile = a.n_q / TT + a.B - 1 - at / a.H_kv;
+          if (b < 0) {
+            int hi = a.B;
+            b = 0;
+            while (hi - b > 1) {
+              const int mid = (b + hi) >> 1;
+              if (start_of(mid) <= tile) b = mid;
+              else hi = mid;
+            }
+          }
+          while (b > 0 && start_of(b) > tile) --b;  // the next one is near the last one
+          while (b + 1 < a.B && start_of(b + 1) <= tile) ++b;
+          w.s = prompt_seq(a, b, false);
+          w.tok0 = (tile - start_of(b)) * TT;
+          w.more = w.tok0 >= 0 && w.tok0 < w.s.lq;
+          if (w.more && w.tok0 == 0 && w.h == 0 && w.half == 0) (void)prompt_seq(a, b, true);  // one reports for the sequence
+        }
+        if (w.more || id < 0) {
+          ok = wait_on(bar(B::WORK_FREE + (it & 1)), ((it >> 1) & 1) ^ 1, stop, kBlockWait);
+          if (ok) {
+            s_work[it & 1] = w;
+            s_scrubbed[it & 3] = 0;  // its readers of four pieces of work ago have long gone on
+            mbar_arrive(bar(B::WORK + (it & 1)));
+            ++it;
+          }
+        }
+        if (w.more && ok) {
+          const Span<D> r(a, w, T);
+          if (r.J1 > r.J0) {
+            ok = wait_on(bar(B::Q_FREE), (q_uses & 1) ^ 1, stop);
+            if (ok) {
+              ++q_uses;
+              mbar_expect_tx(bar(B::Q), C::NQ * (D / 64) * T * G * 128);
+              for (int i = 0; i < C::NQ; ++i)
+                for (int x = 0; x < D / 64; ++x)
+                  tma_load_3d(base + i * C::QTILE + x * C::QCHUNK, &maps.q, 64 * x, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
+            }
+            // in the order in which the MMAs take them
+            for (int j = r.J0; j <= r.J1 && ok; ++j) {
+              if (C::NSB == 2 && j < r.J1) load(&maps.k, w, j, 0, D / 64);
+              if (j > r.J0) load(&maps.v, w, j - 1, w.half * (C::DV / 64), C::DV / 64);
+              if (C::NSB == 1 && j < r.J1) load(&maps.k, w, j, 0, D / 64);
+            }
+          }
+        }
+        if (id < 0 || !ok) break;
+        // asked only now, so that no thread block sits on work that another one is free for
+        mbar_expect_tx(bar(B::STEAL), 16);
+        steal_ask(smem_addr(&s_answer), bar(B::STEAL));
+        if (!wait_stage_inline(bar(B::STEAL), asked & 1, kTileWait)) {
+          *stop = 1;
+          break;
+        }
+        id = steal_answer(smem_addr(&s_answer));
+        fence_proxy_async_smem();
+      }
+      if (!ok || *stop) {
+        // copies on their way land before the block ends (bounded again)
+        if (q_uses > 0) wait_stage_inline(bar(B::Q), (q_uses - 1) & 1, kMaxWaitCycles);
+        for (uint32_t x = 0; x < C::NS && x < issued; ++x) {
+          const uint32_t n = issued - 1 - x;
+          wait_stage_inline(bar(B::FULL + n % C::NS), (n / C::NS) & 1, kMaxWaitCycles);
         }
       }
     }
-  } else if (mine && warp == C::SOFT && lane == 0 && J1 > J0) {
-    // ================================================================================================= TMA loads
-    mbar_expect_tx(bar(B::Q), C::NQ * (D / 64) * T * G * 128);
-    for (int i = 0; i < C::NQ; ++i)
-      for (int x = 0; x < D / 64; ++x)
-        tma_load_3d(base + i * C::QTILE + x * C::QCHUNK, &maps.q, 64 * x, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
-    int slot = 0, issued = 0;
-    uint32_t phase = 1;  // the first pass over the ring finds every slot empty
-    bool ok = true;
-    auto load = [&](const CUtensorMap* map, int j, int chunk0, int chunks) {
-      ok = ok && wait_on(bar(B::EMPTY + slot), phase, stop);
-      if (!ok) return;
-      mbar_expect_tx(bar(B::FULL + slot), chunks * C::KCHUNK);
-      for (int x = 0; x < chunks; ++x)
-        tma_load_3d(base + C::RING + slot * C::SLOT + x * C::KCHUNK, map, 64 * (chunk0 + x), w.h, w.s.k0 + j * C::BN, bar(B::FULL + slot));
-      ++issued;
-      if (++slot == C::NS) {
-        slot = 0;
-        phase ^= 1;
-      }
-    };
-    // in the order in which the MMAs take them
-    for (int j = J0; j <= J1 && ok; ++j) {
-      if (C::NSB == 2) {
-        if (j < J1) load(&maps.k, j, 0, D / 64);
-        if (j > J0) load(&maps.v, j - 1, half * (C::DV / 64), C::DV / 64);
-      } else {
-        if (j > J0) load(&maps.v, j - 1, 0, C::DV / 64);
-        if (j < J1) load(&maps.k, j, 0, D / 64);
-      }
-    }
-    if (!ok) {
-      // copies on their way land before the block ends (bounded again)
-      wait_stage(bar(B::Q), 0);
-      for (int x = 0; x < C::NS && x < issued; ++x) {
-        const int n = issued - 1 - x;
-        wait_stage(bar(B::FULL + n % C::NS), (n / C::NS) & 1);
-      }
-    }
-  } else if (mine && warp == C::SOFT + 1 && lane == 0 && J1 > J0) {
-    // ====================================================================================================== MMAs
+  } else if (warp <= C::SOFT + C::NQ) {
+    // =================================================================================== MMAs of one query tile
+    const int i = warp - C::SOFT - 1;
     const uint32_t id_s = instr_desc(DT == TQ_BF16, 128, C::BN, false) | (a.attn_scale < 0.0f ? kNegateA : 0u);
     const uint32_t id_o = instr_desc(DT == TQ_BF16, 128, C::DV, true);
-    int slot = 0, scrubs = 0, n[C::NQ];
-    uint32_t phase = 0;
-    for (int i = 0; i < C::NQ; ++i) n[i] = 0;
-    const uint32_t q_lo = desc_lo(base, 0), ring_lo = desc_lo(base + C::RING, 0);
-    bool ok = wait_on(bar(B::Q), 0, stop);
-    int issued[C::NQ];  // S tiles
-    for (int i = 0; i < C::NQ; ++i) issued[i] = 0;
-    auto next_slot = [&]() {
-      mma_commit(bar(B::EMPTY + slot));
-      if (++slot == C::NS) {
-        slot = 0;
-        phase ^= 1;
-      }
-    };
-    auto scores = [&](int i, uint32_t k_at) {
-      const int buf = C::NSB == 2 ? (issued[i] & 1) : i;
-      const uint32_t d = tmem + C::S_COL + buf * C::S_STEP;
+    const uint32_t q_lo = desc_lo(base + i * C::QTILE, 0), ring_lo = desc_lo(base + C::RING, 0);
+    const uint32_t o_at = tmem + C::O_COL + i * C::DV;
+    int slot = 0;
+    uint32_t phase = 0, sn = 0, pn = 0, q_uses = 0, turns = 0;  // S and P tiles, and turns so far
+    bool ok = true;
+    Work w;
+    for (int it = 0; ok && next_work(it, w); ++it) {
+      const Span<D> r(a, w, T);
+      if (lane == 0 && r.J1 > r.J0) {
+        const int my0 = i == 0 ? r.j0[0] : r.j0[C::NQ - 1], my1 = i == 0 ? r.j1[0] : r.j1[C::NQ - 1];
+        auto landed = [&](int x, uint32_t ph, bool looked_through) {
+          ok = ok && wait_on(bar(B::FULL + x), ph, stop);
+          // (only behind FULL: before it, READY may still be two phases back, which it cannot tell from this one)
+          if (looked_through) ok = ok && wait_on(bar(B::READY + x), ph, stop);
+        };
+        auto next_slot = [&](int& x, uint32_t& ph) {
+          if (++x == C::NS) {
+            x = 0;
+            ph ^= 1;
+          }
+        };
+        // The tiles take turns with the second half of their outputs and the next scores.  Left to themselves both softmax
+        // warpgroups come to run at the same time, and the tensor cores wait for both (1.27 ms for the 8K prompt).
+        bool mine = C::NQ == 1;
+        auto my_turn = [&]() {
+          if (mine || !ok) return;
+          if (i == 1 || turns > 0) ok = (TQ_SPIN & 1) ? poll_on(bar(B::TURN + (i ^ 1)), (i == 1 ? turns : turns - 1) & 1, stop) : wait_on(bar(B::TURN + (i ^ 1)), (i == 1 ? turns : turns - 1) & 1, stop);
+          mine = true;
+        };
+        auto scores = [&](int x) {
+          const int buf = C::NSB == 2 ? (sn & 1) : i;
+          const uint32_t d = tmem + C::S_COL + buf * C::S_STEP, k_at = ring_lo + x * (C::SLOT >> 4);
 #pragma unroll
-      for (int x = 0; x < D / 16; ++x)
-        mma_ss(d, q_lo + i * (C::QTILE >> 4) + (((x >> 2) * C::QCHUNK + (x & 3) * 32) >> 4),
-               k_at + (((x >> 2) * C::KCHUNK + (x & 3) * 32) >> 4), kDescHi, id_s, x > 0);
-      mma_commit(bar(B::S + buf));
-      ++issued[i];
-    };
-    auto outputs = [&](int i, uint32_t v_at) {
-      const int buf = C::NSB == 2 ? (n[i] & 1) : i;
-      ok = ok && wait_on(bar(B::P + buf), (C::NSB == 2 ? n[i] >> 1 : n[i]) & 1, stop);
-      if (!ok) return;
-      tc_fence_after();
-      const uint32_t p = tmem + C::S_COL + buf * C::S_STEP, d = tmem + C::O_COL + i * C::DV;
+          for (int y = 0; y < D / 16; ++y)
+            mma_ss(d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), k_at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
+                   kDescHi, id_s, y > 0);
+          mma_commit(bar(B::S + buf));
+          ++sn;
+        };
+        auto outputs = [&](int x, bool add) {
+          const int buf = C::NSB == 2 ? (pn & 1) : i;
+          const uint32_t parity = (C::NSB == 2 ? pn >> 1 : pn) & 1;
+          const uint32_t p = tmem + C::S_COL + buf * C::S_STEP;
+          const uint32_t v_at = ring_lo + ((C::KCHUNK >> 4) << 16) + x * (C::SLOT >> 4);
+          constexpr int kSteps = C::BN / 16, kFirst = C::BN >= 64 ? kSteps / 2 : kSteps;
+          ok = ok && ((TQ_SPIN & 1) ? poll_on(bar(B::P + buf), parity, stop) : wait_on(bar(B::P + buf), parity, stop));
+          if (!ok) return;
+          tc_fence_after();
 #pragma unroll
-      for (int x = 0; x < C::BN / 16; ++x) mma_ts(d, p + 8 * x, v_at + (2048 >> 4) * x, kDescHi, id_o, x > 0 || n[i] > 0);
-      mma_commit(bar(B::O + i));
-      ++n[i];
-    };
-    auto take = [&]() {  // the next slot's tile has landed
-      ok = ok && wait_on(bar(B::FULL + slot), phase, stop);
-      return ring_lo + slot * (C::SLOT >> 4);
-    };
-    auto take_v = [&](int j) {
-      const uint32_t x = take() + ((C::KCHUNK >> 4) << 16);
-      if (ok && partly(j)) {
-        mbar_arrive(bar(B::ASK));
-        ok = wait_on(bar(B::SCRUB), scrubs++ & 1, stop);
-      }
-      return x;
-    };
-    for (int j = J0; j <= J1 && ok; ++j) {
-      if (C::NSB == 2) {
-        if (j < J1) {
-          const uint32_t x = take();
-          if (!ok) break;
-          scores(0, x);
-          next_slot();
-        }
-        if (j > J0) {
-          const uint32_t x = take_v(j - 1);
-          if (!ok) break;
-          outputs(0, x);
-          if (!ok) break;
-          next_slot();
-        }
-      } else {
-        // tile 0: its weights times V(j - 1), its scores against K(j); then tile 1
-        uint32_t v_at = 0, k_at = 0;
-        const int v_slot = slot;
-        if (j > J0) {
-          v_at = take_v(j - 1);
-          if (!ok) break;
-          if (++slot == C::NS) {
-            slot = 0;
-            phase ^= 1;
+          for (int y = 0; y < kFirst; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, y > 0 || add);
+          if (kFirst < kSteps) {
+            ok = (TQ_SPIN & 1) ? poll_on(bar(B::P2 + buf), parity, stop) : wait_on(bar(B::P2 + buf), parity, stop);
+            my_turn();
+            if (!ok) return;
+            tc_fence_after();
+#pragma unroll
+            for (int y = kFirst; y < kSteps; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, true);
           }
-        }
-        const int k_slot = slot;
-        bool have_k = false;
-        for (int i = 0; i < C::NQ && ok; ++i) {
-          if (j > J0 && in(i, j - 1)) outputs(i, v_at);
-          if (ok && j < J1 && in(i, j)) {
-            if (!have_k) k_at = take();
-            have_k = true;
-            if (ok) scores(i, k_at);
+          ++pn;
+        };
+        ok = wait_on(bar(B::Q), q_uses++ & 1, stop);
+        for (int j = r.J0; j <= r.J1 && ok; ++j) {
+          const bool do_s = j < r.J1 && j >= my0 && j < my1, do_o = j > r.J0 && j - 1 >= my0 && j - 1 < my1;
+          if (C::NSB == 2) {
+            if (j < r.J1) {
+              landed(slot, phase, false);
+              if (!ok) break;
+              if (do_s) scores(slot);
+              mma_commit(bar(B::EMPTY + slot));
+              next_slot(slot, phase);
+            }
+            if (j > r.J0) {
+              landed(slot, phase, r.partly(j - 1));
+              if (do_o) outputs(slot, j - 1 > my0);
+              if (!ok) break;
+              if (do_o) mma_commit(bar(B::O + i));
+              mma_commit(bar(B::EMPTY + slot));
+              next_slot(slot, phase);
+            }
+          } else {
+            // The scores follow the outputs without a pause: both operands are awaited before, and the arrivals that nobody is
+            // waiting for (the outputs' is needed for a rare rescaling and at the end, where no scores follow) come after.
+            int k_slot = slot;
+            uint32_t k_phase = phase;
+            if (j > r.J0) {
+              landed(slot, phase, r.partly(j - 1));
+              next_slot(k_slot, k_phase);
+            }
+            if (j < r.J1) landed(k_slot, k_phase, false);
+            if (do_o) outputs(slot, j - 1 > my0);
+            my_turn();
+            if (!ok) break;
+            if (do_s) scores(k_slot);
+            mbar_arrive(bar(B::TURN + i));
+            ++turns;
+            mine = false;
+            if (do_o) mma_commit(bar(B::O + i));
+            if (j > r.J0) mma_commit(bar(B::EMPTY + slot));
+            if (j < r.J1) {
+              mma_commit(bar(B::EMPTY + k_slot));
+              next_slot(k_slot, k_phase);
+            }
+            slot = k_slot;
+            phase = k_phase;
           }
-        }
-        if (!ok) break;
-        if (j > J0) mma_commit(bar(B::EMPTY + v_slot));
-        if (j < J1) {
-          mma_commit(bar(B::EMPTY + k_slot));
-          if (++slot == C::NS) {
-            slot = 0;
-            phase ^= 1;
-          }
+          if (j + 1 == r.J1) mma_commit(bar(B::Q_FREE));
         }
       }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
     }
     // everything issued has completed before the block gives its memory back
-    mma_commit(bar(B::DRAIN));
-    if (!wait_stage(bar(B::DRAIN), 0, kTileWait)) *stop = 1;
-  } else if (mine && warp >= C::SOFT + 2) {
+    if (lane == 0) {
+      mma_commit(bar(B::DRAIN));
+      if (!wait_stage_inline(bar(B::DRAIN), 0, kTileWait)) *stop = 1;
+    }
+  } else {
     // ============================================================= V tiles that some row sees in part: finite values
-    const int me = tid - 32 * (C::SOFT + 2);
+    const int me = tid - 32 * (C::SOFT + 1 + C::NQ);
     bool ok = true;
-    int asked = 0;
-    for (int j = J0; j < J1 && ok; ++j) {
-      if (!partly(j)) continue;
-      // the MMA thread asks when it has come to the tile, and holds its slot until the answer
-      ok = warp_wait_on(bar(B::ASK), asked++ & 1, stop, kBlockWait);
-      if (!ok) break;
-      // K(J0) [K(J0+1)] V(J0) K V ...: V(j) is load 2 (j - J0) + 1, or one later where the next K tile is loaded first
-      const int order = 2 * (j - J0) + 1 + (C::NSB == 2 && j + 1 < J1 ? 1 : 0);
-      const int slot = order % C::NS;
-      ok = warp_wait_on(bar(B::FULL + slot), (order / C::NS) & 1, stop);
-      if (!ok) break;
-      uint4* tile = reinterpret_cast<uint4*>(smem + C::RING + slot * C::SLOT);
-      bool found = false;
-#pragma unroll 4
-      for (int x = me; x < (C::DV / 64) * C::KCHUNK / 16; x += 32 * C::SCRUB) {
-        uint4 v = tile[x];
-        if (not_finite2<DT>(v.x) | not_finite2<DT>(v.y) | not_finite2<DT>(v.z) | not_finite2<DT>(v.w)) {
-          auto clean = [](uint32_t y) {
-            const uint32_t bad = not_finite2<DT>(y);
-            return y & ~((bad >> 15) * 0xffffu);
-          };
-          tile[x] = make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
-          found = true;
+    int slot = 0;
+    uint32_t phase = 0;
+    Work w;
+    for (int it = 0; ok && next_work(it, w); ++it) {
+      const Span<D> r(a, w, T);
+      // every slot of the ring in turn, so that none is filled again behind this warp's back
+      const int loads = 2 * (r.J1 - r.J0);
+      for (int x = 0; x < loads && ok; ++x) {
+        // K(J0) V(J0) K V ...; with two score buffers K(J0) K(J0 + 1) V(J0) K V ... V V
+        const bool v_load = C::NSB == 1 ? (x & 1) : (x + 1 == loads || (x > 0 && !(x & 1)));
+        const int j = r.J0 + (C::NSB == 1 ? x >> 1 : (x + 1 == loads ? (loads >> 1) - 1 : (x >> 1) - 1));
+        ok = warp_wait_on(bar(B::FULL + slot), phase, stop);
+        if (!ok) break;
+        if (v_load && r.partly(j)) {
+          uint4* tile = reinterpret_cast<uint4*>(smem + C::RING + slot * C::SLOT);
+          bool found = false;
+#pragma unroll 8
+          for (int y = me; y < (C::DV / 64) * C::KCHUNK / 16; y += 32 * C::SCRUB) {
+            const uint4 v = tile[y];
+            if (not_finite2<DT>(v.x) | not_finite2<DT>(v.y) | not_finite2<DT>(v.z) | not_finite2<DT>(v.w)) {
+              auto clean = [](uint32_t z) {
+                const uint32_t bad = not_finite2<DT>(z);
+                return z & ~((bad >> 15) * 0xffffu);
+              };
+              tile[y] = make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
+              found = true;
+            }
+          }
+          if (found) s_scrubbed[it & 3] = 1;
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(B::READY + slot));
+          mbar_arrive(bar(B::EMPTY + slot));
+        }
+        if (++slot == C::NS) {
+          slot = 0;
+          phase ^= 1;
         }
       }
-      if (found) s_scrubbed = 1;
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B::SCRUB));
     }
   }
 

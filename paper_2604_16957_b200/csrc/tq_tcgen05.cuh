@@ -18,6 +18,25 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                : "memory");
 }
 
+// ---- work stealing from the launch's own grid: asks for a thread block that has not started; the answer (16 bytes of
+// shared memory) completes on the mbarrier.  After a "no" a thread block must not ask again.
+__device__ __forceinline__ void steal_ask(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];\n" ::"r"(answer), "r"(bar)
+               : "memory");
+}
+// blockIdx.x of the thread block that will not start and is this one's now, or -1
+__device__ __forceinline__ int steal_answer(uint32_t answer) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n.reg .b128 v;\n.reg .pred p;\nld.shared.b128 v, [%2];\n"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, v;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, v;\n}\n"
+      : "=r"(got), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  return got ? static_cast<int>(x) : -1;
+}
+
 // ---- tensor memory: 128 lanes x 512 columns of 32 bits.  Address: column in the low half, lane in the high half.
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t columns) {  // whole warp
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_dst), "r"(columns) : "memory");
