@@ -7,14 +7,15 @@
 //     P = 2^(c S - c m), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
 // c = alpha log2 e > 0 (for a negative alpha the MMA negates Q).  m is raised only when a score exceeds it by more than
-// 2^8; then the thread rescales its row of O in TMEM.  With two tiles the tensor cores work on one while the softmax
-// of the other runs; with one tile (d = 256, 512) S has two buffers and the next scores are computed meanwhile.  At
-// d = 512 the accumulator of a row does not fit TMEM: a thread block computes 256 of the 512 output channels, and S is
-// computed twice.
+// 2^8; then the thread rescales its row of O in TMEM.  S has two buffers per tile: the scores of the next keys are made
+// while the softmax of these runs.  That takes key tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at
+// d = 128), for which an MMA of 128 x 64 x 16 reads its operands in 48 cycles instead of the 32 that it computes; with
+// tiles of 128 keys and one buffer the MMAs are faster (64 cycles for twice the work), but outputs, scores and softmax of
+// a tile follow one another: 1.09 ms for the 8K prompt.  At d = 512 the accumulator of a row does not fit TMEM: a thread
+// block computes 256 of the 512 output channels, and S is computed twice.
 //
 // Roles: one warpgroup of softmax threads per tile; a warp that finds the work and issues the TMA loads; a warp per tile
-// that issues its MMAs (one issuing thread could not keep the tensor cores busy over its waits: 1.09 ms for the 8K
-// prompt); one or two warps that look through the V tiles which some row sees in part.  Those may hold tokens of a
+// that issues its MMAs (one issuing thread could not keep the tensor cores busy over its waits); one or two warps that look through the V tiles which some row sees in part.  Those may hold tokens of a
 // neighbouring sequence or of the row's future, whose weight is 0, and 0 * inf is not 0: a value there that is no finite
 // number is replaced by 0 in shared memory, and the rows that do see it get it added back in the epilogue from global
 // memory.
@@ -32,9 +33,6 @@
 #include "tq_prompt.cuh"
 #include "tq_tcgen05.cuh"
 
-#ifndef TQ_POLY
-#define TQ_POLY 0
-#endif
 namespace tq {
 namespace {
 
@@ -44,11 +42,9 @@ constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running max
 template <int D>
 struct Cfg {
   static constexpr int NQ = D <= 128 ? 2 : 1;         // query tiles of a thread block
-  static constexpr int BN = D <= 128 ? 128 : (D == 256 ? 64 : 32);  // keys of a K / V tile
+  static constexpr int BN = D <= 256 ? 64 : 32;       // keys of a K / V tile
   static constexpr int DV = D <= 256 ? D : 256;       // output channels of a thread block
-  static constexpr int NSB = NQ == 2 ? 1 : 2;         // S buffers of a tile
   static constexpr int SOFT = 4 * NQ;                 // softmax warps
-  static constexpr int POLY = NQ == 2 ? TQ_POLY : 0;  // pairs in 16 whose exponentials the FMA units compute
   static constexpr int SCRUB = NQ == 2 ? 1 : 2;
   static constexpr int WARPS = SOFT + 1 + NQ + SCRUB;  // softmax | work and TMA | MMA | scrub
   static constexpr int THREADS = 32 * WARPS;
@@ -56,14 +52,12 @@ struct Cfg {
   static constexpr int QTILE = (D / 64) * QCHUNK;
   static constexpr int KCHUNK = BN * 128;
   static constexpr int SLOT = (D / 64) * KCHUNK;      // a K tile; a V tile needs no more
-  static constexpr int NS = D == 64 ? 8 : (D == 512 ? 3 : 5);  // slots of the K / V ring
+  static constexpr int NS = D <= 128 ? 10 : (D == 256 ? 5 : 3);  // slots of the K / V ring
   static constexpr int RING = NQ * QTILE;
   static constexpr int BARS = RING + NS * SLOT;
   static constexpr int SMEM = BARS + 512 + 1024;      // barriers, and room to align the base
-  static constexpr int S_COL = 0;                     // TMEM columns: S of tile / buffer i at 128 i (P over it), O behind
-  static constexpr int O_COL = D <= 128 ? 256 : (D == 256 ? 128 : 64);
-  static constexpr int S_STEP = BN;
-  static_assert(O_COL >= NQ * NSB * BN && O_COL + NQ * DV <= 512, "tensor memory");
+  static constexpr int O_COL = 2 * NQ * BN;           // TMEM columns: two S buffers per query tile (P over S), O behind
+  static_assert(O_COL + NQ * DV <= 512, "tensor memory");
   static_assert(SMEM <= 232448, "shared memory");
 };
 
@@ -77,10 +71,8 @@ struct Bars {
   using C = Cfg<D>;
   static constexpr int FULL = 0, EMPTY = FULL + C::NS, READY = EMPTY + C::NS;  // K / V slots: landed, free, looked through
   static constexpr int Q = READY + C::NS, Q_FREE = Q + 1;
-  static constexpr int S = Q_FREE + 1, P = S + C::NQ * C::NSB, P2 = P + C::NQ * C::NSB;  // scores, weights (two halves)
-  static constexpr int O = P2 + C::NQ * C::NSB;                                          // outputs
-  static constexpr int WORK = O + C::NQ, WORK_FREE = WORK + 2, STEAL = WORK_FREE + 2, TURN = STEAL + 1,
-                       DRAIN = TURN + 2, COUNT = DRAIN + 1;
+  static constexpr int S = Q_FREE + 1, P = S + 2 * C::NQ, O = P + 2 * C::NQ;  // scores and weights (two buffers), outputs
+  static constexpr int WORK = O + C::NQ, WORK_FREE = WORK + 2, STEAL = WORK_FREE + 2, DRAIN = STEAL + 1, COUNT = DRAIN + 1;
   static_assert(COUNT * 8 <= 512, "room for the barriers");
 };
 
@@ -101,16 +93,6 @@ __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatil
 }
 __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
   if (mbar_try_wait(bar, parity)) return true;
-  return wait_slow(bar, parity, stop, limit);
-}
-#ifndef TQ_SPIN
-#define TQ_SPIN 3
-#endif
-// the same, polled: sooner awake than a wait that lets the hardware suspend the thread
-__device__ __forceinline__ bool poll_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
-#pragma unroll 1
-  for (int i = 0; i < 256; ++i)
-    if (mbar_test_wait(bar, parity)) return true;
   return wait_slow(bar, parity, stop, limit);
 }
 __device__ __forceinline__ bool wait_stage_inline(uint32_t bar, uint32_t parity, long long limit) {
@@ -134,34 +116,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if on
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-
-// 2^y for two y <= 2^7 on the FMA units: y = n + f with n an integer and |f| <= 1/2, 2^f by a polynomial that is minimax
-// in the relative error on that interval (fitted by linear programming: 7.5e-5 at degree 3, 2.6e-6 at degree 4, against
-// the 2^-9 and 2^-12 of the rounding to bf16 and fp16 that follows), n added to the exponent.  The exponential unit does
-// 16 values per cycle and SM; taking a share of them off it is what lets it keep up with the tensor cores.
-template <int DT>
-__device__ __forceinline__ float2 exp2_pair(uint64_t y) {
-  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
-  const float2 v = unpair(y);
-  y = pair(fmaxf(v.x, -126.0f), fmaxf(v.y, -126.0f));
-  const uint64_t t = add2(y, pair(kMagic, kMagic));
-  const uint64_t f = fma2(add2(t, pair(-kMagic, -kMagic)), pair(-1.0f, -1.0f), y);
-  auto both = [](float x) { return pair(x, x); };
-  uint64_t p;
-  if (DT == TQ_BF16) {
-    p = fma2(both(0.05517132207751274f), f, both(0.2426113337278366f));
-    p = fma2(p, f, both(0.6932610869407654f));
-    p = fma2(p, f, both(0.9999280571937561f));
-  } else {
-    p = fma2(both(0.00957053154706955f), f, both(0.05591866374015808f));
-    p = fma2(p, f, both(0.24024735391139984f));
-    p = fma2(p, f, both(0.6931216716766357f));
-    p = fma2(p, f, both(0.9999992847442627f));
-  }
-  const float2 q = unpair(p), n = unpair(t);
-  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(n.x) << 23)),
-                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // nonzero if one of the two 16-bit values of a word is an infinity or a NaN
@@ -233,10 +187,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     }
     mbar_init(bar(B::Q), 1);
     mbar_init(bar(B::Q_FREE), C::NQ);
-    for (int i = 0; i < C::NQ * C::NSB; ++i) {
+    for (int i = 0; i < 2 * C::NQ; ++i) {
       mbar_init(bar(B::S + i), 1);
       mbar_init(bar(B::P + i), 4);
-      mbar_init(bar(B::P2 + i), 4);
     }
     for (int i = 0; i < C::NQ; ++i) mbar_init(bar(B::O + i), 1);
     for (int i = 0; i < 2; ++i) {
@@ -244,7 +197,6 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       mbar_init(bar(B::WORK_FREE + i), C::WARPS - 1);
     }
     mbar_init(bar(B::STEAL), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(bar(B::TURN + i), 1);
     mbar_init(bar(B::DRAIN), C::NQ);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     s_stop = 0;
@@ -255,14 +207,6 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
   const uint32_t tmem = s_tmem;
   pdl_launch_dependents();
   pdl_wait();
-
-  // With two tiles the softmax threads hold a row of 128 scores each: 208 registers for them, 80 for the other warps
-  // (256 x 208 + 128 x 80 = 63488 of the 384 x 168 = 64512 that the block is launched with).
-  if (C::NQ == 2) {
-    static_assert(C::NQ == 1 || (C::THREADS == 384 && 256 * 208 + 128 * 80 <= 384 * 168), "register split");
-    if (warp < C::SOFT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-  }
 
   // the it-th piece of work, for every warp but the one that finds it; false: none, or the block winds down
   auto next_work = [&](int it, Work& w) {
@@ -296,9 +240,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       const int my0 = i == 0 ? r.j0[0] : r.j0[C::NQ - 1], my1 = i == 0 ? r.j1[0] : r.j1[C::NQ - 1];
       for (int j = my0; j < my1 && ok; ++j, ++n) {
         const uint32_t use = total + n;
-        const int buf = C::NSB == 2 ? (use & 1) : i;
-        const uint32_t s_addr = tmem + C::S_COL + buf * C::S_STEP + lanes;
-        ok = __all_sync(0xffffffffu, (TQ_SPIN & 2) ? poll_on(bar(B::S + buf), (C::NSB == 2 ? use >> 1 : use) & 1, stop) : wait_on(bar(B::S + buf), (C::NSB == 2 ? use >> 1 : use) & 1, stop));
+        const int buf = 2 * i + (use & 1);
+        const uint32_t s_addr = tmem + buf * C::BN + lanes;
+        ok = warp_wait_on(bar(B::S + buf), (use >> 1) & 1, stop);
         if (!ok) break;
         tc_fence_after();
         float s[C::BN];
@@ -348,50 +292,35 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           }
         }
         const float mc = m == -INFINITY ? 0.0f : m * c;
-        // The weights go out in two halves: the output MMAs of the first run while the second is made.
         uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
         const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
-        auto weights = [&](int x) {
+#pragma unroll
+        for (int x = 0; x < C::BN; x += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 2) {
-            const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
-            float2 e;
-            if (y / 2 < 16 - C::POLY) {
-              const float2 v = unpair(z);
-              e = make_float2(ex2(v.x), ex2(v.y));
-            } else {
-              e = exp2_pair<DT>(z);
-            }
-            if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
-            else sum0 = add2(sum0, pair(e.x, e.y));
-            p[y >> 1] = pack2<DT>(e.x, e.y);
+            const float2 z = unpair(fma2(pair(s[x + y], s[x + y + 1]), c2, mc2));
+            const float e0 = ex2(z.x), e1 = ex2(z.y);
+            if (y & 2) sum1 = add2(sum1, pair(e0, e1));
+            else sum0 = add2(sum0, pair(e0, e1));
+            p[y >> 1] = pack2<DT>(e0, e1);
           }
           tmem_st16(s_addr + (x >> 1), p);
-        };
-        auto hand_over = [&](int which) {
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(which + buf));
-        };
-        constexpr int kHalf = C::BN >= 64 ? C::BN / 2 : C::BN;
-#pragma unroll
-        for (int x = 0; x < kHalf; x += 32) weights(x);
-        // The epilogue's wait for the last output MMA must find the one before it complete (a barrier tells a phase from
-        // the one before, not from the one before that).  With one S buffer the scores were issued behind it.
-        if (C::NSB == 2 && n > 0 && j + 1 == my1) {
-          ok = warp_wait_on(bar(B::O + i), (use - 1) & 1, stop);
-          if (!ok) break;
         }
-        hand_over(B::P);
-#pragma unroll
-        for (int x = kHalf; x < C::BN; x += 32) weights(x);
-        if (kHalf < C::BN) hand_over(B::P2);
         {
           const float2 v = unpair(add2(sum0, sum1));
           l = v.x + v.y;
         }
+        // The epilogue's wait for the last output MMA must find the one before it complete: a barrier tells a phase from
+        // the one before, not from the one before that.
+        if (n > 0 && j + 1 == my1) {
+          ok = warp_wait_on(bar(B::O + i), (use - 1) & 1, stop);
+          if (!ok) break;
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B::P + buf));
       }
       total += n;
       // ---- epilogue: the thread's row of O
@@ -519,9 +448,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
             }
             // in the order in which the MMAs take them
             for (int j = r.J0; j <= r.J1 && ok; ++j) {
-              if (C::NSB == 2 && j < r.J1) load(&maps.k, w, j, 0, D / 64);
+              if (j < r.J1) load(&maps.k, w, j, 0, D / 64);
               if (j > r.J0) load(&maps.v, w, j - 1, w.half * (C::DV / 64), C::DV / 64);
-              if (C::NSB == 1 && j < r.J1) load(&maps.k, w, j, 0, D / 64);
             }
           }
         }
@@ -553,7 +481,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     const uint32_t q_lo = desc_lo(base + i * C::QTILE, 0), ring_lo = desc_lo(base + C::RING, 0);
     const uint32_t o_at = tmem + C::O_COL + i * C::DV;
     int slot = 0;
-    uint32_t phase = 0, sn = 0, pn = 0, q_uses = 0, turns = 0;  // S and P tiles, and turns so far
+    uint32_t phase = 0, sn = 0, pn = 0, q_uses = 0;  // S and P tiles so far
     bool ok = true;
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
@@ -565,95 +493,46 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           // (only behind FULL: before it, READY may still be two phases back, which it cannot tell from this one)
           if (looked_through) ok = ok && wait_on(bar(B::READY + x), ph, stop);
         };
-        auto next_slot = [&](int& x, uint32_t& ph) {
-          if (++x == C::NS) {
-            x = 0;
-            ph ^= 1;
+        auto release = [&]() {  // the slot, once everything issued so far has read it
+          mma_commit(bar(B::EMPTY + slot));
+          if (++slot == C::NS) {
+            slot = 0;
+            phase ^= 1;
           }
-        };
-        // The tiles take turns with the second half of their outputs and the next scores.  Left to themselves both softmax
-        // warpgroups come to run at the same time, and the tensor cores wait for both (1.27 ms for the 8K prompt).
-        bool mine = C::NQ == 1;
-        auto my_turn = [&]() {
-          if (mine || !ok) return;
-          if (i == 1 || turns > 0) ok = (TQ_SPIN & 1) ? poll_on(bar(B::TURN + (i ^ 1)), (i == 1 ? turns : turns - 1) & 1, stop) : wait_on(bar(B::TURN + (i ^ 1)), (i == 1 ? turns : turns - 1) & 1, stop);
-          mine = true;
-        };
-        auto scores = [&](int x) {
-          const int buf = C::NSB == 2 ? (sn & 1) : i;
-          const uint32_t d = tmem + C::S_COL + buf * C::S_STEP, k_at = ring_lo + x * (C::SLOT >> 4);
-#pragma unroll
-          for (int y = 0; y < D / 16; ++y)
-            mma_ss(d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), k_at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
-                   kDescHi, id_s, y > 0);
-          mma_commit(bar(B::S + buf));
-          ++sn;
-        };
-        auto outputs = [&](int x, bool add) {
-          const int buf = C::NSB == 2 ? (pn & 1) : i;
-          const uint32_t parity = (C::NSB == 2 ? pn >> 1 : pn) & 1;
-          const uint32_t p = tmem + C::S_COL + buf * C::S_STEP;
-          const uint32_t v_at = ring_lo + ((C::KCHUNK >> 4) << 16) + x * (C::SLOT >> 4);
-          constexpr int kSteps = C::BN / 16, kFirst = C::BN >= 64 ? kSteps / 2 : kSteps;
-          ok = ok && ((TQ_SPIN & 1) ? poll_on(bar(B::P + buf), parity, stop) : wait_on(bar(B::P + buf), parity, stop));
-          if (!ok) return;
-          tc_fence_after();
-#pragma unroll
-          for (int y = 0; y < kFirst; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, y > 0 || add);
-          if (kFirst < kSteps) {
-            ok = (TQ_SPIN & 1) ? poll_on(bar(B::P2 + buf), parity, stop) : wait_on(bar(B::P2 + buf), parity, stop);
-            my_turn();
-            if (!ok) return;
-            tc_fence_after();
-#pragma unroll
-            for (int y = kFirst; y < kSteps; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, true);
-          }
-          ++pn;
         };
         ok = wait_on(bar(B::Q), q_uses++ & 1, stop);
         for (int j = r.J0; j <= r.J1 && ok; ++j) {
-          const bool do_s = j < r.J1 && j >= my0 && j < my1, do_o = j > r.J0 && j - 1 >= my0 && j - 1 < my1;
-          if (C::NSB == 2) {
-            if (j < r.J1) {
-              landed(slot, phase, false);
-              if (!ok) break;
-              if (do_s) scores(slot);
-              mma_commit(bar(B::EMPTY + slot));
-              next_slot(slot, phase);
-            }
-            if (j > r.J0) {
-              landed(slot, phase, r.partly(j - 1));
-              if (do_o) outputs(slot, j - 1 > my0);
-              if (!ok) break;
-              if (do_o) mma_commit(bar(B::O + i));
-              mma_commit(bar(B::EMPTY + slot));
-              next_slot(slot, phase);
-            }
-          } else {
-            // The scores follow the outputs without a pause: both operands are awaited before, and the arrivals that nobody is
-            // waiting for (the outputs' is needed for a rare rescaling and at the end, where no scores follow) come after.
-            int k_slot = slot;
-            uint32_t k_phase = phase;
-            if (j > r.J0) {
-              landed(slot, phase, r.partly(j - 1));
-              next_slot(k_slot, k_phase);
-            }
-            if (j < r.J1) landed(k_slot, k_phase, false);
-            if (do_o) outputs(slot, j - 1 > my0);
-            my_turn();
+          if (j < r.J1) {
+            landed(slot, phase, false);
             if (!ok) break;
-            if (do_s) scores(k_slot);
-            mbar_arrive(bar(B::TURN + i));
-            ++turns;
-            mine = false;
-            if (do_o) mma_commit(bar(B::O + i));
-            if (j > r.J0) mma_commit(bar(B::EMPTY + slot));
-            if (j < r.J1) {
-              mma_commit(bar(B::EMPTY + k_slot));
-              next_slot(k_slot, k_phase);
+            if (j >= my0 && j < my1) {
+              // S into the buffer whose weights the output MMAs issued before have read
+              const int buf = 2 * i + (sn & 1);
+              const uint32_t d = tmem + buf * C::BN, k_at = ring_lo + slot * (C::SLOT >> 4);
+#pragma unroll
+              for (int y = 0; y < D / 16; ++y)
+                mma_ss(d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), k_at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
+                       kDescHi, id_s, y > 0);
+              mma_commit(bar(B::S + buf));
+              ++sn;
             }
-            slot = k_slot;
-            phase = k_phase;
+            release();
+          }
+          if (j > r.J0) {
+            landed(slot, phase, r.partly(j - 1));
+            if (!ok) break;
+            if (j - 1 >= my0 && j - 1 < my1) {
+              const int buf = 2 * i + (pn & 1);
+              const uint32_t p = tmem + buf * C::BN, v_at = ring_lo + ((C::KCHUNK >> 4) << 16) + slot * (C::SLOT >> 4);
+              ok = wait_on(bar(B::P + buf), (pn >> 1) & 1, stop);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int y = 0; y < C::BN / 16; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, y > 0 || j - 1 > my0);
+              mma_commit(bar(B::O + i));
+              ++pn;
+            }
+            release();
           }
           if (j + 1 == r.J1) mma_commit(bar(B::Q_FREE));
         }
@@ -677,9 +556,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       // every slot of the ring in turn, so that none is filled again behind this warp's back
       const int loads = 2 * (r.J1 - r.J0);
       for (int x = 0; x < loads && ok; ++x) {
-        // K(J0) V(J0) K V ...; with two score buffers K(J0) K(J0 + 1) V(J0) K V ... V V
-        const bool v_load = C::NSB == 1 ? (x & 1) : (x + 1 == loads || (x > 0 && !(x & 1)));
-        const int j = r.J0 + (C::NSB == 1 ? x >> 1 : (x + 1 == loads ? (loads >> 1) - 1 : (x >> 1) - 1));
+        // K(J0) K(J0 + 1) V(J0) K V ... K V V
+        const bool v_load = x + 1 == loads || (x > 0 && !(x & 1));
+        const int j = r.J0 + (x + 1 == loads ? (loads >> 1) - 1 : (x >> 1) - 1);
         ok = warp_wait_on(bar(B::FULL + slot), phase, stop);
         if (!ok) break;
         if (v_load && r.partly(j)) {
