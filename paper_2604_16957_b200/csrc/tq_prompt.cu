@@ -33,6 +33,9 @@
 #include "tq_prompt.cuh"
 #include "tq_tcgen05.cuh"
 
+#ifndef TQ_POLY
+#define TQ_POLY 0
+#endif
 namespace tq {
 namespace {
 
@@ -51,10 +54,12 @@ struct Cfg {
   static constexpr int QCHUNK = 128 * 128;            // bytes of 128 rows x 64 channels
   static constexpr int QTILE = (D / 64) * QCHUNK;
   static constexpr int KCHUNK = BN * 128;
-  static constexpr int SLOT = (D / 64) * KCHUNK;      // a K tile; a V tile needs no more
-  static constexpr int NS = D <= 128 ? 10 : (D == 256 ? 5 : 3);  // slots of the K / V ring
+  static constexpr int KT = (D / 64) * KCHUNK;        // K tile
+  static constexpr int VT = (DV / 64) * KCHUNK;       // V tile
+  static constexpr int STAGE = KT + VT;               // what step j reads: K(j) for its scores, V(j - 1) for its outputs
+  static constexpr int NS = D == 64 ? 8 : (D == 128 ? 5 : 2);
   static constexpr int RING = NQ * QTILE;
-  static constexpr int BARS = RING + NS * SLOT;
+  static constexpr int BARS = RING + NS * STAGE;
   static constexpr int SMEM = BARS + 512 + 1024;      // barriers, and room to align the base
   static constexpr int O_COL = 2 * NQ * BN;           // TMEM columns: two S buffers per query tile (P over S), O behind
   static_assert(O_COL + NQ * DV <= 512, "tensor memory");
@@ -69,7 +74,7 @@ struct Maps {
 template <int D>
 struct Bars {
   using C = Cfg<D>;
-  static constexpr int FULL = 0, EMPTY = FULL + C::NS, READY = EMPTY + C::NS;  // K / V slots: landed, free, looked through
+  static constexpr int FULL = 0, EMPTY = FULL + C::NS, READY = EMPTY + C::NS;  // stages: landed, free, looked through
   static constexpr int Q = READY + C::NS, Q_FREE = Q + 1;
   static constexpr int S = Q_FREE + 1, P = S + 2 * C::NQ, O = P + 2 * C::NQ;  // scores and weights (two buffers), outputs
   static constexpr int WORK = O + C::NQ, WORK_FREE = WORK + 2, STEAL = WORK_FREE + 2, DRAIN = STEAL + 1, COUNT = DRAIN + 1;
@@ -116,6 +121,33 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if on
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+
+// 2^y for two y <= 2^7 on the FMA units: y = n + f with n an integer and |f| <= 1/2, 2^f by a polynomial that is minimax
+// in the relative error on that interval (fitted by linear programming: 7.5e-5 at degree 3, 2.6e-6 at degree 4, against
+// the 2^-9 and 2^-12 of the rounding to bf16 and fp16 that follows), n added to the exponent.
+template <int DT>
+__device__ __forceinline__ float2 exp2_pair(uint64_t y) {
+  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
+  const float2 v = unpair(y);
+  y = pair(fmaxf(v.x, -126.0f), fmaxf(v.y, -126.0f));
+  const uint64_t t = add2(y, pair(kMagic, kMagic));
+  const uint64_t f = fma2(add2(t, pair(-kMagic, -kMagic)), pair(-1.0f, -1.0f), y);
+  auto both = [](float x) { return pair(x, x); };
+  uint64_t p;
+  if (DT == TQ_BF16) {
+    p = fma2(both(0.05517132207751274f), f, both(0.2426113337278366f));
+    p = fma2(p, f, both(0.6932610869407654f));
+    p = fma2(p, f, both(0.9999280571937561f));
+  } else {
+    p = fma2(both(0.00957053154706955f), f, both(0.05591866374015808f));
+    p = fma2(p, f, both(0.24024735391139984f));
+    p = fma2(p, f, both(0.6931216716766357f));
+    p = fma2(p, f, both(0.9999992847442627f));
+  }
+  const float2 q = unpair(p), n = unpair(t);
+  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(n.x) << 23)),
+                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // nonzero if one of the two 16-bit values of a word is an infinity or a NaN
@@ -227,7 +259,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     // not 0: a hidden key's score is -inf, and has to stay that
     const float c = fmaxf(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f);
     bool ok = true;
-    uint32_t total = 0;  // K / V tiles of this query tile in all work so far
+    uint32_t total = 0, out = 0;  // K / V tiles of this query tile, and arrivals on its outputs, in all work so far
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
       const Span<D> r(a, w, T);
@@ -238,6 +270,12 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       float m = -INFINITY, l = 0.0f;
       int n = 0;  // K / V tiles of this work
       const int my0 = i == 0 ? r.j0[0] : r.j0[C::NQ - 1], my1 = i == 0 ? r.j1[0] : r.j1[C::NQ - 1];
+      // The outputs of the tiles before j are complete once the scores of tile j + 1 are (their MMAs are issued behind);
+      // the last two outputs of a piece of work arrive on a barrier of their own.
+      auto outputs_before = [&](int j, uint32_t use) {
+        if (j + 1 < my1) return warp_wait_on(bar(B::S + 2 * i + ((use + 1) & 1)), ((use + 1) >> 1) & 1, stop);
+        return warp_wait_on(bar(B::O + i), out & 1, stop);
+      };
       for (int j = my0; j < my1 && ok; ++j, ++n) {
         const uint32_t use = total + n;
         const int buf = 2 * i + (use & 1);
@@ -277,8 +315,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           l *= scale;
         }
         if (n > 0 && __any_sync(0xffffffffu, raise)) {
-          // O of the tiles before is complete once its MMA has arrived on O
-          ok = warp_wait_on(bar(B::O + i), (total + n - 1) & 1, stop);
+          ok = outputs_before(j, use);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
@@ -299,11 +336,17 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 2) {
-            const float2 z = unpair(fma2(pair(s[x + y], s[x + y + 1]), c2, mc2));
-            const float e0 = ex2(z.x), e1 = ex2(z.y);
-            if (y & 2) sum1 = add2(sum1, pair(e0, e1));
-            else sum0 = add2(sum0, pair(e0, e1));
-            p[y >> 1] = pack2<DT>(e0, e1);
+            const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
+            float2 e;
+            if (C::NQ == 2 && (y / 2 * TQ_POLY) % 16 + TQ_POLY > 15) {
+              e = exp2_pair<DT>(z);
+            } else {
+              e = unpair(z);
+              e = make_float2(ex2(e.x), ex2(e.y));
+            }
+            if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
+            else sum0 = add2(sum0, pair(e.x, e.y));
+            p[y >> 1] = pack2<DT>(e.x, e.y);
           }
           tmem_st16(s_addr + (x >> 1), p);
         }
@@ -311,11 +354,12 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           const float2 v = unpair(add2(sum0, sum1));
           l = v.x + v.y;
         }
-        // The epilogue's wait for the last output MMA must find the one before it complete: a barrier tells a phase from
-        // the one before, not from the one before that.
+        // The epilogue's wait for the last outputs must find those before them complete: a barrier tells a phase from the
+        // one before, not from the one before that.
         if (n > 0 && j + 1 == my1) {
-          ok = warp_wait_on(bar(B::O + i), (use - 1) & 1, stop);
+          ok = outputs_before(j, use);
           if (!ok) break;
+          ++out;
         }
         tmem_wait_st();
         tc_fence_before();
@@ -324,7 +368,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       }
       total += n;
       // ---- epilogue: the thread's row of O
-      if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), (total - 1) & 1, stop);
+      if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), out++ & 1, stop);
       if (ok) {
         tc_fence_after();
         const float inv = up > lo ? 1.0f / l : 0.0f;
@@ -387,21 +431,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
       // Tiles of a sequence: b starts at tile q_offsets[b] / TT + b, which leaves room for its ceil(lq / TT) tiles.  The late
       // tiles of a sequence see the most keys under the causal mask and go first.
       auto start_of = [&](int b) { return min(max(a.q_offsets[b], 0), a.n_q) / TT + b; };
-      int id = blockIdx.x, b = -1, it = 0, slot = 0, q_uses = 0;
-      uint32_t phase = 1, issued = 0;  // the first pass over the ring finds every slot empty
+      int id = blockIdx.x, b = -1, it = 0, stage = 0, q_uses = 0;
+      uint32_t phase = 1, issued = 0;  // the first pass over the ring finds every stage empty
       bool ok = true;
-      auto load = [&](const CUtensorMap* map, const Work& w, int j, int chunk0, int chunks) {
-        ok = ok && wait_on(bar(B::EMPTY + slot), phase, stop);
-        if (!ok) return;
-        mbar_expect_tx(bar(B::FULL + slot), chunks * C::KCHUNK);
-        for (int x = 0; x < chunks; ++x)
-          tma_load_3d(base + C::RING + slot * C::SLOT + x * C::KCHUNK, map, 64 * (chunk0 + x), w.h, w.s.k0 + j * C::BN, bar(B::FULL + slot));
-        ++issued;
-        if (++slot == C::NS) {
-          slot = 0;
-          phase ^= 1;
-        }
-      };
       for (int asked = 0; ok; ++asked) {
         Work w = {};
         if (id >= 0) {
@@ -446,10 +478,21 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
                 for (int x = 0; x < D / 64; ++x)
                   tma_load_3d(base + i * C::QTILE + x * C::QCHUNK, &maps.q, 64 * x, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
             }
-            // in the order in which the MMAs take them
             for (int j = r.J0; j <= r.J1 && ok; ++j) {
-              if (j < r.J1) load(&maps.k, w, j, 0, D / 64);
-              if (j > r.J0) load(&maps.v, w, j - 1, w.half * (C::DV / 64), C::DV / 64);
+              ok = wait_on(bar(B::EMPTY + stage), phase, stop);
+              if (!ok) break;
+              const uint32_t to = base + C::RING + stage * C::STAGE, full = bar(B::FULL + stage);
+              mbar_expect_tx(full, (j < r.J1 ? C::KT : 0) + (j > r.J0 ? C::VT : 0));
+              if (j < r.J1)
+                for (int x = 0; x < D / 64; ++x) tma_load_3d(to + x * C::KCHUNK, &maps.k, 64 * x, w.h, w.s.k0 + j * C::BN, full);
+              if (j > r.J0)
+                for (int x = 0; x < C::DV / 64; ++x)
+                  tma_load_3d(to + C::KT + x * C::KCHUNK, &maps.v, w.half * C::DV + 64 * x, w.h, w.s.k0 + (j - 1) * C::BN, full);
+              ++issued;
+              if (++stage == C::NS) {
+                stage = 0;
+                phase ^= 1;
+              }
             }
           }
         }
@@ -475,97 +518,89 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     }
   } else if (warp <= C::SOFT + C::NQ) {
     // =================================================================================== MMAs of one query tile
-    const int i = warp - C::SOFT - 1;
+    // The warp stays together and its control flow is uniform (values from shared memory are broadcast from lane 0 to
+    // make that known), see mma_ss.
+    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const int i = uniform(warp) - C::SOFT - 1;
+    const uint32_t leader = elect_one(), tm = uniform(tmem);
     const uint32_t id_s = instr_desc(DT == TQ_BF16, 128, C::BN, false) | (a.attn_scale < 0.0f ? kNegateA : 0u);
     const uint32_t id_o = instr_desc(DT == TQ_BF16, 128, C::DV, true);
     const uint32_t q_lo = desc_lo(base + i * C::QTILE, 0), ring_lo = desc_lo(base + C::RING, 0);
-    const uint32_t o_at = tmem + C::O_COL + i * C::DV;
-    int slot = 0;
+    const uint32_t o_at = tm + C::O_COL + i * C::DV;
+    int stage = 0;
     uint32_t phase = 0, sn = 0, pn = 0, q_uses = 0;  // S and P tiles so far
     bool ok = true;
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
       const Span<D> r(a, w, T);
-      if (lane == 0 && r.J1 > r.J0) {
-        const int my0 = i == 0 ? r.j0[0] : r.j0[C::NQ - 1], my1 = i == 0 ? r.j1[0] : r.j1[C::NQ - 1];
-        auto landed = [&](int x, uint32_t ph, bool looked_through) {
-          ok = ok && wait_on(bar(B::FULL + x), ph, stop);
-          // (only behind FULL: before it, READY may still be two phases back, which it cannot tell from this one)
-          if (looked_through) ok = ok && wait_on(bar(B::READY + x), ph, stop);
-        };
-        auto release = [&]() {  // the slot, once everything issued so far has read it
-          mma_commit(bar(B::EMPTY + slot));
-          if (++slot == C::NS) {
-            slot = 0;
-            phase ^= 1;
-          }
-        };
-        ok = wait_on(bar(B::Q), q_uses++ & 1, stop);
-        for (int j = r.J0; j <= r.J1 && ok; ++j) {
-          if (j < r.J1) {
-            landed(slot, phase, false);
-            if (!ok) break;
-            if (j >= my0 && j < my1) {
-              // S into the buffer whose weights the output MMAs issued before have read
-              const int buf = 2 * i + (sn & 1);
-              const uint32_t d = tmem + buf * C::BN, k_at = ring_lo + slot * (C::SLOT >> 4);
+      const int J0 = uniform(r.J0), J1 = uniform(r.J1), lo = uniform(r.lo), up = uniform(r.up);
+      const int my0 = uniform(i == 0 ? r.j0[0] : r.j0[C::NQ - 1]), my1 = uniform(i == 0 ? r.j1[0] : r.j1[C::NQ - 1]);
+      if (J1 <= J0) continue;
+      // one stage to wait for and to release per step; it is released behind the next step's scores, where the tensor
+      // cores have work
+      constexpr bool kLate = C::NS > 2;
+      int owed = -1;
+      ok = warp_wait_on(bar(B::Q), q_uses++ & 1, stop);
+      for (int j = J0; j <= J1 && ok; ++j) {
+        ok = warp_wait_on(bar(B::FULL + stage), phase, stop);
+        if (!ok) break;
+        const uint32_t at = ring_lo + stage * (C::STAGE >> 4);
+        if (j >= my0 && j < my1) {
+          // S into the buffer whose weights the output MMAs issued before have read
+          const int buf = 2 * i + (sn & 1);
+          const uint32_t d = tm + buf * C::BN;
 #pragma unroll
-              for (int y = 0; y < D / 16; ++y)
-                mma_ss(d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), k_at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
-                       kDescHi, id_s, y > 0);
-              mma_commit(bar(B::S + buf));
-              ++sn;
-            }
-            release();
-          }
-          if (j > r.J0) {
-            landed(slot, phase, r.partly(j - 1));
-            if (!ok) break;
-            if (j - 1 >= my0 && j - 1 < my1) {
-              const int buf = 2 * i + (pn & 1);
-              const uint32_t p = tmem + buf * C::BN, v_at = ring_lo + ((C::KCHUNK >> 4) << 16) + slot * (C::SLOT >> 4);
-              ok = wait_on(bar(B::P + buf), (pn >> 1) & 1, stop);
-              if (!ok) break;
-              tc_fence_after();
+          for (int y = 0; y < D / 16; ++y)
+            mma_ss(leader, d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
+                   kDescHi, id_s, y > 0);
+          mma_commit(leader, bar(B::S + buf));
+          ++sn;
+        }
+        if (j + 1 == J1) mma_commit(leader, bar(B::Q_FREE));
+        if (owed >= 0) mma_commit(leader, bar(B::EMPTY + owed));
+        if (j - 1 >= my0 && j - 1 < my1) {
+          // (READY only behind FULL: before it, READY may still be two phases back, which it cannot tell from this one)
+          if ((j - 1) * C::BN < lo || j * C::BN > up) ok = warp_wait_on(bar(B::READY + stage), phase, stop);
+          const int buf = 2 * i + (pn & 1);
+          const uint32_t p = tm + buf * C::BN, v_at = at + (C::KT >> 4) + ((C::KCHUNK >> 4) << 16);
+          ok = ok && warp_wait_on(bar(B::P + buf), (pn >> 1) & 1, stop);
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll
-              for (int y = 0; y < C::BN / 16; ++y) mma_ts(o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, y > 0 || j - 1 > my0);
-              mma_commit(bar(B::O + i));
-              ++pn;
-            }
-            release();
-          }
-          if (j + 1 == r.J1) mma_commit(bar(B::Q_FREE));
+          for (int y = 0; y < C::BN / 16; ++y)
+            mma_ts(leader, o_at, p + 8 * y, v_at + (2048 >> 4) * y, kDescHi, id_o, y > 0 || j - 1 > my0);
+          if (j + 1 >= my1) mma_commit(leader, bar(B::O + i));
+          ++pn;
+        }
+        if (kLate && j < J1) owed = stage;
+        else mma_commit(leader, bar(B::EMPTY + stage));
+        if (++stage == C::NS) {
+          stage = 0;
+          phase ^= 1;
         }
       }
-      ok = __shfl_sync(0xffffffffu, ok, 0);
     }
     // everything issued has completed before the block gives its memory back
-    if (lane == 0) {
-      mma_commit(bar(B::DRAIN));
-      if (!wait_stage_inline(bar(B::DRAIN), 0, kTileWait)) *stop = 1;
-    }
+    mma_commit(leader, bar(B::DRAIN));
+    if (!__all_sync(0xffffffffu, wait_stage_inline(bar(B::DRAIN), 0, kTileWait))) *stop = 1;
   } else {
     // ============================================================= V tiles that some row sees in part: finite values
     const int me = tid - 32 * (C::SOFT + 1 + C::NQ);
     bool ok = true;
-    int slot = 0;
+    int stage = 0;
     uint32_t phase = 0;
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
       const Span<D> r(a, w, T);
-      // every slot of the ring in turn, so that none is filled again behind this warp's back
-      const int loads = 2 * (r.J1 - r.J0);
-      for (int x = 0; x < loads && ok; ++x) {
-        // K(J0) K(J0 + 1) V(J0) K V ... K V V
-        const bool v_load = x + 1 == loads || (x > 0 && !(x & 1));
-        const int j = r.J0 + (x + 1 == loads ? (loads >> 1) - 1 : (x >> 1) - 1);
-        ok = warp_wait_on(bar(B::FULL + slot), phase, stop);
+      // every stage of the ring in turn, so that none is filled again behind this warp's back
+      for (int j = r.J0; j <= r.J1 && r.J1 > r.J0 && ok; ++j) {
+        ok = warp_wait_on(bar(B::FULL + stage), phase, stop);
         if (!ok) break;
-        if (v_load && r.partly(j)) {
-          uint4* tile = reinterpret_cast<uint4*>(smem + C::RING + slot * C::SLOT);
+        if (j > r.J0 && r.partly(j - 1)) {
+          uint4* tile = reinterpret_cast<uint4*>(smem + C::RING + stage * C::STAGE + C::KT);
           bool found = false;
 #pragma unroll 8
-          for (int y = me; y < (C::DV / 64) * C::KCHUNK / 16; y += 32 * C::SCRUB) {
+          for (int y = me; y < C::VT / 16; y += 32 * C::SCRUB) {
             const uint4 v = tile[y];
             if (not_finite2<DT>(v.x) | not_finite2<DT>(v.y) | not_finite2<DT>(v.z) | not_finite2<DT>(v.w)) {
               auto clean = [](uint32_t z) {
@@ -581,11 +616,11 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
         }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(bar(B::READY + slot));
-          mbar_arrive(bar(B::EMPTY + slot));
+          mbar_arrive(bar(B::READY + stage));
+          mbar_arrive(bar(B::EMPTY + stage));
         }
-        if (++slot == C::NS) {
-          slot = 0;
+        if (++stage == C::NS) {
+          stage = 0;
           phase ^= 1;
         }
       }

@@ -97,27 +97,38 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, int m, int n, bool 
 }
 constexpr uint32_t kNegateA = 1u << 13;
 
-// D (tensor memory) = A B or D + A B; one thread issues, the operation is asynchronous.  The issuing thread feeds the
-// tensor cores an instruction every 64 cycles, so little may stand between two of them: descriptors come as their
-// constant high word and a low word that is a sum of a register and a constant.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
+// One lane of a converged warp, the same one in every call: 1 there, 0 in the others.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t yes;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(yes));
+  return yes;
+}
+// D (tensor memory) = A B or D + A B, issued by the lane whose `leader` is 1; the operation is asynchronous.  The whole
+// warp comes here with the same operands: they live in uniform registers, where the instruction wants them.  (Issued from
+// a branch that one lane takes, every operand is moved there first, and the issuing thread, not the tensor cores, sets
+// the pace.)  Descriptors come as their constant high word and a low word that is a sum of a register and a constant.
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 x, y;\nsetp.ne.u32 p, %5, 0;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}\n" ::"r"(d),
-      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add))
+      "{\n.reg .pred p, q;\n.reg .b64 x, y;\nsetp.ne.u32 p, %5, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add)), "r"(leader)
       : "memory");
 }
 // the same with A in tensor memory (two 16-bit elements of K per column)
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 y;\nsetp.ne.u32 p, %5, 0;\nmov.b64 y, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}\n" ::"r"(d),
-      "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add))
+      "{\n.reg .pred p, q;\n.reg .b64 y;\nsetp.ne.u32 p, %5, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 y, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add)), "r"(leader)
       : "memory");
 }
-// arrives on the mbarrier once every tcgen05.mma that this thread issued before has completed
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
+// arrives on the mbarrier once every tcgen05.mma that the leader issued before has completed
+__device__ __forceinline__ void mma_commit(uint32_t leader, uint32_t bar) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.u32 q, %1, 0;\n"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar),
+      "r"(leader)
+      : "memory");
 }
 
 }  // namespace tq
