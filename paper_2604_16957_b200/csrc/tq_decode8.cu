@@ -252,6 +252,11 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (blockIdx.x == 0 && a.status && (!few || warp == 0) && (len <= 0 || len > a.c.S_cap))
         atomicOr(a.status, (len < 0 || len > a.c.S_cap ? TQ_STATUS_BAD_LEN : 0) | (len <= 0 ? TQ_STATUS_EMPTY_SEQ : 0));
     }
+    if (a.c.B == 1) {  // nothing to sum up
+      own_n = __shfl_sync(0xffffffffu, own_n, 0);
+      W = own_upto = own_n;
+      break;
+    }
     long long all;
     own_upto = scan(own_n, all);
     W += all;
@@ -268,9 +273,11 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   }
 
   // sequences without a token: their rows are zero
-  for (int b = blockIdx.x; b < a.c.B; b += gridDim.x)
-    if (span_of(a, b).blocks() == 0)
+  if (!few || __any_sync(0xffffffffu, lane < a.c.B && own_n == 0))
+    for (int b = blockIdx.x; b < a.c.B; b += gridDim.x) {
+      if (span_of(a, b).blocks() != 0) continue;
       for (int i = tid; i < a.H_q * D; i += C::LAUNCH) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
+    }
   if (static_cast<int>(blockIdx.x) >= N || W == 0) return;
 
   const Shares shares(W, N);
@@ -283,7 +290,10 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       s_start = (upto - n) * a.units;
     }
   };
-  if (few) {
+  if (a.c.B == 1) {
+    first_b = 0;
+    first_at = 0;
+  } else if (few) {
     // the owner's lane tells its warp
     const bool holds = own_n > 0 && own_upto * a.units > g0 && (own_upto - own_n) * a.units <= g0;
     const int from = __ffs(static_cast<int>(__ballot_sync(0xffffffffu, holds))) - 1;
@@ -530,6 +540,13 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       st[2 * C::NW * 8] = l0;
       st[2 * C::NW * 8 + 1] = l1;
     }
+    const bool whole = use.j0 == 0 && use.j1 == use.n;
+    const long long u0 = use.g - use.j0;  // the unit on the line, and the thread blocks that share it
+    int from = 0, to = 0;
+    if (!whole) {
+      from = shares.owner(u0);
+      to = shares.owner(u0 + use.n - 1);
+    }
     join_warps();
     for (int q = warp; q < 8; q += C::NW) {
       const bool has = lane < C::NW;
@@ -551,7 +568,6 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
     }
     join_warps();
-    const bool whole = use.j0 == 0 && use.j1 == use.n;
     const long long part = 2LL * blockIdx.x + (use.g == g0 ? 0 : 1);
     float* const mine = a.parts + part * 8 * (D + 2);
     const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
@@ -601,15 +617,13 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         mine[8 * D + 8 + tid] = sums[16 + tid];
       }
       const long long unit = static_cast<long long>(use.b) * a.units + use.u;
-      const long long u0 = use.g - use.j0, u1 = u0 + use.n;  // the unit on the line
-      const int from = shares.owner(u0), to = shares.owner(u1 - 1);
       join_warps();
       if (tid == 0) {
-        __threadfence();  // the block's writes, ordered before it by the barrier
-        const int got = atomicAdd(a.counters + unit, 1);
+        // releases the block's writes, which the barrier orders before it, and acquires those of the blocks before
+        int got;
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(got) : "l"(a.counters + unit) : "memory");
         s_last = got == to - from;
         if (s_last) a.counters[unit] = 0;  // left as it was found
-        __threadfence();
       }
       join_warps();
       if (s_last) {
@@ -619,16 +633,17 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         // The maxima and sums of all parts at once, one query head per warp for the weights; then the rows.  The loads are
         // independent of each other, and the first CH rows are on their way while the weights are made (a running maximum
         // would wait for a round trip to L2 per part: 17 us of a 64 us launch).
-        constexpr int CH = 16;
+        constexpr int CH = 9;
         float* const wts = merge;  // [2][8][np]
-        float2 rows[CH];
-        const int items = heads * (D / 2);
-        const int q1 = tid / (D / 2), c1st = 2 * (tid - q1 * (D / 2));
-        if (tid < items) {
+        float4 rows[CH];
+        const int items = heads * (D / 4);
+        auto fetch = [&](int i, int p0) {
+          const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
 #pragma unroll
           for (int p = 0; p < CH; ++p)
-            if (p < np) rows[p] = __ldcg(reinterpret_cast<const float2*>(part_of(p) + q1 * D + c1st));
-        }
+            if (p0 + p < np) rows[p] = __ldcg(reinterpret_cast<const float4*>(part_of(p0 + p) + q * D + ch));
+        };
+        if (tid < items) fetch(tid, 0);
         for (int i = tid; i < 8 * np; i += C::THREADS) {
           const float* src = part_of(i >> 3) + 8 * D + (i & 7);
           wts[(i & 7) * np + (i >> 3)] = __ldcg(src);
@@ -651,22 +666,23 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         }
         join_warps();
         for (int i = tid; i < items; i += C::THREADS) {
-          const int q = i / (D / 2), ch = 2 * (i - q * (D / 2));
-          float2 x = make_float2(0.0f, 0.0f);
+          const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
+          float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           for (int p0 = 0; p0 < np; p0 += CH) {
-            if (i != tid || p0 > 0) {
-#pragma unroll
-              for (int p = 0; p < CH; ++p)
-                if (p0 + p < np) rows[p] = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + p) + q * D + ch));
-            }
+            if (i != tid || p0 > 0) fetch(i, p0);
 #pragma unroll
             for (int p = 0; p < CH; ++p)
               if (p0 + p < np) {
-                x.x += wts[q * np + p0 + p] * rows[p].x;
-                x.y += wts[q * np + p0 + p] * rows[p].y;
+                const float w = wts[q * np + p0 + p];
+                x.x += w * rows[p].x;
+                x.y += w * rows[p].y;
+                x.z += w * rows[p].z;
+                x.w += w * rows[p].w;
               }
           }
-          store_out2<OT>(a.out, (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch, x.x * sums[q], x.y * sums[q]);
+          const long long at = (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch;
+          store_out2<OT>(a.out, at, x.x * sums[q], x.y * sums[q]);
+          store_out2<OT>(a.out, at + 2, x.z * sums[q], x.w * sums[q]);
         }
       }
       join_warps();
