@@ -7,7 +7,7 @@
 //     P = 2^(c S - c m), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
 // c = alpha log2 e > 0 (for a negative alpha the MMA negates Q).  m is raised only when a score exceeds it by more than
-// 2^8; then the thread rescales its row of O in TMEM.  S has two buffers per tile: the scores of the next keys are made
+// 2^12; then the thread rescales its row of O in TMEM.  S has two buffers per tile: the scores of the next keys are made
 // while the softmax of these runs.  That takes key tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at
 // d = 128), for which an MMA of 128 x 64 x 16 reads its operands in 48 cycles instead of the 32 that it computes; with
 // tiles of 128 keys and one buffer the MMAs are faster (64 cycles for twice the work), but outputs, scores and softmax of
@@ -40,7 +40,7 @@ namespace tq {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running maximum: weights stay below 2^8
+constexpr float kSlack = 12.0f;  // log2 units a score may exceed the running maximum: weights stay below 2^12
 
 template <int D>
 struct Cfg {
@@ -57,9 +57,11 @@ struct Cfg {
   static constexpr int KT = (D / 64) * KCHUNK;        // K tile
   static constexpr int VT = (DV / 64) * KCHUNK;       // V tile
   static constexpr int STAGE = KT + VT;               // what step j reads: K(j) for its scores, V(j - 1) for its outputs
-  static constexpr int NS = D == 64 ? 8 : (D == 128 ? 5 : 2);
+  static constexpr int NS = D == 64 ? 8 : (D == 128 ? 4 : 2);
   static constexpr int RING = NQ * QTILE;
-  static constexpr int BARS = RING + NS * STAGE;
+  static constexpr int OUT = RING + NS * STAGE;       // output rows on their way out, 4 KB per softmax warp
+  static constexpr bool STAGED = D <= 256;            // (no room at d = 512)
+  static constexpr int BARS = OUT + (STAGED ? SOFT * 4096 : 0);
   static constexpr int SMEM = BARS + 512 + 1024;      // barriers, and room to align the base
   static constexpr int O_COL = 2 * NQ * BN;           // TMEM columns: two S buffers per query tile (P over S), O behind
   static_assert(O_COL + NQ * DV <= 512, "tensor memory");
@@ -240,6 +242,14 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
   pdl_launch_dependents();
   pdl_wait();
 
+  // With two tiles there are 384 threads of 168 registers; the softmax threads take 208 of them and leave 80 to the others
+  // (256 x 208 + 128 x 80 = 63488 of 64512).
+  if (C::NQ == 2) {
+    static_assert(C::NQ == 1 || (C::THREADS == 384 && 256 * 208 + 128 * 80 <= 384 * 168), "register split");
+    if (warp < C::SOFT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
+  }
+
   // the it-th piece of work, for every warp but the one that finds it; false: none, or the block winds down
   auto next_work = [&](int it, Work& w) {
     if (!warp_wait_on(bar(B::WORK + (it & 1)), (it >> 1) & 1, stop, kBlockWait)) return false;
@@ -319,13 +329,15 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
-          for (int x = 0; x < C::DV; x += 16) {
-            uint32_t o[16];
-            tmem_ld16(o_addr + x, o);
+          for (int x = 0; x < C::DV; x += 64) {
+            uint32_t o[64];
+            tmem_ld32(o_addr + x, o);
+            tmem_ld32(o_addr + x + 32, o + 32);
             tmem_wait_ld();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
-            tmem_st16(o_addr + x, o);
+            for (int y = 0; y < 64; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * scale);
+            tmem_st32(o_addr + x, o);
+            tmem_st32(o_addr + x + 32, o + 32);
           }
         }
         const float mc = m == -INFINITY ? 0.0f : m * c;
@@ -375,50 +387,81 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
         const bool mend = s_scrubbed[it & 3] != 0;
         const int head = w.h * G + (row - t * G);
         const long long to = (static_cast<long long>(w.s.q0 + tok) * a.H_q + head) * D + w.half * C::DV;
-#pragma unroll 1
-        for (int x = 0; x < C::DV; x += 32) {
+        // 32 channels of the row, from x on
+        auto channels = [&](int x, float (&f)[32]) {
           uint32_t o[32];
           if (n > 0) {
             tmem_ld32(o_addr + x, o);
             tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = 0;
           }
-          if (!real) continue;
-          float f[32];
 #pragma unroll
           for (int y = 0; y < 32; ++y) f[y] = up > lo ? __uint_as_float(o[y]) * inv : 0.0f;
-          if (mend) {
-            // infinities and NaN of tokens that this row sees, in tiles where they were taken out
-            for (int key = lo; key < up; ++key) {
-              if (!r.partly(key / C::BN)) {
-                key = (key / C::BN + 1) * C::BN - 1;
-                continue;
-              }
-              const uint32_t* src = reinterpret_cast<const uint32_t*>(
-                  static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * D + w.half * C::DV + x);
+          if (!mend) return;
+          // infinities and NaN of tokens that this row sees, in tiles where they were taken out
+          for (int key = lo; key < up; ++key) {
+            if (!r.partly(key / C::BN)) {
+              key = (key / C::BN + 1) * C::BN - 1;
+              continue;
+            }
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(
+                static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * D + w.half * C::DV + x);
 #pragma unroll
-              for (int y = 0; y < 32; y += 2) {
-                const uint32_t v = __ldg(src + (y >> 1));
-                if (not_finite2<DT>(v)) {
-                  const float2 g = unpack2<DT>(v);
-                  f[y] += g.x - g.x != 0.0f || g.x != g.x ? g.x : 0.0f;
-                  f[y + 1] += g.y - g.y != 0.0f || g.y != g.y ? g.y : 0.0f;
-                }
+            for (int y = 0; y < 32; y += 2) {
+              const uint32_t v = __ldg(src + (y >> 1));
+              if (not_finite2<DT>(v)) {
+                const float2 g = unpack2<DT>(v);
+                f[y] += g.x - g.x != 0.0f ? g.x : 0.0f;  // (true of an infinity and of a NaN)
+                f[y + 1] += g.y - g.y != 0.0f ? g.y : 0.0f;
               }
             }
           }
-          if (OT == TQ_FP32) {
-            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to + x);
+        };
+        // 16 bytes of the output row from channel y of f on
+        constexpr int kEach = OT == TQ_FP32 ? 4 : 8;
+        auto bytes16 = [&](const float (&f)[32], int y) {
+          if (OT == TQ_FP32)
+            return make_uint4(__float_as_uint(f[y]), __float_as_uint(f[y + 1]), __float_as_uint(f[y + 2]), __float_as_uint(f[y + 3]));
+          return make_uint4(pack2<DT>(f[y], f[y + 1]), pack2<DT>(f[y + 2], f[y + 3]), pack2<DT>(f[(y + 4) & 31], f[(y + 5) & 31]),
+                            pack2<DT>(f[(y + 6) & 31], f[(y + 7) & 31]));
+        };
+        constexpr long long kSize = OT == TQ_FP32 ? 4 : 2;
+        uint8_t* const dst = static_cast<uint8_t*>(a.out) + to * kSize;
+        if constexpr (C::STAGED) {
+          // Through shared memory, 128 bytes of the warp's 32 rows at a time: straight from the registers every store would
+          // touch 32 rows (8700 cycles for 128 rows of 256 channels).  16-byte piece p of row r lies at p ^ (r % 8).
+          constexpr int kCols = 128 / kSize;
+          uint4* const area = reinterpret_cast<uint4*>(smem + C::OUT + warp * 4096);
+          const unsigned valid = __ballot_sync(0xffffffffu, real);
+          const int sub = lane >> 3, piece = lane & 7;
+          uint8_t* rows[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) dst[y] = make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
-          } else {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to + x);
+          for (int y = 0; y < 8; ++y)
+            rows[y] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), 4 * y + sub)) + 16 * piece;
+#pragma unroll 1
+          for (int x = 0; x < C::DV; x += kCols) {
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              dst[y] = make_uint4(pack2<DT>(f[8 * y], f[8 * y + 1]), pack2<DT>(f[8 * y + 2], f[8 * y + 3]),
-                                  pack2<DT>(f[8 * y + 4], f[8 * y + 5]), pack2<DT>(f[8 * y + 6], f[8 * y + 7]));
+            for (int z = 0; z < kCols; z += 32) {
+              float f[32];
+              channels(x + z, f);
+#pragma unroll
+              for (int y = 0; y < 32; y += kEach) area[8 * lane + (((z + y) / kEach) ^ (lane & 7))] = bytes16(f, y);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              const int from = 4 * y + sub;
+              if (valid >> from & 1) *reinterpret_cast<uint4*>(rows[y] + x * kSize) = area[8 * from + (piece ^ (from & 7))];
+            }
+            __syncwarp();
+          }
+        } else {
+#pragma unroll 1
+          for (int x = 0; x < C::DV; x += 32) {
+            float f[32];
+            channels(x, f);
+            if (real)
+#pragma unroll
+              for (int y = 0; y < 32; y += kEach) *reinterpret_cast<uint4*>(dst + (x + y) * kSize) = bytes16(f, y);
           }
         }
         tc_fence_before();
