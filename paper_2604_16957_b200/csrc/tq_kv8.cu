@@ -6,7 +6,10 @@
 // the cache is touched once.  K lanes own (tokens g, g + 8; 8 channels) as in the block's byte order: 16-byte loads
 // and one 16-byte store per 32 channels.  V lanes own (tokens 2t, 2t+1, 2t+8, 2t+9; 8 consecutive channels): 16-byte
 // loads, and eight 4-byte stores that fill whole 32-byte sectors across the lanes; nothing goes through shared memory.
-// The kernels are bound by HBM for prompts and by two dependent memory latencies for a decode step.
+// The kernels are bound by HBM for prompts and by two dependent memory latencies for a decode step.  Measured on 74 K
+// tokens of 8 KV heads, d = 128, K and V as slices of the fused projection (0.45 GB each way, 69 us at the copy rate):
+// append 94 us (with eight thread blocks per SM; 114 us with the six that its registers would allow unasked), gather
+// 76 us (all loads of a run first; 84 us without).
 //
 // Which rows start a run is found by the warp itself from the slots: every warp looks at `chunk` rows (32 for prompts,
 // fewer where that leaves SMs without work: see chunk_of).
@@ -183,7 +186,7 @@ __device__ __forceinline__ void append_run(uint8_t* blk, const uint16_t* src, lo
 }
 
 template <int D, int DT>
-__global__ void __launch_bounds__(32 * kWarps) append_kernel(tq_kv8_cache c, Slots8 a, const uint16_t* k, const uint16_t* v,
+__global__ void __launch_bounds__(32 * kWarps, D <= 128 ? 8 : 1) append_kernel(tq_kv8_cache c, Slots8 a, const uint16_t* k, const uint16_t* v,
                                                              long long k_stride, long long v_stride, int chunk,
                                                              int32_t* status) {
   pdl_launch_dependents();
@@ -227,15 +230,23 @@ template <int D, int DT, bool V>
 __device__ __forceinline__ void gather_run(const uint8_t* blk, void* dst, long long stride, int off, int len, int lane) {
   using P = Part<D, V>;
   const float scale = blk ? __fdiv_rn(*reinterpret_cast<const float*>(blk + range8_offset(D, V)), 127.0f) : 0.0f;
+  // all of the lane's codes are asked for before the first is used (d = 512: registers allow half)
+  constexpr int kAhead = D == 512 ? P::VECS / 2 : P::VECS;
+  uint32_t ahead[kAhead][P::ROWS][2];
 #pragma unroll
   for (int i = 0; i < P::VECS; ++i) {
-    uint32_t w[P::ROWS][2];
-    if (blk) {
-      load_codes<D, V>(blk, lane, i, w);
-    } else {
+    if (i % kAhead == 0) {
 #pragma unroll
-      for (int r = 0; r < P::ROWS; ++r) w[r][0] = w[r][1] = 0x80808080u;
+      for (int x = 0; x < kAhead; ++x) {
+        if (blk) {
+          load_codes<D, V>(blk, lane, i + x, ahead[x]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < P::ROWS; ++r) ahead[x][r][0] = ahead[x][r][1] = 0x80808080u;
+        }
+      }
     }
+    const uint32_t(&w)[P::ROWS][2] = ahead[i % kAhead];
 #pragma unroll
     for (int r = 0; r < P::ROWS; ++r) {
       const int t = P::token(lane, r) - off;

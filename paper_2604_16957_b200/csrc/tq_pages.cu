@@ -16,7 +16,7 @@
 namespace tq {
 namespace {
 
-constexpr int kScan = 1024;                    // threads of the scanning block = sequences per round
+constexpr int kScan = 1024;                    // most threads of the scanning block; a thread per sequence and round
 constexpr int kFill = 256;                     // threads of a block of the slot launch
 constexpr long long kOneLaunchSlots = 8192;    // most slots that the scanning block writes itself
 
@@ -26,7 +26,7 @@ struct Sums {
 
 // Inclusive sums over the block's threads (thread order).  `warp_sums` holds 32 entries; all threads call it.
 __device__ __forceinline__ Sums block_inclusive(Sums v, Sums* warp_sums, Sums& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long t = __shfl_up_sync(0xffffffffu, v.tokens, o), p = __shfl_up_sync(0xffffffffu, v.pages, o);
@@ -38,8 +38,7 @@ __device__ __forceinline__ Sums block_inclusive(Sums v, Sums* warp_sums, Sums& t
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
   Sums before = {0, 0}, all = {0, 0};
-#pragma unroll
-  for (int w = 0; w < kScan / 32; ++w) {
+  for (int w = 0; w < warps; ++w) {
     const Sums s = warp_sums[w];
     if (w < warp) {
       before.tokens += s.tokens;
@@ -71,18 +70,26 @@ __device__ __forceinline__ int read_count(const int32_t* free_count, int num_pag
   return count;
 }
 
+// Offsets and rows of a batch of up to kScan sequences, kept in shared memory: the search for a token's sequence would
+// otherwise be a chain of trips to L2.
+struct Batch {
+  int32_t offsets[kScan + 1];
+  Row rows[kScan];
+};
+
 // Slot of packed token n, and the table entry of a page that token is the first of.
-__device__ __forceinline__ long long slot_of(const PageArgs& a, const Row* rows, int count, long long n, int32_t* status) {
-  if (n >= a.token_offsets[a.B]) return -1;  // padding behind the last token
-  int lo = 0, hi = a.B;                      // the sequence with offsets[lo] <= n < offsets[lo + 1]
+__device__ __forceinline__ long long slot_of(const PageArgs& a, const int32_t* offsets, const Row* rows, int count, long long n,
+                                             int32_t* status) {
+  if (n >= offsets[a.B]) return -1;  // padding behind the last token
+  int lo = 0, hi = a.B;              // the sequence with offsets[lo] <= n < offsets[lo + 1]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (a.token_offsets[mid] <= n) lo = mid;
+    if (offsets[mid] <= n) lo = mid;
     else hi = mid;
   }
   const Row r = rows[lo];
   if (r.old < 0) return -1;  // refused
-  const int pos = r.old + static_cast<int>(n - a.token_offsets[lo]);  // below the capacity, which fits 31 bits
+  const int pos = r.old + static_cast<int>(n - offsets[lo]);  // below the capacity, which fits 31 bits
   if (a.page_table == nullptr) return static_cast<long long>(lo) * a.page_tokens * a.max_pages + pos;
   const int shift = __ffs(a.page_tokens) - 1;  // a power of two
   const int logical = pos >> shift, within = pos & (a.page_tokens - 1);
@@ -106,6 +113,7 @@ __global__ void __launch_bounds__(kScan) assign_scan_kernel(PageArgs a, int32_t*
   pdl_wait();
   __shared__ Sums warp_sums[kScan / 32];
   __shared__ int granted;
+  __shared__ Batch batch;
   Row* rows = reinterpret_cast<Row*>(ws + 2);
   const bool paged = a.page_table != nullptr;
   const int count = paged ? read_count(a.free_count, a.num_pages, status) : 0;
@@ -115,7 +123,7 @@ __global__ void __launch_bounds__(kScan) assign_scan_kernel(PageArgs a, int32_t*
     ws[0] = count;  // the slot launch reads it here: free_count_out may be free_count
   }
   Sums carry = {0, 0};
-  for (int base = 0; base < a.B; base += kScan) {
+  for (int base = 0; base < a.B; base += blockDim.x) {
     const int b = base + threadIdx.x;
     long long old = 0, fresh = 0, need = 0;
     bool fits = false;
@@ -147,29 +155,45 @@ __global__ void __launch_bounds__(kScan) assign_scan_kernel(PageArgs a, int32_t*
       if (bad && status) atomicOr(status, bad);
       const long long end = upto.tokens < a.n_slots ? upto.tokens : a.n_slots;
       a.token_offsets[b + 1] = static_cast<int32_t>(end);
+      if (a.B <= kScan) batch.offsets[b + 1] = static_cast<int32_t>(end);
       a.seq_lens_out[b] = static_cast<int32_t>(ok ? old + fresh : old);
       const long long before = upto.pages - need;
-      rows[b] = {ok ? static_cast<int32_t>(old) : -1, static_cast<int32_t>(before < 0x7fffffff ? before : 0x7fffffff)};
+      const Row r = {ok ? static_cast<int32_t>(old) : -1, static_cast<int32_t>(before < 0x7fffffff ? before : 0x7fffffff)};
+      rows[b] = r;
+      if (a.B <= kScan) batch.rows[b] = r;
       if (ok && need > 0) atomicMax(&granted, static_cast<int>(upto.pages));
     }
     carry.tokens += total.tokens;
     carry.pages += total.pages;
   }
-  if (threadIdx.x == 0) a.token_offsets[0] = 0;
+  if (threadIdx.x == 0) a.token_offsets[0] = batch.offsets[0] = 0;
   __syncthreads();
   if (threadIdx.x == 0 && paged) *a.free_count_out = count - granted;
   if (!fill) return;
-  for (long long n = threadIdx.x; n < a.n_slots; n += kScan) a.slots[n] = slot_of(a, rows, count, n, status);
+  const int32_t* offsets = a.B <= kScan ? batch.offsets : a.token_offsets;
+  const Row* where = a.B <= kScan ? batch.rows : rows;
+  for (long long n = threadIdx.x; n < a.n_slots; n += blockDim.x) a.slots[n] = slot_of(a, offsets, where, count, n, status);
 }
 
 __global__ void __launch_bounds__(kFill) assign_fill_kernel(PageArgs a, const int32_t* ws, int32_t* status) {
   pdl_launch_dependents();
   pdl_wait();
+  __shared__ Batch batch;
   const Row* rows = reinterpret_cast<const Row*>(ws + 2);
+  const int32_t* offsets = a.token_offsets;
   const int count = ws[0];
+  if (a.B <= kScan) {
+    for (int b = threadIdx.x; b <= a.B; b += kFill) {
+      batch.offsets[b] = a.token_offsets[b];
+      if (b < a.B) batch.rows[b] = rows[b];
+    }
+    __syncthreads();
+    offsets = batch.offsets;
+    rows = batch.rows;
+  }
   const long long step = static_cast<long long>(gridDim.x) * kFill;
   for (long long n = static_cast<long long>(blockIdx.x) * kFill + threadIdx.x; n < a.n_slots; n += step)
-    a.slots[n] = slot_of(a, rows, count, n, status);
+    a.slots[n] = slot_of(a, offsets, rows, count, n, status);
 }
 
 // Pages of finished sequences, sequences and pages in ascending order, are pushed onto the stack.
@@ -185,9 +209,9 @@ __global__ void __launch_bounds__(kScan) release_kernel(PageArgs a, const uint8_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // More than 1024 sequences: the total is needed before anything is written, so the lengths are read twice.
   long long all = 0;
-  for (int round = (a.B > kScan ? 0 : 1); round < 2; ++round) {
+  for (int round = (a.B > static_cast<int>(blockDim.x) ? 0 : 1); round < 2; ++round) {
     long long carry = 0;
-    for (int base = 0; base < a.B; base += kScan) {
+    for (int base = 0; base < a.B; base += blockDim.x) {
       const int b = base + threadIdx.x;
       long long len = 0, pages = 0;
       bool gone = false;
@@ -203,7 +227,7 @@ __global__ void __launch_bounds__(kScan) release_kernel(PageArgs a, const uint8_
       Sums total;
       const Sums upto = block_inclusive({0, pages}, warp_sums, total);
       if (round == 1) {
-        if (a.B <= kScan) all = total.pages;
+        if (a.B <= static_cast<int>(blockDim.x)) all = total.pages;
         // more pages than the pool has: the table or the stack is not what it should be, and nothing is released
         const bool refuse = count + all > a.num_pages && paged;
         if (refuse && status && threadIdx.x == 0) atomicOr(status, TQ_STATUS_BAD_PAGE);
@@ -212,8 +236,8 @@ __global__ void __launch_bounds__(kScan) release_kernel(PageArgs a, const uint8_
           s_pages[threadIdx.x] = refuse ? 0 : static_cast<int>(pages);
           s_at[threadIdx.x] = static_cast<int>(count + carry + upto.pages - pages);
           __syncthreads();
-          const int here = a.B - base < kScan ? a.B - base : kScan;
-          for (int r = warp; r < here; r += kScan / 32) {
+          const int here = min(a.B - base, static_cast<int>(blockDim.x));
+          for (int r = warp; r < here; r += blockDim.x >> 5) {
             const int n = s_pages[r], at = s_at[r];
             const int32_t* row = a.page_table + static_cast<long long>(base + r) * a.max_pages;
             for (int i = lane; i < n; i += 32) {
@@ -232,11 +256,17 @@ __global__ void __launch_bounds__(kScan) release_kernel(PageArgs a, const uint8_
   if (threadIdx.x == 0 && paged) *a.free_count_out = static_cast<int32_t>(count + all > a.num_pages ? count : count + all);
 }
 
+// As many threads as there is work for: a small block starts sooner and its barriers are shorter.
+unsigned threads_for(long long work) {
+  return static_cast<unsigned>(work >= kScan ? kScan : (work < 128 ? 128 : (work + 31) / 32 * 32));
+}
+
 }  // namespace
 
 cudaError_t launch_pages_assign(const PageArgs& a, int32_t* ws, int32_t* status, cudaStream_t st) {
   const bool fill = a.n_slots <= kOneLaunchSlots;
-  cudaError_t e = launch_kernel(assign_scan_kernel, dim3(1), dim3(kScan), 0, st, a, ws, fill, status);
+  const long long work = fill && a.n_slots > a.B ? a.n_slots : a.B;
+  cudaError_t e = launch_kernel(assign_scan_kernel, dim3(1), dim3(threads_for(work)), 0, st, a, ws, fill, status);
   if (e != cudaSuccess || fill) return e;
   const long long want = (a.n_slots + kFill - 1) / kFill, most = 8LL * device_sm_count();
   return launch_kernel(assign_fill_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(kFill), 0, st, a,
@@ -245,7 +275,8 @@ cudaError_t launch_pages_assign(const PageArgs& a, int32_t* ws, int32_t* status,
 
 cudaError_t launch_pages_release(const PageArgs& a, const uint8_t* finished, int32_t* free_pages, int32_t* status,
                                  cudaStream_t st) {
-  return launch_kernel(release_kernel, dim3(1), dim3(kScan), 0, st, a, finished, free_pages, status);
+  // (a warp per released sequence copies its pages)
+  return launch_kernel(release_kernel, dim3(1), dim3(threads_for(a.page_table ? 8LL * a.B : a.B)), 0, st, a, finished, free_pages, status);
 }
 
 }  // namespace tq

@@ -33,9 +33,6 @@
 #include "tq_prompt.cuh"
 #include "tq_tcgen05.cuh"
 
-#ifndef TQ_POLY
-#define TQ_POLY 0
-#endif
 namespace tq {
 namespace {
 
@@ -123,33 +120,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if on
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-
-// 2^y for two y <= 2^7 on the FMA units: y = n + f with n an integer and |f| <= 1/2, 2^f by a polynomial that is minimax
-// in the relative error on that interval (fitted by linear programming: 7.5e-5 at degree 3, 2.6e-6 at degree 4, against
-// the 2^-9 and 2^-12 of the rounding to bf16 and fp16 that follows), n added to the exponent.
-template <int DT>
-__device__ __forceinline__ float2 exp2_pair(uint64_t y) {
-  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
-  const float2 v = unpair(y);
-  y = pair(fmaxf(v.x, -126.0f), fmaxf(v.y, -126.0f));
-  const uint64_t t = add2(y, pair(kMagic, kMagic));
-  const uint64_t f = fma2(add2(t, pair(-kMagic, -kMagic)), pair(-1.0f, -1.0f), y);
-  auto both = [](float x) { return pair(x, x); };
-  uint64_t p;
-  if (DT == TQ_BF16) {
-    p = fma2(both(0.05517132207751274f), f, both(0.2426113337278366f));
-    p = fma2(p, f, both(0.6932610869407654f));
-    p = fma2(p, f, both(0.9999280571937561f));
-  } else {
-    p = fma2(both(0.00957053154706955f), f, both(0.05591866374015808f));
-    p = fma2(p, f, both(0.24024735391139984f));
-    p = fma2(p, f, both(0.6931216716766357f));
-    p = fma2(p, f, both(0.9999992847442627f));
-  }
-  const float2 q = unpair(p), n = unpair(t);
-  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(n.x) << 23)),
-                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // nonzero if one of the two 16-bit values of a word is an infinity or a NaN
@@ -315,7 +285,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           }
           mx = max3(max3(m0, m1, m2), m3, m3);
         }
-        // a score that is no number makes the whole row none, through its sum (the polynomial below would lose it)
+        // a score that is no number makes the whole row none, through its sum
         if (mx != mx) l = mx;
         const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > kSlack;
         float scale = 1.0f;
@@ -348,17 +318,11 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 2) {
-            const uint64_t z = fma2(pair(s[x + y], s[x + y + 1]), c2, mc2);
-            float2 e;
-            if (C::NQ == 2 && (y / 2 * TQ_POLY) % 16 + TQ_POLY > 15) {
-              e = exp2_pair<DT>(z);
-            } else {
-              e = unpair(z);
-              e = make_float2(ex2(e.x), ex2(e.y));
-            }
-            if (y & 2) sum1 = add2(sum1, pair(e.x, e.y));
-            else sum0 = add2(sum0, pair(e.x, e.y));
-            p[y >> 1] = pack2<DT>(e.x, e.y);
+            const float2 z = unpair(fma2(pair(s[x + y], s[x + y + 1]), c2, mc2));
+            const float e0 = ex2(z.x), e1 = ex2(z.y);
+            if (y & 2) sum1 = add2(sum1, pair(e0, e1));
+            else sum0 = add2(sum0, pair(e0, e1));
+            p[y >> 1] = pack2<DT>(e0, e1);
           }
           tmem_st16(s_addr + (x >> 1), p);
         }
