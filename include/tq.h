@@ -506,8 +506,9 @@ int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, in
  *   max_seq_len  : 0, or an upper bound on the lengths that the host knows; it only limits the launch
  *   workspace    : tq_int8_workspace_bytes(B, H_kv, H_q, d) bytes, 16-byte aligned: counters, then the partial results
  *                  of sequences that several thread blocks share.  ZERO the first tq_int8_counter_bytes(B, H_kv, H_q)
- *                  bytes once before the first use; every call leaves them zero.  Calls that may overlap on the GPU
- *                  (other streams, graphs replayed side by side) need workspaces of their own.
+ *                  bytes once before the first use; every call leaves them zero.  A workspace that goes on to calls with
+ *                  other B, H_kv, H_q or d is zeroed again in between.  Calls that may overlap on the GPU (other
+ *                  streams, graphs replayed side by side) need workspaces of their own.
  *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype)
  * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,

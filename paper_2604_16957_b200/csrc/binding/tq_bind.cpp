@@ -77,7 +77,7 @@ class Call {
         (heads > 1 && t.stride(1) != d))
       refuse(where_, (std::string(name) + " must be [" + std::to_string(n) + "][" + std::to_string(heads) + "][" +
                       std::to_string(d) + "] with its heads side by side").c_str());
-    return n > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), heads * d);  // the stride of a single row means nothing
+    return n > 1 ? t.stride(0) : heads * d;  // the stride of a single row means nothing
   }
   int dtype(const at::Tensor& t, const char* name) {
     switch (t.scalar_type()) {

@@ -58,6 +58,11 @@ struct Cfg {
   static_assert(BARS % 8 == 0 && QS % 8 == 0 && STAGE % 16 == 0 && SMEM <= 232448, "shared memory");
 };
 
+// The part of a cut unit that one thread block has done: `rows` rows of output, then their maxima and sums.
+__host__ __device__ constexpr int part_floats(int d, int rows) { return rows * d + (2 * rows + 3) / 4 * 4; }
+// How many there can be: a thread block cuts two units at most, and a line of U units in N shares has N + U - 1 pieces.
+inline long long part_count(long long units, int grid) { return units < grid ? grid + units : 2LL * grid; }
+
 struct Args {
   tq_kv8_cache c;
   const uint16_t* q;
@@ -68,7 +73,9 @@ struct Args {
   int grid;          // thread blocks launched
   int min_blocks;    // fewest cache blocks worth a thread block
   int32_t* counters;
-  float* parts;      // [2 grid][8][D + 2]
+  float* parts;      // see part_floats
+  int rows;          // query heads of a tile: at most 8
+  bool compact;      // fewer units than thread blocks: part of (thread block i, unit u) at i + u, else two per thread block
   void* out;
   int32_t* status;
 };
@@ -568,8 +575,9 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
     }
     join_warps();
-    const long long part = 2LL * blockIdx.x + (use.g == g0 ? 0 : 1);
-    float* const mine = a.parts + part * 8 * (D + 2);
+    const long long unit = static_cast<long long>(use.b) * a.units + use.u;
+    const int stride = part_floats(D, a.rows);
+    float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + (use.g == g0 ? 0 : 1)) * stride;
     const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
     auto emit = [&](int q, int ch, float x, float y) {
       x *= sums[24 + q];
@@ -612,11 +620,10 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       for (int q0 = 0; q0 < heads; q0 += C::MQ) join(merge, q0, std::integral_constant<int, C::MQ>{});
     }
     if (!whole) {
-      if (tid < 8) {
-        mine[8 * D + tid] = sums[tid];
-        mine[8 * D + 8 + tid] = sums[16 + tid];
+      if (tid < a.rows) {
+        mine[a.rows * D + tid] = sums[tid];
+        mine[a.rows * D + a.rows + tid] = sums[16 + tid];
       }
-      const long long unit = static_cast<long long>(use.b) * a.units + use.u;
       join_warps();
       if (tid == 0) {
         // releases the block's writes, which the barrier orders before it, and acquires those of the blocks before
@@ -629,7 +636,9 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (s_last) {
         const int skip = shares.start(from) == u0 ? 0 : 1;  // the first part is its thread block's second one
         const int np = to - from + 1;
-        auto part_of = [&](int p) { return a.parts + (2LL * (from + p) + (p == 0 ? skip : 0)) * 8 * (D + 2); };
+        auto part_of = [&](int p) {
+          return a.parts + (a.compact ? from + p + unit : 2LL * (from + p) + (p == 0 ? skip : 0)) * stride;
+        };
         // The maxima and sums of all parts at once, one query head per warp for the weights; then the rows.  The loads are
         // independent of each other, and the first CH rows are on their way while the weights are made (a running maximum
         // would wait for a round trip to L2 per part: 17 us of a 64 us launch).
@@ -645,9 +654,11 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         };
         if (tid < items) fetch(tid, 0);
         for (int i = tid; i < 8 * np; i += C::THREADS) {
-          const float* src = part_of(i >> 3) + 8 * D + (i & 7);
-          wts[(i & 7) * np + (i >> 3)] = __ldcg(src);
-          wts[8 * np + (i & 7) * np + (i >> 3)] = __ldcg(src + 8);
+          const int p = i >> 3, q = i & 7;
+          if (q >= a.rows) continue;
+          const float* src = part_of(p) + a.rows * D + q;
+          wts[q * np + p] = __ldcg(src);
+          wts[8 * np + q * np + p] = __ldcg(src + a.rows);
         }
         join_warps();
         for (int q = warp; q < heads; q += C::NW) {
@@ -724,6 +735,12 @@ int decode8_grid(int B, int H_kv, int G, int d, int max_len) {
   return static_cast<int>(std::min(worth, most));
 }
 
+// Bytes of the partial results of a call on the current device, whatever its lengths.
+size_t decode8_parts_bytes(int B, int H_kv, int G, int d) {
+  const long long units = static_cast<long long>(B) * H_kv * ((G + 7) / 8);
+  return static_cast<size_t>(part_count(units, std::min(device_sm_count(), kMaxGrid))) * part_floats(d, G < 8 ? G : 8) * sizeof(float);
+}
+
 cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,
                            int window, int grid, int32_t* counters, float* parts, void* out, int out_type, int32_t* status,
                            cudaStream_t st) {
@@ -737,6 +754,8 @@ cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, lon
   a.window = window;
   a.scale_log2 = attn_scale * kLog2e / 127.0f;
   a.units = c.H_kv * a.tiles;
+  a.rows = a.G < 8 ? a.G : 8;
+  a.compact = static_cast<long long>(c.B) * a.units < grid;
   a.grid = grid;
   a.counters = counters;
   a.parts = parts;

@@ -110,8 +110,7 @@ size_t tq_int8_counter_bytes(int32_t B, int32_t H_kv, int32_t H_q) {
 
 size_t tq_int8_workspace_bytes(int32_t B, int32_t H_kv, int32_t H_q, int32_t d) {
   if (B < 1 || H_kv < 1 || H_q < H_kv || d < 1) return 0;
-  // two cut units per thread block, 8 query heads each: output row, maximum, sum
-  return tq_int8_counter_bytes(B, H_kv, H_q) + 2 * static_cast<size_t>(device_sm_count()) * 8 * (d + 2) * sizeof(float);
+  return tq_int8_counter_bytes(B, H_kv, H_q) + decode8_parts_bytes(B, H_kv, H_q / H_kv, d);
 }
 
 int tq_sdpa_int8_decode(const tq_kv8_cache* cache, const void* q, int32_t q_dtype, int64_t q_stride, int32_t H_q,

@@ -32,7 +32,10 @@ def test_block_layout(tq):
 def test_workspace_sizes(tq):
     assert tq._lib.tq_pages_workspace_bytes(0) == 0 and tq._lib.tq_pages_workspace_bytes(7) >= 64
     assert tq._lib.tq_int8_counter_bytes(3, 2, 34) >= 4 * 3 * 2 * 3 and tq._lib.tq_int8_counter_bytes(1, 4, 2) == 0
-    assert tq._lib.tq_int8_workspace_bytes(1, 8, 64, 128) >= tq._lib.tq_int8_counter_bytes(1, 8, 64) + 2 * 148 * 8 * 130 * 4
+    # 148 thread blocks, 8 units: 156 parts of 8 rows, 8 maxima and 8 sums; many units: two parts per thread block
+    assert tq._lib.tq_int8_workspace_bytes(1, 8, 64, 128) == tq._lib.tq_int8_counter_bytes(1, 8, 64) + 156 * 8 * 130 * 4
+    assert tq._lib.tq_int8_workspace_bytes(64, 8, 24, 64) == tq._lib.tq_int8_counter_bytes(64, 8, 24) + 296 * (3 * 64 + 8) * 4
+    assert tq._lib.tq_int8_workspace_bytes(1, 1, 1, 64) == 256 + 149 * 68 * 4
 
 
 F = 0x1000  # never dereferenced: validation fails first
