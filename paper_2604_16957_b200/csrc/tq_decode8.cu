@@ -16,7 +16,8 @@
 //
 // Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
 // block i of N takes the blocks [i W / N, (i + 1) W / N) of the W in all, whatever the lengths: ragged batches load
-// every SM alike, one short sequence still spreads.  A unit that lies in one thread block is finished there; the parts
+// every SM alike, one short sequence still spreads.  (Batches of short sequences are not cut: see by_block and by_warp.)
+// A unit that lies in one thread block is finished there; the parts
 // of a cut one go to the workspace (at most two per thread block), and the last to arrive (a counter per unit) joins
 // them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512: registers), each with a ring of three to
 // six stages of one 16-token block, and one warp that fills the rings, one bulk copy per block (K codes, V codes and
@@ -48,7 +49,8 @@ struct Cfg {
   // of the warps go through them MQ query heads at a time
   static constexpr int ROW = D + 4;  // floats of one query's row: 8 rows x 2 words apart hit different banks
   static constexpr int MQ = 2;
-  static constexpr int WTS = 2 * 8 * kMaxGrid * 4;  // the last to arrive keeps the weights of a unit's parts there
+  // the last to arrive keeps the weights of a unit's parts there, and the teams' sums behind them
+  static constexpr int WTS = 2 * 8 * kMaxGrid * 4 + 16 * THREADS;
   static constexpr int MERGE = NW * MQ * ROW * 4 > WTS ? NW * MQ * ROW * 4 : WTS;
   static constexpr int STATS = RING + MERGE;             // [NW][8] x {M, M', l} and the factors of them
   static constexpr int BARS = STATS + NW * 8 * 3 * 4 + 8 * 4 * 4;
@@ -117,9 +119,12 @@ __device__ __forceinline__ Span span_of(const Args& a, int b) {
   return {window_begin(len, a.window), len};
 }
 
-// A walk over a thread block's share of the line: units, and in a unit the blocks [j0, j1).
+// A walk over a thread block's share of the line: units, and in a unit the blocks [j0, j1).  With hop > 0 it takes whole
+// units instead: unit g (sequences first), then every hop-th one after it.  Positions fit 31 bits (the entry point sees
+// to that): they are held through the main loop, and 64-bit divisions cost half a microsecond of latency apiece.
 struct Walk {
-  long long g, g1;  // position on the line and end of the share
+  int g, g1;  // position on the line and end of the share; unit and their number
+  int hop;
   int b, u, h;      // sequence, unit in it, its KV head
   int j0, j1, n;    // blocks of this visit, blocks of the unit
   Span span;
@@ -128,10 +133,24 @@ struct Walk {
     h = a.tiles == 1 ? u : u / a.tiles;
     n = span.blocks();
     j0 = j;
-    const long long left = g1 - g;
-    j1 = n - j0 < left ? n : j0 + static_cast<int>(left);
+    const int left = g1 - g;
+    j1 = hop > 0 || n - j0 < left ? n : j0 + left;
+  }
+  // the first unit with a token, from g on
+  __device__ bool seek(const Args& a) {
+    for (; g < g1; g += hop) {
+      b = g / a.units;
+      u = g - b * a.units;
+      open(a, 0);
+      if (n > 0) return true;
+    }
+    return false;
   }
   __device__ bool next(const Args& a) {
+    if (hop > 0) {
+      g += hop;
+      return seek(a);
+    }
     g += j1 - j0;
     if (g >= g1) return false;
     if (++u == a.units) {
@@ -174,19 +193,12 @@ __device__ __forceinline__ void store_out2(void* out, long long at, float x, flo
 }
 
 // The line of W blocks cut into N shares: share i starts at floor(i W / N).
-// (64-bit divisions cost half a microsecond of latency apiece; lines beyond 31 bits are rare enough to take them.)
-__device__ __forceinline__ long long divide(long long a, long long b) {
-  return ((a | b) >> 31) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
-}
 struct Shares {
-  long long each;
-  int rest, N;
+  int each, rest, N;
   float per;
-  __device__ Shares(long long W, int n) : each(divide(W, n)), rest(static_cast<int>(W - each * n)), N(n) {
-    per = static_cast<float>(n) / static_cast<float>(W);
-  }
-  __device__ long long start(int i) const { return each * i + i * rest / N; }
-  __device__ int owner(long long g) const {
+  __device__ Shares(int W, int n) : each(W / n), rest(W - each * n), N(n) { per = static_cast<float>(n) / static_cast<float>(W); }
+  __device__ int start(int i) const { return each * i + i * rest / N; }
+  __device__ int owner(int g) const {
     int i = static_cast<int>(static_cast<float>(g) * per);  // off by one at most
     i = i < N ? i : N - 1;
     if (start(i) > g) --i;
@@ -200,8 +212,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   using C = Cfg<D>;
   constexpr int KK = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long s_start;
-  __shared__ long long s_warp[C::NW + 1];
+  __shared__ int s_start, s_warp[C::NW + 1];
   __shared__ int s_b, s_last, s_dead;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t4 = lane & 3;
@@ -223,11 +234,11 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   const bool few = a.c.B <= 32;  // a warp sums the lengths up by itself: every warp does, and no barrier is needed
 
   // ---- where this thread block's share starts: blocks of all sequences, then the sequence that holds the start
-  auto scan = [&](long long v, long long& sum) {  // inclusive sum over the threads; `sum`: that of all
-    long long x = v;
+  auto scan = [&](int v, int& sum) {  // inclusive sum over the threads; `sum`: that of all
+    int x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
     if (few) {
@@ -236,10 +247,10 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    long long add = 0, all = 0;
+    int add = 0, all = 0;
 #pragma unroll
     for (int w = 0; w <= C::NW; ++w) {
-      const long long y = s_warp[w];
+      const int y = s_warp[w];
       if (w < warp) add += y;
       all += y;
     }
@@ -247,9 +258,9 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     sum = all;
     return x + add;
   };
-  long long W = 0;
+  int W = 0;
   int own_n = 0;  // blocks of the thread's sequence and of all up to it, in the last round
-  long long own_upto = 0;
+  int own_upto = 0;
   for (int round = 0; round < a.c.B; round += C::LAUNCH) {
     const int b = few ? lane : round + tid;
     own_n = 0;
@@ -264,19 +275,27 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       W = own_upto = own_n;
       break;
     }
-    long long all;
+    int all;
     own_upto = scan(own_n, all);
     W += all;
   }
   W *= a.units;
-  const long long worth = divide(W + a.min_blocks - 1, a.min_blocks);
-  int N = static_cast<int>(worth < 1 ? 1 : (worth < a.grid ? worth : a.grid));
+  // Short sequences are not cut.  With no more units than thread blocks, of six blocks per warp on average at most, a
+  // thread block takes one unit: joining a cut one costs 6 us, those blocks arrive in that time (16 units of 63 blocks:
+  // 19 us cut into 17 shares).  With more units, of 24 blocks on average at most, a warp takes whole units, without a
+  // merge (18 x 8 units of up to 8 blocks: 168 us while a thread block took one after the other, 4 us for each).
+  const int U = a.c.B * a.units;
+  const bool by_block = U <= static_cast<int>(gridDim.x) && W / (6 * C::NW) < U;
+  const bool by_warp = D < 512 && U > static_cast<int>(gridDim.x) && W / 24 < U;  // (d = 512: the warps share the query's fragments)
+  const int worth = (W - 1) / a.min_blocks + 1;
+  int N = worth < 1 ? 1 : (worth < a.grid ? worth : a.grid);
+  if (U > a.grid) N = W < a.grid ? W : a.grid;
   // One sequence: its units are equally long.  Shares that end where units do save the thread blocks in between a second
   // query and merge (5 us); giving up N % units thread blocks for that lengthens the others by each (N % units) / N
   // blocks of 0.09 us (128K tokens, 8 KV heads: 144 shares instead of 148).
   if (a.c.B == 1 && N > a.units) {
     const int spare = N % a.units;
-    if (spare * divide(W, N) <= 32LL * N) N -= spare;
+    if (spare * (W / N) <= 32 * N) N -= spare;
   }
 
   // sequences without a token: their rows are zero
@@ -285,19 +304,19 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (span_of(a, b).blocks() != 0) continue;
       for (int i = tid; i < a.H_q * D; i += C::LAUNCH) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
     }
-  if (static_cast<int>(blockIdx.x) >= N || W == 0) return;
+  if (W == 0 || (!by_block && !by_warp && static_cast<int>(blockIdx.x) >= N)) return;
 
   const Shares shares(W, N);
-  const long long g0 = shares.start(blockIdx.x);
+  const int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
   int first_b;
-  long long first_at;
-  auto claim = [&](int b, int n, long long upto) {  // the sequence that holds the start of the share
+  int first_at;
+  auto claim = [&](int b, int n, int upto) {  // the sequence that holds the start of the share
     if (n > 0 && upto * a.units > g0 && (upto - n) * a.units <= g0) {
       s_b = b;
       s_start = (upto - n) * a.units;
     }
   };
-  if (a.c.B == 1) {
+  if (a.c.B == 1 || by_block || by_warp) {
     first_b = 0;
     first_at = 0;
   } else if (few) {
@@ -309,42 +328,50 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   } else if (a.c.B <= C::LAUNCH) {
     claim(tid, own_n, own_upto);
   } else {
-    long long carry = 0;
+    int carry = 0;
     for (int round = 0; round < a.c.B; round += C::LAUNCH) {
       const int b = round + tid;
       const int n = b < a.c.B ? span_of(a, b).blocks() : 0;
-      long long all;
-      const long long upto = scan(n, all);
+      int all;
+      const int upto = scan(n, all);
       claim(b, n, carry + upto);
       carry += all;
     }
   }
-  if (!few) {
+  if (!few && !by_block && !by_warp) {
     __syncthreads();
     first_b = s_b;
     first_at = s_start;
   }
   Walk use;
-  use.g = g0;
-  use.g1 = shares.start(blockIdx.x + 1);
-  use.b = first_b;
-  {
+  bool any = true;
+  if (by_block || by_warp) {
+    use.g = by_block ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * C::NW + (warp < C::NW ? warp : lane);
+    use.g1 = warp == C::NW && lane >= C::NW ? 0 : U;
+    use.hop = by_block ? static_cast<int>(gridDim.x) : static_cast<int>(gridDim.x) * C::NW;
+    any = use.seek(a);
+  } else {
+    use.hop = 0;
+    use.g = g0;
+    use.g1 = shares.start(blockIdx.x + 1);
+    use.b = first_b;
     const int n = span_of(a, use.b).blocks();
-    const long long r = g0 - first_at;
-    use.u = static_cast<int>(divide(r, n));
-    use.open(a, static_cast<int>(r - static_cast<long long>(use.u) * n));
+    const int r = g0 - first_at;
+    use.u = r / n;
+    use.open(a, r - use.u * n);
   }
 
   if (warp == C::NW) {
     // ---- copies: lane w fills warp w's ring, ahead of its arithmetic and on into the next units
-    bool more = lane < C::NW;
-    int j = use.j0 + lane, stage = 0;
+    bool more = any && lane < C::NW;
+    const int at = by_warp ? 0 : lane, step = by_warp ? 1 : C::NW;
+    int j = any ? use.j0 + at : 0, stage = 0;
     uint32_t phase = 1;  // the first pass over a ring finds every stage free
     long long since = clock64();
     while (true) {
       while (more && j >= use.j1) {  // the warp's next block may lie in a later unit
         more = use.next(a);
-        j = use.j0 + lane;
+        j = use.j0 + at;
       }
       if (!__any_sync(0xffffffffu, more)) break;
       bool sent = false;
@@ -352,7 +379,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         const uint8_t* src = block_at(a, use.b, use.h, use.span.first() + j);
         mbar_expect_tx(full(lane, stage), C::STAGE);
         bulk_g2s(base + (lane * C::NST + stage) * C::STAGE, src, C::STAGE, full(lane, stage));
-        j += C::NW;
+        j += step;
         if (++stage == C::NST) {
           stage = 0;
           phase ^= 1;
@@ -369,8 +396,8 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     // whatever is still on its way after that lands before the warp ends (bounded)
     if (more)
       for (int s = 0; s < C::NST; ++s) {
-        const int at = (stage + s) % C::NST;
-        wait_stage(full(lane, at), at >= stage ? phase : phase ^ 1);
+        const int x = (stage + s) % C::NST;
+        wait_stage(full(lane, x), x >= stage ? phase : phase ^ 1);
       }
     return;
   }
@@ -380,7 +407,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   uint32_t phase = 0;
   bool dead = false;
 
-  for (bool go = true; go; go = use.next(a)) {
+  for (bool go = any; go; go = use.next(a)) {
     const int h = use.h, tile = use.u - h * a.tiles;
     const int head0 = h * a.G + tile * 8;
     const int heads = a.G - tile * 8 < 8 ? a.G - tile * 8 : 8;
@@ -444,7 +471,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     for (int m = 0; m < 2 * KK; ++m) o[m][0] = o[m][1] = o[m][2] = o[m][3] = 0.0f;
     float M0 = kNoMax, M1 = kNoMax, P0 = kNoMax, P1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
 
-    for (int j = use.j0 + warp; j < use.j1; j += C::NW) {
+    for (int j = use.j0 + (by_warp ? 0 : warp); j < use.j1; j += by_warp ? 1 : C::NW) {
       if (!dead && !wait_stage(full(warp, stage), phase)) {
         dead = true;
         s_dead = 1;
@@ -538,6 +565,23 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       l0 += __shfl_xor_sync(0xffffffffu, l0, x);
       l1 += __shfl_xor_sync(0xffffffffu, l1, x);
     }
+    if (by_warp) {
+      // the warp's own unit: straight out of the accumulators
+      const float f0 = ex2(P0 - M0) / (127.0f * l0), f1 = ex2(P1 - M1) / (127.0f * l1);
+      const long long at = (static_cast<long long>(use.b) * a.H_q + head0 + 2 * t4) * D + gid;
+#pragma unroll
+      for (int m = 0; m < 2 * KK; ++m) {
+        if (2 * t4 < heads) {
+          store_out<OT>(a.out, at + 16 * m, o[m][0] * f0);
+          store_out<OT>(a.out, at + 16 * m + 8, o[m][2] * f0);
+        }
+        if (2 * t4 + 1 < heads) {
+          store_out<OT>(a.out, at + D + 16 * m, o[m][1] * f1);
+          store_out<OT>(a.out, at + D + 16 * m + 8, o[m][3] * f1);
+        }
+      }
+      continue;
+    }
     if (gid == 0) {
       float* st = stats + warp * 8 + 2 * t4;
       st[0] = M0;
@@ -548,7 +592,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       st[2 * C::NW * 8 + 1] = l1;
     }
     const bool whole = use.j0 == 0 && use.j1 == use.n;
-    const long long u0 = use.g - use.j0;  // the unit on the line, and the thread blocks that share it
+    const int u0 = use.g - use.j0;  // the unit on the line, and the thread blocks that share it
     int from = 0, to = 0;
     if (!whole) {
       from = shares.owner(u0);
@@ -614,7 +658,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     };
     // On the thread block's last visit nothing is on its way into the rings any more (every warp has used what it asked
     // for, and the barriers above are behind that): all eight rows at once through the rings' memory.
-    if (use.g + (use.j1 - use.j0) >= use.g1 && !s_dead) {
+    if ((use.hop > 0 ? use.g + use.hop : use.g + (use.j1 - use.j0)) >= use.g1 && !s_dead) {
       join(reinterpret_cast<float*>(smem), 0, std::integral_constant<int, 8>{});
     } else {
       for (int q0 = 0; q0 < heads; q0 += C::MQ) join(merge, q0, std::integral_constant<int, C::MQ>{});
@@ -642,17 +686,23 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         // The maxima and sums of all parts at once, one query head per warp for the weights; then the rows.  The loads are
         // independent of each other, and the first CH rows are on their way while the weights are made (a running maximum
         // would wait for a round trip to L2 per part: 17 us of a 64 us launch).
+        // Few rows and many parts: `teams` of threads share the parts of a row.
         constexpr int CH = 9;
         float* const wts = merge;  // [2][8][np]
         float4 rows[CH];
         const int items = heads * (D / 4);
-        auto fetch = [&](int i, int p0) {
+        int teams = 1;
+        while (2 * teams * items <= C::THREADS && 2 * teams <= np) teams *= 2;
+        const int each = (np + teams - 1) / teams;
+        auto fetch = [&](int i, int p0, int end) {
           const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
 #pragma unroll
           for (int p = 0; p < CH; ++p)
-            if (p0 + p < np) rows[p] = __ldcg(reinterpret_cast<const float4*>(part_of(p0 + p) + q * D + ch));
+            if (p0 + p < end) rows[p] = __ldcg(reinterpret_cast<const float4*>(part_of(p0 + p) + q * D + ch));
         };
-        if (tid < items) fetch(tid, 0);
+        const int team = teams > 1 ? tid / items : 0, item = teams > 1 ? tid - team * items : tid;
+        const int p_first = team * each, p_end = min(np, p_first + each);
+        if (team < teams && item < items) fetch(item, p_first, p_end);
         for (int i = tid; i < 8 * np; i += C::THREADS) {
           const int p = i >> 3, q = i & 7;
           if (q >= a.rows) continue;
@@ -676,14 +726,14 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
           if (lane == 0) sums[q] = 1.0f / l;
         }
         join_warps();
-        for (int i = tid; i < items; i += C::THREADS) {
-          const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
+        auto sum_of = [&](int i, bool first) {
+          const int q = i / (D / 4);
           float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int p0 = 0; p0 < np; p0 += CH) {
-            if (i != tid || p0 > 0) fetch(i, p0);
+          for (int p0 = p_first; p0 < p_end; p0 += CH) {
+            if (!first || p0 > p_first) fetch(i, p0, p_end);
 #pragma unroll
             for (int p = 0; p < CH; ++p)
-              if (p0 + p < np) {
+              if (p0 + p < p_end) {
                 const float w = wts[q * np + p0 + p];
                 x.x += w * rows[p].x;
                 x.y += w * rows[p].y;
@@ -691,9 +741,31 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
                 x.w += w * rows[p].w;
               }
           }
+          return x;
+        };
+        auto put = [&](int i, const float4& x) {
+          const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
           const long long at = (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch;
           store_out2<OT>(a.out, at, x.x * sums[q], x.y * sums[q]);
           store_out2<OT>(a.out, at + 2, x.z * sums[q], x.w * sums[q]);
+        };
+        if (teams == 1) {
+          for (int i = tid; i < items; i += C::THREADS) put(i, sum_of(i, i == tid));
+        } else {
+          float4* const half = reinterpret_cast<float4*>(merge + (2 * 8 * np + 3) / 4 * 4);  // [teams][items], behind the weights
+          if (team < teams) half[tid] = sum_of(item, true);
+          join_warps();
+          if (team == 0) {
+            float4 x = half[item];
+            for (int t = 1; t < teams; ++t) {
+              const float4 y = half[t * items + item];
+              x.x += y.x;
+              x.y += y.y;
+              x.z += y.z;
+              x.w += y.w;
+            }
+            put(item, x);
+          }
         }
       }
       join_warps();
@@ -731,7 +803,8 @@ cudaError_t launch_d(const Args& a, int q_type, int out_type, cudaStream_t st) {
 int decode8_grid(int B, int H_kv, int G, int d, int max_len) {
   const long long warps = d <= 128 ? Cfg<128>::NW : (d == 256 ? Cfg<256>::NW : Cfg<512>::NW);
   const long long blocks = static_cast<long long>(B) * H_kv * ((G + 7) / 8) * ((max_len + 15LL) / 16 + 1);
-  const long long worth = (blocks + warps - 1) / warps, most = std::min(device_sm_count(), kMaxGrid);
+  const long long units = static_cast<long long>(B) * H_kv * ((G + 7) / 8);
+  const long long worth = std::max(units, (blocks + warps - 1) / warps), most = std::min(device_sm_count(), kMaxGrid);
   return static_cast<int>(std::min(worth, most));
 }
 

@@ -342,7 +342,11 @@ def _check_decode(torch, out, q, values, alpha, window, d):
     ([3001], 32, 16, 256, 0, "fp16", 0, 6), ([100, 1, 900], 6, 2, 256, 32, "bf16", 0, 7),
     ([500, 77], 8, 2, 512, 16, "fp16", 0, 8), ([2500], 40, 2, 64, 128, "bf16", 0, 9),       # 20 heads: three tiles
     ([1500, 100, 64, 63], 8, 2, 128, 16, "fp16", 64, 10), ([4000], 64, 8, 128, 0, "fp16", 1000, 11),
-    ([2000, 5], 12, 4, 256, 64, "bf16", 1, 12), ([20] * 300, 4, 4, 64, 16, "fp16", 0, 13), ([20000], 8, 1, 128, 0, "fp16", 0, 14)])
+    ([2000, 5], 12, 4, 256, 64, "bf16", 1, 12), ([20] * 300, 4, 4, 64, 16, "fp16", 0, 13), ([20000], 8, 1, 128, 0, "fp16", 0, 14),
+    # units of a few blocks each: one per thread block, several per warp; wide heads, where a warp never takes a unit
+    ([5, 118, 0, 33] * 4, 64, 8, 128, 0, "fp16", 0, 15), ([3, 0, 70, 200] * 20, 24, 8, 128, 16, "bf16", 0, 16),
+    ([40, 1] * 60, 8, 4, 256, 16, "fp16", 20, 17), ([9, 300] * 30, 20, 4, 512, 32, "bf16", 0, 18), ([16] * 700, 3, 1, 64, 0, "bf16", 0, 19),
+    ([400, 0, 390] * 60, 2, 2, 128, 64, "fp16", 0, 20)])
 def test_int8_decode(gpu, lens, H_q, H_kv, d, page, kind, window, seed):
     tq, torch = gpu
     rng = np.random.default_rng(100 + seed)

@@ -99,6 +99,8 @@ def test_decode_refuses(tq):
         assert tq._lib.tq_sdpa_int8_decode(*args) == code, args
     for c, code in _caches(tq):
         assert tq._lib.tq_sdpa_int8_decode(C.byref(c), *good[1:]) == code
+    huge = _paged(tq, B=65535, H_kv=8, S_cap=1 << 20, page_tokens=1 << 16, max_pages=16, num_pages=9)
+    assert tq._lib.tq_sdpa_int8_decode(C.byref(huge), *good[1:]) == S
 
 
 def test_prompt_refuses(tq):
