@@ -439,7 +439,8 @@ int tq_pages_release(const int32_t* page_table, const int32_t* seq_lens, const u
  * (TQ_STATUS_CACHE_FULL), if the pages wanted by it and the sequences before it exceed the stack
  * (TQ_STATUS_POOL_EMPTY), if its rows do not fit n_slots or a length is out of range (TQ_STATUS_BAD_LEN).  A sequence
  * that needs no fresh page is never refused for the pool's sake.  An entry of the stack or of the table outside
- * the pool sets TQ_STATUS_BAD_PAGE and its tokens get slot -1.  Requirements as tq_pages_release; n_slots in 1..2^31 - 1.
+ * the pool sets TQ_STATUS_BAD_PAGE and its tokens get slot -1.  Requirements as tq_pages_release; n_slots in 0..2^31 - 1
+ * (0: a step without new tokens; slots may be NULL).
  */
 size_t tq_pages_workspace_bytes(int32_t B);
 int tq_pages_assign(int32_t* page_table, const int32_t* seq_lens, const int32_t* new_lens, int32_t B, int32_t page_tokens,
@@ -485,7 +486,7 @@ size_t tq_cache8_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d);
  *                  as present.  A slot outside the cache, or a row that is out of order inside its block, sets TQ_STATUS_BAD_SLOT and
  *                  is skipped with the rest of its run.  A block that is met in two places of one call is the caller's mistake: its contents
  *                  are then unspecified (nothing outside it is touched).
- * seq_lens is not read.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (cache requirements as tq_kv_cache, n < 1, strides, dtype
+ * seq_lens is not read.  n = 0 does nothing, here and in tq_kv8_gather.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (cache requirements as tq_kv_cache, n < 0, strides, dtype
  * TQ_FP32), TQ_ERR_ALIGN, TQ_ERR_CUDA.
  */
 int tq_kv8_append(const tq_kv8_cache* cache /* host */, const void* k_new, const void* v_new, int32_t dtype,
@@ -529,7 +530,8 @@ int tq_sdpa_int8_decode(const tq_kv8_cache* cache /* host */, const void* q, int
  * nothing gives zeros.
  *   q, k, v      : device, fp16 or bf16 (dtype): row i, head h at i * stride + h * d elements (slices of a fused
  *                  projection's output are fine); strides multiples of 8 elements and at least heads * d
- *   n_q, n_kv    : rows of q and of k, v; offsets are clamped to them (TQ_STATUS_BAD_LEN)
+ *   n_q, n_kv    : rows of q and of k, v (0: none, and their addresses may be NULL); offsets are clamped to them
+ *                  (TQ_STATUS_BAD_LEN)
  *   q_offsets, kv_offsets : device [B + 1] int32, ascending; the same array where the keys are the queries' own tokens
  *   out          : device [n_q][H_q][d], of dtype or fp32 (out_dtype).  Rows of no sequence are left as they were.
  * d in {64, 128, 256, 512}; H_q a multiple of H_kv, H_q / H_kv <= 64; causal = 0 with a window is TQ_ERR_SHAPE.

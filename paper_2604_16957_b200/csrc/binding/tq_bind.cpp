@@ -120,8 +120,23 @@ struct Cache {
   bool cuda;
   int dev;
   PyObject* keep[3];
+  int64_t numel[3];
+  // The tensors' addresses as they are now; false if one has another size or device than it came with.
+  bool refresh() {
+    void* at[3] = {};
+    for (int i = 0; i < 3; ++i) {
+      if (!keep[i]) continue;
+      const at::Tensor& t = THPVariable_Unpack(keep[i]);
+      if (t.numel() != numel[i] || !t.is_contiguous() || t.is_cuda() != cuda || (cuda && t.get_device() != dev)) return false;
+      at[i] = t.data_ptr();
+    }
+    c.blocks = static_cast<uint8_t*>(at[0]);
+    c.seq_lens = static_cast<int32_t*>(at[1]);
+    c.page_table = static_cast<int32_t*>(at[2]);
+    return true;
+  }
 };
-const char kCache[] = "tq_kv8_cache";
+const char kCache[] = "tq_kv8_cache", kMoved[] = "a tensor of the cache was resized or moved to another device";
 void free_cache(PyObject* capsule) {
   auto* x = static_cast<Cache*>(PyCapsule_GetPointer(capsule, kCache));
   for (PyObject* k : x->keep) Py_XDECREF(k);
@@ -186,6 +201,7 @@ PyObject* py_cache8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     x.dev = x.cuda ? blocks.get_device() : -1;
     for (int i = 0; i < (paged ? 3 : 2); ++i) {
       x.keep[i] = a[i];
+      x.numel[i] = THPVariable_Unpack(a[i]).numel();
       Py_INCREF(a[i]);
     }
     PyObject* capsule = PyCapsule_New(new Cache(x), kCache, free_cache);
@@ -201,13 +217,18 @@ PyObject* py_sizes(PyObject*, PyObject* o) {
 }
 PyObject* py_address(PyObject*, PyObject* o) {
   auto* x = static_cast<Cache*>(PyCapsule_GetPointer(o, kCache));
-  return x ? PyLong_FromVoidPtr(&x->c) : nullptr;
+  if (!x) return nullptr;
+  return guarded([&]() -> PyObject* {
+    if (!x->refresh()) refuse("KV8Cache", kMoved);
+    return PyLong_FromVoidPtr(&x->c);
+  });
 }
 
 const Cache& cache_of(PyObject* o, const char* where) {
   if (!PyCapsule_IsValid(o, kCache)) refuse(where, "cache must be a KV8Cache or a PagedKV8Cache");
   auto* x = static_cast<Cache*>(PyCapsule_GetPointer(o, kCache));
   if (!x->cuda || x->dev != c10::cuda::current_device()) refuse(where, "the cache is not on the current CUDA device");
+  if (!x->refresh()) refuse(where, kMoved);
   return *x;
 }
 void beside(const Cache& c, const at::Tensor& t, const char* where) {
@@ -293,7 +314,6 @@ PyObject* py_kv8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k.scalar_type() != v.scalar_type()) refuse(w, "k_new and v_new must be of one type");
     const int64_t ks = call.rows(k, "k_new", rows, c.c.H_kv, c.c.d), vs = call.rows(v, "v_new", rows, c.c.H_kv, c.c.d);
     int32_t* status = call.status(a[4]);
-    if (rows == 0) Py_RETURN_NONE;
     return call.done(lib.kv8_append(&c.c, k.data_ptr(), v.data_ptr(), call.dtype(k, "k_new"), ks, vs, slots, rows, status, call.stream(a[5])));
   });
 }
@@ -314,7 +334,6 @@ PyObject* py_kv8_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k.scalar_type() != v.scalar_type() || !k.is_contiguous() || !v.is_contiguous())
       refuse(w, "k_out and v_out must be contiguous and of one type");
     int32_t* status = call.status(a[4]);
-    if (rows == 0) Py_RETURN_NONE;
     return call.done(lib.kv8_gather(&c.c, slots, rows, k.data_ptr(), v.data_ptr(), call.dtype(k, "k_out"), status, call.stream(a[5])));
   });
 }
@@ -358,7 +377,6 @@ PyObject* py_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n_q > INT32_MAX || n_kv > INT32_MAX || H_q > INT32_MAX || H_kv > INT32_MAX || d > INT32_MAX || B > INT32_MAX)
       refuse(w, "a size beyond 32 bits");
     int32_t* status = call.status(a[9]);
-    if (n_q == 0) Py_RETURN_NONE;
     return call.done(lib.prompt(q.data_ptr(), k.data_ptr(), v.data_ptr(), call.dtype(q, "q"), qs, ks, vs, static_cast<int32_t>(n_q),
                                 static_cast<int32_t>(n_kv), q_at, k_at, static_cast<int32_t>(B), static_cast<int32_t>(H_q),
                                 static_cast<int32_t>(H_kv), static_cast<int32_t>(d), call.f32(a[5]), causal, call.i32(a[8]), out.data_ptr(),

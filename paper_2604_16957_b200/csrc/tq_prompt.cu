@@ -691,9 +691,11 @@ cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
   const long long blocks = (static_cast<long long>(a.n_q) / (C::NQ * T) + a.B) * a.H_kv * (D / C::DV);
   if (!encode_fn() || blocks > 0x7fffffffLL) return cudaErrorNotSupported;
   Maps maps;
+  // (without a single key the maps of K and V describe a row of q; nothing is loaded through them)
+  const bool keys = a.n_kv > 0;
   if (!make_map(&maps.q, a.q, a.dtype, D, a.H_q, a.n_q, a.q_stride, G, T) ||
-      !make_map(&maps.k, a.k, a.dtype, D, a.H_kv, a.n_kv, a.k_stride, 1, C::BN) ||
-      !make_map(&maps.v, a.v, a.dtype, D, a.H_kv, a.n_kv, a.v_stride, 1, C::BN))
+      !make_map(&maps.k, keys ? a.k : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.k_stride : a.q_stride, 1, C::BN) ||
+      !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN))
     return cudaErrorInvalidValue;
   return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T);
 }

@@ -59,10 +59,10 @@ int tq_pages_assign(int32_t* page_table, const int32_t* seq_lens, const int32_t*
                     int32_t max_pages, int32_t num_pages, const int32_t* free_pages, const int32_t* free_count,
                     int32_t* seq_lens_out, int32_t* free_count_out, int32_t* token_offsets, int64_t* slots,
                     int64_t n_slots, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
-  if (!seq_lens || !new_lens || !seq_lens_out || !token_offsets || !slots || !workspace) return TQ_ERR_NULL;
+  if (!seq_lens || !new_lens || !seq_lens_out || !token_offsets || (!slots && n_slots > 0) || !workspace) return TQ_ERR_NULL;
   if (page_table && (!free_pages || !free_count || !free_count_out)) return TQ_ERR_NULL;
   if (int r = check_pages(page_table, B, page_tokens, max_pages, num_pages)) return r;
-  if (n_slots < 1 || n_slots > 0x7fffffffLL) return TQ_ERR_SHAPE;
+  if (n_slots < 0 || n_slots > 0x7fffffffLL) return TQ_ERR_SHAPE;
   if (!aligned(page_table, 4) || !aligned(seq_lens, 4) || !aligned(new_lens, 4) || !aligned(free_pages, 4) ||
       !aligned(free_count, 4) || !aligned(seq_lens_out, 4) || !aligned(free_count_out, 4) || !aligned(token_offsets, 4) ||
       !aligned(slots, 8) || !aligned(workspace, 16) || !aligned(status, 4))
@@ -85,6 +85,7 @@ size_t tq_cache8_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d) {
 int tq_kv8_append(const tq_kv8_cache* cache, const void* k_new, const void* v_new, int32_t dtype, int64_t k_stride,
                   int64_t v_stride, const int64_t* slots, int64_t n, int32_t* status, void* stream) {
   if (int r = check_cache8(cache)) return r;
+  if (n == 0) return TQ_OK;
   if (!k_new || !v_new || !slots) return TQ_ERR_NULL;
   const int64_t row = static_cast<int64_t>(cache->H_kv) * cache->d;
   if (!is16(dtype) || n < 1 || n > 0x7fffffffLL || k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8)
@@ -97,6 +98,7 @@ int tq_kv8_append(const tq_kv8_cache* cache, const void* k_new, const void* v_ne
 int tq_kv8_gather(const tq_kv8_cache* cache, const int64_t* slots, int64_t n, void* k_out, void* v_out, int32_t dtype,
                   int32_t* status, void* stream) {
   if (int r = check_cache8(cache)) return r;
+  if (n == 0) return TQ_OK;
   if (!slots || !k_out || !v_out) return TQ_ERR_NULL;
   if ((!is16(dtype) && dtype != TQ_FP32) || n < 1 || n > 0x7fffffffLL) return TQ_ERR_SHAPE;
   if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(slots, 8) || !aligned(status, 4)) return TQ_ERR_ALIGN;
@@ -138,15 +140,17 @@ int tq_sdpa_prompt(const void* q, const void* k, const void* v, int32_t dtype, i
                    int64_t v_stride, int32_t n_q, int32_t n_kv, const int32_t* q_offsets, const int32_t* kv_offsets,
                    int32_t B, int32_t H_q, int32_t H_kv, int32_t d, float attn_scale, int32_t causal, int32_t window,
                    void* out, int32_t out_dtype, int32_t* status, void* stream) {
-  if (!q || !k || !v || !q_offsets || !kv_offsets || !out) return TQ_ERR_NULL;
+  if (n_q > 0 && (!q || !out || (n_kv > 0 && (!k || !v)))) return TQ_ERR_NULL;
+  if (!q_offsets || !kv_offsets) return TQ_ERR_NULL;
   if (B < 1 || B > 65535 || H_kv < 1 || H_kv > 4096 || H_q < 1 || H_q % H_kv != 0 || H_q / H_kv > 64) return TQ_ERR_SHAPE;
-  if (!(d == 64 || d == 128 || d == 256 || d == 512) || n_q < 1 || n_kv < 1) return TQ_ERR_SHAPE;
+  if (!(d == 64 || d == 128 || d == 256 || d == 512) || n_q < 0 || n_kv < 0) return TQ_ERR_SHAPE;
   if (!is16(dtype) || (out_dtype != dtype && out_dtype != TQ_FP32) || window < 0 || (window > 0 && !causal)) return TQ_ERR_SHAPE;
   const int64_t rq = static_cast<int64_t>(H_q) * d, rk = static_cast<int64_t>(H_kv) * d;
   if (q_stride < rq || k_stride < rk || v_stride < rk || q_stride % 8 || k_stride % 8 || v_stride % 8) return TQ_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(q_offsets, 4) ||
       !aligned(kv_offsets, 4) || !aligned(status, 4))
     return TQ_ERR_ALIGN;
+  if (n_q == 0) return TQ_OK;
   const PromptArgs a = {q, k, v, dtype, q_stride, k_stride, v_stride, n_q, n_kv, q_offsets, kv_offsets, B, H_q, H_kv, d,
                         attn_scale, causal != 0, window, out, out_dtype, status};
   return finish(launch_prompt(a, static_cast<cudaStream_t>(stream)));

@@ -448,7 +448,7 @@ _bind.attach(_refuse, _check, *(C.cast(f, _vp).value for f in (
 class KV8Cache:
     """Device buffer of one layer's 8-bit KV cache, contiguous: `blocks` [B][H_kv][S_cap/16][block bytes]."""
 
-    __slots__ = ("blocks", "seq_lens", "page_table", "_handle")
+    __slots__ = ("_tensors", "_handle")
 
     def __init__(self, B, H_kv, S_cap, d, device="cuda"):
         if S_cap % 16 or d not in (64, 128, 256, 512):
@@ -465,8 +465,12 @@ class KV8Cache:
 
     def _hold(self, blocks, seq_lens, page_table):
         self._handle = _bind.cache8(blocks, seq_lens, page_table)
-        self.blocks, self.seq_lens, self.page_table = blocks, seq_lens, page_table
+        self._tensors = blocks, seq_lens, page_table
 
+    # (read only: a cache over other tensors is another object)
+    blocks = property(lambda self: self._tensors[0])
+    seq_lens = property(lambda self: self._tensors[1])
+    page_table = property(lambda self: self._tensors[2])
     B = property(lambda self: _bind.sizes(self._handle)[0])
     H_kv = property(lambda self: _bind.sizes(self._handle)[1])
     S_cap = property(lambda self: _bind.sizes(self._handle)[2])

@@ -651,3 +651,29 @@ def test_a_serving_loop(gpu, captured):
     assert count.tolist() == [num_pages - used]
     live = set(free.tolist()[:num_pages - used]) | {s // P for p in place for s in p}
     assert live == set(range(num_pages))                        # no page lost, none twice
+
+
+def test_a_step_that_only_ends_sequences(gpu):
+    """Every sequence leaves and none comes: no rows, no slots; the pages are back.  Queries without a single key give zeros."""
+    tq, torch = gpu
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens, table = ints([20, 16]), ints([[3, 1], [2, 0]])
+    free, count = ints([0, 4, 0, 0, 0]), ints([2])
+    offsets, slots = ints([9, 9, 9]), torch.empty(0, dtype=torch.int64, device="cuda")
+    status = ints([0])
+    tq.tq_pages_release(table, lens, torch.ones(2, dtype=torch.bool, device="cuda"), 16, 5, free, count, lens, count, status)
+    tq.tq_pages_assign(table, lens, ints([0, 0]), 16, 5, free, count, lens, count, offsets, slots, tq.alloc_pages_workspace(2), status)
+    assert lens.tolist() == [0, 0] and count.tolist() == [5] and free.tolist() == [0, 4, 3, 1, 2]
+    assert offsets.tolist() == [0, 0, 0] and status.tolist() == [0]
+    tq.tq_pages_assign(table, lens, ints([1, 0]), 16, 5, free, count, lens, count, offsets, slots, tq.alloc_pages_workspace(2), status)
+    assert lens.tolist() == [0, 0] and count.tolist() == [5] and offsets.tolist() == [0, 0, 0] and status.tolist() == [tq.TQ_STATUS_BAD_LEN]
+    cache = tq.PagedKV8Cache(2, 2, 16, 2, 5, 64)
+    none = torch.empty((0, 2, 64), dtype=torch.float16, device="cuda")
+    tq.tq_kv8_append(cache, none, none, slots)
+    tq.tq_kv8_gather(cache, slots, none, none)
+    q = torch.ones((3, 4, 64), dtype=torch.float16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    status.zero_()
+    tq.tq_sdpa_prompt(q, none, none, ints([0, 2, 2]), ints([0, 0, 0]), 1.0, out, status=status)
+    assert (out[:2] == 0).all() and (out[2] == 7).all() and status.tolist() == [tq.TQ_STATUS_EMPTY_SEQ]
+    tq.tq_sdpa_prompt(q[:0], none, none, ints([0, 0]), ints([0, 0]), 1.0, out[:0])

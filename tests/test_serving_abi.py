@@ -75,13 +75,13 @@ def test_append_and_gather_refuse(tq):
     ok = _cache(tq)
     good = [C.byref(ok), F, F, tq.TQ_FP16, 256, 256, F, 5, None, None]
     for args, code in _vary(good, [(0, None, N), (1, None, N), (2, None, N), (6, None, N), (3, tq.TQ_FP32, S), (3, 7, S), (4, 255, S),
-                                   (4, 248, S), (5, 260, S), (7, 0, S), (7, -1, S), (7, 1 << 31, S), (1, F + 8, A), (2, F + 2, A),
+                                   (4, 248, S), (5, 260, S), (7, -1, S), (7, 1 << 31, S), (1, F + 8, A), (2, F + 2, A),
                                    (6, F + 4, A), (8, F + 2, A)]):
         assert tq._lib.tq_kv8_append(*args) == code, args
     for c, code in _caches(tq):
         assert tq._lib.tq_kv8_append(C.byref(c), *good[1:]) == code
     good = [C.byref(ok), F, 5, F, F, tq.TQ_FP32, None, None]
-    for args, code in _vary(good, [(0, None, N), (1, None, N), (3, None, N), (4, None, N), (5, 3, S), (2, 0, S), (1, F + 4, A), (3, F + 8, A),
+    for args, code in _vary(good, [(0, None, N), (1, None, N), (3, None, N), (4, None, N), (5, 3, S), (2, -1, S), (1, F + 4, A), (3, F + 8, A),
                                    (6, F + 1, A)]):
         assert tq._lib.tq_kv8_gather(*args) == code, args
     for c, code in _caches(tq):
@@ -108,7 +108,7 @@ def test_prompt_refuses(tq):
     #       q  k  v  dtype       strides          n_q n_kv offsets B  Hq Hk d    scale c  w  out dtype status stream
     good = [F, F, F, tq.TQ_BF16, 1024, 256, 256, 10, 10, F, F, 2, 8, 2, 128, 1.0, 1, 0, F, tq.TQ_FP32, None, None]
     for args, code in _vary(good, [(0, None, N), (1, None, N), (2, None, N), (9, None, N), (10, None, N), (18, None, N), (3, tq.TQ_FP32, S),
-                                   (3, 5, S), (4, 1016, S), (4, 1025, S), (5, 250, S), (6, 128, S), (7, 0, S), (8, 0, S), (11, 0, S),
+                                   (3, 5, S), (4, 1016, S), (4, 1025, S), (5, 250, S), (6, 128, S), (7, -1, S), (8, -1, S), (11, 0, S),
                                    (11, 65536, S), (12, 7, S), (12, 0, S), (13, 0, S), (14, 96, S), (17, -1, S), (19, tq.TQ_FP16, S),
                                    (0, F + 8, A), (1, F + 2, A), (2, F + 8, A), (9, F + 2, A), (18, F + 8, A), (20, F + 1, A)]):
         assert tq._lib.tq_sdpa_prompt(*args) == code, args
@@ -132,12 +132,39 @@ def test_pages_refuse(tq):
     room = tq._lib.tq_pages_workspace_bytes(4)
     good = [F, F, F, 4, 16, 8, 30, F, F, F, F, F, F, 9, F, room, None, None]
     for args, code in _vary(good, [(1, None, N), (2, None, N), (7, None, N), (8, None, N), (9, None, N), (10, None, N), (11, None, N), (12, None, N),
-                                   (14, None, N), (13, 0, S), (13, 1 << 31, S), (4, 17, S), (15, room - 1, tq.TQ_ERR_WORKSPACE), (12, F + 4, A),
+                                   (14, None, N), (13, -1, S), (13, 1 << 31, S), (4, 17, S), (15, room - 1, tq.TQ_ERR_WORKSPACE), (12, F + 4, A),
                                    (14, F + 8, A), (11, F + 2, A)]):
         assert tq._lib.tq_pages_assign(*args) == code, args
     contiguous = list(good)
     contiguous[0], contiguous[4] = None, 24            # a capacity that is no multiple of 16
     assert tq._lib.tq_pages_assign(*contiguous) == S
+
+
+def test_a_step_without_tokens_is_no_error(tq):
+    """A batch of which every sequence has just ended: no rows, so no addresses either."""
+    c, bad = _cache(tq), _cache(tq, d=100)
+    assert tq._lib.tq_kv8_append(C.byref(c), None, None, tq.TQ_FP16, 256, 256, None, 0, None, None) == tq.TQ_OK
+    assert tq._lib.tq_kv8_gather(C.byref(c), None, 0, None, None, tq.TQ_FP32, None, None) == tq.TQ_OK
+    assert tq._lib.tq_kv8_append(C.byref(bad), None, None, tq.TQ_FP16, 256, 256, None, 0, None, None) == tq.TQ_ERR_SHAPE
+    prompt = [None, None, None, tq.TQ_BF16, 1024, 256, 256, 0, 0, F, F, 2, 8, 2, 128, 1.0, 1, 0, None, tq.TQ_FP32, None, None]
+    assert tq._lib.tq_sdpa_prompt(*prompt) == tq.TQ_OK
+    prompt[7] = 3                                      # queries, but no address of theirs
+    assert tq._lib.tq_sdpa_prompt(*prompt) == tq.TQ_ERR_NULL
+
+
+def test_a_cache_follows_its_tensors(tq):
+    """Storage that was swapped under a tensor is found again; a tensor of another size is refused; the attributes cannot
+    be set past the cache."""
+    import torch
+    cache = tq.KV8Cache(2, 2, 32, 64, device="cpu")
+    cache.blocks.data = cache.blocks.clone()
+    assert cache.struct().blocks == cache.blocks.data_ptr()
+    with pytest.raises(AttributeError):
+        cache.seq_lens = torch.zeros(2, dtype=torch.int32)
+    cache.blocks.data = cache.blocks[:1].clone()
+    with pytest.raises(tq.TqError) as e:
+        cache.struct()
+    assert e.value.code == tq.TQ_ERR_SHAPE and "resized" in str(e.value)
 
 
 def test_the_binding_refuses_tensors_it_cannot_use(tq):
