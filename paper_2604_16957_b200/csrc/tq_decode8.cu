@@ -12,17 +12,19 @@
 //
 // What bounds it: HBM.  2 d + 0.5 bytes per token and KV head; per 16-token block a warp issues 2 x d / 16 MMAs, 3 d / 8
 // integer and half-precision instructions that widen the codes, and 8 exponentials per lane (2 per score): a quarter
-// of what an SM could do in the time that the block takes to arrive.
+// of what an SM could do in the time that the block takes to arrive.  Measured at d = 128, 64 heads on 8: 128K tokens
+// 51.4 us (5.2 TB/s over all; the loop itself takes 38 us, 7.1 TB/s, and the rest is the start, 2 us, the merge of the
+// warps, 2.5, and the joining of cut units, 5); 16 sequences of 4K to 64K, 193 us (5.9 TB/s); 1K tokens 9.2 us, all of
+// it latency.  d = 256, 32K tokens, 32 heads on 16: 48 us.
 //
 // Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
 // block i of N takes the blocks [i W / N, (i + 1) W / N) of the W in all, whatever the lengths: ragged batches load
 // every SM alike, one short sequence still spreads.  (Batches of short sequences are not cut: see by_block and by_warp.)
-// A unit that lies in one thread block is finished there; the parts
-// of a cut one go to the workspace (at most two per thread block), and the last to arrive (a counter per unit) joins
-// them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512: registers), each with a ring of three to
-// six stages of one 16-token block, and one warp that fills the rings, one bulk copy per block (K codes, V codes and
-// ranges are contiguous): 200 KB in flight per SM, no barrier in the main loop, and the copies run on into the thread
-// block's next unit while this one is merged.
+// A unit that lies in one thread block is finished there; the parts of a cut one go to the workspace, and the last to
+// arrive (a counter per unit) joins them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
+// registers), each with a ring of three to six stages of one 16-token block, and one warp that fills the rings, one bulk
+// copy per block (K codes, V codes and ranges are contiguous): 200 KB in flight per SM, no barrier in the main loop, and
+// the copies run on into the thread block's next unit while this one is merged.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,8 +1,8 @@
 // Attention of packed prompts on the tensor cores (tcgen05, TMEM, TMA): tq_sdpa_prompt.
 //
 // A tile is 128 query rows of one KV head: T = 128 / G tokens times the G query heads that share the head, token by
-// token, so K and V are read once per KV head whatever G is.  A thread block works on NQ tiles (two at d <= 128, one
-// above) over a common stream of K / V tiles of BN keys:
+// token, so K and V are read once per KV head whatever G is.  A thread block works on NQ tiles over a common stream of
+// K / V tiles of BN keys:
 //     S = Q K^T   (tcgen05.mma, both operands in shared memory, S in TMEM)
 //     P = 2^(c S - c m), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
@@ -14,18 +14,26 @@
 // a tile follow one another: 1.09 ms for the 8K prompt.  At d = 512 the accumulator of a row does not fit TMEM: a thread
 // block computes 256 of the 512 output channels, and S is computed twice.
 //
+// NQ is 2 at d <= 128 and 1 above (TMEM).  A launch of so few tiles that every one finds an SM of its own takes one tile
+// per thread block at any d: a step of 64 keys is then 0.6 to 0.8 us instead of 0.9 (16 sequences of up to 300 tokens,
+// 4 heads on 1: 8.5 us instead of 9.9; one KV head, 1211 tokens, window 100: 8.1 instead of 11.8).  With more tiles than
+// SMs two per thread block share what they read: 12.4 us instead of 14.2 at 4076 tokens, 8 heads on 1, window 100.
+//
 // Roles: one warpgroup of softmax threads per tile; a warp that finds the work and issues the TMA loads; a warp per tile
-// that issues its MMAs (one issuing thread could not keep the tensor cores busy over its waits); one or two warps that look through the V tiles which some row sees in part.  Those may hold tokens of a
-// neighbouring sequence or of the row's future, whose weight is 0, and 0 * inf is not 0: a value there that is no finite
-// number is replaced by 0 in shared memory, and the rows that do see it get it added back in the epilogue from global
-// memory.
+// that issues its MMAs (one issuing thread could not keep the tensor cores busy over its waits); one or two warps that
+// look through the V tiles which some row sees in part.  Those may hold tokens of a neighbouring sequence or of the row's
+// future, whose weight is 0, and 0 * inf is not 0: a value there that is no finite number is replaced by 0 in shared
+// memory, and the rows that do see it get it added back in the epilogue from global memory.
 //
 // A thread block starts with the tile of its own index and then takes over thread blocks of the grid that have not
 // started (cluster launch control), so the loads and the first scores of the next tile run under the last softmax and the
 // epilogue of this one, and tiles of very different cost (causal masks, ragged lengths) even out.
 //
-// What bounds it: at d = 128 a 128 x 128 tile costs the tensor cores 1024 cycles and the exponential unit 1024 cycles (16
-// per cycle and SM).
+// What bounds it, d = 128, per 64 keys of two tiles: the exponential unit 1024 cycles (16 per cycle and SM), the tensor
+// cores 2 x (8 x 48 + 4 x 64) = 1280 with their operands from shared memory; a step takes 1540, and a
+// hand-over of S and P costs 250 of latency that two tiles do not quite hide.  The 8K prompt (64 heads on 8): 1.03 to
+// 1.1 ms, 1.0 to 1.07 PFLOP/s, at the card's power limit (1.65 GHz).  Ragged prompts of 256 to 2048 tokens: 0.75 to
+// 0.84 PFLOP/s; there an epilogue of 1500 (d = 64) to 2900 cycles comes every 2 to 32 steps.
 #include <cuda.h>
 
 #include "tq_async.cuh"
@@ -39,9 +47,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 12.0f;  // log2 units a score may exceed the running maximum: weights stay below 2^12
 
-template <int D>
+template <int D, int TILES>
 struct Cfg {
-  static constexpr int NQ = D <= 128 ? 2 : 1;         // query tiles of a thread block
+  static constexpr int D_ = D;
+  static constexpr int NQ = TILES;                    // query tiles of a thread block
   static constexpr int BN = D <= 256 ? 64 : 32;       // keys of a K / V tile
   static constexpr int DV = D <= 256 ? D : 256;       // output channels of a thread block
   static constexpr int SOFT = 4 * NQ;                 // softmax warps
@@ -70,9 +79,8 @@ struct Maps {
 };
 
 // mbarriers of a thread block, 8 bytes each
-template <int D>
+template <typename C>
 struct Bars {
-  using C = Cfg<D>;
   static constexpr int FULL = 0, EMPTY = FULL + C::NS, READY = EMPTY + C::NS;  // stages: landed, free, looked through
   static constexpr int Q = READY + C::NS, Q_FREE = Q + 1;
   static constexpr int S = Q_FREE + 1, P = S + 2 * C::NQ, O = P + 2 * C::NQ;  // scores and weights (two buffers), outputs
@@ -112,7 +120,7 @@ __device__ __forceinline__ bool warp_wait_on(uint32_t bar, uint32_t parity, vola
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  asm volatile("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -138,9 +146,8 @@ struct Work {
 
 // Key tiles of a piece of work: [j0, j1) of each query tile, [J0, J1) of all; the keys that every query sees are
 // [lo, up).
-template <int D>
+template <typename C>
 struct Span {
-  using C = Cfg<D>;
   int j0[C::NQ], j1[C::NQ], J0, J1, lo, up;
   __device__ Span(const PromptArgs& a, const Work& w, int T) : J0(0), J1(0) {
     int x, y;
@@ -165,11 +172,11 @@ struct Span {
   __device__ bool partly(int j) const { return j * C::BN < lo || (j + 1) * C::BN > up; }
 };
 
-template <int D, int DT, int OT>
-__global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps maps, const PromptArgs a,
+template <int D, int NQ, int DT, int OT>
+__global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps maps, const PromptArgs a,
                                                                     int G, int T) {
-  using C = Cfg<D>;
-  using B = Bars<D>;
+  using C = Cfg<D, NQ>;
+  using B = Bars<C>;
   extern __shared__ uint8_t raw[];
   __shared__ __align__(16) uint4 s_answer;
   __shared__ Work s_work[2];
@@ -242,7 +249,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     uint32_t total = 0, out = 0;  // K / V tiles of this query tile, and arrivals on its outputs, in all work so far
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
-      const Span<D> r(a, w, T);
+      const Span<C> r(a, w, T);
       const int tok = w.tok0 + i * T + t;
       const bool real = row < T * G && tok < w.s.lq;
       int lo = 0, up = 0;
@@ -268,10 +275,15 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
         for (int x = 0; x < C::BN; x += 32) tmem_ld32(s_addr + x, reinterpret_cast<uint32_t*>(s) + x);
         tmem_wait_ld();
         const int k0 = j * C::BN;
-        if (__any_sync(0xffffffffu, lo > k0 || up < k0 + C::BN)) {
-          const int from = lo - k0, to = up - k0;
+        if (__any_sync(0xffffffffu, up < k0 + C::BN)) {
+          const int to = up - k0;
 #pragma unroll
-          for (int x = 0; x < C::BN; ++x) s[x] = x >= from && x < to ? s[x] : -INFINITY;
+          for (int x = 0; x < C::BN; ++x) s[x] = x < to ? s[x] : -INFINITY;
+        }
+        if (__any_sync(0xffffffffu, lo > k0)) {
+          const int from = lo - k0;
+#pragma unroll
+          for (int x = 0; x < C::BN; ++x) s[x] = x >= from ? s[x] : -INFINITY;
         }
         float mx;
         {
@@ -435,10 +447,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     // ====================================================================================== the work, and TMA loads
     if (lane == 0) {
       const int TT = C::NQ * T, halves = D / C::DV;
-      // Tiles of a sequence: b starts at tile q_offsets[b] / TT + b, which leaves room for its ceil(lq / TT) tiles.  The late
+      // Tiles of a sequence: b starts at tile start_of(b) = q_offsets[b] / TT + b, which leaves room for its ceil(lq / TT) tiles.  The late
       // tiles of a sequence see the most keys under the causal mask and go first.
-      auto start_of = [&](int b) { return min(max(a.q_offsets[b], 0), a.n_q) / TT + b; };
-      int id = blockIdx.x, b = -1, it = 0, stage = 0, q_uses = 0;
+      int id = blockIdx.x, it = 0, stage = 0, q_uses = 0;
       uint32_t phase = 1, issued = 0;  // the first pass over the ring finds every stage empty
       bool ok = true;
       for (int asked = 0; ok; ++asked) {
@@ -449,19 +460,14 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           at /= halves;
           w.h = at % a.H_kv;
           const int tile = a.n_q / TT + a.B - 1 - at / a.H_kv;
-          if (b < 0) {
-            int hi = a.B;
-            b = 0;
-            while (hi - b > 1) {
-              const int mid = (b + hi) >> 1;
-              if (start_of(mid) <= tile) b = mid;
-              else hi = mid;
-            }
+          int b = 0;  // the last sequence with start_of(b) <= tile, that is q_offsets[b] < (tile - b + 1) TT
+          for (int hi = a.B; hi - b > 1;) {
+            const int mid = (b + hi) >> 1;
+            if (min(max(a.q_offsets[mid], 0), a.n_q) < (tile - mid + 1LL) * TT) b = mid;
+            else hi = mid;
           }
-          while (b > 0 && start_of(b) > tile) --b;  // the next one is near the last one
-          while (b + 1 < a.B && start_of(b + 1) <= tile) ++b;
           w.s = prompt_seq(a, b, false);
-          w.tok0 = (tile - start_of(b)) * TT;
+          w.tok0 = (tile - w.s.q0 / TT - b) * TT;
           w.more = w.tok0 >= 0 && w.tok0 < w.s.lq;
           if (w.more && w.tok0 == 0 && w.h == 0 && w.half == 0) (void)prompt_seq(a, b, true);  // one reports for the sequence
         }
@@ -475,7 +481,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
           }
         }
         if (w.more && ok) {
-          const Span<D> r(a, w, T);
+          const Span<C> r(a, w, T);
           if (r.J1 > r.J0) {
             ok = wait_on(bar(B::Q_FREE), (q_uses & 1) ^ 1, stop);
             if (ok) {
@@ -539,7 +545,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     bool ok = true;
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
-      const Span<D> r(a, w, T);
+      const Span<C> r(a, w, T);
       const int J0 = uniform(r.J0), J1 = uniform(r.J1), lo = uniform(r.lo), up = uniform(r.up);
       const int my0 = uniform(i == 0 ? r.j0[0] : r.j0[C::NQ - 1]), my1 = uniform(i == 0 ? r.j1[0] : r.j1[C::NQ - 1]);
       if (J1 <= J0) continue;
@@ -598,7 +604,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) prompt_kernel(const __grid
     uint32_t phase = 0;
     Work w;
     for (int it = 0; ok && next_work(it, w); ++it) {
-      const Span<D> r(a, w, T);
+      const Span<C> r(a, w, T);
       // every stage of the ring in turn, so that none is filled again behind this warp's back
       for (int j = r.J0; j <= r.J1 && r.J1 > r.J0 && ok; ++j) {
         ok = warp_wait_on(bar(B::FULL + stage), phase, stop);
@@ -675,10 +681,17 @@ bool make_map(CUtensorMap* map, const void* p, int dtype, int d, int heads, long
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int DT, int OT>
-cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
-  using C = Cfg<D>;
-  auto* kernel = prompt_kernel<D, DT, OT>;
+// Thread blocks of a launch: no less than there are pieces of work, whatever the lengths.
+template <typename C>
+long long blocks_of(const PromptArgs& a) {
+  const int T = 128 / (a.H_q / a.H_kv);
+  return (static_cast<long long>(a.n_q) / (C::NQ * T) + a.B) * a.H_kv * (C::D_ / C::DV);
+}
+
+template <int D, int NQ, int DT, int OT>
+cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st) {
+  using C = Cfg<D, NQ>;
+  auto* kernel = prompt_kernel<D, NQ, DT, OT>;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
@@ -688,7 +701,7 @@ cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
   const int G = a.H_q / a.H_kv, T = 128 / G;
-  const long long blocks = (static_cast<long long>(a.n_q) / (C::NQ * T) + a.B) * a.H_kv * (D / C::DV);
+  const long long blocks = blocks_of<C>(a);
   if (!encode_fn() || blocks > 0x7fffffffLL) return cudaErrorNotSupported;
   Maps maps;
   // (without a single key the maps of K and V describe a row of q; nothing is loaded through them)
@@ -698,6 +711,14 @@ cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
       !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN))
     return cudaErrorInvalidValue;
   return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T);
+}
+
+template <int D, int DT, int OT>
+cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
+  if constexpr (D <= 128) {  // (the rule is explained at the top)
+    if (blocks_of<Cfg<D, 1>>(a) > device_sm_count()) return launch_tiles<D, 2, DT, OT>(a, st);
+  }
+  return launch_tiles<D, 1, DT, OT>(a, st);
 }
 
 template <int D>
