@@ -481,11 +481,18 @@ PROMPTS = [
     ([1100], 0, 8, 2, 128, "fp16", True, 0), ([700], 0, 2, 1, 256, "bf16", True, 0)]
 
 
+# Empty sequences behind the others: a padded batch.  They also count towards the tiles by which the kernel's form is
+# chosen (d <= 128: two tiles per thread block where there are more tiles than SMs).
+PADDED = pytest.mark.parametrize("padded", [0, 200])
+
+
+@PADDED
 @pytest.mark.parametrize("lq,past,H_q,H_kv,d,kind,causal,window", PROMPTS)
-def test_prompt(gpu, lq, past, H_q, H_kv, d, kind, causal, window):
+def test_prompt(gpu, lq, past, H_q, H_kv, d, kind, causal, window, padded):
     """past < 0: fewer keys than queries, so the first queries see nothing.  Rows behind the last sequence stay."""
     tq, torch = gpu
     rng = np.random.default_rng(sum(lq) + d)
+    lq = lq + [0] * padded
     lk = [max(0, n + past) if n else 0 for n in lq]
     fused = past == 0
     extra = 3
@@ -502,8 +509,9 @@ def test_prompt(gpu, lq, past, H_q, H_kv, d, kind, causal, window):
         _check_prompt(torch, out, q, k, v, q_at, k_at, d ** -0.5, causal, window)
 
 
+@PADDED
 @pytest.mark.parametrize("d,kind", [(64, "bf16"), (128, "fp16"), (256, "bf16")])
-def test_prompt_infinities_and_nans_stay_with_their_readers(gpu, d, kind):
+def test_prompt_infinities_and_nans_stay_with_their_readers(gpu, d, kind, padded):
     """NaN and infinities in K and V: of a neighbouring sequence, of later tokens of the same sequence, of tokens outside
     the window, and of tokens that are seen."""
     tq, torch = gpu
@@ -516,7 +524,7 @@ def test_prompt_infinities_and_nans_stay_with_their_readers(gpu, d, kind):
     v[100, 0, 3], v[101, 1, 5], v[240, 0, 7] = float("inf"), float("nan"), -float("inf")
     k[120, 1, 2] = float("nan")
     v[300:], k[300:] = float("nan"), float("nan")
-    dq = torch.tensor(at, dtype=torch.int32, device="cuda")
+    dq = torch.tensor(at + [300] * padded, dtype=torch.int32, device="cuda")
     for window in (0, 20):
         out = torch.empty(q.shape, dtype=torch.float32, device="cuda")
         tq.tq_sdpa_prompt(q, k, v, dq, dq, d ** -0.5, out, window=window)
@@ -537,23 +545,25 @@ def test_prompt_infinities_and_nans_stay_with_their_readers(gpu, d, kind):
         _check_prompt(torch, o[240:], q[240:300], k[240:300], v[240:300], [0, 60], [0, 60], d ** -0.5, True, window)
 
 
-def test_prompt_large_scores_and_odd_scales(gpu):
+@PADDED
+def test_prompt_large_scores_and_odd_scales(gpu, padded):
     """Scores far beyond the range of exp, a negative and a zero scale."""
     tq, torch = gpu
     rng = np.random.default_rng(9)
     q, k, v = _packed(torch, rng, [200], [200], 4, 2, 128, "fp16", True)
     q = q * 30
-    at = torch.tensor([0, 200], dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, 200] + [200] * padded, dtype=torch.int32, device="cuda")
     for alpha in (1.0, -0.3, 0.0):
         out = torch.empty(q.shape, dtype=torch.float32, device="cuda")
         tq.tq_sdpa_prompt(q, k, v, at, at, alpha, out)
         _check_prompt(torch, out, q, k, v, [0, 200], [0, 200], alpha, True, 0)
 
 
-def test_prompt_offsets_outside_the_buffers(gpu):
+@PADDED
+def test_prompt_offsets_outside_the_buffers(gpu, padded):
     tq, torch = gpu
     q, k, v = _packed(torch, np.random.default_rng(3), [64], [64], 2, 1, 64, "fp16", False)
-    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    dev = lambda x: torch.tensor(x + x[-1:] * (padded if len(x) > 1 else 0), dtype=torch.int32, device="cuda")  # noqa: E731
     status = dev([0])
     out = torch.full(q.shape, 5.0, device="cuda")
     tq.tq_sdpa_prompt(q, k, v, dev([0, 20, 90]), dev([0, 20, 90]), 0.125, out, status=status)   # the second one ends at row 64
