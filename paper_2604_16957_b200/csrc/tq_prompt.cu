@@ -75,7 +75,7 @@ struct Cfg {
 };
 
 struct Maps {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, o;
 };
 
 // mbarriers of a thread block, 8 bytes each
@@ -404,10 +404,16 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         uint8_t* const dst = static_cast<uint8_t*>(a.out) + to * kSize;
         if constexpr (C::STAGED) {
           // Through shared memory, 128 bytes of the warp's 32 rows at a time: straight from the registers every store would
-          // touch 32 rows (8700 cycles for 128 rows of 256 channels).  16-byte piece p of row r lies at p ^ (r % 8).
+          // touch 32 rows (8700 cycles for 128 rows of 256 channels).  16-byte piece p of row r lies at p ^ (r % 8), as a
+          // tensor map with a 128-byte swizzle has it.  With two tiles, whose warps are in each other's way, one TMA store
+          // takes the 128 bytes out where the rows are whole tokens of the sequence (6 sequences of 67 to 539 tokens, 128
+          // heads on 16: 51.7 us instead of 57.1); a single tile gains nothing from it (12 short sequences, d = 256: 13.6
+          // instead of 12.8).
           constexpr int kCols = 128 / kSize;
+          constexpr bool kTma = C::NQ == 2;
           uint4* const area = reinterpret_cast<uint4*>(smem + C::OUT + warp * 4096);
           const unsigned valid = __ballot_sync(0xffffffffu, real);
+          const bool whole = kTma && valid == 0xffffffffu && (32 % G) == 0;
           const int sub = lane >> 3, piece = lane & 7;
           uint8_t* rows[8];
 #pragma unroll
@@ -419,8 +425,21 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
             for (int z = 0; z < kCols; z += 32) {
               float f[32];
               channels(x + z, f);
+              if (kTma && z == 0) {
+                if (lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+              }
 #pragma unroll
               for (int y = 0; y < 32; y += kEach) area[8 * lane + (((z + y) / kEach) ^ (lane & 7))] = bytes16(f, y);
+            }
+            if (whole) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&maps.o, w.half * C::DV + x, w.h * G, w.s.q0 + tok, base + C::OUT + warp * 4096);
+                bulk_commit();
+              }
+              continue;
             }
             __syncwarp();
 #pragma unroll
@@ -443,6 +462,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         tc_fence_before();
       }
     }
+    if (C::NQ == 2 && lane == 0) bulk_wait_read<0>();  // shared memory stays until it is read
   } else if (warp == C::SOFT) {
     // ====================================================================================== the work, and TMA loads
     if (lane == 0) {
@@ -668,15 +688,18 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// [rows][heads][d] 16-bit values, rows `stride` elements apart, boxes of 64 channels x `heads_box` x `rows_box`
+// [rows][heads][d] values, rows `stride` elements apart, boxes of 128 bytes x `heads_box` x `rows_box`
 bool make_map(CUtensorMap* map, const void* p, int dtype, int d, int heads, long long rows, long long stride, int heads_box,
               int rows_box) {
+  const int size = dtype == TQ_FP32 ? 4 : 2;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(stride) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(heads_box), static_cast<cuuint32_t>(rows_box)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * size, static_cast<cuuint64_t>(stride) * size};
+  const cuuint32_t box[3] = {128u / size, static_cast<cuuint32_t>(heads_box), static_cast<cuuint32_t>(rows_box)};
   const cuuint32_t ones[3] = {1, 1, 1};
-  return encode_fn()(map, dtype == TQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                     const_cast<void*>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const CUtensorMapDataType type = dtype == TQ_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == TQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                      : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode_fn()(map, type, 3, const_cast<void*>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -708,7 +731,8 @@ cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st) {
   const bool keys = a.n_kv > 0;
   if (!make_map(&maps.q, a.q, a.dtype, D, a.H_q, a.n_q, a.q_stride, G, T) ||
       !make_map(&maps.k, keys ? a.k : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.k_stride : a.q_stride, 1, C::BN) ||
-      !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN))
+      !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN) ||
+      !make_map(&maps.o, a.out, a.out_dtype, D, a.H_q, a.n_q, static_cast<long long>(a.H_q) * D, G > 32 ? 1 : G, G > 32 ? 1 : 32 / G))
     return cudaErrorInvalidValue;
   return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T);
 }

@@ -17,6 +17,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];\n" ::"l"(map), "r"(x), "r"(y), "r"(z),
+               "r"(src)
+               : "memory");
+}
 
 // ---- work stealing from the launch's own grid: asks for a thread block that has not started; the answer (16 bytes of
 // shared memory) completes on the mbarrier.  After a "no" a thread block must not ask again.
