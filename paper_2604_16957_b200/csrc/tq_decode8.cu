@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   constexpr int KK = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_start, s_warp[C::NW + 1];
-  __shared__ int s_b, s_last, s_dead;
+  __shared__ int s_b, s_last, s_dead, s_from, s_to;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t4 = lane & 3;
   float* const merge = reinterpret_cast<float*>(smem + C::RING);
@@ -292,12 +292,24 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   const int worth = (W - 1) / a.min_blocks + 1;
   int N = worth < 1 ? 1 : (worth < a.grid ? worth : a.grid);
   if (U > a.grid) N = W < a.grid ? W : a.grid;
-  // One sequence: its units are equally long.  Shares that end where units do save the thread blocks in between a second
-  // query and merge (5 us); giving up N % units thread blocks for that lengthens the others by each (N % units) / N
-  // blocks of 0.09 us (128K tokens, 8 KV heads: 144 shares instead of 148).
-  if (a.c.B == 1 && N > a.units) {
-    const int spare = N % a.units;
-    if (spare * (W / N) <= 32 * N) N -= spare;
+  // Few units: shares that end where units do save the thread blocks in between a second query and merge (5 us).  Each
+  // unit of a sequence gets floor(its part of the line x N) of them; that lengthens the longest share, by 0.09 us per
+  // block, and is done up to 32 blocks (128K tokens, 8 KV heads: 144 shares instead of 148).
+  int cuts = 0, cuts_upto = 0;  // shares of each unit of the lane's sequence, and of those up to it
+  bool snapped = false;
+  if (few && !by_block && !by_warp && U < a.grid && U <= N) {
+    const int n = lane < a.c.B ? own_n : 0;
+    const float part = static_cast<float>(n) / static_cast<float>(W / a.units);  // (1 exactly for a single sequence)
+    cuts = min(n, max(1, static_cast<int>(part * static_cast<float>(N / a.units))));  // (none of them is empty)
+    cuts_upto = cuts;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, cuts_upto, o);
+      if (lane >= o) cuts_upto += y;
+    }
+    const bool fits = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units <= N;
+    snapped = fits && __all_sync(0xffffffffu, n == 0 || (n - 1) / cuts + 1 <= W / N + 32);
+    if (snapped) N = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units;
   }
 
   // sequences without a token: their rows are zero
@@ -309,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   if (W == 0 || (!by_block && !by_warp && static_cast<int>(blockIdx.x) >= N)) return;
 
   const Shares shares(W, N);
-  const int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
+  int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
   int first_b;
   int first_at;
   auto claim = [&](int b, int n, int upto) {  // the sequence that holds the start of the share
@@ -318,7 +330,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       s_start = (upto - n) * a.units;
     }
   };
-  if (a.c.B == 1 || by_block || by_warp) {
+  if (by_block || by_warp || snapped) {
     first_b = 0;
     first_at = 0;
   } else if (few) {
@@ -352,6 +364,24 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     use.g1 = warp == C::NW && lane >= C::NW ? 0 : U;
     use.hop = by_block ? static_cast<int>(gridDim.x) : static_cast<int>(gridDim.x) * C::NW;
     any = use.seek(a);
+  } else if (snapped) {
+    const int i = blockIdx.x;
+    const int from = __ffs(static_cast<int>(__ballot_sync(0xffffffffu, cuts_upto * a.units > i))) - 1;
+    const int c = __shfl_sync(0xffffffffu, cuts, from), at = i - (__shfl_sync(0xffffffffu, cuts_upto, from) - c) * a.units;
+    use.hop = 0;
+    use.b = from;
+    use.u = at / c;
+    const int x = at - use.u * c, n = __shfl_sync(0xffffffffu, own_n, from);
+    const int each = n / c, rest = n - each * c;  // part x has the blocks [floor(n x / c), floor(n (x + 1) / c))
+    const int lo = each * x + rest * x / c, hi = each * (x + 1) + rest * (x + 1) / c;
+    use.g = g0 = (__shfl_sync(0xffffffffu, own_upto, from) - n) * a.units + use.u * n + lo;
+    use.g1 = use.g + hi - lo;
+    any = hi > lo;
+    use.open(a, lo);
+    if (tid == 0) {
+      s_from = i - x;
+      s_to = i - x + c - 1;
+    }
   } else {
     use.hop = 0;
     use.g = g0;
@@ -596,11 +626,15 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     const bool whole = use.j0 == 0 && use.j1 == use.n;
     const int u0 = use.g - use.j0;  // the unit on the line, and the thread blocks that share it
     int from = 0, to = 0;
-    if (!whole) {
+    if (!whole && !snapped) {
       from = shares.owner(u0);
       to = shares.owner(u0 + use.n - 1);
     }
     join_warps();
+    if (snapped) {
+      from = s_from;
+      to = s_to;
+    }
     for (int q = warp; q < 8; q += C::NW) {
       const bool has = lane < C::NW;
       const float wm = has ? stats[lane * 8 + q] : kNoMax, wp = has ? stats[(C::NW + lane) * 8 + q] : kNoMax;
@@ -680,7 +714,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
       join_warps();
       if (s_last) {
-        const int skip = shares.start(from) == u0 ? 0 : 1;  // the first part is its thread block's second one
+        const int skip = snapped || shares.start(from) == u0 ? 0 : 1;  // the first part is its thread block's second one
         const int np = to - from + 1;
         auto part_of = [&](int p) {
           return a.parts + (a.compact ? from + p + unit : 2LL * (from + p) + (p == 0 ? skip : 0)) * stride;
