@@ -512,7 +512,7 @@ int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, in
  *                  streams, graphs replayed side by side) need workspaces of their own.
  *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype)
  * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64;
- * B * H_kv * ceil(H_q / H_kv / 8) * S_cap / 16 below 2^31 - 2^16.
+ * B * H_kv * ceil(H_q / H_kv / 8) * (S_cap / 16 + 64) at most 2^31 - 2^16.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,
  * TQ_STATUS_BAD_PAGE, TQ_STATUS_TIMEOUT (zero the counters again after it).
  */

@@ -18,8 +18,11 @@
 // it latency.  d = 256, 32K tokens, 32 heads on 16: 48 us.
 //
 // Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
-// block i of N takes the blocks [i W / N, (i + 1) W / N) of the W in all, whatever the lengths: ragged batches load
+// block i of N takes the positions [i L / N, (i + 1) L / N) of the L in all, whatever the lengths: ragged batches load
 // every SM alike, one short sequence still spreads.  (Batches of short sequences are not cut: see by_block and by_warp.)
+// With more units than thread blocks each unit also has `lead` positions before its blocks, for what its query, merge and
+// output cost; without them a share of many short units took three times as long as one of a few long ones (45
+// sequences of 320 to 5130 tokens, 16 KV heads: 199 us).
 // A unit that lies in one thread block is finished there; the parts of a cut one go to the workspace, and the last to
 // arrive (a counter per unit) joins them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
 // registers), each with a ring of three to six stages of one 16-token block, and one warp that fills the rings, one bulk
@@ -76,6 +79,7 @@ struct Args {
   int units;         // H_kv * tiles
   int grid;          // thread blocks launched
   int min_blocks;    // fewest cache blocks worth a thread block
+  int lead;          // positions on the line before a unit's blocks (see the top)
   int32_t* counters;
   float* parts;      // see part_floats
   int rows;          // query heads of a tile: at most 8
@@ -125,7 +129,7 @@ __device__ __forceinline__ Span span_of(const Args& a, int b) {
 // units instead: unit g (sequences first), then every hop-th one after it.  Positions fit 31 bits (the entry point sees
 // to that): they are held through the main loop, and 64-bit divisions cost half a microsecond of latency apiece.
 struct Walk {
-  int g, g1;  // position on the line and end of the share; unit and their number
+  int g, g1;  // start of the unit on the line and end of the share; unit and their number
   int hop;
   int b, u, h;      // sequence, unit in it, its KV head
   int j0, j1, n;    // blocks of this visit, blocks of the unit
@@ -135,8 +139,7 @@ struct Walk {
     h = a.tiles == 1 ? u : u / a.tiles;
     n = span.blocks();
     j0 = j;
-    const int left = g1 - g;
-    j1 = hop > 0 || n - j0 < left ? n : j0 + left;
+    j1 = hop > 0 ? n : min(n, g1 - g - a.lead);
   }
   // the first unit with a token, from g on
   __device__ bool seek(const Args& a) {
@@ -153,7 +156,7 @@ struct Walk {
       g += hop;
       return seek(a);
     }
-    g += j1 - j0;
+    g += a.lead + n;
     if (g >= g1) return false;
     if (++u == a.units) {
       u = 0;
@@ -165,7 +168,7 @@ struct Walk {
       } while (span_of(a, b).blocks() == 0);
     }
     open(a, 0);
-    return true;
+    return j1 > 0;  // (no: the share ends before the unit's blocks)
   }
 };
 
@@ -194,11 +197,11 @@ __device__ __forceinline__ void store_out2(void* out, long long at, float x, flo
   else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + at) = pack2<OT>(x, y);
 }
 
-// The line of W blocks cut into N shares: share i starts at floor(i W / N).
+// The line of L positions cut into N shares: share i starts at floor(i L / N).
 struct Shares {
   int each, rest, N;
   float per;
-  __device__ Shares(int W, int n) : each(W / n), rest(W - each * n), N(n) { per = static_cast<float>(n) / static_cast<float>(W); }
+  __device__ Shares(int L, int n) : each(L / n), rest(L - each * n), N(n) { per = static_cast<float>(n) / static_cast<float>(L); }
   __device__ int start(int i) const { return each * i + i * rest / N; }
   __device__ int owner(int g) const {
     int i = static_cast<int>(static_cast<float>(g) * per);  // off by one at most
@@ -214,7 +217,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   using C = Cfg<D>;
   constexpr int KK = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int s_start, s_warp[C::NW + 1];
+  __shared__ int s_start, s_warp[C::NW + 1], s_top[C::NW + 1];
   __shared__ int s_b, s_last, s_dead, s_from, s_to;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t4 = lane & 3;
@@ -236,8 +239,10 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   const bool few = a.c.B <= 32;  // a warp sums the lengths up by itself: every warp does, and no barrier is needed
 
   // ---- where this thread block's share starts: blocks of all sequences, then the sequence that holds the start
+  int most = 0;                       // longest unit on the line
   auto scan = [&](int v, int& sum) {  // inclusive sum over the threads; `sum`: that of all
     int x = v;
+    const int top = __reduce_max_sync(0xffffffffu, v);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -245,9 +250,13 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
     if (few) {
       sum = __shfl_sync(0xffffffffu, x, 31);
+      most = top;
       return x;
     }
-    if (lane == 31) s_warp[warp] = x;
+    if (lane == 31) {
+      s_warp[warp] = x;
+      s_top[warp] = top;
+    }
     __syncthreads();
     int add = 0, all = 0;
 #pragma unroll
@@ -255,51 +264,56 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       const int y = s_warp[w];
       if (w < warp) add += y;
       all += y;
+      most = max(most, s_top[w]);
     }
     __syncthreads();
     sum = all;
     return x + add;
   };
-  int W = 0;
-  int own_n = 0;  // blocks of the thread's sequence and of all up to it, in the last round
+  auto on_line = [&](int n) { return n > 0 ? n + a.lead : 0; };  // a unit's length
+  int L = 0;
+  int own_n = 0;  // a unit of the thread's sequence on the line, and of all up to it, in the last round
   int own_upto = 0;
   for (int round = 0; round < a.c.B; round += C::LAUNCH) {
     const int b = few ? lane : round + tid;
     own_n = 0;
     if (b < a.c.B) {
-      own_n = span_of(a, b).blocks();
+      own_n = on_line(span_of(a, b).blocks());
       const int len = a.c.seq_lens[b];
       if (blockIdx.x == 0 && a.status && (!few || warp == 0) && (len <= 0 || len > a.c.S_cap))
         atomicOr(a.status, (len < 0 || len > a.c.S_cap ? TQ_STATUS_BAD_LEN : 0) | (len <= 0 ? TQ_STATUS_EMPTY_SEQ : 0));
     }
     if (a.c.B == 1) {  // nothing to sum up
       own_n = __shfl_sync(0xffffffffu, own_n, 0);
-      W = own_upto = own_n;
+      L = own_upto = most = own_n;
       break;
     }
     int all;
     own_upto = scan(own_n, all);
-    W += all;
+    L += all;
   }
-  W *= a.units;
-  // Short sequences are not cut.  With no more units than thread blocks, of six blocks per warp on average at most, a
-  // thread block takes one unit: joining a cut one costs 6 us, those blocks arrive in that time (16 units of 63 blocks:
-  // 19 us cut into 17 shares).  With more units, of 24 blocks on average at most, a warp takes whole units, without a
-  // merge (18 x 8 units of up to 8 blocks: 168 us while a thread block took one after the other, 4 us for each).
+  L *= a.units;
   const int U = a.c.B * a.units;
-  const bool by_block = U <= static_cast<int>(gridDim.x) && W / (6 * C::NW) < U;
-  const bool by_warp = D < 512 && U > static_cast<int>(gridDim.x) && W / 24 < U;  // (d = 512: the warps share the query's fragments)
-  const int worth = (W - 1) / a.min_blocks + 1;
+  const int worth = (L - 1) / a.min_blocks + 1;
   int N = worth < 1 ? 1 : (worth < a.grid ? worth : a.grid);
-  if (U > a.grid) N = W < a.grid ? W : a.grid;
+  if (a.lead > 0) N = max(1, min(L, a.grid));
+  // Short sequences are not cut.  With no more units than thread blocks, the longest of which is at most 66 blocks (6 us)
+  // above a share, a thread block takes one unit: joining a cut one costs that (16 units of 63 blocks: 19 us cut into 17
+  // shares).  With more units a warp takes whole units, without a merge, where the longest, at 0.5 us per block, is done
+  // before the shares would be, at 0.075 us per position and 8 us for the joining (18 x 8 units of up to 8 blocks: 168 us
+  // in shares without leads; 58 x 16 of up to 99: 132 us so, 51 by warps).
+  const bool by_block = U <= static_cast<int>(gridDim.x) && most <= L / N + 66;
+  const bool by_warp = D < 512 && a.lead > 0 && !by_block &&  // (d = 512: the warps share the query's fragments)
+                       most - a.lead <= L / N / 7 + 16;
+
   // Few units: shares that end where units do save the thread blocks in between a second query and merge (5 us).  Each
   // unit of a sequence gets floor(its part of the line x N) of them; that lengthens the longest share, by 0.09 us per
   // block, and is done up to 32 blocks (128K tokens, 8 KV heads: 144 shares instead of 148).
   int cuts = 0, cuts_upto = 0;  // shares of each unit of the lane's sequence, and of those up to it
   bool snapped = false;
-  if (few && !by_block && !by_warp && U < a.grid && U <= N) {
+  if (few && !by_block && a.lead == 0 && U <= N) {
     const int n = lane < a.c.B ? own_n : 0;
-    const float part = static_cast<float>(n) / static_cast<float>(W / a.units);  // (1 exactly for a single sequence)
+    const float part = static_cast<float>(n) / static_cast<float>(L / a.units);  // (1 exactly for a single sequence)
     cuts = min(n, max(1, static_cast<int>(part * static_cast<float>(N / a.units))));  // (none of them is empty)
     cuts_upto = cuts;
 #pragma unroll
@@ -308,7 +322,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (lane >= o) cuts_upto += y;
     }
     const bool fits = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units <= N;
-    snapped = fits && __all_sync(0xffffffffu, n == 0 || (n - 1) / cuts + 1 <= W / N + 32);
+    snapped = fits && __all_sync(0xffffffffu, n == 0 || (n - 1) / cuts + 1 <= L / N + 32);
     if (snapped) N = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units;
   }
 
@@ -318,10 +332,10 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (span_of(a, b).blocks() != 0) continue;
       for (int i = tid; i < a.H_q * D; i += C::LAUNCH) store_out<OT>(a.out, static_cast<long long>(b) * a.H_q * D + i, 0.0f);
     }
-  if (W == 0 || (!by_block && !by_warp && static_cast<int>(blockIdx.x) >= N)) return;
+  if (L == 0 || (!by_block && !by_warp && static_cast<int>(blockIdx.x) >= N)) return;
 
-  const Shares shares(W, N);
-  int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
+  const Shares shares(L, N);
+  const int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
   int first_b;
   int first_at;
   auto claim = [&](int b, int n, int upto) {  // the sequence that holds the start of the share
@@ -345,7 +359,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     int carry = 0;
     for (int round = 0; round < a.c.B; round += C::LAUNCH) {
       const int b = round + tid;
-      const int n = b < a.c.B ? span_of(a, b).blocks() : 0;
+      const int n = b < a.c.B ? on_line(span_of(a, b).blocks()) : 0;
       int all;
       const int upto = scan(n, all);
       claim(b, n, carry + upto);
@@ -360,7 +374,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   Walk use;
   bool any = true;
   if (by_block || by_warp) {
-    use.g = by_block ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * C::NW + (warp < C::NW ? warp : lane);
+    use.g = by_block ? static_cast<int>(blockIdx.x) : (warp < C::NW ? warp : lane) * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
     use.g1 = warp == C::NW && lane >= C::NW ? 0 : U;
     use.hop = by_block ? static_cast<int>(gridDim.x) : static_cast<int>(gridDim.x) * C::NW;
     any = use.seek(a);
@@ -374,9 +388,8 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     const int x = at - use.u * c, n = __shfl_sync(0xffffffffu, own_n, from);
     const int each = n / c, rest = n - each * c;  // part x has the blocks [floor(n x / c), floor(n (x + 1) / c))
     const int lo = each * x + rest * x / c, hi = each * (x + 1) + rest * (x + 1) / c;
-    use.g = g0 = (__shfl_sync(0xffffffffu, own_upto, from) - n) * a.units + use.u * n + lo;
-    use.g1 = use.g + hi - lo;
-    any = hi > lo;
+    use.g = (__shfl_sync(0xffffffffu, own_upto, from) - n) * a.units + use.u * n;
+    use.g1 = use.g + hi;
     use.open(a, lo);
     if (tid == 0) {
       s_from = i - x;
@@ -384,13 +397,15 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
   } else {
     use.hop = 0;
-    use.g = g0;
     use.g1 = shares.start(blockIdx.x + 1);
     use.b = first_b;
-    const int n = span_of(a, use.b).blocks();
+    const int n = on_line(span_of(a, use.b).blocks());
     const int r = g0 - first_at;
     use.u = r / n;
-    use.open(a, r - use.u * n);
+    const int at = r - use.u * n;
+    use.g = g0 - at;
+    use.open(a, max(0, at - a.lead));
+    any = use.j1 > use.j0;
   }
 
   if (warp == C::NW) {
@@ -624,7 +639,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       st[2 * C::NW * 8 + 1] = l1;
     }
     const bool whole = use.j0 == 0 && use.j1 == use.n;
-    const int u0 = use.g - use.j0;  // the unit on the line, and the thread blocks that share it
+    const int u0 = use.g + a.lead;  // the unit's first block on the line, and the thread blocks that share the unit
     int from = 0, to = 0;
     if (!whole && !snapped) {
       from = shares.owner(u0);
@@ -657,7 +672,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     join_warps();
     const long long unit = static_cast<long long>(use.b) * a.units + use.u;
     const int stride = part_floats(D, a.rows);
-    float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + (use.g == g0 ? 0 : 1)) * stride;
+    float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + (use.g <= g0 ? 0 : 1)) * stride;
     const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
     auto emit = [&](int q, int ch, float x, float y) {
       x *= sums[24 + q];
@@ -694,7 +709,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     };
     // On the thread block's last visit nothing is on its way into the rings any more (every warp has used what it asked
     // for, and the barriers above are behind that): all eight rows at once through the rings' memory.
-    if ((use.hop > 0 ? use.g + use.hop : use.g + (use.j1 - use.j0)) >= use.g1 && !s_dead) {
+    if ((use.hop > 0 ? use.g + use.hop : u0 + use.j1) >= use.g1 && !s_dead) {
       join(reinterpret_cast<float*>(smem), 0, std::integral_constant<int, 8>{});
     } else {
       for (int q0 = 0; q0 < heads; q0 += C::MQ) join(merge, q0, std::integral_constant<int, C::MQ>{});
@@ -714,7 +729,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
       join_warps();
       if (s_last) {
-        const int skip = snapped || shares.start(from) == u0 ? 0 : 1;  // the first part is its thread block's second one
+        const int skip = snapped || shares.start(from) >= use.g ? 0 : 1;  // the first part is its thread block's second one
         const int np = to - from + 1;
         auto part_of = [&](int p) {
           return a.parts + (a.compact ? from + p + unit : 2LL * (from + p) + (p == 0 ? skip : 0)) * stride;
@@ -865,6 +880,9 @@ cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, lon
   a.units = c.H_kv * a.tiles;
   a.rows = a.G < 8 ? a.G : 8;
   a.compact = static_cast<long long>(c.B) * a.units < grid;
+  // A unit's query, merge and output cost as much as 57 blocks with 8 query heads (d = 128: 7800 cycles, 143 per block),
+  // 33 with 2 (d = 64: 3400, 103 per block).
+  a.lead = a.compact ? 0 : 25 + 4 * a.rows;
   a.grid = grid;
   a.counters = counters;
   a.parts = parts;

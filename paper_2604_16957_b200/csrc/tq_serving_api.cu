@@ -121,7 +121,9 @@ int tq_sdpa_int8_decode(const tq_kv8_cache* cache, const void* q, int32_t q_dtyp
   if (int r = check_cache8(cache)) return r;
   if (!q || !workspace || !out) return TQ_ERR_NULL;
   if (H_q < 1 || H_q % cache->H_kv != 0 || H_q / cache->H_kv > 64) return TQ_ERR_SHAPE;
-  if (static_cast<int64_t>(cache->B) * cache->H_kv * ((H_q / cache->H_kv + 7) / 8) * (cache->S_cap / 16) > 0x7fff0000LL) return TQ_ERR_SHAPE;
+  // (positions on the line, see tq_decode8.cu, are 31 bits)
+  if (static_cast<int64_t>(cache->B) * cache->H_kv * ((H_q / cache->H_kv + 7) / 8) * (cache->S_cap / 16 + 64) > 0x7fff0000LL)
+    return TQ_ERR_SHAPE;
   if (!is16(q_dtype) || (out_dtype != q_dtype && out_dtype != TQ_FP32) || window < 0 || max_seq_len < 0 ||
       q_stride < static_cast<int64_t>(H_q) * cache->d || q_stride % 8)
     return TQ_ERR_SHAPE;

@@ -346,7 +346,11 @@ def _check_decode(torch, out, q, values, alpha, window, d):
     # units of a few blocks each: one per thread block, several per warp; wide heads, where a warp never takes a unit
     ([5, 118, 0, 33] * 4, 64, 8, 128, 0, "fp16", 0, 15), ([3, 0, 70, 200] * 20, 24, 8, 128, 16, "bf16", 0, 16),
     ([40, 1] * 60, 8, 4, 256, 16, "fp16", 20, 17), ([9, 300] * 30, 20, 4, 512, 32, "bf16", 0, 18), ([16] * 700, 3, 1, 64, 0, "bf16", 0, 19),
-    ([400, 0, 390] * 60, 2, 2, 128, 64, "fp16", 0, 20)])
+    ([400, 0, 390] * 60, 2, 2, 128, 64, "fp16", 0, 20),
+    # more units than thread blocks, long and short ones on one line; a padded batch with one long sequence; equal shares
+    ([20, 2500, 300] * 15, 8, 8, 64, 0, "bf16", 0, 21), ([2500] * 6 + [17] * 40, 16, 4, 128, 64, "fp16", 0, 22),
+    ([0] * 30 + [9000] + [0] * 25, 24, 4, 128, 16, "bf16", 0, 23), ([1900, 40] * 20, 8, 4, 256, 32, "bf16", 1500, 24),
+    ([1500, 10, 0] * 13, 32, 8, 512, 16, "fp16", 0, 25), ([700, 3, 1], 8, 4, 64, 0, "fp16", 0, 26), ([6000, 5900, 1], 16, 2, 128, 16, "fp16", 0, 27)])
 def test_int8_decode(gpu, lens, H_q, H_kv, d, page, kind, window, seed):
     tq, torch = gpu
     rng = np.random.default_rng(100 + seed)
