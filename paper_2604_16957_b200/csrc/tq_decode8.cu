@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   constexpr int KK = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_start, s_warp[C::NW + 1], s_top[C::NW + 1];
-  __shared__ int s_b, s_last, s_dead, s_from, s_to;
+  __shared__ int s_b, s_last, s_dead, s_from, s_to, s_line[3];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t4 = lane & 3;
   float* const merge = reinterpret_cast<float*>(smem + C::RING);
@@ -336,6 +336,12 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
 
   const Shares shares(L, N);
   const int g0 = shares.start(min(static_cast<int>(blockIdx.x), N));
+  if (tid == 0) {  // for the merges of cut units: kept out of the main loop's registers
+    s_line[0] = L;
+    s_line[1] = N;
+    s_line[2] = g0;
+    s_from = -1;
+  }
   int first_b;
   int first_at;
   auto claim = [&](int b, int n, int upto) {  // the sequence that holds the start of the share
@@ -640,15 +646,17 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
     const bool whole = use.j0 == 0 && use.j1 == use.n;
     const int u0 = use.g + a.lead;  // the unit's first block on the line, and the thread blocks that share the unit
-    int from = 0, to = 0;
-    if (!whole && !snapped) {
-      from = shares.owner(u0);
-      to = shares.owner(u0 + use.n - 1);
-    }
     join_warps();
-    if (snapped) {
+    int from = 0, to = 0, slot = 0;  // the thread blocks that share the unit; which of this one's two parts it is
+    if (!whole) {
+      slot = use.g <= s_line[2] ? 0 : 1;
       from = s_from;
       to = s_to;
+      if (from < 0) {
+        const Shares shares(s_line[0], s_line[1]);
+        from = shares.owner(u0);
+        to = shares.owner(u0 + use.n - 1);
+      }
     }
     for (int q = warp; q < 8; q += C::NW) {
       const bool has = lane < C::NW;
@@ -672,7 +680,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     join_warps();
     const long long unit = static_cast<long long>(use.b) * a.units + use.u;
     const int stride = part_floats(D, a.rows);
-    float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + (use.g <= g0 ? 0 : 1)) * stride;
+    float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + slot) * stride;
     const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
     auto emit = [&](int q, int ch, float x, float y) {
       x *= sums[24 + q];
@@ -729,7 +737,8 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
       join_warps();
       if (s_last) {
-        const int skip = snapped || shares.start(from) >= use.g ? 0 : 1;  // the first part is its thread block's second one
+        // the first part is its thread block's second one
+        const int skip = a.compact || Shares(s_line[0], s_line[1]).start(from) >= use.g ? 0 : 1;
         const int np = to - from + 1;
         auto part_of = [&](int p) {
           return a.parts + (a.compact ? from + p + unit : 2LL * (from + p) + (p == 0 ? skip : 0)) * stride;
