@@ -13,16 +13,16 @@
 // What bounds it: HBM.  2 d + 0.5 bytes per token and KV head; per 16-token block a warp issues 2 x d / 16 MMAs, 3 d / 8
 // integer and half-precision instructions that widen the codes, and 8 exponentials per lane (2 per score): a quarter
 // of what an SM could do in the time that the block takes to arrive.  Measured at d = 128, 64 heads on 8: 128K tokens
-// 51.4 us (5.2 TB/s over all; the loop itself takes 38 us, 7.1 TB/s, and the rest is the start, 2 us, the merge of the
-// warps, 2.5, and the joining of cut units, 5); 16 sequences of 4K to 64K, 193 us (5.9 TB/s); 1K tokens 9.2 us, all of
-// it latency.  d = 256, 32K tokens, 32 heads on 16: 48 us.
+// 51.8 us (5.2 TB/s over all; the loop itself takes 38 us, 7.1 TB/s, and the rest is the start, 2 us, the merge of the
+// warps, 2.5, and the joining of cut units, 5); 16 sequences of 4K to 64K, 195 us (5.9 TB/s); 1K tokens 9.1 us, all of
+// it latency.  d = 256, 32K tokens, 32 heads on 16: 49 us.
 //
 // Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
 // block i of N takes the positions [i L / N, (i + 1) L / N) of the L in all, whatever the lengths: ragged batches load
 // every SM alike, one short sequence still spreads.  (Batches of short sequences are not cut: see by_block and by_warp.)
 // With more units than thread blocks each unit also has `lead` positions before its blocks, for what its query, merge and
 // output cost; without them a share of many short units took three times as long as one of a few long ones (45
-// sequences of 320 to 5130 tokens, 16 KV heads: 199 us).
+// sequences of 320 to 5130 tokens, 128 heads on 16: 199 us instead of 100).
 // A unit that lies in one thread block is finished there; the parts of a cut one go to the workspace, and the last to
 // arrive (a counter per unit) joins them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
 // registers), each with a ring of three to six stages of one 16-token block, and one warp that fills the rings, one bulk
