@@ -306,15 +306,18 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   const bool by_warp = D < 512 && a.lead > 0 && !by_block &&  // (d = 512: the warps share the query's fragments)
                        most - a.lead <= L / N / 7 + 16;
 
-  // Few units: shares that end where units do save the thread blocks in between a second query and merge (5 us).  Each
+  // Few units: shares that end where units do save the thread blocks in between a second query and merge (6 us).  Each
   // unit of a sequence gets floor(its part of the line x N) of them; that lengthens the longest share, by 0.09 us per
-  // block, and is done up to 32 blocks (128K tokens, 8 KV heads: 144 shares instead of 148).
+  // block, and is done up to 66 blocks (10 sequences of 207 to 3321 tokens, one KV head: 14.4 us, not so 20).  No unit
+  // gets more than half the root of its blocks: one thread block joins the parts, at 0.15 to 0.6 us each (30 000 tokens,
+  // one KV head of 256: 67 parts 55 us, 16 parts 29).
   int cuts = 0, cuts_upto = 0;  // shares of each unit of the lane's sequence, and of those up to it
   bool snapped = false;
   if (few && !by_block && a.lead == 0 && U <= N) {
     const int n = lane < a.c.B ? own_n : 0;
     const float part = static_cast<float>(n) / static_cast<float>(L / a.units);  // (1 exactly for a single sequence)
-    cuts = min(n, max(1, static_cast<int>(part * static_cast<float>(N / a.units))));  // (none of them is empty)
+    const int even = max(1, static_cast<int>(part * static_cast<float>(N / a.units)));
+    cuts = min(min(n, even), max(1, static_cast<int>(0.5f * sqrtf(static_cast<float>(n)))));  // (none of them is empty)
     cuts_upto = cuts;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       if (lane >= o) cuts_upto += y;
     }
     const bool fits = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units <= N;
-    snapped = fits && __all_sync(0xffffffffu, n == 0 || (n - 1) / cuts + 1 <= L / N + 32);
+    snapped = fits && __all_sync(0xffffffffu, n == 0 || (n - 1) / even + 1 <= L / N + 66);
     if (snapped) N = __shfl_sync(0xffffffffu, cuts_upto, 31) * a.units;
   }
 
@@ -747,7 +750,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         // independent of each other, and the first CH rows are on their way while the weights are made (a running maximum
         // would wait for a round trip to L2 per part: 17 us of a 64 us launch).
         // Few rows and many parts: `teams` of threads share the parts of a row.
-        constexpr int CH = 9;
+        constexpr int CH = D <= 128 ? 9 : 16;
         float* const wts = merge;  // [2][8][np]
         float4 rows[CH];
         const int items = heads * (D / 4);
