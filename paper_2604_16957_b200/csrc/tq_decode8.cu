@@ -4,11 +4,13 @@
 //   Scores:  alpha q . k^ = (alpha a_K / 127) sum_c q_c code_c -- the range of a block is one number per KV head and 16
 //            tokens, so it multiplies the fp32 accumulator and the tensor cores see exact integer codes in fp16.
 //   Output:  o = sum_j 2^(s_j) a_V(j) code_j / (127 sum_j 2^(s_j)).  The weight that enters the second MMA in fp16 is
-//            w_j = 2^(s_j + log2 a_V(j) - M'), with M' the running maximum of the whole exponent: a block whose values
-//            are small is weighed against the largest contribution, not against the largest score, so its rounding
-//            (2^-11 relative) never exceeds what it contributes.  The denominator has a maximum M of its own, and the
-//            factor 2^(M' - M) joins them at the end.
-//   Both maxima are raised only when a score exceeds them by more than 2^8 (weights stay below 256).
+//            w_j = 2^(s_j + log2 a_V(j) - M' + 7), with M' the running maximum of the whole exponent: a block whose
+//            values are small is weighed against the largest contribution, not against the largest score.  The
+//            denominator has a maximum M of its own, kept in fp32, and the factor 2^(M' - M) / 2^7 joins them at the end.
+//   Both maxima are raised only when a score exceeds them by more than 2^8: weights stay below 2^15, inside fp16.  The
+//   7 puts the subnormals of fp16 as low as that allows: a weight is rounded by 2^-11 of itself down to 2^-21 of the
+//   largest contribution, below that by 2^-32 of it (at most; 2^-25 without the 7, where a token of 2^-22.5 was off by
+//   6 %, and a long tail of such tokens with it).
 //
 // What bounds it: HBM.  2 d + 0.5 bytes per token and KV head; per 16-token block a warp issues 2 x d / 16 MMAs, 3 d / 8
 // integer and half-precision instructions that widen the codes, and 8 exponentials per lane (2 per score): a quarter
@@ -40,6 +42,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1.0e30f;
 constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running maxima
+constexpr float kRaise = 7.0f;  // log2 of the weight in fp16 that a contribution as large as M' has
+constexpr float kLower = 1.0f / 128.0f;  // undoes it, in the accumulators: 2^(M' - M) may be the smallest normal number
 constexpr int kMaxGrid = 160;   // thread blocks of a launch (one per SM)
 
 template <int D>
@@ -593,7 +597,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
       l0 += ex2(s0 - M0) + ex2(s2 - M0);
       l1 += ex2(s1 - M1) + ex2(s3 - M1);
-      const float w0 = lg - P0, w1 = lg - P1;
+      const float w0 = lg - P0 + kRaise, w1 = lg - P1 + kRaise;
       const uint32_t v0 = transpose8x8(pack2<TQ_FP16>(ex2(s0 + w0), ex2(s1 + w1)));  // tokens 2 t4, + 1 of query gid
       const uint32_t v1 = transpose8x8(pack2<TQ_FP16>(ex2(s2 + w0), ex2(s3 + w1)));  // tokens 2 t4 + 8, + 9
 #pragma unroll
@@ -628,12 +632,12 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
 #pragma unroll
       for (int m = 0; m < 2 * KK; ++m) {
         if (2 * t4 < heads) {
-          store_out<OT>(a.out, at + 16 * m, o[m][0] * f0);
-          store_out<OT>(a.out, at + 16 * m + 8, o[m][2] * f0);
+          store_out<OT>(a.out, at + 16 * m, o[m][0] * kLower * f0);
+          store_out<OT>(a.out, at + 16 * m + 8, o[m][2] * kLower * f0);
         }
         if (2 * t4 + 1 < heads) {
-          store_out<OT>(a.out, at + D + 16 * m, o[m][1] * f1);
-          store_out<OT>(a.out, at + D + 16 * m + 8, o[m][3] * f1);
+          store_out<OT>(a.out, at + D + 16 * m, o[m][1] * kLower * f1);
+          store_out<OT>(a.out, at + D + 16 * m + 8, o[m][3] * kLower * f1);
         }
       }
       continue;
@@ -684,7 +688,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     const long long unit = static_cast<long long>(use.b) * a.units + use.u;
     const int stride = part_floats(D, a.rows);
     float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + slot) * stride;
-    const float c0 = ex2(P0 - sums[8 + 2 * t4]), c1 = ex2(P1 - sums[8 + 2 * t4 + 1]);
+    const float c0 = ex2(P0 - sums[8 + 2 * t4]) * kLower, c1 = ex2(P1 - sums[8 + 2 * t4 + 1]) * kLower;
     auto emit = [&](int q, int ch, float x, float y) {
       x *= sums[24 + q];
       y *= sums[24 + q];

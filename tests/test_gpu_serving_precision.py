@@ -1,0 +1,88 @@
+"""Attention of the serving operators where its numbers are hard: many tokens of a tiny weight each beside a dominant one,
+and scores far from zero."""
+import numpy as np
+import pytest
+
+import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    from paper_2604_16957_b200 import tq
+    assert torch.cuda.is_available()
+    return tq, torch
+
+
+def _dominant_and_tail(n, H, d, offset):
+    """K and V of n tokens (float64 [n][H][d]): the first of every 16 scores 0 with q = e_0 and has the value e_0; the others
+    score `offset` (in units of log 2 / alpha) and have the value 1 in every other channel."""
+    k, v = np.zeros((n, H, d)), np.zeros((n, H, d))
+    tail = np.arange(n) % 16 != 0
+    k[tail, :, 0] = offset
+    v[tail, :, 1:] = 1.0
+    v[~tail, :, 0] = 1.0
+    return k, v
+
+
+# one unit in a thread block; cut units; several whole units per warp; many units on one line; wide heads
+@pytest.mark.parametrize("lens,H_q,H_kv,d,kind", [
+    ([500], 8, 2, 64, "fp16"), ([20000], 8, 1, 128, "fp16"), ([400] * 40, 16, 8, 64, "bf16"), ([2500] * 40, 8, 8, 64, "fp16"),
+    ([3000], 4, 2, 256, "bf16"), ([300], 4, 1, 512, "fp16")])
+@pytest.mark.parametrize("offset", [-22.5, -18.25])
+def test_decode_keeps_a_tail_of_small_weights(gpu, lens, H_q, H_kv, d, kind, offset):
+    """The tail's weights are 2^-22.5 of the largest contribution each.  They enter the matrix product in 16 bits: a weight may be
+    off by 2^-11 of itself, or by half a step of the subnormals, which lie 2^7 below the place that the largest contribution has:
+    2^-25 / 2^7 = 2^-32 of it."""
+    tq, torch = gpu
+    t = {"fp16": torch.float16, "bf16": torch.bfloat16}[kind]
+    B, n = len(lens), max(lens)
+    cap = -(-n // 16) * 16
+    k, v = _dominant_and_tail(n, H_kv, d, offset)
+    cache = tq.KV8Cache(B, H_kv, cap, d)
+    rows = torch.cat([torch.arange(x) + b * cap for b, x in enumerate(lens)]).cuda()
+    kk, vv = (torch.cat([torch.from_numpy(y[:x]) for x in lens]).to(t).cuda() for y in (k, v))
+    tq.tq_kv8_append(cache, kk, vv, rows)
+    cache.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    model = R.Cache8(cap // 16, H_kv, d)
+    model.append(k, v, np.arange(n))
+    km, vm = model.values(np.arange(n))
+    q = torch.zeros((B, H_q, d), dtype=t, device="cuda")
+    q[..., 0] = 1.0
+    out = torch.empty((B, H_q, d), device="cuda")
+    alpha = float(np.log(2.0))
+    tq.tq_sdpa_int8_decode(cache, q, alpha, 0, 0, tq.alloc_int8_workspace(B, H_kv, H_q, d), out)
+    ref, weighed, p, mag = R.attention(q[0, :1].double().cpu(), km[:, 0], vm[:, 0], alpha)
+    tol = R.bound(ref, weighed, p, mag, n, d, 2.0 ** -11, 1.0, 0.0, subnormal=2.0 ** -32)
+    got = out.double().cpu()
+    assert torch.all((got - ref).abs() <= tol), float(((got - ref).abs() / tol).max())
+    assert float((tol / ref)[0, 1]) < 0.003     # (the bound says something)
+
+
+@pytest.mark.parametrize("B,n", [(1, 3000), (160, 50)])   # a cut unit; whole units by warp
+@pytest.mark.parametrize("size", [2.0 ** -120])
+def test_decode_of_tiny_values(gpu, B, n, size):
+    """bf16 values near the smallest normal numbers: what undoes the scaling of the weights does not make zeros of them."""
+    tq, torch = gpu
+    d, H = 64, 4
+    rng = np.random.default_rng(4)
+    cap = -(-n // 16) * 16
+    cache = tq.KV8Cache(B, H, cap, d)
+    k = torch.from_numpy(rng.standard_normal((n, H, d))).bfloat16()
+    v = (torch.from_numpy(rng.uniform(0.25, 1.0, (n, H, d))) * size).bfloat16()
+    tq.tq_kv8_append(cache, k.repeat(B, 1, 1).cuda(), v.repeat(B, 1, 1).cuda(),
+                     torch.cat([torch.arange(n) + b * cap for b in range(B)]).cuda())
+    cache.seq_lens.fill_(n)
+    model = R.Cache8(cap // 16, H, d)
+    model.append(k.double().numpy(), v.double().numpy(), np.arange(n))
+    km, vm = model.values(np.arange(n))
+    q = torch.from_numpy(rng.standard_normal((1, H, d))).bfloat16()
+    out = torch.empty((B, H, d), device="cuda")
+    tq.tq_sdpa_int8_decode(cache, q.repeat(B, 1, 1).cuda(), 0.125, 0, 0, tq.alloc_int8_workspace(B, H, H, d), out)
+    for h in range(H):
+        ref, weighed, p, mag = R.attention(q[0, h:h + 1].double(), km[:, h], vm[:, h], 0.125)
+        # 127 l products of 2^-120 / 127 / l: the last factor may be subnormal, 2^-120 / 127 / 3000 = 2^-139 in steps of 2^-149
+        tol = R.bound(ref, weighed, p, mag, n, d, 2.0 ** -11, size, 0.0, subnormal=2.0 ** -32) + ref.abs() * 2.0 ** -10
+        assert torch.all((out[:, h].double().cpu() - ref).abs() <= tol)
