@@ -795,13 +795,14 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         join_warps();
         auto sum_of = [&](int i, bool first) {
           const int q = i / (D / 4);
+          const float inv = sums[q];  // in every weight, not behind the sum: rows may be near the largest number
           float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           for (int p0 = p_first; p0 < p_end; p0 += CH) {
             if (!first || p0 > p_first) fetch(i, p0, p_end);
 #pragma unroll
             for (int p = 0; p < CH; ++p)
               if (p0 + p < p_end) {
-                const float w = wts[q * np + p0 + p];
+                const float w = wts[q * np + p0 + p] * inv;
                 x.x += w * rows[p].x;
                 x.y += w * rows[p].y;
                 x.z += w * rows[p].z;
@@ -813,8 +814,8 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         auto put = [&](int i, const float4& x) {
           const int q = i / (D / 4), ch = 4 * (i - q * (D / 4));
           const long long at = (static_cast<long long>(use.b) * a.H_q + head0 + q) * D + ch;
-          store_out2<OT>(a.out, at, x.x * sums[q], x.y * sums[q]);
-          store_out2<OT>(a.out, at + 2, x.z * sums[q], x.w * sums[q]);
+          store_out2<OT>(a.out, at, x.x, x.y);
+          store_out2<OT>(a.out, at + 2, x.z, x.w);
         };
         if (teams == 1) {
           for (int i = tid; i < items; i += C::THREADS) put(i, sum_of(i, i == tid));

@@ -86,3 +86,19 @@ def test_decode_of_tiny_values(gpu, B, n, size):
         # 127 l products of 2^-120 / 127 / l: the last factor may be subnormal, 2^-120 / 127 / 3000 = 2^-139 in steps of 2^-149
         tol = R.bound(ref, weighed, p, mag, n, d, 2.0 ** -11, size, 0.0, subnormal=2.0 ** -32) + ref.abs() * 2.0 ** -10
         assert torch.all((out[:, h].double().cpu() - ref).abs() <= tol)
+
+
+def test_decode_joins_huge_values(gpu):
+    """Parts of a cut unit whose values are near the largest number: their weighted sum does not overflow on its way."""
+    tq, torch = gpu
+    d, n = 64, 6000
+    cache = tq.KV8Cache(1, 1, n, d)
+    k = torch.randn((n, 1, d)).bfloat16()
+    v = torch.full((n, 1, d), 2.0 ** 127, dtype=torch.bfloat16)
+    v[:, :, 1::2] *= -1
+    tq.tq_kv8_append(cache, k.cuda(), v.cuda(), torch.arange(n, device="cuda"))
+    cache.seq_lens.fill_(n)
+    out = torch.empty((1, 3, d), device="cuda")
+    tq.tq_sdpa_int8_decode(cache, torch.randn((1, 3, d), device="cuda").bfloat16(), 0.125, 0, 0, tq.alloc_int8_workspace(1, 1, 3, d), out)
+    # weights of equal values: their rounding in 16 bits is all that is left of the error, 2^-11 of the value
+    assert torch.all((out.double().cpu() / v[:1].double() - 1).abs() <= 2.0 ** -11 + 2.0 ** -16)
