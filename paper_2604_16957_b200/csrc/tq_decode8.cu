@@ -6,7 +6,9 @@
 //   Output:  o = sum_j 2^(s_j) a_V(j) code_j / (127 sum_j 2^(s_j)).  The weight that enters the second MMA in fp16 is
 //            w_j = 2^(s_j + log2 a_V(j) - M' + 7), with M' the running maximum of the whole exponent: a block whose
 //            values are small is weighed against the largest contribution, not against the largest score.  The
-//            denominator has a maximum M of its own, kept in fp32, and the factor 2^(M' - M) / 2^7 joins them at the end.
+//            denominator has a maximum M of its own, kept in fp32, and the factor 2^(M' - M) / 2^7 joins them at the end.  M' is kept
+//            as its distance R = M' - M, so that log2 a_V is never added to a score: next to one of 10^6 it would lose
+//            its digits, and the values their scale.
 //   Both maxima are raised only when a score exceeds them by more than 2^8: weights stay below 2^15, inside fp16.  The
 //   7 puts the subnormals of fp16 as low as that allows: a weight is rounded by 2^-11 of itself down to 2^-21 of the
 //   largest contribution, below that by 2^-32 of it (at most; 2^-25 without the 7, where a token of 2^-22.5 was off by
@@ -40,7 +42,7 @@ namespace tq {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoMax = -1.0e30f;
+constexpr float kNoMax = -3.0e38f;  // below every score of fp32 (bf16 inputs reach its whole range), and finite
 constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running maxima
 constexpr float kRaise = 7.0f;  // log2 of the weight in fp16 that a contribution as large as M' has
 constexpr float kLower = 1.0f / 128.0f;  // undoes it, in the accumulators: 2^(M' - M) may be the smallest normal number
@@ -61,7 +63,7 @@ struct Cfg {
   // the last to arrive keeps the weights of a unit's parts there, and the teams' sums behind them
   static constexpr int WTS = 2 * 8 * kMaxGrid * 4 + 16 * THREADS;
   static constexpr int MERGE = NW * MQ * ROW * 4 > WTS ? NW * MQ * ROW * 4 : WTS;
-  static constexpr int STATS = RING + MERGE;             // [NW][8] x {M, M', l} and the factors of them
+  static constexpr int STATS = RING + MERGE;             // [NW][8] x {M, R, l} and the factors of them
   static constexpr int BARS = STATS + NW * 8 * 3 * 4 + 8 * 4 * 4;
   static constexpr int QS = BARS + 2 * NW * NST * 8;         // d = 512: the query's B fragments, 8 bytes per lane and step
   static constexpr int QBYTES = D == 512 ? (D / 16) * 32 * 8 : 0;
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   const int gid = lane >> 2, t4 = lane & 3;
   float* const merge = reinterpret_cast<float*>(smem + C::RING);
   float* const stats = reinterpret_cast<float*>(smem + C::STATS);  // [3][NW][8]
-  float* const sums = stats + 3 * C::NW * 8;                       // [8] x {M, M', l, factor}
+  float* const sums = stats + 3 * C::NW * 8;                       // [8] x {M, R, l, factor}
   // warp w's ring of NST stages, and the barriers "stage s is full" and "stage s may be filled" behind all rings
   uint32_t base;
   asm("{ .reg .u64 p; cvta.to.shared.u64 p, %1; cvt.u32.u64 %0, p; }\n" : "=r"(base) : "l"(smem));
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     float o[2 * KK][4];  // channels 16 m + gid (+ 8), queries 2 t4 (+ 1)
 #pragma unroll
     for (int m = 0; m < 2 * KK; ++m) o[m][0] = o[m][1] = o[m][2] = o[m][3] = 0.0f;
-    float M0 = kNoMax, M1 = kNoMax, P0 = kNoMax, P1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
+    float M0 = kNoMax, M1 = kNoMax, R0 = kNoMax, R1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
 
     for (int j = use.j0 + (by_warp ? 0 : warp); j < use.j1; j += by_warp ? 1 : C::NW) {
       if (!dead && !wait_stage(full(warp, stage), phase)) {
@@ -572,21 +574,22 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       float lg;  // log2 of the value range; -inf for a block of zeros
       asm("lg2.approx.f32 %0, %1;\n" : "=f"(lg) : "f"(range.y));
       const float b0 = fmaxf(s0, s2), b1 = fmaxf(s1, s3);
-      if (__any_sync(0xffffffffu, b0 > M0 + kSlack || b1 > M1 + kSlack || b0 + lg > P0 + kSlack || b1 + lg > P1 + kSlack)) {
+      if (__any_sync(0xffffffffu, b0 > M0 + kSlack || b1 > M1 + kSlack || b0 - M0 + lg > R0 + kSlack || b1 - M1 + lg > R1 + kSlack)) {
         float m0 = b0, m1 = b1;
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) {
           m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
           m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
         }
-        const float n0 = fmaxf(M0, m0), n1 = fmaxf(M1, m1), p0 = fmaxf(P0, m0 + lg), p1 = fmaxf(P1, m1 + lg);
-        l0 *= ex2(M0 - n0);
-        l1 *= ex2(M1 - n1);
-        const float c0 = ex2(P0 - p0), c1 = ex2(P1 - p1);
+        const float n0 = fmaxf(M0, m0), n1 = fmaxf(M1, m1), d0 = M0 - n0, d1 = M1 - n1;
+        const float r0 = fmaxf(kNoMax, fmaxf(R0 + d0, m0 - n0 + lg)), r1 = fmaxf(kNoMax, fmaxf(R1 + d1, m1 - n1 + lg));
+        l0 *= ex2(d0);
+        l1 *= ex2(d1);
+        const float c0 = ex2(d0 + R0 - r0), c1 = ex2(d1 + R1 - r1);
         M0 = n0;
         M1 = n1;
-        P0 = p0;
-        P1 = p1;
+        R0 = r0;
+        R1 = r1;
 #pragma unroll
         for (int m = 0; m < 2 * KK; ++m) {
           o[m][0] *= c0;
@@ -595,9 +598,13 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
           o[m][3] *= c1;
         }
       }
-      l0 += ex2(s0 - M0) + ex2(s2 - M0);
-      l1 += ex2(s1 - M1) + ex2(s3 - M1);
-      const float w0 = lg - P0 + kRaise, w1 = lg - P1 + kRaise;
+      s0 -= M0;
+      s1 -= M1;
+      s2 -= M0;
+      s3 -= M1;
+      l0 += ex2(s0) + ex2(s2);
+      l1 += ex2(s1) + ex2(s3);
+      const float w0 = lg - R0 + kRaise, w1 = lg - R1 + kRaise;
       const uint32_t v0 = transpose8x8(pack2<TQ_FP16>(ex2(s0 + w0), ex2(s1 + w1)));  // tokens 2 t4, + 1 of query gid
       const uint32_t v1 = transpose8x8(pack2<TQ_FP16>(ex2(s2 + w0), ex2(s3 + w1)));  // tokens 2 t4 + 8, + 9
 #pragma unroll
@@ -627,7 +634,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
     if (by_warp) {
       // the warp's own unit: straight out of the accumulators
-      const float f0 = ex2(P0 - M0) / (127.0f * l0), f1 = ex2(P1 - M1) / (127.0f * l1);
+      const float f0 = ex2(R0) / (127.0f * l0), f1 = ex2(R1) / (127.0f * l1);
       const long long at = (static_cast<long long>(use.b) * a.H_q + head0 + 2 * t4) * D + gid;
 #pragma unroll
       for (int m = 0; m < 2 * KK; ++m) {
@@ -646,8 +653,8 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       float* st = stats + warp * 8 + 2 * t4;
       st[0] = M0;
       st[1] = M1;
-      st[C::NW * 8] = P0;
-      st[C::NW * 8 + 1] = P1;
+      st[C::NW * 8] = R0;
+      st[C::NW * 8 + 1] = R1;
       st[2 * C::NW * 8] = l0;
       st[2 * C::NW * 8 + 1] = l1;
     }
@@ -667,28 +674,29 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     }
     for (int q = warp; q < 8; q += C::NW) {
       const bool has = lane < C::NW;
-      const float wm = has ? stats[lane * 8 + q] : kNoMax, wp = has ? stats[(C::NW + lane) * 8 + q] : kNoMax;
-      float m = wm, p = wp;
+      const float wm = has ? stats[lane * 8 + q] : kNoMax;
+      float m = wm, r = has ? stats[(C::NW + lane) * 8 + q] : kNoMax;
 #pragma unroll
       for (int x = 1; x < 16; x <<= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        p = fmaxf(p, __shfl_xor_sync(0xffffffffu, p, x));
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, x), r2 = __shfl_xor_sync(0xffffffffu, r, x), n = fmaxf(m, m2);
+        r = fmaxf(r + (m - n), r2 + (m2 - n));
+        m = n;
       }
       float l = has ? stats[(2 * C::NW + lane) * 8 + q] * ex2(wm - m) : 0.0f;
 #pragma unroll
       for (int x = 1; x < 16; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
       if (lane == 0) {
         sums[q] = m;
-        sums[8 + q] = p;
+        sums[8 + q] = r;
         sums[16 + q] = l;
-        sums[24 + q] = ex2(p - m) / (127.0f * l);
+        sums[24 + q] = ex2(r) / (127.0f * l);
       }
     }
     join_warps();
     const long long unit = static_cast<long long>(use.b) * a.units + use.u;
     const int stride = part_floats(D, a.rows);
     float* const mine = a.parts + (a.compact ? blockIdx.x + unit : 2LL * blockIdx.x + slot) * stride;
-    const float c0 = ex2(P0 - sums[8 + 2 * t4]) * kLower, c1 = ex2(P1 - sums[8 + 2 * t4 + 1]) * kLower;
+    const float c0 = ex2(M0 - sums[2 * t4] + R0 - sums[8 + 2 * t4]) * kLower, c1 = ex2(M1 - sums[2 * t4 + 1] + R1 - sums[8 + 2 * t4 + 1]) * kLower;
     auto emit = [&](int q, int ch, float x, float y) {
       x *= sums[24 + q];
       y *= sums[24 + q];

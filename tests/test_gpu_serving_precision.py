@@ -102,3 +102,24 @@ def test_decode_joins_huge_values(gpu):
     tq.tq_sdpa_int8_decode(cache, torch.randn((1, 3, d), device="cuda").bfloat16(), 0.125, 0, 0, tq.alloc_int8_workspace(1, 1, 3, d), out)
     # weights of equal values: their rounding in 16 bits is all that is left of the error, 2^-11 of the value
     assert torch.all((out.double().cpu() / v[:1].double() - 1).abs() <= 2.0 ** -11 + 2.0 ** -16)
+
+
+@pytest.mark.parametrize("B,n", [(1, 1), (1, 40), (1, 5000), (160, 50)])
+@pytest.mark.parametrize("size", [-2.0 ** 52, -2.0 ** -46, 2.0 ** -46, 2.0 ** 52])
+def test_decode_of_scores_far_from_zero(gpu, B, n, size):
+    """Every score near 2^18 or 2^118, of either sign: equal keys weigh their values equally, whatever the score is."""
+    tq, torch = gpu
+    d, H = 64, 4
+    cap = -(-n // 16) * 16
+    cache = tq.KV8Cache(B, H, cap, d)
+    k = torch.full((B * n, H, d), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
+    v = (torch.rand((n, H, d)) + 0.5).bfloat16()
+    tq.tq_kv8_append(cache, k, v.repeat(B, 1, 1).cuda(), torch.cat([torch.arange(n) + b * cap for b in range(B)]).cuda())
+    cache.seq_lens.fill_(n)
+    model = R.Cache8(cap // 16, H, d)
+    model.append(np.zeros((n, H, d)), v.double().numpy(), np.arange(n))
+    q = torch.full((B, H, d), size, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty((B, H, d), device="cuda")
+    tq.tq_sdpa_int8_decode(cache, q, 1.0, 0, 0, tq.alloc_int8_workspace(B, H, H, d), out)
+    ref = torch.as_tensor(model.values(np.arange(n))[1].mean(0))
+    assert torch.all((out.double().cpu() - ref).abs() <= 2.0 ** -11 * 1.5 + 2.0 ** -15)   # weights in 16 bits, values up to 1.5
