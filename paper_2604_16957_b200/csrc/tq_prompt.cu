@@ -4,11 +4,14 @@
 // token, so K and V are read once per KV head whatever G is.  A thread block works on NQ tiles over a common stream of
 // K / V tiles of BN keys:
 //     S = Q K^T   (tcgen05.mma, both operands in shared memory, S in TMEM)
-//     P = 2^(c S - c m), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
+//     P = 2^(c S - c m + e), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
 // c = alpha log2 e > 0 (for a negative alpha the MMA negates Q).  m is raised only when a score exceeds it by more than
-// 2^12; then the thread rescales its row of O in TMEM.  S has two buffers per tile: the scores of the next keys are made
-// while the softmax of these runs.  That takes key tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at
+// 2^12 (bf16) or 2^8 (fp16); then the thread rescales its row of O in TMEM.  The row sums are of unrounded weights, in
+// fp32.  A bf16 weight is rounded by 2^-8 of itself, e = 0.  In fp16 weights stay below 2^15 with e = 7, which puts its
+// subnormals as low as that allows: rounded by 2^-11 of itself, or by 2^-32 of the largest weight (with 2^12 and e = 0 by
+// 2^-25: a token of weight 2^-22.5 was off by 6 %).  The sooner raising costs fp16 1 % (8K) to 5 % (d = 256, window 1024).
+// S has two buffers per tile: the scores of the next keys are made while the softmax of these runs.  That takes key tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at
 // d = 128), for which an MMA of 128 x 64 x 16 reads its operands in 48 cycles instead of the 32 that it computes; with
 // tiles of 128 keys and one buffer the MMAs are faster (64 cycles for twice the work), but outputs, scores and softmax of
 // a tile follow one another: 1.09 ms for the 8K prompt.  At d = 512 the accumulator of a row does not fit TMEM: a thread
@@ -45,7 +48,12 @@ namespace tq {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 12.0f;  // log2 units a score may exceed the running maximum: weights stay below 2^12
+// Log2 units that a score may exceed the running maximum, and log2 of the weight of a score as large as it (see the top).
+template <int DT>
+struct Weights {
+  static constexpr float kSlack = DT == TQ_BF16 ? 12.0f : 8.0f;
+  static constexpr float kRaise = DT == TQ_BF16 ? 0.0f : 7.0f;
+};
 
 template <int D, int TILES>
 struct Cfg {
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         }
         // a score that is no number makes the whole row none, through its sum
         if (mx != mx) l = mx;
-        const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > kSlack;
+        const bool raise = m == -INFINITY ? mx > -INFINITY : (mx - m) * c > Weights<DT>::kSlack;
         float scale = 1.0f;
         if (raise) {
           scale = m == -INFINITY ? 0.0f : ex2((m - mx) * c);
@@ -322,15 +330,15 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
             tmem_st32(o_addr + x + 32, o + 32);
           }
         }
-        const float mc = m == -INFINITY ? 0.0f : m * c;
+        const float shift = m == -INFINITY ? 0.0f : __fmaf_rn(-m, c, Weights<DT>::kRaise);
         uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
-        const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
+        const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
 #pragma unroll
         for (int x = 0; x < C::BN; x += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 2) {
-            const float2 z = unpair(fma2(pair(s[x + y], s[x + y + 1]), c2, mc2));
+            const float2 z = unpair(fma2(pair(s[x + y], s[x + y + 1]), c2, shift2));
             const float e0 = ex2(z.x), e1 = ex2(z.y);
             if (y & 2) sum1 = add2(sum1, pair(e0, e1));
             else sum0 = add2(sum0, pair(e0, e1));

@@ -123,3 +123,28 @@ def test_decode_of_scores_far_from_zero(gpu, B, n, size):
     tq.tq_sdpa_int8_decode(cache, q, 1.0, 0, 0, tq.alloc_int8_workspace(B, H, H, d), out)
     ref = torch.as_tensor(model.values(np.arange(n))[1].mean(0))
     assert torch.all((out.double().cpu() - ref).abs() <= 2.0 ** -11 * 1.5 + 2.0 ** -15)   # weights in 16 bits, values up to 1.5
+
+
+@pytest.mark.parametrize("padded", [0, 200])   # one tile per thread block, and two
+@pytest.mark.parametrize("d", [64, 128, 256, 512])
+@pytest.mark.parametrize("offset", [-22.5, -18.25])
+def test_prompt_keeps_a_tail_of_small_weights(gpu, padded, d, offset):
+    """As for decode: fp16 weights are off by 2^-11 of themselves or by 2^-32 of the largest one."""
+    tq, torch = gpu
+    n, H_q, H = 300, 4, 2
+    k, v = _dominant_and_tail(n, H, d, offset)
+    k, v = (torch.from_numpy(x).half().cuda() for x in (k, v))
+    q = torch.zeros((n, H_q, d), dtype=torch.float16, device="cuda")
+    q[..., 0] = 1.0
+    at = torch.tensor([0, n] + [n] * padded, dtype=torch.int32, device="cuda")
+    out = torch.empty((n, H_q, d), device="cuda")
+    alpha = float(np.log(2.0))
+    tq.tq_sdpa_prompt(q, k, v, at, at, alpha, out)
+    seen = torch.arange(n)[None, :] <= torch.arange(n)[:, None]
+    ref, weighed, p, mag = R.attention(q[:, 0].double().cpu(), k[:, 0].double().cpu(), v[:, 0].double().cpu(), alpha, seen)
+    tol = R.bound(ref, weighed, p, mag, n, d, 2.0 ** -11, 1.0, 0.0, subnormal=2.0 ** -32)
+    got = out.double().cpu()
+    for h in range(H_q):
+        assert torch.all((got[:, h] - ref).abs() <= tol), float(((got[:, h] - ref).abs() / tol).max())
+    # the bound says something (in the last row: it counts all n tokens as seen, row i sees i + 1)
+    assert float((tol / ref)[-1, 1]) < 0.003
