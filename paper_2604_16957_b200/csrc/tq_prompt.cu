@@ -7,15 +7,16 @@
 //     P = 2^(c S - c m + e), rounded to 16 bits, back into TMEM over S   (a thread per row, online softmax)
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
 // c = alpha log2 e > 0 (for a negative alpha the MMA negates Q).  m is raised only when a score exceeds it by more than
-// 2^12 (bf16) or 2^8 (fp16); then the thread rescales its row of O in TMEM.  The row sums are of unrounded weights, in
+// 2^12 (bf16) or 2^7.9 (fp16); then the thread rescales its row of O in TMEM.  The row sums are of unrounded weights, in
 // fp32.  A bf16 weight is rounded by 2^-8 of itself, e = 0.  In fp16 weights stay below 2^15 with e = 7, which puts its
 // subnormals as low as that allows: rounded by 2^-11 of itself, or by 2^-32 of the largest weight (with 2^12 and e = 0 by
 // 2^-25: a token of weight 2^-22.5 was off by 6 %).  The sooner raising costs fp16 1 % (8K) to 5 % (d = 256, window 1024).
-// S has two buffers per tile: the scores of the next keys are made while the softmax of these runs.  That takes key tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at
-// d = 128), for which an MMA of 128 x 64 x 16 reads its operands in 48 cycles instead of the 32 that it computes; with
-// tiles of 128 keys and one buffer the MMAs are faster (64 cycles for twice the work), but outputs, scores and softmax of
-// a tile follow one another: 1.09 ms for the 8K prompt.  At d = 512 the accumulator of a row does not fit TMEM: a thread
-// block computes 256 of the 512 output channels, and S is computed twice.
+// S has two buffers per tile: the scores of the next keys are made while the softmax of these runs.  That takes key
+// tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at d = 128), for which an MMA of 128 x 64 x 16
+// reads its operands in 48 cycles instead of the 32 that it computes; with tiles of 128 keys and one buffer the MMAs are
+// faster (64 cycles for twice the work), but outputs, scores and softmax of a tile follow one another: 1.09 ms for the
+// 8K prompt.  At d = 512 the accumulator of a row does not fit TMEM: a thread block computes 256 of the 512 output
+// channels, and S is computed twice.
 //
 // NQ is 2 at d <= 128 and 1 above (TMEM).  A launch of so few tiles that every one finds an SM of its own takes one tile
 // per thread block at any d: a step of 64 keys is then 0.6 to 0.8 us instead of 0.9 (16 sequences of up to 300 tokens,
@@ -49,10 +50,15 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 // Log2 units that a score may exceed the running maximum, and log2 of the weight of a score as large as it (see the top).
+// From kFar on, the rounding of c m (2^-25 of it, the same for all weights of the row) could take weights out of their
+// type.  There the power of two below c stands in its place, whose product with m is exact: the scores themselves are
+// then 0.5 (fp16) or 64 (bf16) log2 units apart, so what decides is which of them are equal to the largest.  (There the
+// sum of -c m and kRaise is rounded, and the 7 of fp16 becomes 8 at most: with 7.9 weights stay below 2^16.)
 template <int DT>
 struct Weights {
-  static constexpr float kSlack = DT == TQ_BF16 ? 12.0f : 8.0f;
+  static constexpr float kSlack = DT == TQ_BF16 ? 12.0f : 7.9f;
   static constexpr float kRaise = DT == TQ_BF16 ? 0.0f : 7.0f;
+  static constexpr float kFar = DT == TQ_BF16 ? 1073741824.0f : 8388608.0f;  // 2^30, 2^23
 };
 
 template <int D, int TILES>
@@ -330,9 +336,10 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
             tmem_st32(o_addr + x + 32, o + 32);
           }
         }
-        const float shift = m == -INFINITY ? 0.0f : __fmaf_rn(-m, c, Weights<DT>::kRaise);
+        const float cm = fabsf(m) * c > Weights<DT>::kFar ? __uint_as_float(__float_as_uint(c) & 0xff800000u) : c;
+        const float shift = m == -INFINITY ? 0.0f : __fmaf_rn(-m, cm, Weights<DT>::kRaise);
         uint64_t sum0 = pair(l, 0.0f), sum1 = 0;
-        const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
+        const uint64_t c2 = pair(cm, cm), shift2 = pair(shift, shift);
 #pragma unroll
         for (int x = 0; x < C::BN; x += 32) {
           uint32_t p[16];

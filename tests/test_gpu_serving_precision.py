@@ -105,7 +105,7 @@ def test_decode_joins_huge_values(gpu):
 
 
 @pytest.mark.parametrize("B,n", [(1, 1), (1, 40), (1, 5000), (160, 50)])
-@pytest.mark.parametrize("size", [-2.0 ** 52, -2.0 ** -46, 2.0 ** -46, 2.0 ** 52])
+@pytest.mark.parametrize("size", [-1.3671875 * 2.0 ** 52, -1.3671875 * 2.0 ** -46, 1.3671875 * 2.0 ** -46, 1.3671875 * 2.0 ** 52])
 def test_decode_of_scores_far_from_zero(gpu, B, n, size):
     """Every score near 2^18 or 2^118, of either sign: equal keys weigh their values equally, whatever the score is."""
     tq, torch = gpu
@@ -148,3 +148,39 @@ def test_prompt_keeps_a_tail_of_small_weights(gpu, padded, d, offset):
         assert torch.all((got[:, h] - ref).abs() <= tol), float(((got[:, h] - ref).abs() / tol).max())
     # the bound says something (in the last row: it counts all n tokens as seen, row i sees i + 1)
     assert float((tol / ref)[-1, 1]) < 0.003
+
+
+@pytest.mark.parametrize("padded", [0, 200])
+@pytest.mark.parametrize("d", [64, 128, 256, 512])
+@pytest.mark.parametrize("size", [-1.3671875 * 2.0 ** 52, -1.3671875 * 2.0 ** -46, 1.3671875 * 2.0 ** -46, 1.3671875 * 2.0 ** 52])
+def test_prompt_of_scores_far_from_zero(gpu, padded, d, size):
+    """Every score near 2^18 or 2^118 or beyond, of either sign: equal keys weigh their values equally, whatever the score is.  A query
+    of zeros among the others (weights of 1) is not disturbed."""
+    tq, torch = gpu
+    n, H = 300, 2
+    k = torch.full((n, H, d), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
+    v = (torch.rand((n, H, d)) + 0.5).bfloat16().cuda()
+    q = torch.full((n, 4, d), size, dtype=torch.bfloat16, device="cuda")
+    q[100:110] = 0
+    at = torch.tensor([0, n] + [n] * padded, dtype=torch.int32, device="cuda")
+    out = torch.empty((n, 4, d), device="cuda")
+    tq.tq_sdpa_prompt(q, k, v, at, at, 1.0, out)
+    ref = (v.double().cumsum(0) / torch.arange(1, n + 1, device="cuda")[:, None, None]).repeat_interleave(2, 1)
+    assert torch.all((out.double() - ref).abs() <= 1.5 * 2.0 ** -8)   # weights in bf16, values up to 1.5
+
+
+@pytest.mark.parametrize("padded", [0, 200])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("size", [-44800.0, -11.0, 1.37, 3.3, 11.0, 44800.0])
+def test_prompt_of_fp16_scores_far_from_zero(gpu, padded, d, size):
+    """The same in fp16, whose weights have less room: scores of 2^22 to 2^38."""
+    tq, torch = gpu
+    n, H = 300, 2
+    k = torch.full((n, H, d), 42112.0, dtype=torch.float16, device="cuda")
+    v = (torch.rand((n, H, d)) + 0.5).half().cuda()
+    q = torch.full((n, 4, d), size, dtype=torch.float16, device="cuda")
+    at = torch.tensor([0, n] + [n] * padded, dtype=torch.int32, device="cuda")
+    out = torch.empty((n, 4, d), device="cuda")
+    tq.tq_sdpa_prompt(q, k, v, at, at, 1.0, out)
+    ref = (v.double().cumsum(0) / torch.arange(1, n + 1, device="cuda")[:, None, None]).repeat_interleave(2, 1)
+    assert torch.all((out.double() - ref).abs() <= 1.5 * (2.0 ** -11 + 2.0 ** -15))
