@@ -9,6 +9,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "tq.h"
 
 namespace {
@@ -120,14 +122,14 @@ struct Cache {
   bool cuda;
   int dev;
   PyObject* keep[3];
-  int64_t numel[3];
-  // The tensors' addresses as they are now; false if one has another size or device than it came with.
+  std::vector<int64_t> sizes[3];
+  // The tensors' addresses as they are now; false if one has another type, shape or device than it came with.
   bool refresh() {
     void* at[3] = {};
     for (int i = 0; i < 3; ++i) {
       if (!keep[i]) continue;
       const at::Tensor& t = THPVariable_Unpack(keep[i]);
-      if (t.numel() != numel[i] || !t.is_contiguous() || t.is_cuda() != cuda || (cuda && t.get_device() != dev)) return false;
+      if (t.scalar_type() != (i == 0 ? at::kByte : at::kInt) || t.sizes() != sizes[i] || !t.is_contiguous() || t.is_cuda() != cuda || (cuda && t.get_device() != dev)) return false;
       at[i] = t.data_ptr();
     }
     c.blocks = static_cast<uint8_t*>(at[0]);
@@ -136,7 +138,7 @@ struct Cache {
     return true;
   }
 };
-const char kCache[] = "tq_kv8_cache", kMoved[] = "a tensor of the cache was resized or moved to another device";
+const char kCache[] = "tq_kv8_cache", kMoved[] = "a tensor of the cache was resized, or has another type or device than it had";
 void free_cache(PyObject* capsule) {
   auto* x = static_cast<Cache*>(PyCapsule_GetPointer(capsule, kCache));
   for (PyObject* k : x->keep) Py_XDECREF(k);
@@ -201,7 +203,7 @@ PyObject* py_cache8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     x.dev = x.cuda ? blocks.get_device() : -1;
     for (int i = 0; i < (paged ? 3 : 2); ++i) {
       x.keep[i] = a[i];
-      x.numel[i] = THPVariable_Unpack(a[i]).numel();
+      x.sizes[i] = THPVariable_Unpack(a[i]).sizes().vec();
       Py_INCREF(a[i]);
     }
     PyObject* capsule = PyCapsule_New(new Cache(x), kCache, free_cache);

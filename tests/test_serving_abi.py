@@ -194,3 +194,19 @@ def test_the_binding_refuses_tensors_it_cannot_use(tq):
     assert (paged.B, paged.H_kv, paged.S_cap, paged.d, paged.page_tokens, paged.max_pages, paged.num_pages) == (3, 2, 128, 128, 32, 4, 9)
     c = paged.struct()
     assert (c.blocks, c.seq_lens, c.page_table) == (paged.blocks.data_ptr(), paged.seq_lens.data_ptr(), paged.page_table.data_ptr())
+
+
+def test_a_cache_refuses_tensors_of_another_type_or_shape(tq):
+    """What stands in a tensor's place has to be of its type and shape, not of as many elements alone: an int64 or int16 table
+    would be read as int32."""
+    import torch
+    for name, swap in (("seq_lens", lambda t: t.long()), ("seq_lens", lambda t: t.to(torch.int16)), ("page_table", lambda t: t.to(torch.uint8)),
+                       ("page_table", lambda t: t.t().contiguous()), ("blocks", lambda t: t.to(torch.float32)),
+                       ("blocks", lambda t: t.reshape(t.shape[1], t.shape[0], *t.shape[2:]))):
+        cache = tq.PagedKV8Cache(3, 2, 32, 4, 9, 128, device="cpu")
+        assert cache.struct().B == 3
+        tensor = getattr(cache, name)
+        tensor.data = swap(tensor)
+        with pytest.raises(tq.TqError) as e:
+            cache.struct()
+        assert e.value.code == tq.TQ_ERR_SHAPE, name
