@@ -477,7 +477,8 @@ class KV8Cache:
     d = property(lambda self: _bind.sizes(self._handle)[3])
 
     def struct(self):
-        return tq_kv8_cache.from_address(_bind.address(self._handle))
+        # a copy: the handle's own struct goes with it
+        return tq_kv8_cache.from_buffer_copy(tq_kv8_cache.from_address(_bind.address(self._handle)))
 
 
 class PagedKV8Cache(KV8Cache):

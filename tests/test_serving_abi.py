@@ -210,3 +210,20 @@ def test_a_cache_refuses_tensors_of_another_type_or_shape(tq):
         with pytest.raises(tq.TqError) as e:
             cache.struct()
         assert e.value.code == tq.TQ_ERR_SHAPE, name
+
+
+def test_a_cache_struct_outlives_its_cache(tq):
+    """The C struct is the caller's own: it stays as it is when the cache object is gone, and when it is used again."""
+    import gc
+    import torch
+    blocks, lens = torch.zeros((3, 2, 2, tq.TQ_BLOCK8_BYTES(64)), dtype=torch.uint8), torch.zeros(3, dtype=torch.int32)
+    c = tq.KV8Cache.over(blocks, lens).struct()
+    gc.collect()
+    others = [tq.KV8Cache.over(torch.zeros((1, 1, 1, tq.TQ_BLOCK8_BYTES(128)), dtype=torch.uint8), torch.zeros(1, dtype=torch.int32))
+              for _ in range(50)]
+    assert (c.blocks, c.seq_lens, c.B, c.H_kv, c.S_cap, c.d) == (blocks.data_ptr(), lens.data_ptr(), 3, 2, 32, 64)
+    cache = tq.KV8Cache.over(blocks, lens)
+    first = cache.struct()
+    blocks.data = blocks.clone()
+    assert cache.struct().blocks == blocks.data_ptr() != first.blocks
+    del others
