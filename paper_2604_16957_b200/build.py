@@ -1,4 +1,4 @@
-"""Build libtq.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Build libtq.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, then the serving operators' Python binding.
 
     python -m paper_2604_16957_b200.build [--force] [--verbose]
     python -m paper_2604_16957_b200.build --probe copies|math    # timing-probe builds of the decode kernel
@@ -9,8 +9,10 @@ taken out.  They produce meaningless results and exist only to time (`bench.py -
 """
 import glob
 import os
+import re
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -18,7 +20,6 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libtq.so")
-BIND = os.path.join(HERE, "_tq_bind.so")  # native binding of the serving operators (a CPython extension)
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -41,14 +42,20 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
-def build_binding(force: bool = False) -> str:
-    """The CPython extension that hands torch tensors to libtq; needs torch's headers, no CUDA compiler."""
-    src = os.path.join(CSRC, "binding", "tq_bind.cpp")
-    if not force and os.path.exists(BIND) and all(os.path.getmtime(p) <= os.path.getmtime(BIND)
-                                                  for p in [src] + glob.glob(os.path.join(INCLUDE, "*.h"))):
-        return BIND
-    import sysconfig
+def binding_path() -> str:
+    """Native binding of the serving operators: a CPython extension of this torch, its C++ ABI and this Python, all of which
+    its name tells, so that one made for others is neither loaded nor taken for up to date."""
+    import torch
+    made_for = re.sub(r"[^0-9A-Za-z.]", "_", f"torch{torch.__version__}_abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}")
+    return os.path.join(HERE, f"_tq_bind.{made_for}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
+
+def build_binding(force: bool = False) -> str:
+    """The extension that hands torch tensors to libtq; needs g++ and torch's headers, no CUDA compiler."""
+    src, out = os.path.join(CSRC, "binding", "tq_bind.cpp"), binding_path()
+    if not force and os.path.exists(out) and all(os.path.getmtime(p) <= os.path.getmtime(out)
+                                                 for p in [src] + glob.glob(os.path.join(INCLUDE, "*.h"))):
+        return out
     import torch
     from torch.utils import cpp_extension
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
@@ -56,15 +63,25 @@ def build_binding(force: bool = False) -> str:
     for path in cpp_extension.include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]:
         cmd += ["-isystem", path]
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd += ["-I", INCLUDE, src, "-o", BIND, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
-    subprocess.run(cmd, check=True)
-    return BIND
+    made = f"{out}.{os.getpid()}.tmp"  # a process that has the old one loaded keeps it
+    cmd += ["-I", INCLUDE, src, "-o", made, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    try:
+        subprocess.run(cmd, check=True)
+        os.replace(made, out)
+    finally:
+        if os.path.exists(made):
+            os.remove(made)
+    return out
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    if force or _stale():
+        build_library(verbose)
     build_binding(force)
-    if not force and not _stale():
-        return LIB
+    return LIB
+
+
+def build_library(verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     extra = ["-Xptxas", "-v"] if verbose else []
     with tempfile.TemporaryDirectory() as tmp:  # one nvcc per source file, side by side

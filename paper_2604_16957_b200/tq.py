@@ -4,13 +4,16 @@ operators, whose kernels can be shorter than that, through a small extension mod
 Tensors are torch CUDA tensors (torch supplies device memory and streams, nothing else); every
 function forwards data pointers and sizes to the C entry point and raises TqError on a non-zero
 result.  There is no CPU fallback: importing this module fails if the library has not been
-built (python -m paper_2604_16957_b200.build), and calls fail without a CUDA device.
+built (python -m paper_2604_16957_b200.build), the serving operators raise if their extension module has not been built for
+this torch and Python, and calls fail without a CUDA device.
 """
 import ctypes as C
 import importlib.util
 import os
 
 import torch
+
+from . import build as _build
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # TQ_LIBRARY names another build of the same library (the timing probes of build.py); never a fallback
@@ -426,12 +429,30 @@ def alloc_partials(B, H_q, d, num_splits, device="cuda"):
 
 # ---- serving: pages and slots, the 8-bit cache, attention over it and over whole prompts (see tq.h)
 
-_BIND_PATH = os.path.join(_HERE, "_tq_bind.so")
-if not os.path.exists(_BIND_PATH):
-    raise ImportError(f"{_BIND_PATH} is missing: build it with `python -m paper_2604_16957_b200.build`")
-_spec = importlib.util.spec_from_file_location("_tq_bind", _BIND_PATH)
-_bind = importlib.util.module_from_spec(_spec)
-_spec.loader.exec_module(_bind)
+class _NoBinding:
+    """Stands where the binding is missing or cannot be loaded: the serving operators raise, the others work as ever."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"the serving operators' binding: {self._why}; build it with `python -m paper_2604_16957_b200.build`")
+
+
+def _load_binding():
+    path = _build.binding_path()
+    if not os.path.exists(path):
+        return _NoBinding(f"{path} is missing")
+    try:
+        spec = importlib.util.spec_from_file_location("_tq_bind", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        return _NoBinding(str(e))
+    return module
+
+
+_bind = _load_binding()
 
 
 def _refuse(where, why):
@@ -440,9 +461,10 @@ def _refuse(where, why):
     raise e
 
 
-_bind.attach(_refuse, _check, *(C.cast(f, _vp).value for f in (
-    _lib.tq_pages_release, _lib.tq_pages_assign, _lib.tq_kv8_append, _lib.tq_kv8_gather, _lib.tq_sdpa_int8_decode,
-    _lib.tq_sdpa_prompt)))
+if not isinstance(_bind, _NoBinding):
+    _bind.attach(_refuse, _check, *(C.cast(f, _vp).value for f in (
+        _lib.tq_pages_release, _lib.tq_pages_assign, _lib.tq_kv8_append, _lib.tq_kv8_gather, _lib.tq_sdpa_int8_decode,
+        _lib.tq_sdpa_prompt)))
 
 
 class KV8Cache:

@@ -227,3 +227,64 @@ def test_a_cache_struct_outlives_its_cache(tq):
     blocks.data = blocks.clone()
     assert cache.struct().blocks == blocks.data_ptr() != first.blocks
     del others
+
+
+def _python(code):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    return subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+
+
+@pytest.mark.parametrize("there", [False, True])
+def test_without_its_binding_only_the_serving_operators_are_missing(tq, tmp_path, there):
+    """The extension module is missing, or is none: the rest of tq imports and works, and the serving operators say why not."""
+    path = tmp_path / "_tq_bind.other.so"
+    if there:
+        path.write_bytes(b"made for something else")
+    p = _python(f"""
+from paper_2604_16957_b200 import build
+build.binding_path = lambda: {str(path)!r}
+from paper_2604_16957_b200 import tq
+assert "sm_100a" in tq.tq_version() and tq.KVCache(1, 2, 32, 64, device="cpu").struct().H_kv == 2
+assert tq.tq_auto_splits(1, 8, 64, 128, 1000) > 0
+import torch
+z = torch.zeros(1, dtype=torch.int32)
+for call in (lambda: tq.KV8Cache(1, 2, 32, 64, device="cpu"), lambda: tq.PagedKV8Cache(1, 2, 32, 2, 2, 64, device="cpu"),
+             lambda: tq.tq_pages_release(None, z, z, 16, 0, None, None, z, None),
+             lambda: tq.tq_sdpa_prompt(z, z, z, z, z, 1.0, z)):
+    try:
+        call()
+    except ImportError as e:
+        assert "_tq_bind.other.so" in str(e) and "build" in str(e), e
+    else:
+        raise AssertionError("no error")
+print("fine")
+""")
+    assert p.returncode == 0 and p.stdout.strip() == "fine", p.stderr
+
+
+def test_the_binding_is_named_after_what_it_was_built_for(monkeypatch):
+    """Another torch, another Python: another file, which is then built and not taken over."""
+    import sysconfig
+
+    import torch
+    from paper_2604_16957_b200 import build
+    here = build.binding_path()
+    assert here.endswith(sysconfig.get_config_var("EXT_SUFFIX"))
+    monkeypatch.setattr(torch, "__version__", "9.9.0+other")
+    assert build.binding_path() != here
+    monkeypatch.undo()
+    real = sysconfig.get_config_var
+    monkeypatch.setattr(sysconfig, "get_config_var", lambda k: ".cpython-399.so" if k == "EXT_SUFFIX" else real(k))
+    assert build.binding_path() != here
+    monkeypatch.undo()
+    commands = []
+    monkeypatch.setattr(torch, "__version__", "9.9.0+other")
+    monkeypatch.setattr(build.subprocess, "run", lambda cmd, **kw: (commands.append(cmd), open(cmd[cmd.index("-o") + 1], "w").close()))
+    out = build.build_binding()
+    try:
+        assert len(commands) == 1 and out == build.binding_path() and out != here
+    finally:
+        build.os.remove(out)
