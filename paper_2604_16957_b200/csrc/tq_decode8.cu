@@ -92,6 +92,9 @@ struct Args {
   bool compact;      // fewer units than thread blocks: part of (thread block i, unit u) at i + u, else two per thread block
   void* out;
   int32_t* status;
+  // instrumented instantiation only (the library's own tests, see TestHooks): limit of the stage waits in SM cycles, and
+  // the 16-token block of every unit whose copy announces 16 bytes too many: its barrier never completes, the data lands
+  int wait_cycles, fault_block;
 };
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -218,7 +221,7 @@ struct Shares {
   }
 };
 
-template <int D, int QT, int OT>
+template <int D, int QT, int OT, bool TEST = false>
 __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a) {
   using C = Cfg<D>;
   constexpr int KK = D / 32;
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       bool sent = false;
       if (more && mbar_test_wait(empty(lane, stage), phase)) {
         const uint8_t* src = block_at(a, use.b, use.h, use.span.first() + j);
-        mbar_expect_tx(full(lane, stage), C::STAGE);
+        mbar_expect_tx(full(lane, stage), C::STAGE + (TEST && use.span.first() + j == a.fault_block ? 16 : 0));
         bulk_g2s(base + (lane * C::NST + stage) * C::STAGE, src, C::STAGE, full(lane, stage));
         j += step;
         if (++stage == C::NST) {
@@ -455,8 +458,9 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
         __nanosleep(64);
       }
     }
-    // whatever is still on its way after that lands before the warp ends (bounded)
-    if (more)
+    // Whatever is still on its way lands before the warp ends (bounded): a reader that has given up did not wait for it.
+    // (A stage that was never filled answers at once.)
+    if (lane < C::NW)
       for (int s = 0; s < C::NST; ++s) {
         const int x = (stage + s) % C::NST;
         wait_stage(full(lane, x), x >= stage ? phase : phase ^ 1);
@@ -534,7 +538,7 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
     float M0 = kNoMax, M1 = kNoMax, R0 = kNoMax, R1 = kNoMax, l0 = 0.0f, l1 = 0.0f;
 
     for (int j = use.j0 + (by_warp ? 0 : warp); j < use.j1; j += by_warp ? 1 : C::NW) {
-      if (!dead && !wait_stage(full(warp, stage), phase)) {
+      if (!dead && !wait_stage(full(warp, stage), phase, TEST ? a.wait_cycles : kMaxWaitCycles)) {
         dead = true;
         s_dead = 1;
         if (a.status && lane == 0) atomicOr(a.status, TQ_STATUS_TIMEOUT);
@@ -849,10 +853,19 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
   }
 }
 
-template <int D, int QT, int OT>
+template <int D, int QT, int OT, bool TEST = false>
 cudaError_t launch_dqo(const Args& a, cudaStream_t st) {
   using C = Cfg<D>;
-  auto* kernel = decode8_kernel<D, QT, OT>;
+  if constexpr (D == 128 && QT == TQ_FP16 && OT == TQ_FP32 && !TEST) {
+    const int limit = test_hooks().spin_limit.load(std::memory_order_relaxed), fault = test_hooks().fault_block.load(std::memory_order_relaxed);
+    if (limit > 0 || fault >= 0) {
+      Args x = a;
+      x.wait_cycles = limit > 0 ? limit : static_cast<int>(kMaxWaitCycles);
+      x.fault_block = fault;
+      return launch_dqo<D, QT, OT, true>(x, st);
+    }
+  }
+  auto* kernel = decode8_kernel<D, QT, OT, TEST>;
   static std::atomic<uint64_t> ready{0};  // devices on which the shared-memory limit has been raised
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;

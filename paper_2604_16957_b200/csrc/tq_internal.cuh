@@ -205,8 +205,11 @@ cudaError_t launch_prompt(const PromptArgs& a, cudaStream_t st);
 // the test suite but not declared in tq.h: not part of the ABI).  Read with relaxed loads on the call path.
 struct TestHooks {
   std::atomic<int> decode_impl{0};   // key 0: 0 = tensor-core kernel, 1 = the scalar Algorithm-1 kernel of tq_attend_simple.cu
-  std::atomic<int> spin_limit{0};    // key 1: > 0 = poll limit of the decode kernel's stage waits (instrumented instantiation)
-  std::atomic<int> fault_block{-1};  // key 2: >= 0 = the copy of this 16-token block announces 16 bytes that never arrive
+  // keys 1 and 2, served by instrumented instantiations (4-bit decode; 8-bit decode and prompt attention at d = 128 from
+  // fp16 to fp32): > 0 = limit of the waits for a copy; >= 0 = the copy of this 16-token block (prompt attention: of the key
+  // tiles of this number) announces 16 bytes that never arrive
+  std::atomic<int> spin_limit{0};
+  std::atomic<int> fault_block{-1};
 };
 TestHooks& test_hooks();
 extern "C" int tq_internal_test_hook(int key, int value);
