@@ -117,7 +117,7 @@ __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatil
   }
   return true;
 }
-__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
   if (mbar_try_wait(bar, parity)) return true;
   return wait_slow(bar, parity, stop, limit);
 }
@@ -128,7 +128,7 @@ __device__ __forceinline__ bool wait_stage_inline(uint32_t bar, uint32_t parity,
   return true;
 }
 // the same for a whole warp: all its lanes go on, or none
-__device__ __forceinline__ bool warp_wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = kTileWait) {
+__device__ __forceinline__ bool warp_wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
   return __all_sync(0xffffffffu, wait_on(bar, parity, stop, limit));
 }
 
@@ -186,9 +186,15 @@ struct Span {
   __device__ bool partly(int j) const { return j * C::BN < lo || (j + 1) * C::BN > up; }
 };
 
-template <int D, int NQ, int DT, int OT>
+// Instrumented instantiation only (the library's own tests, see TestHooks): limit of the waits for a tile in SM cycles, and the
+// key tile whose loads announce 16 bytes too many: their barrier never completes, the data lands.
+struct Hook {
+  int wait_cycles, fault_tile;
+};
+
+template <int D, int NQ, int DT, int OT, bool TEST>
 __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps maps, const PromptArgs a,
-                                                                    int G, int T) {
+                                                                    int G, int T, const Hook hook) {
   using C = Cfg<D, NQ>;
   using B = Bars<C>;
   extern __shared__ uint8_t raw[];
@@ -202,6 +208,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
   const uint32_t bars = base + C::BARS;
   auto bar = [&](int i) { return bars + 8 * i; };
   volatile int* const stop = &s_stop;
+  const long long tile_wait = TEST ? hook.wait_cycles : kTileWait;
 
   if (warp == C::SOFT + 1) tmem_alloc(smem_addr(&s_tmem), 512);
   if (tid == 0) {
@@ -274,14 +281,14 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
       // The outputs of the tiles before j are complete once the scores of tile j + 1 are (their MMAs are issued behind);
       // the last two outputs of a piece of work arrive on a barrier of their own.
       auto outputs_before = [&](int j, uint32_t use) {
-        if (j + 1 < my1) return warp_wait_on(bar(B::S + 2 * i + ((use + 1) & 1)), ((use + 1) >> 1) & 1, stop);
-        return warp_wait_on(bar(B::O + i), out & 1, stop);
+        if (j + 1 < my1) return warp_wait_on(bar(B::S + 2 * i + ((use + 1) & 1)), ((use + 1) >> 1) & 1, stop, tile_wait);
+        return warp_wait_on(bar(B::O + i), out & 1, stop, tile_wait);
       };
       for (int j = my0; j < my1 && ok; ++j, ++n) {
         const uint32_t use = total + n;
         const int buf = 2 * i + (use & 1);
         const uint32_t s_addr = tmem + buf * C::BN + lanes;
-        ok = warp_wait_on(bar(B::S + buf), (use >> 1) & 1, stop);
+        ok = warp_wait_on(bar(B::S + buf), (use >> 1) & 1, stop, tile_wait);
         if (!ok) break;
         tc_fence_after();
         float s[C::BN];
@@ -371,7 +378,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
       }
       total += n;
       // ---- epilogue: the thread's row of O
-      if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), out++ & 1, stop);
+      if (n > 0 && ok) ok = warp_wait_on(bar(B::O + i), out++ & 1, stop, tile_wait);
       if (ok) {
         tc_fence_after();
         const float inv = up > lo ? 1.0f / l : 0.0f;
@@ -477,6 +484,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         tc_fence_before();
       }
     }
+    tmem_wait_st();  // (weights that were on their way when a wait ran out: before the block gives its memory back)
     if (C::NQ == 2 && lane == 0) bulk_wait_read<0>();  // shared memory stays until it is read
   } else if (warp == C::SOFT) {
     // ====================================================================================== the work, and TMA loads
@@ -518,7 +526,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         if (w.more && ok) {
           const Span<C> r(a, w, T);
           if (r.J1 > r.J0) {
-            ok = wait_on(bar(B::Q_FREE), (q_uses & 1) ^ 1, stop);
+            ok = wait_on(bar(B::Q_FREE), (q_uses & 1) ^ 1, stop, tile_wait);
             if (ok) {
               ++q_uses;
               mbar_expect_tx(bar(B::Q), C::NQ * (D / 64) * T * G * 128);
@@ -527,10 +535,10 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
                   tma_load_3d(base + i * C::QTILE + x * C::QCHUNK, &maps.q, 64 * x, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
             }
             for (int j = r.J0; j <= r.J1 && ok; ++j) {
-              ok = wait_on(bar(B::EMPTY + stage), phase, stop);
+              ok = wait_on(bar(B::EMPTY + stage), phase, stop, tile_wait);
               if (!ok) break;
               const uint32_t to = base + C::RING + stage * C::STAGE, full = bar(B::FULL + stage);
-              mbar_expect_tx(full, (j < r.J1 ? C::KT : 0) + (j > r.J0 ? C::VT : 0));
+              mbar_expect_tx(full, (j < r.J1 ? C::KT : 0) + (j > r.J0 ? C::VT : 0) + (TEST && j == hook.fault_tile ? 16 : 0));
               if (j < r.J1)
                 for (int x = 0; x < D / 64; ++x) tma_load_3d(to + x * C::KCHUNK, &maps.k, 64 * x, w.h, w.s.k0 + j * C::BN, full);
               if (j > r.J0)
@@ -555,8 +563,9 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         id = steal_answer(smem_addr(&s_answer));
         fence_proxy_async_smem();
       }
-      if (!ok || *stop) {
-        // copies on their way land before the block ends (bounded again)
+      {
+        // Loads on their way land before the block ends (bounded again): whoever waits for them may have given up, or may
+        // yet do so.
         if (q_uses > 0) wait_stage_inline(bar(B::Q), (q_uses - 1) & 1, kMaxWaitCycles);
         for (uint32_t x = 0; x < C::NS && x < issued; ++x) {
           const uint32_t n = issued - 1 - x;
@@ -588,9 +597,9 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
       // cores have work
       constexpr bool kLate = C::NS > 2;
       int owed = -1;
-      ok = warp_wait_on(bar(B::Q), q_uses++ & 1, stop);
+      ok = warp_wait_on(bar(B::Q), q_uses++ & 1, stop, tile_wait);
       for (int j = J0; j <= J1 && ok; ++j) {
-        ok = warp_wait_on(bar(B::FULL + stage), phase, stop);
+        ok = warp_wait_on(bar(B::FULL + stage), phase, stop, tile_wait);
         if (!ok) break;
         const uint32_t at = ring_lo + stage * (C::STAGE >> 4);
         if (j >= my0 && j < my1) {
@@ -608,10 +617,10 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
         if (owed >= 0) mma_commit(leader, bar(B::EMPTY + owed));
         if (j - 1 >= my0 && j - 1 < my1) {
           // (READY only behind FULL: before it, READY may still be two phases back, which it cannot tell from this one)
-          if ((j - 1) * C::BN < lo || j * C::BN > up) ok = warp_wait_on(bar(B::READY + stage), phase, stop);
+          if ((j - 1) * C::BN < lo || j * C::BN > up) ok = warp_wait_on(bar(B::READY + stage), phase, stop, tile_wait);
           const int buf = 2 * i + (pn & 1);
           const uint32_t p = tm + buf * C::BN, v_at = at + (C::KT >> 4) + ((C::KCHUNK >> 4) << 16);
-          ok = ok && warp_wait_on(bar(B::P + buf), (pn >> 1) & 1, stop);
+          ok = ok && warp_wait_on(bar(B::P + buf), (pn >> 1) & 1, stop, tile_wait);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -642,7 +651,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
       const Span<C> r(a, w, T);
       // every stage of the ring in turn, so that none is filled again behind this warp's back
       for (int j = r.J0; j <= r.J1 && r.J1 > r.J0 && ok; ++j) {
-        ok = warp_wait_on(bar(B::FULL + stage), phase, stop);
+        ok = warp_wait_on(bar(B::FULL + stage), phase, stop, tile_wait);
         if (!ok) break;
         if (j > r.J0 && r.partly(j - 1)) {
           uint4* tile = reinterpret_cast<uint4*>(smem + C::RING + stage * C::STAGE + C::KT);
@@ -726,10 +735,14 @@ long long blocks_of(const PromptArgs& a) {
   return (static_cast<long long>(a.n_q) / (C::NQ * T) + a.B) * a.H_kv * (C::D_ / C::DV);
 }
 
-template <int D, int NQ, int DT, int OT>
-cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st) {
+template <int D, int NQ, int DT, int OT, bool TEST = false>
+cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st, Hook hook = {}) {
   using C = Cfg<D, NQ>;
-  auto* kernel = prompt_kernel<D, NQ, DT, OT>;
+  if constexpr (D == 128 && DT == TQ_FP16 && OT == TQ_FP32 && !TEST) {
+    const int limit = test_hooks().spin_limit.load(std::memory_order_relaxed), fault = test_hooks().fault_block.load(std::memory_order_relaxed);
+    if (limit > 0 || fault >= 0) return launch_tiles<D, NQ, DT, OT, true>(a, st, {limit > 0 ? limit : static_cast<int>(kTileWait), fault});
+  }
+  auto* kernel = prompt_kernel<D, NQ, DT, OT, TEST>;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
@@ -749,7 +762,7 @@ cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st) {
       !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN) ||
       !make_map(&maps.o, a.out, a.out_dtype, D, a.H_q, a.n_q, static_cast<long long>(a.H_q) * D, G > 32 ? 1 : G, G > 32 ? 1 : 32 / G))
     return cudaErrorInvalidValue;
-  return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T);
+  return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T, hook);
 }
 
 template <int D, int DT, int OT>

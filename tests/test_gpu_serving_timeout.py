@@ -2,9 +2,10 @@
 TQ_STATUS_TIMEOUT and returns, and the next one is right.  As in test_gpu_timeout.py the instrumented instantiations make one
 chosen copy's barrier expect 16 bytes that never arrive (the data itself lands), or shorten the limit.  Nothing here faults,
 traps or waits without a bound."""
+import numpy as np
 import pytest
 
-from test_gpu_serving import _check_decode, _filled
+from test_gpu_serving import _check_decode, _check_prompt, _filled, _packed
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +69,43 @@ def test_decode_with_short_waits(gpu, lens, H_q, H_kv, limit):
         work.zero_()
         tq.tq_sdpa_int8_decode(cache, q, 0.09, 0, 0, work, out)
     _check_decode(torch, out, q, values, 0.09, 0, d)
+
+
+# one tile per thread block, and two; thread blocks that take over several pieces of work; a window
+PROMPTS = [([300], 8, 1, 0), ([700, 40], 64, 8, 0), ([400, 1, 900, 33], 32, 8, 100), ([130] * 30, 16, 8, 0)]
+
+
+def _prompt(tq, torch, lq, H_q, H):
+    d = 128
+    q, k, v = _packed(torch, np.random.default_rng(len(lq)), lq, lq, H_q, H, d, "fp16", True)
+    cum = np.concatenate([[0], np.cumsum(lq)]).tolist()
+    guard = torch.full(((len(q) + 2) * H_q * d,), 5.0, device="cuda")
+    return q, k, v, cum, torch.tensor(cum, dtype=torch.int32, device="cuda"), guard, guard.view(-1, H_q, d)[1:-1]
+
+
+@pytest.mark.parametrize("lq,H_q,H,window", PROMPTS)
+@pytest.mark.parametrize("fault", [0, 1, 2])
+def test_prompt_gives_up_on_a_tile(gpu, lq, H_q, H, window, fault):
+    tq, torch = gpu
+    q, k, v, cum, at, guard, out = _prompt(tq, torch, lq, H_q, H)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    _hooked(tq, torch, lambda: tq.tq_sdpa_prompt(q, k, v, at, at, 0.09, out, window=window, status=status), 100000, fault)
+    assert int(status.item()) == tq.TQ_STATUS_TIMEOUT
+    assert torch.all(guard.view(-1, H_q, 128)[0] == 5.0) and torch.all(guard.view(-1, H_q, 128)[-1] == 5.0)
+    status.zero_()
+    tq.tq_sdpa_prompt(q, k, v, at, at, 0.09, out, window=window, status=status)
+    assert int(status.item()) == 0
+    _check_prompt(torch, out, q, k, v, cum, cum, 0.09, True, window)
+
+
+@pytest.mark.parametrize("lq,H_q,H,window", PROMPTS)
+@pytest.mark.parametrize("limit", [1, 2000])
+def test_prompt_with_short_waits(gpu, lq, H_q, H, window, limit):
+    tq, torch = gpu
+    q, k, v, cum, at, guard, out = _prompt(tq, torch, lq, H_q, H)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    _hooked(tq, torch, lambda: tq.tq_sdpa_prompt(q, k, v, at, at, 0.09, out, window=window, status=status), limit, -1)
+    assert int(status.item()) in (0, tq.TQ_STATUS_TIMEOUT)
+    if int(status.item()):
+        tq.tq_sdpa_prompt(q, k, v, at, at, 0.09, out, window=window)
+    _check_prompt(torch, out, q, k, v, cum, cum, 0.09, True, window)
