@@ -505,11 +505,11 @@ int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, in
  *   q            : device, fp16 or bf16 (q_dtype): sequence b, head h at b * q_stride + h * d elements (q_stride a
  *                  multiple of 8, at least H_q * d)
  *   max_seq_len  : 0, or an upper bound on the lengths that the host knows; it only limits the launch
- *   workspace    : tq_int8_workspace_bytes(B, H_kv, H_q, d) bytes, 16-byte aligned: counters, then the partial results
- *                  of sequences that several thread blocks share.  ZERO the first tq_int8_counter_bytes(B, H_kv, H_q)
- *                  bytes once before the first use; every call leaves them zero.  A workspace that goes on to calls with
- *                  other B, H_kv, H_q or d is zeroed again in between.  Calls that may overlap on the GPU (other
- *                  streams, graphs replayed side by side) need workspaces of their own.
+ *   workspace    : tq_int8_workspace_bytes(B, H_kv, H_q, d) bytes or more, 16-byte aligned: counters, then the partial
+ *                  results of sequences that several thread blocks share.  ZERO the first tq_int8_counter_bytes(B, H_kv,
+ *                  H_q) bytes (256, whatever the shape) once before the first use; every call leaves them zero, and the
+ *                  workspace may go on to calls of any other shape that it is large enough for.  Calls that may overlap
+ *                  on the GPU (other streams, graphs replayed side by side) need workspaces of their own.
  *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype)
  * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64;
  * B * H_kv * ceil(H_q / H_kv / 8) * (S_cap / 16 + 64) at most 2^31 - 2^16.

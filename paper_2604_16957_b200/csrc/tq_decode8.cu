@@ -28,7 +28,7 @@
 // output cost; without them a share of many short units took three times as long as one of a few long ones (45
 // sequences of 320 to 5130 tokens, 128 heads on 16: 199 us instead of 100).
 // A unit that lies in one thread block is finished there; the parts of a cut one go to the workspace, and the last to
-// arrive (a counter per unit) joins them.  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
+// arrive joins them (counters in 256 bytes, a byte per thread block, whatever the shape).  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
 // registers), each with a ring of three to six stages of one 16-token block, and one warp that fills the rings, one bulk
 // copy per block (K codes, V codes and ranges are contiguous): 200 KB in flight per SM, no barrier in the main loop, and
 // the copies run on into the thread block's next unit while this one is merged.
@@ -47,6 +47,7 @@ constexpr float kSlack = 8.0f;  // log2 units a score may exceed the running max
 constexpr float kRaise = 7.0f;  // log2 of the weight in fp16 that a contribution as large as M' has
 constexpr float kLower = 1.0f / 128.0f;  // undoes it, in the accumulators: 2^(M' - M) may be the smallest normal number
 constexpr int kMaxGrid = 160;   // thread blocks of a launch (one per SM)
+static_assert(kMaxGrid <= kCounterBytes && kMaxGrid < 256, "arrival counters");
 
 template <int D>
 struct Cfg {
@@ -86,7 +87,7 @@ struct Args {
   int grid;          // thread blocks launched
   int min_blocks;    // fewest cache blocks worth a thread block
   int lead;          // positions on the line before a unit's blocks (see the top)
-  int32_t* counters;
+  uint32_t* counters;  // a byte for each thread block
   float* parts;      // see part_floats
   int rows;          // query heads of a tile: at most 8
   bool compact;      // fewer units than thread blocks: part of (thread block i, unit u) at i + u, else two per thread block
@@ -748,11 +749,14 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
       }
       join_warps();
       if (tid == 0) {
-        // releases the block's writes, which the barrier orders before it, and acquires those of the blocks before
-        int got;
-        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(got) : "l"(a.counters + unit) : "memory");
-        s_last = got == to - from;
-        if (s_last) a.counters[unit] = 0;  // left as it was found
+        // The unit's counter is the byte of the thread block that holds its first part (at most one cut unit begins there).
+        // This releases the block's writes, which the barrier orders before it, and acquires those of the blocks before.
+        uint32_t* const word = a.counters + (from >> 2);
+        const uint32_t shift = 8 * (from & 3);
+        uint32_t got;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;\n" : "=r"(got) : "l"(word), "r"(1u << shift) : "memory");
+        s_last = static_cast<int>(got >> shift & 0xff) == to - from;
+        if (s_last) atomicSub(word, static_cast<uint32_t>(to - from + 1) << shift);  // left as it was found
       }
       join_warps();
       if (s_last) {
@@ -904,7 +908,7 @@ size_t decode8_parts_bytes(int B, int H_kv, int G, int d) {
 }
 
 cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,
-                           int window, int grid, int32_t* counters, float* parts, void* out, int out_type, int32_t* status,
+                           int window, int grid, uint32_t* counters, float* parts, void* out, int out_type, int32_t* status,
                            cudaStream_t st) {
   Args a = {};
   a.c = c;

@@ -181,10 +181,11 @@ cudaError_t launch_kv8_append(const tq_kv8_cache& c, const void* k, const void* 
                               long long v_stride, const int64_t* slots, long long n, int32_t* status, cudaStream_t st);
 cudaError_t launch_kv8_gather(const tq_kv8_cache& c, const int64_t* slots, long long n, void* k, void* v, int dtype,
                               int32_t* status, cudaStream_t st);
+constexpr int kCounterBytes = 256;  // arrival counters of the 8-bit decode, for every shape
 int decode8_grid(int B, int H_kv, int G, int d, int max_len);
 size_t decode8_parts_bytes(int B, int H_kv, int G, int d);
 cudaError_t launch_decode8(const tq_kv8_cache& c, const void* q, int q_type, long long q_stride, int H_q, float attn_scale,
-                           int window, int grid, int32_t* counters, float* parts, void* out, int out_type, int32_t* status,
+                           int window, int grid, uint32_t* counters, float* parts, void* out, int out_type, int32_t* status,
                            cudaStream_t st);
 struct PromptArgs {
   const void *q, *k, *v;

@@ -5,7 +5,6 @@ namespace tq {
 namespace {
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-inline size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 inline bool is16(int dtype) { return dtype == TQ_FP16 || dtype == TQ_BF16; }
 
 // The requirements of tq_kv_cache, which the 8-bit cache shares.
@@ -107,7 +106,7 @@ int tq_kv8_gather(const tq_kv8_cache* cache, const int64_t* slots, int64_t n, vo
 
 size_t tq_int8_counter_bytes(int32_t B, int32_t H_kv, int32_t H_q) {
   if (B < 1 || H_kv < 1 || H_q < H_kv) return 0;
-  return align256(static_cast<size_t>(B) * H_kv * ((H_q / H_kv + 7) / 8) * sizeof(int32_t));
+  return kCounterBytes;
 }
 
 size_t tq_int8_workspace_bytes(int32_t B, int32_t H_kv, int32_t H_q, int32_t d) {
@@ -132,8 +131,8 @@ int tq_sdpa_int8_decode(const tq_kv8_cache* cache, const void* q, int32_t q_dtyp
   int most = max_seq_len && max_seq_len < cache->S_cap ? max_seq_len : cache->S_cap;
   if (window && window < most) most = window;
   const int grid = decode8_grid(cache->B, cache->H_kv, H_q / cache->H_kv, cache->d, most);
-  auto* counters = static_cast<int32_t*>(workspace);
-  auto* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + tq_int8_counter_bytes(cache->B, cache->H_kv, H_q));
+  auto* counters = static_cast<uint32_t*>(workspace);
+  auto* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
   return finish(launch_decode8(*cache, q, q_dtype, q_stride, H_q, attn_scale, window, grid, counters, parts, out, out_dtype,
                                status, static_cast<cudaStream_t>(stream)));
 }

@@ -266,3 +266,19 @@ def test_the_binding_refuses(gpu):
     x = z(1, 6, 128)
     tq.tq_kv8_append(cache, x.as_strided((1, 2, 128), (3, 128, 1)), x[:, 2:4], _dev(torch, [0], torch.int64))
     torch.cuda.synchronize()
+
+
+def test_one_workspace_for_batches_of_any_shape(gpu):
+    """Zeroed once, it goes from call to call whatever their batch, heads and head dimension: a server's batch changes from step to
+    step."""
+    tq, torch = gpu
+    shapes = [([9000, 50], 16, 2, 128), ([2500, 700] * 32, 8, 8, 64), ([3000], 4, 2, 256), ([1500] * 40, 32, 8, 128), ([30000], 8, 1, 128),
+              ([20, 2500, 300] * 15, 16, 8, 64), ([600, 900], 8, 2, 512)]
+    work = torch.zeros(max(int(tq._lib.tq_int8_workspace_bytes(len(l), H, H_q, d)) for l, H_q, H, d in shapes), dtype=torch.uint8, device="cuda")
+    filled = [_filled(tq, torch, l, H, d, 0, "fp16", 40 + i) for i, (l, H_q, H, d) in enumerate(shapes)]
+    for turn in range(2):
+        for (lens, H_q, H, d), (cache, values) in zip(shapes, filled):
+            q = torch.randn((len(lens), H_q, d), device="cuda").half()
+            out = torch.full((len(lens), H_q, d), 3.0, device="cuda")
+            tq.tq_sdpa_int8_decode(cache, q, d ** -0.5, 0, 0, work, out)
+            _check_decode(torch, out, q, values, d ** -0.5, 0, d)
