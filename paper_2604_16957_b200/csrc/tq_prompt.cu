@@ -264,8 +264,8 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t o_addr = tmem + C::O_COL + i * C::DV + lanes;
     const int t = row / G;
-    // not 0: a hidden key's score is -inf, and has to stay that
-    const float c = fmaxf(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f);
+    // not 0: a hidden key's score is -inf, and has to stay that (but a NaN stays one)
+    const float c = max3(fabsf(a.attn_scale) * kLog2e, 1.17549435e-38f, 1.17549435e-38f);
     bool ok = true;
     uint32_t total = 0, out = 0;  // K / V tiles of this query tile, and arrivals on its outputs, in all work so far
     Work w;

@@ -98,3 +98,19 @@ def test_chunked_prompts_over_the_cache(gpu, d, kind, window):
         tq.tq_kv8_append(cache, k, v, slots, status)
         model.append(k.double().cpu().numpy(), v.double().cpu().numpy(), slots.cpu().numpy())
     assert int(status.item()) == 0 and lens.tolist() == [222, 191, 184]
+
+
+@pytest.mark.parametrize("padded", [0, 200])
+def test_a_scale_that_is_no_number(gpu, padded):
+    """It gives NaN, as it does in decode, and no average of the values; queries that see nothing stay zero."""
+    tq, torch = gpu
+    q, k, v = _packed(torch, np.random.default_rng(7), [70], [70], 4, 2, 64, "fp16", True)
+    out = torch.empty(q.shape, device="cuda")
+    tq.tq_sdpa_prompt(q, k[:40], v[:40], _dev(torch, [0, 70] + [70] * padded), _dev(torch, [0, 40] + [40] * padded), float("nan"), out)
+    assert torch.isnan(out[30:]).all() and torch.all(out[:30] == 0)
+    cache = tq.KV8Cache(1, 2, 64, 64)
+    tq.tq_kv8_append(cache, k[:40], v[:40], torch.arange(40, device="cuda"))
+    cache.seq_lens.fill_(40)
+    out = torch.empty((1, 4, 64), device="cuda")
+    tq.tq_sdpa_int8_decode(cache, q[:1], float("nan"), 0, 0, tq.alloc_int8_workspace(1, 2, 4, 64), out)
+    assert torch.isnan(out).all()
