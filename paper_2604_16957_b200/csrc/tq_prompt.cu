@@ -8,9 +8,10 @@
 //     O += P V    (A operand P from TMEM, V as it lies in memory: rows along K)
 // c = alpha log2 e > 0 (for a negative alpha the MMA negates Q).  m is raised only when a score exceeds it by more than
 // 2^12 (bf16) or 2^7.9 (fp16); then the thread rescales its row of O in TMEM.  The row sums are of unrounded weights, in
-// fp32.  A bf16 weight is rounded by 2^-8 of itself, e = 0.  In fp16 weights stay below 2^15 with e = 7, which puts its
-// subnormals as low as that allows: rounded by 2^-11 of itself, or by 2^-32 of the largest weight (with 2^12 and e = 0 by
-// 2^-25: a token of weight 2^-22.5 was off by 6 %).  The sooner raising costs fp16 1 % (8K) to 5 % (d = 256, window 1024).
+// fp32.  A bf16 weight is rounded by 2^-8 of itself; e = -20, so that a million values near the largest number do not
+// overflow in O (an e of 0 left room for none).  In fp16 weights stay below 2^15 with e = 7, which puts its subnormals
+// as low as that allows: rounded by 2^-11 of itself, or by 2^-32 of the largest weight (with 2^12 and e = 0 by 2^-25: a
+// token of weight 2^-22.5 was off by 6 %).  The sooner raising costs fp16 1 % (8K) to 5 % (d = 256, window 1024).
 // S has two buffers per tile: the scores of the next keys are made while the softmax of these runs.  That takes key
 // tiles of 64 (two tiles, two buffers and two outputs are all of TMEM at d = 128), for which an MMA of 128 x 64 x 16
 // reads its operands in 48 cycles instead of the 32 that it computes; with tiles of 128 keys and one buffer the MMAs are
@@ -57,7 +58,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 template <int DT>
 struct Weights {
   static constexpr float kSlack = DT == TQ_BF16 ? 12.0f : 7.9f;
-  static constexpr float kRaise = DT == TQ_BF16 ? 0.0f : 7.0f;
+  static constexpr float kRaise = DT == TQ_BF16 ? -20.0f : 7.0f;
   static constexpr float kFar = DT == TQ_BF16 ? 1073741824.0f : 8388608.0f;  // 2^30, 2^23
 };
 

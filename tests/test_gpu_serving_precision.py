@@ -184,3 +184,21 @@ def test_prompt_of_fp16_scores_far_from_zero(gpu, padded, d, size):
     tq.tq_sdpa_prompt(q, k, v, at, at, 1.0, out)
     ref = (v.double().cumsum(0) / torch.arange(1, n + 1, device="cuda")[:, None, None]).repeat_interleave(2, 1)
     assert torch.all((out.double() - ref).abs() <= 1.5 * (2.0 ** -11 + 2.0 ** -15))
+
+
+@pytest.mark.parametrize("padded", [0, 200])
+@pytest.mark.parametrize("d", [64, 128, 256, 512])
+@pytest.mark.parametrize("size", [2.0 ** 127, 2.0 ** -100])
+def test_prompt_of_huge_and_tiny_values(gpu, padded, d, size):
+    """bf16 values near the largest number: the sum of a row's weighted values does not overflow before it is divided.  And small
+    ones, of which nothing is lost for that."""
+    tq, torch = gpu
+    n, H = 1500, 1
+    v = torch.full((n, H, d), size, dtype=torch.bfloat16, device="cuda")
+    v[..., 1::2] *= -1
+    q, k = torch.randn((n, 2, d), device="cuda").bfloat16(), torch.randn((n, H, d), device="cuda").bfloat16()
+    at = torch.tensor([0, n] + [n] * padded, dtype=torch.int32, device="cuda")
+    out = torch.empty((n, 2, d), device="cuda")
+    tq.tq_sdpa_prompt(q, k, v, at, at, d ** -0.5, out)
+    # equal values: what is left of the error is the rounding of the weights, 2^-8
+    assert torch.all((out.double() / v.double() - 1).abs() <= 2.0 ** -8 + 2.0 ** -15)
