@@ -398,7 +398,14 @@ int tq_sdpa_int4_attend_static(const tq_kv_cache* cache /* host */, const void* 
  *   tq_kv8_append                       per layer: the new tokens into the 8-bit cache, through the slots
  *   tq_sdpa_int8_decode                 per layer: one query token per sequence over that cache
  *   tq_kv8_gather                       cached tokens back as 16-bit values (the past of a chunked prompt)
- * All rules at the top of this file hold.  Unlike the paper's kernels these take fp16 and bf16.
+ * All rules at the top of this file hold, but for the alignment of small arrays: int32 arrays here are 4-byte aligned,
+ * slots 8-byte, finished not at all.  Unlike the paper's kernels these take fp16 and bf16.
+ * A token that is cached already has the slot page_table[b][p / page_tokens] * page_tokens + p % page_tokens (p its
+ * position; without a page table b * S_cap + p): what tq_kv8_gather wants for a sequence's past is one indexing of the
+ * table.
+ * The 4-bit cache has no append through slots.  tq_kv_quantize_append and the step write at seq_lens[b] and advance it
+ * themselves, T tokens for every sequence alike, so a paged 4-bit cache takes from tq_pages_assign the pages of such a
+ * step: call it with seq_lens_out in an array of its own and leave the cache's seq_lens to the append.
  */
 typedef enum tq_dtype { TQ_FP16 = 0, TQ_FP32 = 1, TQ_BF16 = 2 } tq_dtype;
 
@@ -461,7 +468,7 @@ int tq_pages_assign(int32_t* page_table, const int32_t* seq_lens, const int32_t*
  *     K: 512 (c / 32) + 64 (t % 8) + 16 (c % 32 / 8) + 8 (t / 8) + c % 8
  *     V: 512 (c / 32) + 64 (c % 8) + 16 (t % 8 / 2) + 4 (c % 32 / 8) + 2 (t / 8) + t % 2   (after the K codes)
  *   -- the operand order of the decode kernel's matrix instructions.  tq_cache8_code_offset addresses single codes.
- * 2.5 % more than half the bytes of an fp16 cache, 1.6 times those of the 4-bit one.
+ * 0.4 % more than half the bytes of an fp16 cache at d = 128 (0.8 % at 64), 1.6 times those of the 4-bit one.
  * Rows of a block behind the last token, and of blocks that no token was appended to, are unspecified.
  */
 #define TQ_BLOCK8_BYTES(d) (32 * (d) + 16)
@@ -510,7 +517,8 @@ int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, in
  *                  H_q) bytes (256, whatever the shape) once before the first use; every call leaves them zero, and the
  *                  workspace may go on to calls of any other shape that it is large enough for.  Calls that may overlap
  *                  on the GPU (other streams, graphs replayed side by side) need workspaces of their own.
- *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype)
+ *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype); weights are rounded to fp16 before their product with
+ *                  the codes, scores, maxima and sums are fp32
  * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64;
  * B * H_kv * ceil(H_q / H_kv / 8) * (S_cap / 16 + 64) at most 2^31 - 2^16.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,
@@ -535,7 +543,8 @@ int tq_sdpa_int8_decode(const tq_kv8_cache* cache /* host */, const void* q, int
  *   q_offsets, kv_offsets : device [B + 1] int32, ascending; the same array where the keys are the queries' own tokens
  *   out          : device [n_q][H_q][d], of dtype or fp32 (out_dtype).  Rows of no sequence are left as they were.
  * d in {64, 128, 256, 512}; H_q a multiple of H_kv, H_q / H_kv <= 64; causal = 0 with a window is TQ_ERR_SHAPE.
- * A NaN or an infinity in k or v reaches only the queries that attend its token.
+ * A NaN or an infinity in k or v reaches only the queries that attend its token.  Weights are rounded to the inputs' type
+ * before their product with v; scores, maxima and sums are fp32.
  * Status: TQ_STATUS_BAD_LEN, TQ_STATUS_EMPTY_SEQ (queries of a sequence without keys), TQ_STATUS_TIMEOUT; the first two
  * are set for sequences that have queries.
  */

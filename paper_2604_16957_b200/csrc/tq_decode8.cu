@@ -6,9 +6,9 @@
 //   Output:  o = sum_j 2^(s_j) a_V(j) code_j / (127 sum_j 2^(s_j)).  The weight that enters the second MMA in fp16 is
 //            w_j = 2^(s_j + log2 a_V(j) - M' + 7), with M' the running maximum of the whole exponent: a block whose
 //            values are small is weighed against the largest contribution, not against the largest score.  The
-//            denominator has a maximum M of its own, kept in fp32, and the factor 2^(M' - M) / 2^7 joins them at the end.  M' is kept
-//            as its distance R = M' - M, so that log2 a_V is never added to a score: next to one of 10^6 it would lose
-//            its digits, and the values their scale.
+//            denominator has a maximum M of its own, kept in fp32, and the factor 2^(M' - M) / 2^7 joins them at the end.
+//            M' is kept as its distance R = M' - M, so that log2 a_V is never added to a score: next to one of 10^6 it
+//            would lose its digits, and the values their scale.
 //   Both maxima are raised only when a score exceeds them by more than 2^8: weights stay below 2^15, inside fp16.  The
 //   7 puts the subnormals of fp16 as low as that allows: a weight is rounded by 2^-11 of itself down to 2^-21 of the
 //   largest contribution, below that by 2^-32 of it (at most; 2^-25 without the 7, where a token of 2^-22.5 was off by
@@ -17,9 +17,12 @@
 // What bounds it: HBM.  2 d + 0.5 bytes per token and KV head; per 16-token block a warp issues 2 x d / 16 MMAs, 3 d / 8
 // integer and half-precision instructions that widen the codes, and 8 exponentials per lane (2 per score): a quarter
 // of what an SM could do in the time that the block takes to arrive.  Measured at d = 128, 64 heads on 8: 128K tokens
-// 51.8 us (5.2 TB/s over all; the loop itself takes 38 us, 7.1 TB/s, and the rest is the start, 2 us, the merge of the
-// warps, 2.5, and the joining of cut units, 5); 16 sequences of 4K to 64K, 195 us (5.9 TB/s); 1K tokens 9.1 us, all of
-// it latency.  d = 256, 32K tokens, 32 heads on 16: 49 us.
+// 51.7 us (5.2 TB/s over all; the loop itself takes 38 us, 7.1 TB/s, and the rest is the start, 2 us, the merge of the
+// warps, 2.5, and the joining of cut units, 5); 16 sequences of 4K to 64K, 195 us (5.9 TB/s); d = 256, 32K tokens, 32
+// heads on 16: 49 us.  1K tokens 9.3 us, latency: 8 thread blocks take a KV head each, five blocks deep in every warp,
+// then merge their warps; nothing is cut.  One KV head or two leave most SMs without a share (see `cuts`): 100 000
+// tokens, 8 heads on 1, 27 us where the bytes take 4; d = 512 has four warps of arithmetic only: 20 000 tokens, 16 heads
+// on 2, 59 us where they take 6.
 //
 // Work split.  All (sequence, KV head, tile of 8 query heads) units' blocks lie on one line, sequences first; thread
 // block i of N takes the positions [i L / N, (i + 1) L / N) of the L in all, whatever the lengths: ragged batches load
@@ -28,10 +31,11 @@
 // output cost; without them a share of many short units took three times as long as one of a few long ones (45
 // sequences of 320 to 5130 tokens, 128 heads on 16: 199 us instead of 100).
 // A unit that lies in one thread block is finished there; the parts of a cut one go to the workspace, and the last to
-// arrive joins them (counters in 256 bytes, a byte per thread block, whatever the shape).  A thread block has 15 warps of arithmetic (7 and 4 at d = 256 and 512:
-// registers), each with a ring of three to six stages of one 16-token block, and one warp that fills the rings, one bulk
-// copy per block (K codes, V codes and ranges are contiguous): 200 KB in flight per SM, no barrier in the main loop, and
-// the copies run on into the thread block's next unit while this one is merged.
+// arrive joins them (counters in 256 bytes, a byte per thread block, whatever the shape).  A thread block has 15 warps of
+// arithmetic (7 and 4 at d = 256 and 512: registers), each with a ring of three to six stages of one 16-token block, and
+// one warp that fills the rings, one bulk copy per block (K codes, V codes and ranges are contiguous): 185 KB in flight
+// per SM at d <= 128, 172 and 197 KB at 256 and 512, no barrier in the main loop, and the copies run on into the
+// thread block's next unit while this one is merged.
 #include <algorithm>
 #include <type_traits>
 
@@ -318,9 +322,12 @@ __global__ void __launch_bounds__(Cfg<D>::LAUNCH, 1) decode8_kernel(const Args a
 
   // Few units: shares that end where units do save the thread blocks in between a second query and merge (6 us).  Each
   // unit of a sequence gets floor(its part of the line x N) of them; that lengthens the longest share, by 0.09 us per
-  // block, and is done up to 66 blocks (10 sequences of 207 to 3321 tokens, one KV head: 14.4 us, not so 20).  No unit
+  // block, and is done up to 66 blocks (10 sequences of 207 to 3321 tokens, one KV head: 14.8 us, not so 20).  No unit
   // gets more than half the root of its blocks: one thread block joins the parts, at 0.15 to 0.6 us each (30 000 tokens,
-  // one KV head of 256: 67 parts 55 us, 16 parts 29).
+  // one KV head of 256: 67 parts 55 us, 16 parts 30).  The 66 do not count what this second limit lengthens: 8192 blocks
+  // of one KV head make 45 shares of 182, where 148 would have 56 each.  (Batches of more than 32 stay on the line,
+  // because only there does a warp have all sums, not because it serves them better: 60 sequences of 147 to 2357 tokens,
+  // one KV head, 28 us; 22 of 171 to 2738, two KV heads, in shares that end with units 14.6, on the line 26.)
   int cuts = 0, cuts_upto = 0;  // shares of each unit of the lane's sequence, and of those up to it
   bool snapped = false;
   if (few && !by_block && a.lead == 0 && U <= N) {

@@ -66,13 +66,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
       : "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-      : TQ_R8(r, 0), TQ_R8(r, 8)
-      : "r"(addr)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "

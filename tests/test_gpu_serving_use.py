@@ -282,3 +282,35 @@ def test_one_workspace_for_batches_of_any_shape(gpu):
             out = torch.full((len(lens), H_q, d), 3.0, device="cuda")
             tq.tq_sdpa_int8_decode(cache, q, d ** -0.5, 0, 0, work, out)
             _check_decode(torch, out, q, values, d ** -0.5, 0, d)
+
+
+def test_pages_for_the_4_bit_cache(gpu):
+    """Pages from tq_pages_assign serve a paged 4-bit cache whose lengths the append advances: bit for bit the contiguous
+    cache's contents and attention."""
+    tq, torch = gpu
+    B, H, d, P, pages = 3, 2, 128, 16, 30
+    paged, plain = tq.PagedKVCache(B, H, P, 8, pages, d), tq.KVCache(B, H, 128, d)
+    free, count = torch.randperm(pages).int().cuda(), _dev(torch, [pages])
+    after, offsets, status = _dev(torch, [0] * B), _dev(torch, [0] * (B + 1)), _dev(torch, [0])
+    work = tq.alloc_pages_workspace(B)
+    for T in (37, 1, 1, 16, 9, 1):
+        slots = torch.empty(B * T, dtype=torch.int64, device="cuda")
+        tq.tq_pages_assign(paged.page_table, paged.seq_lens, _dev(torch, [T] * B), P, pages, free, count, after, count, offsets, slots, work,
+                           status)
+        k, v = (torch.randn((B, H, T, d), device="cuda").half() for _ in range(2))
+        for cache in (paged, plain):
+            tq.tq_kv_quantize_append(cache, k, v, status)
+        assert paged.seq_lens.tolist() == after.tolist() == plain.seq_lens.tolist()
+    n = plain.seq_lens.tolist()[0]
+    assert n == 65 and count.tolist() == [pages - 3 * 5] and int(status.item()) == 0
+    for a, b in zip(paged.arrays_token_major(), plain.arrays_token_major()):
+        assert torch.equal(a[:, :, :n], b[:, :, :n])
+    q = torch.randn((B, 8, d), device="cuda").half()
+    outs = []
+    for cache in (paged, plain):
+        o, m, l = tq.alloc_partials(B, 8, d, 2)
+        out = torch.empty((B, 8, d), device="cuda")
+        tq.tq_sdpa_int4_decode(cache, q, 0.09, 2, o, m, l, status)
+        tq.tq_sdpa_int4_combine(o, m, l, out)
+        outs.append(out)
+    assert torch.equal(*outs) and outs[0].abs().sum() > 0
