@@ -489,12 +489,12 @@ size_t tq_cache8_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d);
  *                  projection's output [n][H_q + 2 H_kv][d] (stride (H_q + 2 H_kv) d); strides multiples of 8 elements
  *                  and at least H_kv * d
  *   slots        : device [n] int64, one per row, as tq_pages_assign writes them: the rows of a block stand together in
- *                  ascending order without gaps; -1 skips a row.  The tokens of a block before the first one appended are taken
- *                  as present.  A slot outside the cache, or a row that is out of order inside its block, sets TQ_STATUS_BAD_SLOT and
- *                  is skipped with the rest of its run.  A block that is met in two places of one call is the caller's mistake: its contents
- *                  are then unspecified (nothing outside it is touched).
- * seq_lens is not read.  n = 0 does nothing, here and in tq_kv8_gather.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (cache requirements as tq_kv_cache, n < 0, strides, dtype
- * TQ_FP32), TQ_ERR_ALIGN, TQ_ERR_CUDA.
+ *                  ascending order without gaps; -1 skips a row.  The tokens of a block before the first one appended
+ *                  are taken as present.  A slot outside the cache, or a row that is out of order inside its block, sets
+ *                  TQ_STATUS_BAD_SLOT and is skipped with the rest of its run.  A block that is met in two places of one
+ *                  call is the caller's mistake: its contents are then unspecified (nothing outside it is touched).
+ * seq_lens is not read.  n = 0 does nothing, here and in tq_kv8_gather.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (cache
+ * requirements as tq_kv_cache, n < 0, strides, dtype TQ_FP32), TQ_ERR_ALIGN, TQ_ERR_CUDA.
  */
 int tq_kv8_append(const tq_kv8_cache* cache /* host */, const void* k_new, const void* v_new, int32_t dtype,
                   int64_t k_stride, int64_t v_stride, const int64_t* slots, int64_t n, int32_t* status, void* stream);
@@ -517,8 +517,8 @@ int tq_kv8_gather(const tq_kv8_cache* cache /* host */, const int64_t* slots, in
  *                  H_q) bytes (256, whatever the shape) once before the first use; every call leaves them zero, and the
  *                  workspace may go on to calls of any other shape that it is large enough for.  Calls that may overlap
  *                  on the GPU (other streams, graphs replayed side by side) need workspaces of their own.
- *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype); weights are rounded to fp16 before their product with
- *                  the codes, scores, maxima and sums are fp32
+ *   out          : device [B][H_q][d], of q's type or fp32 (out_dtype); weights are rounded to fp16 before their product
+ *                  with the codes, scores, maxima and sums are fp32
  * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  H_q a multiple of H_kv, H_q / H_kv <= 64;
  * B * H_kv * ceil(H_q / H_kv / 8) * (S_cap / 16 + 64) at most 2^31 - 2^16.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,
