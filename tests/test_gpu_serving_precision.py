@@ -202,3 +202,30 @@ def test_prompt_of_huge_and_tiny_values(gpu, padded, d, size):
     tq.tq_sdpa_prompt(q, k, v, at, at, d ** -0.5, out)
     # equal values: what is left of the error is the rounding of the weights, 2^-8
     assert torch.all((out.double() / v.double() - 1).abs() <= 2.0 ** -8 + 2.0 ** -15)
+
+
+@pytest.mark.parametrize("B,n,H_q,H,d,kind", [(1, 300, 16, 2, 128, "fp16"), (200, 60, 12, 4, 64, "bf16"), (3, 9000, 16, 2, 128, "bf16"),
+                                              (1, 5000, 8, 1, 256, "fp16")])
+def test_a_query_of_infinities_or_nans_stays_in_its_row(gpu, B, n, H_q, H, d, kind):
+    """Decode and prompt attention: the other heads and tokens give the same bits as without it."""
+    tq, torch = gpu
+    t = {"fp16": torch.float16, "bf16": torch.bfloat16}[kind]
+    cap = -(-n // 16) * 16
+    cache = tq.KV8Cache(B, H, cap, d)
+    k, v = (torch.randn((B * n, H, d), device="cuda").to(t) for _ in range(2))
+    tq.tq_kv8_append(cache, k, v, torch.cat([torch.arange(n, device="cuda") + b * cap for b in range(B)]))
+    cache.seq_lens.fill_(n)
+    work = tq.alloc_int8_workspace(B, H, H_q, d)
+    at = torch.tensor([0, 200, 300], dtype=torch.int32, device="cuda")
+    for rows, call in ((B, lambda q, o: tq.tq_sdpa_int8_decode(cache, q, 0.1, 0, 0, work, o)),
+                       (300, lambda q, o: tq.tq_sdpa_prompt(q, k[:300], v[:300], at, at, 0.1, o))):
+        q = torch.randn((rows, H_q, d), device="cuda").to(t)
+        bad = torch.zeros((rows, H_q), dtype=torch.bool, device="cuda")
+        outs = []
+        for _ in range(2):
+            outs.append(torch.empty((rows, H_q, d), device="cuda"))
+            call(q, outs[-1])
+            for b, h, c, x in ((0, 1, 3, "nan"), (-1, -1, 0, "inf"), (rows // 2, 4, 5, "-inf")):
+                q[b, h, c] = float(x)
+                bad[b, h] = True
+        assert torch.equal(outs[0][~bad], outs[1][~bad]) and torch.isnan(outs[1][bad]).any(-1).all()
