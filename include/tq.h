@@ -55,7 +55,7 @@ typedef enum tq_result {
 #define TQ_STATUS_TIMEOUT 8    /* a bounded wait for an asynchronous copy ran out; that call's results are not valid */
 #define TQ_STATUS_BAD_PAGE 16  /* a page-table entry outside [0, num_pages) was met */
 #define TQ_STATUS_POOL_EMPTY 32 /* tq_pages_assign: too few free pages; that sequence was refused */
-#define TQ_STATUS_BAD_SLOT 64   /* tq_kv8_append, tq_kv8_gather: a slot outside the cache or out of order; that row was skipped */
+#define TQ_STATUS_BAD_SLOT 64   /* appends, gathers: a slot outside the cache (tq_kv8_append: or out of order); that row was skipped */
 
 #define TQ_GROUP 32         /* quantisation group size g (fixed) */
 #define TQ_SPLIT_QUANTUM 16 /* split boundaries fall on multiples of this many tokens */
@@ -552,6 +552,109 @@ int tq_sdpa_prompt(const void* q, const void* k, const void* v, int32_t dtype, i
                    int64_t v_stride, int32_t n_q, int32_t n_kv, const int32_t* q_offsets, const int32_t* kv_offsets,
                    int32_t B, int32_t H_q, int32_t H_kv, int32_t d, float attn_scale, int32_t causal, int32_t window,
                    void* out, int32_t out_dtype, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Latent attention: one latent vector and one positional key per token, shared by all heads (the paper's models have keys
+ * and values of their own per head; these entry points have no counterpart there).  A model projects a token's state
+ * down to a latent c of d_c channels and a positional key r of 64; a head expands c into its own key and value.  Two
+ * forms of the same attention:
+ *   tq_sdpa_latent_prompt  expanded: keys [k_n | r] and values v per head, for the tokens of whole prompts
+ *   tq_sdpa_latent_decode  absorbed: the query is multiplied by the key's expansion instead, attends the cached latents
+ *                          themselves and gives a latent back, to which the caller applies the value's expansion
+ *   tq_latent_append       the tokens' latents and positional keys into an 8-bit cache, through slots of tq_pages_assign
+ *   tq_latent_gather       cached tokens back as 16-bit values (the past of a chunked prompt, to be expanded)
+ * All rules of the serving operators above hold.
+ *
+ * The cache of ONE layer: d_c in {128, 256, 512}; contiguous or paged as tq_kv_cache, without heads.  A block of
+ * TQ_BLOCK_LATENT_BYTES(d_c) = 16 (d_c + 136) bytes holds 16 tokens (10368 bytes at d_c = 512: 648 a token, where 16-bit
+ * values take 1152):
+ *     codes (d_c bytes a token) | positional keys (fp16 [16][64]) | {a, s} (fp32) of each token
+ *   latent:         range a = max |c| of the token, code = round_half_even(127 c / a), stored as code + 128 in one byte;
+ *                   c^ = code * a / 127.  Every code is the exact rounding of the true quotient.
+ *   positional key: fp16(r / s) with s the power of two that brings max |r| into [2^15, 2^16) (at least 2^-126; 1 where
+ *                   all are zero); r^ = s * that: r itself, but for bf16 channels below 2^-32 of the largest.
+ *   A NaN is stored as 0, an infinity as the largest finite value of its type, a magnitude above 2^64 as 2^64; a latent
+ *   without any magnitude of 2^-64 as zero (a = 0, codes 0).
+ *   The code of (token t, channel c) is byte d_c t + 128 (c / 128) + 16 (c % 64 / 8) + 8 (c % 128 / 64) + c % 8, see
+ *   tq_cache_latent_code_offset.
+ * Rows of a block that no token was appended to are unspecified.
+ */
+#define TQ_LATENT_ROPE 64
+#define TQ_BLOCK_LATENT_BYTES(d_c) (16 * ((d_c) + 136))
+typedef struct tq_latent_cache {
+  uint8_t* blocks;    /* [B][S_cap/16][TQ_BLOCK_LATENT_BYTES(d_c)]; with paging [num_pages][page_tokens/16][...] */
+  int32_t* seq_lens;  /* [B]; read by tq_sdpa_latent_decode, not advanced by tq_latent_append */
+  int32_t B, S_cap, d_c;
+  const int32_t* page_table; /* as in tq_kv_cache */
+  int32_t page_tokens, max_pages, num_pages;
+} tq_latent_cache;
+size_t tq_cache_latent_code_offset(int32_t d_c, int32_t t, int32_t c);
+size_t tq_cache_latent_bytes(int32_t B, int32_t S_cap, int32_t d_c);
+
+/* Values of several heads: row i, head h at data + i * row_stride + h * head_stride elements, its channels side by side.
+ * data is 16-byte aligned, both strides are multiples of 8 elements and at least the number of channels; [rows][heads] and
+ * [heads][rows] orders and slices of wider projections all have this form. */
+typedef struct tq_heads {
+  const void* data;
+  int64_t row_stride, head_stride;
+} tq_heads;
+
+/*
+ * Append n tokens through their slots, in any order.
+ *   c_new   : device, fp16 or bf16 (dtype): row i at i * c_stride elements, d_c channels; strides are multiples of 8 and at
+ *             least the row's width (c and r may be slices of one projection's output)
+ *   r_new   : the same, 64 channels, r_stride
+ *   slots   : device [n] int64; negative: the row is skipped.  A slot outside the cache sets TQ_STATUS_BAD_SLOT and is
+ *             skipped.  A slot that is named twice in one call is the caller's mistake: its token is then unspecified.
+ * seq_lens is not read.  n = 0 does nothing, here and in tq_latent_gather.  Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN,
+ * TQ_ERR_CUDA.
+ */
+int tq_latent_append(const tq_latent_cache* cache /* host */, const void* c_new, const void* r_new, int32_t dtype, int64_t c_stride,
+                     int64_t r_stride, const int64_t* slots, int64_t n, int32_t* status, void* stream);
+
+/*
+ * Values of n slots, in any order and as often as asked: c_out [n][d_c] and r_out [n][64], device, of dtype (fp16, bf16 or
+ * fp32; in fp16 what is beyond its range becomes an infinity).  Rows of negative slots are zero; a slot beyond the cache
+ * sets TQ_STATUS_BAD_SLOT and its rows are zero.
+ */
+int tq_latent_gather(const tq_latent_cache* cache /* host */, const int64_t* slots, int64_t n, void* c_out, void* r_out,
+                     int32_t dtype, int32_t* status, void* stream);
+
+/*
+ * out_h = sum_t p_ht c_t,  p_h = softmax_t(attn_scale (qc_h . c_t + qr_h . r_t)),  one query token per sequence over its
+ * cached tokens [max(0, seq_lens[b] - window), seq_lens[b]) (window = 0: all of them), all heads on the same tokens.
+ *   q_c, q_r    : fp16 or bf16 (q_dtype): rows are sequences; d_c channels a head (the query multiplied by the head's key
+ *                 expansion) and 64.  A head whose query holds an infinity or a NaN gives NaN, and only that head.  A query
+ *                 keeps its digits but for channels below 2^-29 of the head's largest (of both parts), off by 2^-40 of it.
+ *   H           : query heads, 1 .. 1024
+ *   max_seq_len : 0, or an upper bound on the lengths that the host knows; it only limits the launch
+ *   workspace   : tq_latent_workspace_bytes(B, H, d_c) bytes or more, 16-byte aligned, contents destroyed.  Calls that may
+ *                 overlap on the GPU (other streams, graphs replayed side by side) need workspaces of their own.
+ *   out         : device [B][H][d_c], of q's type or fp32 (out_dtype).  Weights, multiplied by their token's range, are
+ *                 rounded to fp16 before their product with the codes (by 2^-11, or by 2^-33 of the head's largest);
+ *                 scores, maxima and sums are fp32.
+ * A sequence without tokens gives zeros and sets TQ_STATUS_EMPTY_SEQ.  B * ceil(H / 64) * (S_cap / 64 + 8) at most 2^30.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_ALIGN, TQ_ERR_WORKSPACE, TQ_ERR_CUDA.  Status also: TQ_STATUS_BAD_LEN,
+ * TQ_STATUS_BAD_PAGE, TQ_STATUS_TIMEOUT (a bounded wait ran out; that call's results are not valid).
+ */
+size_t tq_latent_workspace_bytes(int32_t B, int32_t H, int32_t d_c);
+int tq_sdpa_latent_decode(const tq_latent_cache* cache /* host */, const tq_heads* q_c /* host */, const tq_heads* q_r /* host */,
+                          int32_t q_dtype, int32_t H, float attn_scale, int32_t window, int32_t max_seq_len, void* workspace,
+                          size_t workspace_bytes, void* out, int32_t out_dtype, int32_t* status, void* stream);
+
+/*
+ * The expanded form: tq_sdpa_prompt with scores attn_scale (qn_ih . kn_jh + qr_ih . kr_j), every query head with keys and
+ * values of its own and a positional key that the heads share.
+ *   q_n, q_r, k_n, v : rows are packed tokens, H heads; d channels (q_r: 64)
+ *   k_r, kr_stride   : device, row j at j * kr_stride elements, 64 channels; the stride a multiple of 8, at least 64
+ *   out              : device [n_q][H][d]
+ * d in {64, 128}, H in 1 .. 4096; everything else as tq_sdpa_prompt.
+ */
+int tq_sdpa_latent_prompt(const tq_heads* q_n /* host */, const tq_heads* q_r /* host */, const tq_heads* k_n /* host */,
+                          const void* k_r, int64_t kr_stride, const tq_heads* v /* host */, int32_t dtype, int32_t n_q,
+                          int32_t n_kv, const int32_t* q_offsets, const int32_t* kv_offsets, int32_t B, int32_t H, int32_t d,
+                          float attn_scale, int32_t causal, int32_t window, void* out, int32_t out_dtype, int32_t* status,
+                          void* stream);
 
 /* Bytes of one layer's cache arrays (packed + scales + zeros, K and V), i.e. Eq. 1 with the int4 format. */
 size_t tq_cache_bytes(int32_t B, int32_t H_kv, int32_t S_cap, int32_t d);

@@ -191,6 +191,10 @@ struct PromptArgs {
   const void *q, *k, *v;
   int dtype;
   long long q_stride, k_stride, v_stride;
+  long long q_head, k_head, v_head;  // distances of heads
+  // a positional part behind q and k (64 channels, shared by the heads of k), or NULL
+  const void *q_r, *k_r;
+  long long qr_stride, qr_head, kr_stride;
   int n_q, n_kv;
   const int32_t *q_offsets, *kv_offsets;
   int B, H_q, H_kv, d;
@@ -201,6 +205,24 @@ struct PromptArgs {
   int32_t* status;
 };
 cudaError_t launch_prompt(const PromptArgs& a, cudaStream_t st);
+// Latent attention (tq_latent.cu, tq_latent_decode.cu)
+cudaError_t launch_latent_append(const tq_latent_cache& c, const void* lat, const void* rope, int dtype, long long lat_stride,
+                                 long long rope_stride, const int64_t* slots, long long n, int32_t* status, cudaStream_t st);
+cudaError_t launch_latent_gather(const tq_latent_cache& c, const int64_t* slots, long long n, void* lat, void* rope, int dtype,
+                                 int32_t* status, cudaStream_t st);
+size_t latent_workspace_bytes(int B, int H, int d_c);
+struct LatentArgs {
+  tq_latent_cache c;
+  tq_heads q_c, q_r;
+  int q_dtype, H;
+  float attn_scale;
+  int window, max_len;  // max_len: upper bound of the tokens that a sequence attends
+  void* workspace;
+  void* out;
+  int out_dtype;
+  int32_t* status;
+};
+cudaError_t launch_latent_decode(const LatentArgs& a, cudaStream_t st);
 
 // Knobs for the library's own tests, set through tq_internal_test_hook (exported from the shared object for
 // the test suite but not declared in tq.h: not part of the ABI).  Read with relaxed loads on the call path.

@@ -62,9 +62,10 @@ struct Weights {
   static constexpr float kFar = DT == TQ_BF16 ? 1073741824.0f : 8388608.0f;  // 2^30, 2^23
 };
 
-template <int D, int TILES>
+template <int D, int TILES, int ROPE = 0>
 struct Cfg {
   static constexpr int D_ = D;
+  static constexpr int DK = D + ROPE;                 // channels of a key: its own and the shared positional part
   static constexpr int NQ = TILES;                    // query tiles of a thread block
   static constexpr int BN = D <= 256 ? 64 : 32;       // keys of a K / V tile
   static constexpr int DV = D <= 256 ? D : 256;       // output channels of a thread block
@@ -73,12 +74,12 @@ struct Cfg {
   static constexpr int WARPS = SOFT + 1 + NQ + SCRUB;  // softmax | work and TMA | MMA | scrub
   static constexpr int THREADS = 32 * WARPS;
   static constexpr int QCHUNK = 128 * 128;            // bytes of 128 rows x 64 channels
-  static constexpr int QTILE = (D / 64) * QCHUNK;
+  static constexpr int QTILE = (DK / 64) * QCHUNK;
   static constexpr int KCHUNK = BN * 128;
-  static constexpr int KT = (D / 64) * KCHUNK;        // K tile
+  static constexpr int KT = (DK / 64) * KCHUNK;       // K tile
   static constexpr int VT = (DV / 64) * KCHUNK;       // V tile
   static constexpr int STAGE = KT + VT;               // what step j reads: K(j) for its scores, V(j - 1) for its outputs
-  static constexpr int NS = D == 64 ? 8 : (D == 128 ? 4 : 2);
+  static constexpr int NS = ROPE ? (D == 64 ? 5 : (NQ == 2 ? 2 : 4)) : (D == 64 ? 8 : (D == 128 ? 4 : 2));
   static constexpr int RING = NQ * QTILE;
   static constexpr int OUT = RING + NS * STAGE;       // output rows on their way out, 4 KB per softmax warp
   static constexpr bool STAGED = D <= 256;            // (no room at d = 512)
@@ -89,8 +90,13 @@ struct Cfg {
   static_assert(SMEM <= 232448, "shared memory");
 };
 
+template <bool R>
 struct Maps {
   CUtensorMap q, k, v, o;
+};
+template <>
+struct Maps<true> : Maps<false> {  // with positional parts
+  CUtensorMap q_r, k_r;
 };
 
 // mbarriers of a thread block, 8 bytes each
@@ -193,10 +199,10 @@ struct Hook {
   int wait_cycles, fault_tile;
 };
 
-template <int D, int NQ, int DT, int OT, bool TEST>
-__global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps maps, const PromptArgs a,
-                                                                    int G, int T, const Hook hook) {
-  using C = Cfg<D, NQ>;
+template <int D, int NQ, int DT, int OT, bool TEST, int ROPE>
+__global__ void __launch_bounds__(Cfg<D, NQ, ROPE>::THREADS, 1) prompt_kernel(const __grid_constant__ Maps<(ROPE > 0)> maps,
+                                                                          const PromptArgs a, int G, int T, const Hook hook) {
+  using C = Cfg<D, NQ, ROPE>;
   using B = Bars<C>;
   extern __shared__ uint8_t raw[];
   __shared__ __align__(16) uint4 s_answer;
@@ -403,7 +409,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
               continue;
             }
             const uint32_t* src = reinterpret_cast<const uint32_t*>(
-                static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * D + w.half * C::DV + x);
+                static_cast<const uint16_t*>(a.v) + (w.s.k0 + static_cast<long long>(key)) * a.v_stride + w.h * a.v_head + w.half * C::DV + x);
 #pragma unroll
             for (int y = 0; y < 32; y += 2) {
               const uint32_t v = __ldg(src + (y >> 1));
@@ -530,18 +536,23 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
             ok = wait_on(bar(B::Q_FREE), (q_uses & 1) ^ 1, stop, tile_wait);
             if (ok) {
               ++q_uses;
-              mbar_expect_tx(bar(B::Q), C::NQ * (D / 64) * T * G * 128);
-              for (int i = 0; i < C::NQ; ++i)
+              mbar_expect_tx(bar(B::Q), C::NQ * (C::DK / 64) * T * G * 128);
+              for (int i = 0; i < C::NQ; ++i) {
                 for (int x = 0; x < D / 64; ++x)
                   tma_load_3d(base + i * C::QTILE + x * C::QCHUNK, &maps.q, 64 * x, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
+                if constexpr (ROPE > 0)
+                  tma_load_3d(base + i * C::QTILE + (D / 64) * C::QCHUNK, &maps.q_r, 0, w.h * G, w.s.q0 + w.tok0 + i * T, bar(B::Q));
+              }
             }
             for (int j = r.J0; j <= r.J1 && ok; ++j) {
               ok = wait_on(bar(B::EMPTY + stage), phase, stop, tile_wait);
               if (!ok) break;
               const uint32_t to = base + C::RING + stage * C::STAGE, full = bar(B::FULL + stage);
               mbar_expect_tx(full, (j < r.J1 ? C::KT : 0) + (j > r.J0 ? C::VT : 0) + (TEST && j == hook.fault_tile ? 16 : 0));
-              if (j < r.J1)
+              if (j < r.J1) {
                 for (int x = 0; x < D / 64; ++x) tma_load_3d(to + x * C::KCHUNK, &maps.k, 64 * x, w.h, w.s.k0 + j * C::BN, full);
+                if constexpr (ROPE > 0) tma_load_3d(to + (D / 64) * C::KCHUNK, &maps.k_r, 0, 0, w.s.k0 + j * C::BN, full);
+              }
               if (j > r.J0)
                 for (int x = 0; x < C::DV / 64; ++x)
                   tma_load_3d(to + C::KT + x * C::KCHUNK, &maps.v, w.half * C::DV + 64 * x, w.h, w.s.k0 + (j - 1) * C::BN, full);
@@ -608,7 +619,7 @@ __global__ void __launch_bounds__(Cfg<D, NQ>::THREADS, 1) prompt_kernel(const __
           const int buf = 2 * i + (sn & 1);
           const uint32_t d = tm + buf * C::BN;
 #pragma unroll
-          for (int y = 0; y < D / 16; ++y)
+          for (int y = 0; y < C::DK / 16; ++y)
             mma_ss(leader, d, q_lo + (((y >> 2) * C::QCHUNK + (y & 3) * 32) >> 4), at + (((y >> 2) * C::KCHUNK + (y & 3) * 32) >> 4),
                    kDescHi, id_s, y > 0);
           mma_commit(leader, bar(B::S + buf));
@@ -713,12 +724,12 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// [rows][heads][d] values, rows `stride` elements apart, boxes of 128 bytes x `heads_box` x `rows_box`
-bool make_map(CUtensorMap* map, const void* p, int dtype, int d, int heads, long long rows, long long stride, int heads_box,
+// [rows][heads][d] values, rows `stride` elements apart and heads `head`, boxes of 128 bytes x `heads_box` x `rows_box`
+bool make_map(CUtensorMap* map, const void* p, int dtype, int d, int heads, long long rows, long long stride, long long head, int heads_box,
               int rows_box) {
   const int size = dtype == TQ_FP32 ? 4 : 2;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * size, static_cast<cuuint64_t>(stride) * size};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(head) * size, static_cast<cuuint64_t>(stride) * size};
   const cuuint32_t box[3] = {128u / size, static_cast<cuuint32_t>(heads_box), static_cast<cuuint32_t>(rows_box)};
   const cuuint32_t ones[3] = {1, 1, 1};
   const CUtensorMapDataType type = dtype == TQ_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
@@ -736,14 +747,14 @@ long long blocks_of(const PromptArgs& a) {
   return (static_cast<long long>(a.n_q) / (C::NQ * T) + a.B) * a.H_kv * (C::D_ / C::DV);
 }
 
-template <int D, int NQ, int DT, int OT, bool TEST = false>
+template <int D, int NQ, int DT, int OT, int ROPE, bool TEST = false>
 cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st, Hook hook = {}) {
-  using C = Cfg<D, NQ>;
+  using C = Cfg<D, NQ, ROPE>;
   if constexpr (D == 128 && DT == TQ_FP16 && OT == TQ_FP32 && !TEST) {
     const int limit = test_hooks().spin_limit.load(std::memory_order_relaxed), fault = test_hooks().fault_block.load(std::memory_order_relaxed);
-    if (limit > 0 || fault >= 0) return launch_tiles<D, NQ, DT, OT, true>(a, st, {limit > 0 ? limit : static_cast<int>(kTileWait), fault});
+    if (limit > 0 || fault >= 0) return launch_tiles<D, NQ, DT, OT, ROPE, true>(a, st, {limit > 0 ? limit : static_cast<int>(kTileWait), fault});
   }
-  auto* kernel = prompt_kernel<D, NQ, DT, OT, TEST>;
+  auto* kernel = prompt_kernel<D, NQ, DT, OT, TEST, ROPE>;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
@@ -755,34 +766,41 @@ cudaError_t launch_tiles(const PromptArgs& a, cudaStream_t st, Hook hook = {}) {
   const int G = a.H_q / a.H_kv, T = 128 / G;
   const long long blocks = blocks_of<C>(a);
   if (!encode_fn() || blocks > 0x7fffffffLL) return cudaErrorNotSupported;
-  Maps maps;
+  Maps<(ROPE > 0)> maps;
   // (without a single key the maps of K and V describe a row of q; nothing is loaded through them)
   const bool keys = a.n_kv > 0;
-  if (!make_map(&maps.q, a.q, a.dtype, D, a.H_q, a.n_q, a.q_stride, G, T) ||
-      !make_map(&maps.k, keys ? a.k : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.k_stride : a.q_stride, 1, C::BN) ||
-      !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, 1, C::BN) ||
-      !make_map(&maps.o, a.out, a.out_dtype, D, a.H_q, a.n_q, static_cast<long long>(a.H_q) * D, G > 32 ? 1 : G, G > 32 ? 1 : 32 / G))
+  if (!make_map(&maps.q, a.q, a.dtype, D, a.H_q, a.n_q, a.q_stride, a.q_head, G, T) ||
+      !make_map(&maps.k, keys ? a.k : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.k_stride : a.q_stride, keys ? a.k_head : a.q_head, 1, C::BN) ||
+      !make_map(&maps.v, keys ? a.v : a.q, a.dtype, D, a.H_kv, keys ? a.n_kv : 1, keys ? a.v_stride : a.q_stride, keys ? a.v_head : a.q_head, 1, C::BN) ||
+      !make_map(&maps.o, a.out, a.out_dtype, D, a.H_q, a.n_q, static_cast<long long>(a.H_q) * D, D, G > 32 ? 1 : G, G > 32 ? 1 : 32 / G))
     return cudaErrorInvalidValue;
+  if constexpr (ROPE > 0) {
+    if (!make_map(&maps.q_r, a.q_r, a.dtype, ROPE, a.H_q, a.n_q, a.qr_stride, a.qr_head, G, T) ||
+        !make_map(&maps.k_r, keys ? a.k_r : a.q_r, a.dtype, ROPE, 1, keys ? a.n_kv : 1, keys ? a.kr_stride : ROPE, ROPE, 1, C::BN))
+      return cudaErrorInvalidValue;
+  }
   return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(C::THREADS), C::SMEM, st, maps, a, G, T, hook);
 }
 
-template <int D, int DT, int OT>
+template <int D, int DT, int OT, int ROPE>
 cudaError_t launch_dto(const PromptArgs& a, cudaStream_t st) {
   if constexpr (D <= 128) {  // (the rule is explained at the top)
-    if (blocks_of<Cfg<D, 1>>(a) > device_sm_count()) return launch_tiles<D, 2, DT, OT>(a, st);
+    if (blocks_of<Cfg<D, 1, ROPE>>(a) > device_sm_count()) return launch_tiles<D, 2, DT, OT, ROPE>(a, st);
   }
-  return launch_tiles<D, 1, DT, OT>(a, st);
+  return launch_tiles<D, 1, DT, OT, ROPE>(a, st);
 }
 
-template <int D>
+template <int D, int ROPE = 0>
 cudaError_t launch_d(const PromptArgs& a, cudaStream_t st) {
-  if (a.dtype == TQ_BF16) return a.out_dtype == TQ_FP32 ? launch_dto<D, TQ_BF16, TQ_FP32>(a, st) : launch_dto<D, TQ_BF16, TQ_BF16>(a, st);
-  return a.out_dtype == TQ_FP32 ? launch_dto<D, TQ_FP16, TQ_FP32>(a, st) : launch_dto<D, TQ_FP16, TQ_FP16>(a, st);
+  if (a.dtype == TQ_BF16)
+    return a.out_dtype == TQ_FP32 ? launch_dto<D, TQ_BF16, TQ_FP32, ROPE>(a, st) : launch_dto<D, TQ_BF16, TQ_BF16, ROPE>(a, st);
+  return a.out_dtype == TQ_FP32 ? launch_dto<D, TQ_FP16, TQ_FP32, ROPE>(a, st) : launch_dto<D, TQ_FP16, TQ_FP16, ROPE>(a, st);
 }
 
 }  // namespace
 
 cudaError_t launch_prompt(const PromptArgs& a, cudaStream_t st) {
+  if (a.q_r) return a.d == 64 ? launch_d<64, TQ_LATENT_ROPE>(a, st) : launch_d<128, TQ_LATENT_ROPE>(a, st);
   switch (a.d) {
     case 64: return launch_d<64>(a, st);
     case 128: return launch_d<128>(a, st);

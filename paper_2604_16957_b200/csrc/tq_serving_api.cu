@@ -152,7 +152,7 @@ int tq_sdpa_prompt(const void* q, const void* k, const void* v, int32_t dtype, i
       !aligned(kv_offsets, 4) || !aligned(status, 4))
     return TQ_ERR_ALIGN;
   if (n_q == 0) return TQ_OK;
-  const PromptArgs a = {q, k, v, dtype, q_stride, k_stride, v_stride, n_q, n_kv, q_offsets, kv_offsets, B, H_q, H_kv, d,
+  const PromptArgs a = {q, k, v, dtype, q_stride, k_stride, v_stride, d, d, d, nullptr, nullptr, 0, 0, 0, n_q, n_kv, q_offsets, kv_offsets, B, H_q, H_kv, d,
                         attn_scale, causal != 0, window, out, out_dtype, status};
   return finish(launch_prompt(a, static_cast<cudaStream_t>(stream)));
 }

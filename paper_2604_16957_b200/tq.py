@@ -40,7 +40,9 @@ SYMBOLS = ("tq_kv_quantize_append", "tq_auto_splits", "tq_split_range", "tq_sdpa
            "tq_split_range_stable", "tq_sdpa_int4_step", "tq_sdpa_int4_step_ragged", "tq_sdpa_int4_step_window", "tq_step_workspace_bytes", "tq_step_counter_bytes", "tq_auto_splits_step",
            "tq_pages_release", "tq_pages_assign", "tq_pages_workspace_bytes", "tq_cache8_code_offset", "tq_cache8_bytes",
            "tq_kv8_append", "tq_kv8_gather", "tq_int8_counter_bytes", "tq_int8_workspace_bytes", "tq_sdpa_int8_decode",
-           "tq_sdpa_prompt")
+           "tq_sdpa_prompt",
+           "tq_cache_latent_code_offset", "tq_cache_latent_bytes", "tq_latent_append", "tq_latent_gather", "tq_latent_workspace_bytes",
+           "tq_sdpa_latent_decode", "tq_sdpa_latent_prompt")
 
 
 class tq_kv_cache(C.Structure):
@@ -59,6 +61,22 @@ class tq_kv8_cache(C.Structure):
 
 def TQ_BLOCK8_BYTES(d):
     return 32 * d + 16
+
+
+TQ_LATENT_ROPE = 64
+
+
+class tq_latent_cache(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("seq_lens", C.c_void_p), ("B", C.c_int32), ("S_cap", C.c_int32), ("d_c", C.c_int32),
+                ("page_table", C.c_void_p), ("page_tokens", C.c_int32), ("max_pages", C.c_int32), ("num_pages", C.c_int32)]
+
+
+def TQ_BLOCK_LATENT_BYTES(d_c):
+    return 16 * (d_c + 136)
+
+
+class tq_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 _vp, _i32, _f32, _sz = C.c_void_p, C.c_int32, C.c_float, C.c_size_t
@@ -138,6 +156,22 @@ _lib.tq_sdpa_int8_decode.restype = C.c_int
 _lib.tq_sdpa_prompt.argtypes = [_vp, _vp, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _f32, _i32,
                                 _i32, _vp, _i32, _vp, _vp]
 _lib.tq_sdpa_prompt.restype = C.c_int
+_latent_p, _heads_p = C.POINTER(tq_latent_cache), C.POINTER(tq_heads)
+_lib.tq_cache_latent_code_offset.argtypes = [_i32] * 3
+_lib.tq_cache_latent_code_offset.restype = _sz
+_lib.tq_cache_latent_bytes.argtypes = [_i32] * 3
+_lib.tq_cache_latent_bytes.restype = _sz
+_lib.tq_latent_append.argtypes = [_latent_p, _vp, _vp, _i32, _i64, _i64, _vp, _i64, _vp, _vp]
+_lib.tq_latent_append.restype = C.c_int
+_lib.tq_latent_gather.argtypes = [_latent_p, _vp, _i64, _vp, _vp, _i32, _vp, _vp]
+_lib.tq_latent_gather.restype = C.c_int
+_lib.tq_latent_workspace_bytes.argtypes = [_i32] * 3
+_lib.tq_latent_workspace_bytes.restype = _sz
+_lib.tq_sdpa_latent_decode.argtypes = [_latent_p, _heads_p, _heads_p, _i32, _i32, _f32, _i32, _i32, _vp, _sz, _vp, _i32, _vp, _vp]
+_lib.tq_sdpa_latent_decode.restype = C.c_int
+_lib.tq_sdpa_latent_prompt.argtypes = [_heads_p, _heads_p, _heads_p, _vp, _i64, _heads_p, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _i32,
+                                       _f32, _i32, _i32, _vp, _i32, _vp, _vp]
+_lib.tq_sdpa_latent_prompt.restype = C.c_int
 _lib.tq_last_cuda_error.restype = C.c_int
 _lib.tq_version.restype = C.c_char_p
 # knob of the library's own tests (exported by the shared object, not declared in tq.h, not part of the ABI)
@@ -464,7 +498,7 @@ def _refuse(where, why):
 if not isinstance(_bind, _NoBinding):
     _bind.attach(_refuse, _check, *(C.cast(f, _vp).value for f in (
         _lib.tq_pages_release, _lib.tq_pages_assign, _lib.tq_kv8_append, _lib.tq_kv8_gather, _lib.tq_sdpa_int8_decode,
-        _lib.tq_sdpa_prompt)))
+        _lib.tq_sdpa_prompt, _lib.tq_latent_append, _lib.tq_latent_gather, _lib.tq_sdpa_latent_decode, _lib.tq_sdpa_latent_prompt)))
 
 
 class KV8Cache:
@@ -577,3 +611,98 @@ def tq_sdpa_prompt(q, k, v, q_offsets, kv_offsets, attn_scale, out, causal=True,
     """Attention of packed sequences: q [n_q][H_q][d], k and v [n_kv][H_kv][d], fp16 or bf16, heads side by side; offsets
     [B + 1] int32 on the device; out: contiguous [n_q][H_q][d] of q's type or fp32."""
     _bind.prompt(q, k, v, q_offsets, kv_offsets, attn_scale, out, causal, window, status, stream)
+
+
+# ---- latent attention: the 8-bit cache of latents, absorbed and expanded attention (see tq.h)
+
+class LatentCache:
+    """Device buffer of one layer's latent cache, contiguous: `blocks` [B][S_cap/16][block bytes]."""
+
+    __slots__ = ("_tensors", "_handle")
+
+    def __init__(self, B, S_cap, d_c, device="cuda"):
+        if S_cap % 16 or d_c not in (128, 256, 512):
+            _refuse("LatentCache", "S_cap must be a multiple of 16 and d_c one of 128, 256, 512")
+        self._hold(torch.zeros((B, S_cap // 16, TQ_BLOCK_LATENT_BYTES(d_c)), dtype=torch.uint8, device=device),
+                   torch.zeros((B,), dtype=torch.int32, device=device), None)
+
+    @classmethod
+    def over(cls, blocks, seq_lens):
+        """The cache in tensors of the caller: blocks as above, seq_lens [B] int32 (shared by the layers, if need be)."""
+        self = cls.__new__(cls)
+        self._hold(blocks, seq_lens, None)
+        return self
+
+    def _hold(self, blocks, seq_lens, page_table):
+        self._handle = _bind.latent(blocks, seq_lens, page_table)
+        self._tensors = blocks, seq_lens, page_table
+
+    # (read only: a cache over other tensors is another object)
+    blocks = property(lambda self: self._tensors[0])
+    seq_lens = property(lambda self: self._tensors[1])
+    page_table = property(lambda self: self._tensors[2])
+    B = property(lambda self: _bind.latent_sizes(self._handle)[0])
+    S_cap = property(lambda self: _bind.latent_sizes(self._handle)[1])
+    d_c = property(lambda self: _bind.latent_sizes(self._handle)[2])
+
+    def struct(self):
+        # a copy: the handle's own struct goes with it
+        return tq_latent_cache.from_buffer_copy(tq_latent_cache.from_address(_bind.latent_address(self._handle)))
+
+
+class PagedLatentCache(LatentCache):
+    """The same served from a pool of pages: `blocks` [num_pages][page_tokens/16][block bytes], `page_table`
+    [B][max_pages] int32 (shared by the layers, if need be)."""
+
+    __slots__ = ()
+
+    def __init__(self, B, page_tokens, max_pages, num_pages, d_c, device="cuda"):
+        if page_tokens < 16 or page_tokens & (page_tokens - 1) or d_c not in (128, 256, 512):
+            _refuse("PagedLatentCache", "page_tokens must be a power of two >= 16 and d_c one of 128, 256, 512")
+        self._hold(torch.zeros((num_pages, page_tokens // 16, TQ_BLOCK_LATENT_BYTES(d_c)), dtype=torch.uint8, device=device),
+                   torch.zeros((B,), dtype=torch.int32, device=device),
+                   torch.zeros((B, max_pages), dtype=torch.int32, device=device))
+
+    @classmethod
+    def over(cls, blocks, seq_lens, page_table):
+        self = cls.__new__(cls)
+        self._hold(blocks, seq_lens, page_table)
+        return self
+
+    page_tokens = property(lambda self: _bind.latent_sizes(self._handle)[3])
+    max_pages = property(lambda self: _bind.latent_sizes(self._handle)[4])
+    num_pages = property(lambda self: _bind.latent_sizes(self._handle)[5])
+
+
+def _latent_of(cache):
+    return cache._handle if isinstance(cache, LatentCache) else None
+
+
+def tq_latent_append(cache, c_new, r_new, slots, status=None, stream=None):
+    """c_new [n][d_c], r_new [n][64], fp16 or bf16, channels side by side (slices of one projection's output will do); slots
+    [n] int64."""
+    _bind.latent_append(_latent_of(cache), c_new, r_new, slots, status, stream)
+
+
+def tq_latent_gather(cache, slots, c_out, r_out, status=None, stream=None):
+    """Values of the slots into c_out [n][d_c] and r_out [n][64]: contiguous, fp16, bf16 or fp32."""
+    _bind.latent_gather(_latent_of(cache), slots, c_out, r_out, status, stream)
+
+
+def alloc_latent_workspace(B, H, d_c, device="cuda"):
+    """Workspace of tq_sdpa_latent_decode as a uint8 tensor."""
+    return torch.empty(int(_lib.tq_latent_workspace_bytes(B, H, d_c)), dtype=torch.uint8, device=device)
+
+
+def tq_sdpa_latent_decode(cache, q_c, q_r, attn_scale, window, max_seq_len, workspace, out, status=None, stream=None):
+    """q_c [B][H][d_c] and q_r [B][H][64], fp16 or bf16, channels side by side, rows and heads in any order; out: contiguous
+    [B][H][d_c] of their type or fp32.  window = 0: all cached tokens; max_seq_len = 0: no bound known."""
+    _bind.latent_decode(_latent_of(cache), q_c, q_r, attn_scale, window, max_seq_len, workspace, out, status, stream)
+
+
+def tq_sdpa_latent_prompt(q_n, q_r, k_n, k_r, v, q_offsets, kv_offsets, attn_scale, out, causal=True, window=0, status=None,
+                          stream=None):
+    """Attention of packed sequences with keys [k_n | k_r]: q_n [n_q][H][d], q_r [n_q][H][64], k_n and v [n_kv][H][d], k_r
+    [n_kv][64], fp16 or bf16, channels side by side; offsets [B + 1] int32 on the device; out: contiguous [n_q][H][d] of
+    their type or fp32."""
+    _bind.latent_prompt(q_n, q_r, k_n, k_r, v, q_offsets, kv_offsets, attn_scale, out, causal, window, status, stream)
