@@ -69,4 +69,35 @@ __device__ __forceinline__ bool wait_stage(uint32_t bar, uint32_t parity, long l
   return wait_stage_slow(bar, parity, limit);
 }
 
+// ---- thread blocks of several roles that wait for one another
+// Bounded wait that also gives up when another warp of the thread block has: false, and the block winds down.  (Inline:
+// registers cannot be moved between warps, as the kernel does, around a function call.)
+constexpr long long kTileWait = 16 * kMaxWaitCycles;  // 35 ms: a wait may span some other role's work on a few tiles
+constexpr long long kBlockWait = 1LL << 34;           // 9 s: a wait for the next piece of work may span a whole sequence
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*stop) return false;
+    if (clock64() - t0 > limit) {
+      *stop = 1;
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
+  if (mbar_try_wait(bar, parity)) return true;
+  return wait_slow(bar, parity, stop, limit);
+}
+__device__ __forceinline__ bool wait_stage_inline(uint32_t bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > limit) return false;
+  return true;
+}
+// the same for a whole warp: all its lanes go on, or none
+__device__ __forceinline__ bool warp_wait_on(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
+  return __all_sync(0xffffffffu, wait_on(bar, parity, stop, limit));
+}
+
 }  // namespace tq

@@ -1,102 +1,807 @@
-// Attention of single tokens over the latent cache, absorbed form: tq_sdpa_latent_decode.
+// Attention of single tokens over the latent cache on the tensor cores (tcgen05, TMEM), absorbed form:
+// tq_sdpa_latent_decode.
 //
-// A thread block per (sequence, head) walks over the tokens 64 at a time: scores (a warp per token), online softmax, and
-// the sum of the latents by their weights (a thread per channel), all in fp32.
+// All heads of a sequence attend the same tokens, so both products have the heads as their narrow side, and the tokens and
+// channels as the wide one.  A thread block takes a group of up to N = 16, 32 or 64 heads over a run of tiles of 64 tokens:
+//     S^T = [codes | r] [qc | qr]^T     64 tokens x N heads: codes and positional part apart, a = 64 rows
+//     z = alpha log2 e (a / 127 S_c + s S_r),   P^T = 2^(z - ref + log2(a / 127)),   rounded to fp16
+//     O^T += codes^T P^T                d_c channels x N heads, accumulated in TMEM: d_c / 128 times N columns
+// The codes, made fp16 once (they are exact), serve both products: rows of tokens are K-major for the first and MN-major for
+// the second, in the same shared memory.  Neither the token's range nor the latent's rounding enters the products: the range
+// goes into the score in fp32 and, as its logarithm, into the weight's exponent, so weights of tokens of any size share one
+// fp16 scale.  The sum of weights takes it out again (P^T times 127 / a, before rounding, in fp32).
+//
+// ref is per head, in two parts that add up to ref: a score (subtracted first, which is exact where it matters: equal scores of
+// any size give equal weights) and an offset.  It is set so that the largest weight of the first tile is 2^8, and raised when one
+// exceeds 2^15.5; then O^T and the sums are rescaled.  fp16 weights are rounded by 2^-11 of themselves, or by 2^-25: 2^-33
+// of the largest.
+//
+// The query of a head is multiplied by a power of two that brings its largest channel into [2^15, 2^16) and held in fp16, for
+// either input type.
+//
+// Roles: four warps of softmax and epilogue (a thread has a token and half of the heads: S^T of 64 rows fills 16 lanes of every
+// quarter of TMEM), eight warps that turn codes into operands (a tile's loads are in registers while the tile before is
+// turned), one that issues the MMAs, one that finds the work, looks up pages and asks for the tiles' blocks to be brought to L2.
+//
+// Work: the tiles of all sequences lie on a line, each sequence with kFixed places for its start in front; every thread block
+// takes an equal share.  Sequences that are cut leave partial results (O^T, ref, sums) and a second kernel joins them.
+#include <cuda.h>
+
+#include "tq_async.cuh"
 #include "tq_latent.cuh"
+#include "tq_tcgen05.cuh"
 
 namespace tq {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTok = 64;                       // tokens of a tile
+constexpr int kBatch = 8;                      // tiles whose pages are looked up together: a lane per block
+constexpr int kSoft = 4, kConv = 8;            // warps of softmax, of conversion
+constexpr int kMmaWarp = kSoft + kConv, kFeedWarp = kMmaWarp + 1, kWarps = kFeedWarp + 1, kThreads = 32 * kWarps;
+constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
+constexpr int kFixed = 2;                      // what the start of a sequence costs, in tiles
+constexpr int kMinShare = 4;                   // places on the line that a thread block takes at least
+constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
 
-template <int DT>
-__device__ __forceinline__ float to_float(uint16_t x) {
-  return unpack2<DT>(x).x;
+// A part: [N][DC] sums, then [N] scores and offsets of ref, and [N] sums of weights.
+__host__ __device__ constexpr int part_floats(int dc, int n) { return n * (dc + 4); }
+__host__ __device__ constexpr size_t info_bytes(int B) { return (8 * static_cast<size_t>(B) + 255) & ~static_cast<size_t>(255); }
+
+template <int DC, int N_>
+struct Cfg {
+  static constexpr int N = N_;                         // columns: heads of a thread block
+  static constexpr int HN = N / 2;                     // heads of a softmax thread
+  static constexpr int UNITS = DC / 128;               // a tile's codes are handed over 128 channels at a time
+  static constexpr int PANELS = DC / 64 + 1;           // 64 channels each; the last one is the positional part
+  static constexpr int TILE = PANELS * kPanel;
+  static constexpr int QPANEL = N * 128;
+  static constexpr int Q = 0, P = Q + PANELS * QPANEL, RING = P + kPanel;
+  static constexpr int SMALL_BYTES = 3072;
+  static constexpr int FIT = (232448 - SMALL_BYTES - RING) / TILE;
+  static constexpr int NB = FIT < 4 ? FIT : 4;         // tiles in shared memory
+  static constexpr int SMALL = RING + NB * TILE;
+  static constexpr int SMEM = SMALL + SMALL_BYTES;
+  static constexpr int S_COL = 0, O_COL = 4 * N;       // TMEM: two buffers of scores in two parts, then O^T
+  static constexpr int COLS = 8 * N;
+  static_assert(NB >= 2 && SMEM <= 232448 && O_COL + UNITS * N <= COLS && COLS <= 512, "");
+  // mbarriers
+  static constexpr int FULL = 0, EMPTY = FULL + NB * UNITS;                     // operands: by buffer and unit
+  static constexpr int SCORES = EMPTY + NB * UNITS, WEIGHTS = SCORES + 2, DONE = WEIGHTS + 1;  // S^T, P^T, and O^T += of a tile
+  static constexpr int QUERY = DONE + 1, QUERY_FREE = QUERY + 1, DRAINED = QUERY_FREE + 1;     // O^T has been read
+  static constexpr int WORK = DRAINED + 1, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
+                       BARS = END + 1;
+};
+
+// A piece of work: tiles [0, n) of 64 tokens from token t0 on (a multiple of 16), of which [lo, len) are seen.
+struct Work {
+  int b, t0, n, lo, len, part, more;  // part: number of its partial result, or -1: the whole sequence; more = 0: there is none
+};
+
+template <int DC, int N>
+struct Small {
+  float ref_z[N], ref_o[N], scale[2][N], tmp[N], red[kSoft][N];  // (scale: two pieces of work in turn)
+  int pages[2][4 * kBatch];
+  Work work[2];
+  uint64_t bars[Cfg<DC, N>::BARS];
+  int sums[kWarps], start_b, start_p, total, stop;
+  uint32_t tmem;
+};
+
+// Instrumented instantiation only (the library's own tests, see TestHooks): limit of the waits for a tile in SM cycles, and the
+// tile of each thread block whose operands are never announced.
+struct Hook {
+  int wait_cycles, fault_tile;
+};
+
+// pred over the four softmax warps: true for all if true for one
+__device__ __forceinline__ bool any_of_group(bool p) {
+  uint32_t r;
+  asm volatile(
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, 1, 128, p;\nselp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(p))
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void group_sync() { asm volatile("barrier.cta.sync 1, 128;\n" ::: "memory"); }
+
+struct Max {
+  __device__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+struct Sum {
+  __device__ static float of(float a, float b) { return a + b; }
+};
+// Reduces v[i] (i: head `base` + i) over the 16 lanes of a half warp into row[head].  The lanes share the heads out as they go.
+template <typename Op, int HN>
+__device__ __forceinline__ void reduce_half(float (&v)[HN], int lane, int base, float* row) {
+  int n = HN;
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) {
+    if (n > 1) {
+      n /= 2;
+      const bool up = lane & off;
+#pragma unroll
+      for (int i = 0; i < HN / 2; ++i) {
+        if (i >= n) continue;
+        const float keep = up ? v[i + n] : v[i], give = up ? v[i] : v[i + n];
+        v[i] = Op::of(keep, __shfl_xor_sync(0xffffffffu, give, off));
+      }
+      base += up ? n : 0;
+    } else {
+      v[0] = Op::of(v[0], __shfl_xor_sync(0xffffffffu, v[0], off));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < (HN >= 16 ? HN / 16 : 1); ++i) row[base + i] = v[i];
 }
 
-template <int DC, int DT, int OT>
-__global__ void __launch_bounds__(kThreads) latent_decode_kernel(const LatentArgs a) {
-  __shared__ float q[DC + kRope], p[kTile];
-  __shared__ long long at[kTile / 16 + 1];
+__device__ __forceinline__ int tiles_of(int len, int window) {
+  return len > 0 ? (len - (window_begin(len, window) & ~15) + kTok - 1) / kTok : 0;
+}
+__device__ __forceinline__ int clamped_len(const LatentArgs& a, int b) { return min(max(a.c.seq_lens[b], 0), a.c.S_cap); }
+
+// four codes as stored -> two words of exact fp16 numbers
+__device__ __forceinline__ uint2 halves_of(uint32_t w) {
+  const __half2 k = __half2half2(__ushort_as_half(0x6480));  // 1024 + 128
+  const uint32_t lo = __byte_perm(w, 0x64646464u, 0x4140), hi = __byte_perm(w, 0x64646464u, 0x4342);
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&lo), k), y = __hsub2(*reinterpret_cast<const __half2*>(&hi), k);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+}
+
+template <int DC, int N, bool TEST>
+__global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a, int groups, int per_group, const Hook hook) {
+  using C = Cfg<DC, N>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  auto& sm = *reinterpret_cast<Small<DC, N>*>(smem + C::SMALL);
+  static_assert(sizeof(Small<DC, N>) <= C::SMALL_BYTES, "");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t base = smem_addr(smem);
+  auto bar = [&](int i) { return smem_addr(&sm.bars[i]); };
+  volatile int* const stop = &sm.stop;
+  const long long tile_wait = TEST ? hook.wait_cycles : kTileWait;
+  const int group = blockIdx.x % groups, line = blockIdx.x / groups, lines = gridDim.x / groups;
+  const int h0 = group * per_group, heads = min(per_group, a.H - h0);
+
+  if (warp == kMmaWarp) tmem_alloc(smem_addr(&sm.tmem), C::COLS);
+  if (tid == 0) {
+    for (int i = 0; i < C::NB * C::UNITS; ++i) {
+      mbar_init(bar(C::FULL + i), kConv);
+      mbar_init(bar(C::EMPTY + i), 1);
+    }
+    mbar_init(bar(C::SCORES), 1);
+    mbar_init(bar(C::SCORES + 1), 1);
+    mbar_init(bar(C::WEIGHTS), kSoft);
+    mbar_init(bar(C::DONE), 1);
+    mbar_init(bar(C::QUERY), kConv);
+    mbar_init(bar(C::QUERY_FREE), 1);
+    mbar_init(bar(C::DRAINED), kSoft);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(C::WORK + i), 1);
+      mbar_init(bar(C::WORK_FREE + i), kSoft + kConv + 1);
+      mbar_init(bar(C::PAGES + i), 1);
+      mbar_init(bar(C::PAGES_FREE + i), kSoft + kConv);
+    }
+    mbar_init(bar(C::END), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    sm.stop = 0;
+    sm.start_b = a.c.B;
+    sm.start_p = 0;
+  }
   pdl_launch_dependents();
   pdl_wait();
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int len = checked_len(a.c.seq_lens, b, a.c.S_cap, h == 0 ? a.status : nullptr);
-  const int lo = window_begin(len, a.window);
-  const uint16_t* qc = static_cast<const uint16_t*>(a.q_c.data) + b * a.q_c.row_stride + h * a.q_c.head_stride;
-  const uint16_t* qr = static_cast<const uint16_t*>(a.q_r.data) + b * a.q_r.row_stride + h * a.q_r.head_stride;
-  for (int i = tid; i < DC + kRope; i += kThreads) q[i] = to_float<DT>(i < DC ? qc[i] : qr[i - DC]);
-  float m = -INFINITY, l = 0.0f, o[(DC + kThreads - 1) / kThreads] = {};
-  for (int t0 = lo & ~15; t0 < len; t0 += kTile) {
+
+  // ---- this thread block's share of the line: [x0, x1), and the sequence it begins in
+  {
+    int sum = 0;
+    for (int b = tid; b < a.c.B; b += kThreads) sum += tiles_of(clamped_len(a, b), a.window) + kFixed;
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    if (lane == 0) sm.sums[warp] = sum;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  int length = 0;
+  for (int i = 0; i < kWarps; ++i) length += sm.sums[i];
+  const int share = max(kMinShare, (length + lines - 1) / lines);
+  const int x0 = min(line * share, length), x1 = min(x0 + share, length);
+  for (int b0 = 0, p0 = 0; b0 < a.c.B && p0 <= x0; b0 += kThreads) {
     __syncthreads();
-    if (tid < kTile / 16 && t0 + 16 * tid < len) {
-      bool ok;
-      at[tid] = latent_block(a.c, b, (t0 >> 4) + tid, ok);
-      if (!ok && a.status) atomicOr(a.status, TQ_STATUS_BAD_PAGE);
+    const int b = b0 + tid, cost = b < a.c.B ? tiles_of(clamped_len(a, b), a.window) + kFixed : 0;
+    int upto = cost;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += y;
     }
+    if (lane == 31) sm.sums[warp] = upto;
     __syncthreads();
-    for (int i = warp; i < kTile; i += kThreads / 32) {
-      const int t = t0 + i;
-      float z = -INFINITY;
-      if (t >= lo && t < len) {
-        const uint8_t* blk = a.c.blocks + at[i >> 4] * latent_block_bytes(DC);
-        const float2 s = *reinterpret_cast<const float2*>(blk + latent_scale_offset(DC, t & 15));
-        float zc = 0.0f, zr = 0.0f;
-        for (int c = lane; c < DC; c += 32) zc += q[c] * (blk[latent_code_offset(DC, t & 15, c)] - 128.0f);
-        const __half* r = reinterpret_cast<const __half*>(blk + latent_rope_offset(DC, t & 15));
-        for (int c = lane; c < kRope; c += 32) zr += q[DC + c] * __half2float(r[c]);
-        zc = zc * (s.x / 127.0f) + zr * s.y;
-        for (int off = 16; off > 0; off >>= 1) zc += __shfl_xor_sync(0xffffffffu, zc, off);
-        z = zc * a.attn_scale;
+    int before = p0;
+    for (int i = 0; i < kWarps; ++i) {
+      before += i < warp ? sm.sums[i] : 0;
+      p0 += sm.sums[i];
+    }
+    const int p = before + upto - cost;
+    if (cost > 0 && p <= x0 && x0 < p + cost) {
+      sm.start_b = b;
+      sm.start_p = p;
+    }
+  }
+  __syncthreads();
+  const uint32_t tmem = sm.tmem;
+
+  // the it-th piece of work, for every warp but the one that finds it; false: none, or the block winds down
+  auto next_work = [&](int it, Work& w, bool live) {
+    if (live) live = warp_wait_on(bar(C::WORK + (it & 1)), (it >> 1) & 1, stop, kBlockWait);
+    w = sm.work[it & 1];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(C::WORK_FREE + (it & 1)));
+    return live;
+  };
+
+  if (warp < kSoft) {
+    // =========================================================================================== softmax, epilogue
+    // The four warps meet at named barriers, so none leaves the others: a warp whose wait ran out goes on without waiting
+    // (what it computes means nothing then), and they leave together between pieces of work.
+    const int row = 16 * warp + (lane & 15), hbase = (lane >> 4) * C::HN;
+    const uint32_t quarter = static_cast<uint32_t>(32 * warp) << 16;
+    uint8_t* const p_row = smem + C::P + row * 128;
+    float* const parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + info_bytes(a.c.B));
+    bool live = true;
+    uint32_t tile = 0, batch = 0, pieces = 0;  // tiles, batches of pages, pieces of work with tiles so far
+    auto wait = [&](uint32_t b, uint32_t parity) {
+      if (live) live = warp_wait_on(b, parity, stop, tile_wait);
+    };
+    Work w;
+    for (int it = 0;; ++it) {
+      const bool got = next_work(it, w, live);
+      if (any_of_group(!got) || !w.more) break;
+      float l[C::HN];
+#pragma unroll
+      for (int i = 0; i < C::HN; ++i) l[i] = 0.0f;
+      // scales of this thread's token, a tile ahead
+      auto scales = [&](int i) {
+        if (i % kBatch == 0) wait(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1);
+        const long long blk = sm.pages[batch & 1][4 * (i % kBatch) + warp];
+        if (i % kBatch == kBatch - 1 || i == w.n - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
+          ++batch;
+        }
+        return *reinterpret_cast<const float2*>(a.c.blocks + (live ? blk : 0) * latent_block_bytes(DC) + latent_scale_offset(DC, row & 15));
+      };
+      float2 next = w.n > 0 ? scales(0) : make_float2(0.0f, 0.0f);
+      for (int i = 0; i < w.n; ++i, ++tile) {
+        const float2 sc = next;
+        if (i + 1 < w.n) next = scales(i + 1);
+        const int at = w.t0 + kTok * i + row;
+        const bool seen = at >= w.lo && at < w.len;
+        // (a token without a range has codes of 0 and counts as the smallest: 2^-64 / 127, about 2^-71)
+        const float unit = seen ? (sc.x > 0.0f ? __fdiv_rn(sc.x, 127.0f) : 0.0f) : 0.0f, pos = seen ? sc.y : 0.0f;
+        const float lg = seen ? (sc.x > 0.0f ? __log2f(unit) : -71.0f) : -INFINITY;
+        const float inv = seen ? (sc.x > 0.0f ? __fdiv_rn(127.0f, sc.x) : 2.3611832414348226e21f) : 0.0f;
+        const uint32_t s_at = tmem + quarter + C::S_COL + (tile & 1) * 2 * N;
+        // (the operands' barrier shows the queries' scales, too)
+        if (i == 0) wait(bar(C::FULL + (tile % C::NB) * C::UNITS), (tile / C::NB) & 1);
+        wait(bar(C::SCORES + (tile & 1)), (tile >> 1) & 1);
+        tc_fence_after();
+        float z[C::HN], e[C::HN];
+        tmem_ld_halves<C::HN>(s_at, reinterpret_cast<uint32_t*>(z));
+        tmem_ld_halves<C::HN>(s_at + N, reinterpret_cast<uint32_t*>(e));
+        tmem_wait_ld();
+        if (__any_sync(0xffffffffu, !seen)) {
+          // (rows that no token was appended to may hold anything)
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) {
+            z[x] = seen ? z[x] : 0.0f;
+            e[x] = seen ? e[x] : 0.0f;
+          }
+        }
+        const uint64_t unit2 = pair(unit, unit), pos2 = pair(pos, pos), lg2 = pair(lg, lg), inv2 = pair(inv, inv);
+        auto consts = [&](const float* c, int x) { return pair(c[hbase + x], c[hbase + x + 1]); };
+#pragma unroll
+        for (int x = 0; x < C::HN; x += 2) {
+          const uint64_t y = fma2(pair(z[x], z[x + 1]), unit2, mul2(pair(e[x], e[x + 1]), pos2));
+          const float2 v = unpair(mul2(y, consts(sm.scale[pieces & 1], x)));
+          z[x] = v.x;
+          z[x + 1] = v.y;
+        }
+        auto exponents = [&] {  // returns the largest
+          float top = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < C::HN; x += 2) {
+            const float2 r = unpair(consts(sm.ref_z, x)), o = unpair(consts(sm.ref_o, x));
+            const float2 v = unpair(add2(add2(add2(pair(z[x], z[x + 1]), pair(-r.x, -r.y)), lg2), pair(-o.x, -o.y)));
+            e[x] = v.x;
+            e[x + 1] = v.y;
+            top = fmaxf(top, fmaxf(v.x, v.y));
+          }
+          return top;
+        };
+        bool raise = i == 0;
+        if (i > 0) raise = exponents() > kMost;
+        if (any_of_group(raise)) {
+          // ref anew: the largest score, then the largest exponent beside it
+          float v[C::HN];
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) v[x] = seen ? z[x] : -INFINITY;
+          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[warp]);
+          group_sync();
+          float new_z = 0.0f;
+          if (tid < N) sm.tmp[tid] = new_z = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid]));
+          group_sync();
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) v[x] = (z[x] - sm.tmp[hbase + x]) + lg;
+          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[warp]);
+          group_sync();
+          if (tid < N) {
+            const float new_o = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid])) - kTop;
+            const float up = (new_z - sm.ref_z[tid]) + (new_o - sm.ref_o[tid]);
+            const bool take = i == 0 || up > kMost - kTop;  // (by itself: no head's result depends on another's)
+            sm.tmp[tid] = take ? ex2(-up) : 1.0f;
+            if (take) {
+              sm.ref_z[tid] = new_z;
+              sm.ref_o[tid] = new_o;
+            }
+          }
+          group_sync();
+          if (i > 0) {
+#pragma unroll
+            for (int x = 0; x < C::HN; ++x) l[x] *= sm.tmp[hbase + x];
+            wait(bar(C::DONE), (tile - 1) & 1);
+            tc_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < C::UNITS * N; x += 16) {
+              uint32_t o[16];
+              tmem_ld16(tmem + quarter + C::O_COL + x, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * sm.tmp[(x + y) % N]);
+              tmem_st16(tmem + quarter + C::O_COL + x, o);
+            }
+            tmem_wait_st();
+          }
+          exponents();
+        }
+        uint32_t p[C::HN / 2];
+#pragma unroll
+        for (int x = 0; x < C::HN; x += 2) {
+          const float e0 = ex2(e[x]), e1 = ex2(e[x + 1]);
+          const float2 s = unpair(fma2(pair(e0, e1), inv2, pair(l[x], l[x + 1])));
+          l[x] = s.x;
+          l[x + 1] = s.y;
+          p[x >> 1] = pack2<TQ_FP16>(e0, e1);
+        }
+        if (tile > 0) wait(bar(C::DONE), (tile - 1) & 1);
+#pragma unroll
+        for (int x = 0; x < C::HN / 8; ++x)
+          *reinterpret_cast<uint4*>(p_row + (((hbase / 8 + x) ^ (row & 7)) << 4)) = make_uint4(p[4 * x], p[4 * x + 1], p[4 * x + 2], p[4 * x + 3]);
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::WEIGHTS));
       }
-      if (lane == 0) p[i] = z;
+      // ---- epilogue: a thread has a channel of every 128, for all heads
+      reduce_half<Sum, C::HN>(l, lane, hbase, sm.red[warp]);
+      group_sync();
+      if (tid < N) {
+        const float sum = (sm.red[0][tid] + sm.red[1][tid]) + (sm.red[2][tid] + sm.red[3][tid]);
+        sm.tmp[tid] = w.part < 0 ? (w.n > 0 ? __fdiv_rn(1.0f, sum) : 0.0f) : 1.0f;
+        if (w.part >= 0) {
+          float* const more = parts + static_cast<long long>(w.part) * part_floats(DC, N) + N * DC;
+          more[tid] = sm.ref_z[tid];
+          more[N + tid] = sm.ref_o[tid];
+          more[2 * N + tid] = sum;
+        }
+      }
+      group_sync();
+      if (w.n > 0) wait(bar(C::DONE), (tile - 1) & 1);
+      tc_fence_after();
+#pragma unroll 1
+      for (int x = 0; x < C::UNITS * N; x += 16) {
+        uint32_t o[16];
+        if (w.n > 0) {
+          tmem_ld16(tmem + quarter + C::O_COL + x, o);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int y = 0; y < 16; ++y) o[y] = 0;
+        }
+        const int head = x % N, channel = 128 * (x / N) + 32 * warp + lane;
+        if (w.part >= 0) {
+          float* const dst = parts + static_cast<long long>(w.part) * part_floats(DC, N) + head * DC + channel;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) dst[y * DC] = __uint_as_float(o[y]);
+        } else {
+          const long long to = (static_cast<long long>(w.b) * a.H + h0 + head) * DC + channel;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            if (head + y >= heads) continue;
+            const float v = __uint_as_float(o[y]) * sm.tmp[head + y];
+            if (a.out_dtype == TQ_FP32) static_cast<float*>(a.out)[to + y * DC] = v;
+            else if (a.out_dtype == TQ_BF16) static_cast<__nv_bfloat16*>(a.out)[to + y * DC] = __float2bfloat16_rn(v);
+            else static_cast<__half*>(a.out)[to + y * DC] = __float2half_rn(v);
+          }
+        }
+      }
+      if (w.n > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::DRAINED));
+        ++pieces;
+      }
+    }
+  } else if (warp < kMmaWarp) {
+    // ================================================================================= queries, codes into operands
+    const int me = tid - 32 * kSoft, cw = warp - kSoft;
+    const int row = me >> 3, piece = me & 7;                   // rows `row` and `row` + 32 of a tile, a 16-byte piece of each
+    const uint32_t to = row * 128 + ((piece ^ (row & 7)) << 4);  // (row + 32 has the same place in its group of 8)
+    bool ok = true;
+    uint32_t tile = 0, batch = 0, queries = 0;
+    Work w;
+    for (int it = 0; ok && next_work(it, w, true) && w.more; ++it) {
+      if (w.n == 0) continue;
+      uint4 code[C::UNITS][2], rope[2];
+      const uint8_t* src[2];
+      auto find = [&](int i) {  // the two rows of tile i
+        if (i % kBatch == 0 && !warp_wait_on(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1, stop, tile_wait)) return false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          src[x] = a.c.blocks + static_cast<long long>(sm.pages[batch & 1][4 * (i % kBatch) + 2 * x + (row >> 4)]) * latent_block_bytes(DC);
+        if (i % kBatch == kBatch - 1 || i == w.n - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
+          ++batch;
+        }
+        return true;
+      };
+      auto load_unit = [&](int u) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) code[u][x] = *reinterpret_cast<const uint4*>(src[x] + DC * (row & 15) + 128 * u + 16 * piece);
+      };
+      auto load_rope = [&] {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) rope[x] = *reinterpret_cast<const uint4*>(src[x] + latent_rope_offset(DC, row & 15) + 16 * piece);
+      };
+      ok = find(0);
+      if (!ok) break;
+      load_rope();
+#pragma unroll
+      for (int u = 0; u < C::UNITS; ++u) load_unit(u);
+      // ---- the queries of this piece's sequence
+      ok = warp_wait_on(bar(C::QUERY_FREE), (queries++ & 1) ^ 1, stop, kBlockWait);
+      if (!ok) break;
+      for (int h = cw; h < N; h += kConv) {
+        constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32;
+        uint4 v[PER];
+        const uint16_t* qc = static_cast<const uint16_t*>(a.q_c.data) + w.b * a.q_c.row_stride + (h0 + h) * a.q_c.head_stride;
+        const uint16_t* qr = static_cast<const uint16_t*>(a.q_r.data) + w.b * a.q_r.row_stride + (h0 + h) * a.q_r.head_stride;
+        uint32_t top = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int c = lane + 32 * x;
+          v[x] = make_uint4(0, 0, 0, 0);
+          if (h < heads && c < CHUNKS) v[x] = *reinterpret_cast<const uint4*>(c < DC / 8 ? qc + 8 * c : qr + 8 * c - DC);
+          top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu)),
+                         __vmaxu2(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu));
+        }
+        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+        const bool bf16 = a.q_dtype == TQ_BF16;
+        const bool bad = top >= (bf16 ? 0x7f80u : 0x7c00u);  // an infinity or a NaN: the head gives NaN
+        const float most = bf16 ? unpack2<TQ_BF16>(top).x : unpack2<TQ_FP16>(top).x;
+        const int ex = most > 0.0f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 15, -126) : 0;
+        const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+        if (lane == 0) sm.scale[(queries & 1) ^ 1][h] = h < heads ? (bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + ex) << 23)) : 0.0f;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int c = lane + 32 * x;
+          if (c >= CHUNKS) continue;
+          const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+          uint32_t o[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = bf16 ? unpack2<TQ_BF16>(y[k]) : unpack2<TQ_FP16>(y[k]);
+            o[k] = bad ? 0 : pack2<TQ_FP16>(__fmul_rn(f.x, up), __fmul_rn(f.y, up));
+          }
+          *reinterpret_cast<uint4*>(smem + C::Q + (c >> 3) * C::QPANEL + h * 128 + (((c & 7) ^ (h & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::QUERY));
+      // ---- tiles
+      for (int i = 0; i < w.n && ok; ++i, ++tile) {
+        const bool more = i + 1 < w.n;
+        if (more && !find(i + 1)) {
+          ok = false;
+          break;
+        }
+        const int buf = tile % C::NB;
+        const uint32_t parity = ((tile / C::NB) & 1) ^ 1;
+        uint8_t* const dst = smem + C::RING + buf * C::TILE + to;
+#pragma unroll
+        for (int u = 0; u < C::UNITS; ++u) {
+          if (ok) ok = warp_wait_on(bar(C::EMPTY + buf * C::UNITS + u), parity, stop, tile_wait);
+          if (!ok) break;
+          if (u == 0) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) *reinterpret_cast<uint4*>(dst + (C::PANELS - 1) * kPanel + 4096 * x) = rope[x];
+            if (more) load_rope();
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint4 k = code[u][x];
+            const uint2 f0 = halves_of(k.x), f1 = halves_of(k.y), f2 = halves_of(k.z), f3 = halves_of(k.w);
+            *reinterpret_cast<uint4*>(dst + 2 * u * kPanel + 4096 * x) = make_uint4(f0.x, f0.y, f1.x, f1.y);
+            *reinterpret_cast<uint4*>(dst + (2 * u + 1) * kPanel + 4096 * x) = make_uint4(f2.x, f2.y, f3.x, f3.y);
+          }
+          if (more) load_unit(u);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && !(TEST && static_cast<int>(tile) == hook.fault_tile)) mbar_arrive(bar(C::FULL + buf * C::UNITS + u));
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ========================================================================================================== MMAs
+    // The warp stays together and its control flow is uniform, see mma_ss.
+    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const uint32_t leader = elect_one(), tm = uniform(tmem);
+    const uint32_t id_s = instr_desc(false, kTok, N, false), id_o = instr_desc(false, 128, N, true) | kMnMajorA;
+    const uint32_t q_lo = desc_lo(base + C::Q, 0), p_lo = desc_lo(base + C::P, 0), k_lo = desc_lo(base + C::RING, 0),
+                   v_lo = desc_lo(base + C::RING, kPanel);
+    bool ok = true;
+    uint32_t tile = 0, pieces = 0;
+    // O^T += codes^T P^T of tile x
+    auto outputs = [&](uint32_t x, bool first) {
+      ok = ok && warp_wait_on(bar(C::WEIGHTS), x & 1, stop, tile_wait);
+      if (ok && first) ok = warp_wait_on(bar(C::DRAINED), (pieces & 1) ^ 1, stop, tile_wait);
+      if (!ok) return;
+      tc_fence_after();
+      const int buf = x % C::NB;
+      const uint32_t v = v_lo + ((buf * C::TILE) >> 4);
+#pragma unroll
+      for (int m = 0; m < C::UNITS; ++m) {
+#pragma unroll
+        for (int y = 0; y < kTok / 16; ++y)
+          mma_ss(leader, tm + C::O_COL + m * N, v + ((2 * m * kPanel + y * 2048) >> 4), p_lo + (y * 2048 >> 4), kDescHi, id_o, y > 0 || !first);
+        mma_commit(leader, bar(C::EMPTY + buf * C::UNITS + m));
+      }
+      mma_commit(leader, bar(C::DONE));
+    };
+    Work w;
+    for (int it = 0; ok && next_work(it, w, true); ++it) {
+      const int n = uniform(w.n);
+      if (!uniform(w.more)) break;
+      if (n == 0) continue;
+      ok = warp_wait_on(bar(C::QUERY), pieces & 1, stop, kBlockWait);
+      for (int i = 0; i < n && ok; ++i, ++tile) {
+        const int buf = tile % C::NB;
+        const uint32_t parity = (tile / C::NB) & 1, d = tm + C::S_COL + (tile & 1) * 2 * N, k = k_lo + ((buf * C::TILE) >> 4);
+#pragma unroll
+        for (int u = 0; u < C::UNITS; ++u) {
+          ok = ok && warp_wait_on(bar(C::FULL + buf * C::UNITS + u), parity, stop, tile_wait);
+          if (!ok) break;
+          tc_fence_after();
+          if (u == 0) {
+#pragma unroll
+            for (int y = 0; y < kRope / 16; ++y)
+              mma_ss(leader, d + N, k + (((C::PANELS - 1) * kPanel + y * 32) >> 4), q_lo + (((C::PANELS - 1) * C::QPANEL + y * 32) >> 4), kDescHi, id_s, y > 0);
+          }
+#pragma unroll
+          for (int y = 8 * u; y < 8 * u + 8; ++y)
+            mma_ss(leader, d, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > 0);
+        }
+        if (!ok) break;
+        mma_commit(leader, bar(C::SCORES + (tile & 1)));
+        if (i + 1 == n) mma_commit(leader, bar(C::QUERY_FREE));
+        if (i > 0) outputs(tile - 1, i == 1);
+      }
+      if (ok) outputs(tile - 1, n == 1);
+      ++pieces;
+    }
+    // everything issued has completed before the block gives its memory back
+    mma_commit(leader, bar(C::END));
+    if (!__all_sync(0xffffffffu, wait_stage_inline(bar(C::END), 0, kTileWait))) *stop = 1;
+  } else {
+    // ============================================================================================ the work, and pages
+    int2* const info = static_cast<int2*>(a.workspace);
+    int b = sm.start_b, p = sm.start_p, it = 0, known = 0, first = b;  // lane i holds the length of sequence first + i
+    bool ok = true;
+    uint32_t batch = 0;
+    auto post = [&](const Work& w) {
+      ok = warp_wait_on(bar(C::WORK_FREE + (it & 1)), ((it >> 1) & 1) ^ 1, stop, kBlockWait);
+      if (!ok) return;
+      if (lane == 0) {
+        sm.work[it & 1] = w;
+        mbar_arrive(bar(C::WORK + (it & 1)));
+      }
+      ++it;
+    };
+    for (bool fresh = true; b < a.c.B && p < x1 && x0 < x1 && ok; ++b) {
+      if (fresh || b - first == 32) {
+        first = b;
+        known = b + lane < a.c.B ? a.c.seq_lens[b + lane] : 0;
+        fresh = false;
+      }
+      const int raw = __shfl_sync(0xffffffffu, known, b - first), len = min(max(raw, 0), a.c.S_cap);
+      const int n = tiles_of(len, a.window), lo = window_begin(len, a.window);
+      const int k0 = max(0, x0 - p - kFixed), k1 = min(n, x1 - p - kFixed);
+      if (k1 > k0 || (n == 0 && p >= x0)) {
+        const int first_line = (p + kFixed) / share, parts = n > 0 ? (p + kFixed + n - 1) / share - first_line + 1 : 1;
+        if (k0 == 0 && group == 0 && lane == 0) {
+          info[b] = make_int2(first_line, parts);
+          const int bits = (raw != len ? TQ_STATUS_BAD_LEN : 0) | (len == 0 ? TQ_STATUS_EMPTY_SEQ : 0);
+          if (bits && a.status) atomicOr(a.status, bits);
+        }
+        Work w;
+        w.b = b;
+        w.n = max(0, k1 - k0);
+        w.t0 = (lo & ~15) + kTok * k0;
+        w.lo = lo;
+        w.len = len;
+        w.part = parts > 1 ? (2 * line + (k0 == 0)) * groups + group : -1;
+        w.more = 1;
+        post(w);
+        const int last = (len - 1) >> 4;
+        for (int i = 0; i < w.n && ok; i += kBatch, ++batch) {
+          ok = warp_wait_on(bar(C::PAGES_FREE + (batch & 1)), ((batch >> 1) & 1) ^ 1, stop, kBlockWait);
+          if (!ok) break;
+          const int j = (w.t0 >> 4) + 4 * i + lane;
+          bool good;
+          const long long blk = latent_block(a.c, b, min(j, last), good);
+          if (!good && a.status) atomicOr(a.status, TQ_STATUS_BAD_PAGE);
+          sm.pages[batch & 1][lane] = static_cast<int>(blk);
+          if (j <= last && lane < 4 * (w.n - i))
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC)), "r"(latent_block_bytes(DC)) : "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::PAGES + (batch & 1)));
+        }
+      }
+      p += n + kFixed;
+    }
+    if (ok) post(Work{});
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_free(tmem, C::COLS);
+  if (tid == 0 && sm.stop && a.status) atomicOr(a.status, TQ_STATUS_TIMEOUT);
+}
+
+// ---- joining: out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^(ref_i - max ref)
+// A thread has four channels of a head; LANES threads share the parts of such a piece.
+constexpr int kJoin = 256;
+
+template <int DC, int N>
+__global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines, int lanes) {
+  __shared__ float4 s_sum[kJoin];
+  __shared__ float s_z[32], s_o[32], s_l[kJoin];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int tid = threadIdx.x;
+  const int columns = kJoin / lanes, chunks = DC / 4 / columns;
+  const float* const parts = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + info_bytes(a.c.B));
+  const int2* const info = static_cast<const int2*>(a.workspace);
+  const long long pieces = static_cast<long long>(a.c.B) * a.H * chunks;
+  for (long long x = blockIdx.x; x < pieces; x += gridDim.x) {
+    const int b = static_cast<int>(x / (static_cast<long long>(a.H) * chunks)), y = static_cast<int>(x % (static_cast<long long>(a.H) * chunks));
+    const int h = y / chunks, chunk = y % chunks;
+    const int2 in = info[b];  // first line, number of parts
+    // (the second: what a call that gave up has left behind)
+    if (in.y < 2 || in.x < 0 || in.y > lines - in.x) continue;
+    const int group = h / per_group, head = h % per_group;
+    auto part = [&](int i) { return parts + static_cast<long long>((2 * (in.x + i) + (i == 0)) * groups + group) * part_floats(DC, N); };
+    // ref of the joined row: the largest score part, and the largest of the rest beside it
+    float z = -INFINITY;
+    for (int i = tid; i < in.y; i += kJoin) z = fmaxf(z, part(i)[N * DC + head]);
+    auto block_max = [&](float v, float* s) {
+      for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+      if ((tid & 31) == 0) s[tid >> 5] = v;
+      __syncthreads();
+      v = s[0];
+      for (int i = 1; i < kJoin / 32; ++i) v = fmaxf(v, s[i]);
+      return v;
+    };
+    z = block_max(z, s_z);
+    float o = -INFINITY;
+    for (int i = tid; i < in.y; i += kJoin) o = fmaxf(o, (part(i)[N * DC + head] - z) + part(i)[N * DC + N + head]);
+    o = block_max(o, s_o);
+    const int column = chunk * columns + tid % columns, first = tid / columns;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float l = 0.0f;
+#pragma unroll 4
+    for (int i = first; i < in.y; i += lanes) {
+      const float* const q = part(i);
+      const float4 v = *reinterpret_cast<const float4*>(q + head * DC + 4 * column);
+      const float f = ex2((q[N * DC + head] - z) + (q[N * DC + N + head] - o));
+      sum.x = fmaf(f, v.x, sum.x);
+      sum.y = fmaf(f, v.y, sum.y);
+      sum.z = fmaf(f, v.z, sum.z);
+      sum.w = fmaf(f, v.w, sum.w);
+      l = fmaf(f, q[N * DC + 2 * N + head], l);
+    }
+    s_sum[tid] = sum;
+    s_l[tid] = l;
+    __syncthreads();
+    if (tid < columns) {
+      for (int i = 1; i < lanes; ++i) {
+        const float4 v = s_sum[tid + i * columns];
+        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        l += s_l[tid + i * columns];
+      }
+      const float inv = __fdiv_rn(1.0f, l);
+      const long long to = (static_cast<long long>(b) * a.H + h) * DC + 4 * column;
+      const float4 v = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+      if (a.out_dtype == TQ_FP32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = v;
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) =
+          a.out_dtype == TQ_BF16 ? make_uint2(pack2<TQ_BF16>(v.x, v.y), pack2<TQ_BF16>(v.z, v.w)) : make_uint2(pack2<TQ_FP16>(v.x, v.y), pack2<TQ_FP16>(v.z, v.w));
     }
     __syncthreads();
-    float top = m;
-    for (int i = 0; i < kTile; ++i) top = fmaxf(top, p[i]);
-    const float scale = m == -INFINITY ? 0.0f : expf(m - top);
-    m = top;
-    l *= scale;
-#pragma unroll
-    for (float& x : o) x *= scale;
-    // (sums of a tile of their own: a long row added token by token would lose digits)
-    float tile_l = 0.0f, tile_o[(DC + kThreads - 1) / kThreads] = {};
-    for (int i = 0; i < kTile; ++i) {
-      const int t = t0 + i;
-      if (t < lo || t >= len) continue;
-      const uint8_t* blk = a.c.blocks + at[i >> 4] * latent_block_bytes(DC);
-      const float w = expf(p[i] - m);
-      tile_l += w;
-      const float ws = w * (*reinterpret_cast<const float*>(blk + latent_scale_offset(DC, t & 15)) / 127.0f);
-      for (int c = tid, x = 0; c < DC; c += kThreads, ++x) tile_o[x] += ws * (blk[latent_code_offset(DC, t & 15, c)] - 128.0f);
-    }
-    l += tile_l;
-#pragma unroll
-    for (int x = 0; x < (DC + kThreads - 1) / kThreads; ++x) o[x] += tile_o[x];
   }
-  const long long to = (static_cast<long long>(b) * a.H + h) * DC;
-  for (int c = tid, x = 0; c < DC; c += kThreads, ++x) {
-    const float y = len > 0 ? o[x] / l : 0.0f;
-    if (OT == TQ_FP32) static_cast<float*>(a.out)[to + c] = y;
-    else static_cast<uint16_t*>(a.out)[to + c] = static_cast<uint16_t>(pack2<DT>(y, y));
+}
+
+// ---- host
+
+// Heads of a thread block (of N columns), and groups of them: at most 64, shared out evenly.
+struct Shape {
+  int groups, per_group, n, lines;
+};
+Shape shape_of(int H) {
+  Shape s;
+  s.groups = (H + 63) / 64;
+  s.per_group = (H + s.groups - 1) / s.groups;
+  s.n = s.per_group <= 16 ? 16 : (s.per_group <= 32 ? 32 : 64);
+  s.lines = device_sm_count() / s.groups;
+  if (s.lines < 1) s.lines = 1;
+  return s;
+}
+
+template <int DC, int N, bool TEST = false>
+cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook hook = {}) {
+  using C = Cfg<DC, N>;
+  if constexpr (DC == 512 && !TEST) {
+    const int limit = test_hooks().spin_limit.load(std::memory_order_relaxed), fault = test_hooks().fault_block.load(std::memory_order_relaxed);
+    if (limit > 0 || fault >= 0) return launch_n<DC, N, true>(a, s, st, {limit > 0 ? limit : static_cast<int>(kTileWait), fault});
   }
+  auto* kernel = latent_kernel<DC, N, TEST>;
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit) || !bit) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM)) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  // no more lines than the longest possible one has shares
+  const long long longest = static_cast<long long>(a.c.B) * ((a.max_len + kTok - 1) / kTok + 1 + kFixed);
+  const long long most = (longest + kMinShare - 1) / kMinShare;
+  const int lines = most < s.lines ? static_cast<int>(most) : s.lines;
+  if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, a, s.groups, s.per_group, hook)) return e;
+  if (lines == 1) return cudaSuccess;  // nothing is cut
+  // threads that share a piece's parts: as many as there are parts, about, but pieces enough for the GPU
+  int lanes = kJoin / (DC / 4);
+  while (lanes < 16 && static_cast<long long>(a.c.B) * a.H * (lanes * DC / 4 / kJoin) < 2 * device_sm_count() && lanes * a.c.B < lines) lanes *= 2;
+  const long long pieces = static_cast<long long>(a.c.B) * a.H * (DC / 4 / (kJoin / lanes));
+  const long long blocks = 8LL * device_sm_count();
+  return launch_kernel(latent_join_kernel<DC, N>, dim3(static_cast<unsigned>(pieces < blocks ? pieces : blocks)), dim3(kJoin), 0, st, a, s.groups,
+                       s.per_group, lines, lanes);
 }
 
 template <int DC>
 cudaError_t launch_dc(const LatentArgs& a, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.H), static_cast<unsigned>(a.c.B));
-  if (a.q_dtype == TQ_BF16)
-    return a.out_dtype == TQ_FP32 ? launch_kernel(latent_decode_kernel<DC, TQ_BF16, TQ_FP32>, grid, dim3(kThreads), 0, st, a)
-                                  : launch_kernel(latent_decode_kernel<DC, TQ_BF16, TQ_BF16>, grid, dim3(kThreads), 0, st, a);
-  return a.out_dtype == TQ_FP32 ? launch_kernel(latent_decode_kernel<DC, TQ_FP16, TQ_FP32>, grid, dim3(kThreads), 0, st, a)
-                                : launch_kernel(latent_decode_kernel<DC, TQ_FP16, TQ_FP16>, grid, dim3(kThreads), 0, st, a);
+  const Shape s = shape_of(a.H);
+  if (s.n == 16) return launch_n<DC, 16>(a, s, st);
+  return s.n == 32 ? launch_n<DC, 32>(a, s, st) : launch_n<DC, 64>(a, s, st);
 }
 
 }  // namespace
 
 size_t latent_workspace_bytes(int B, int H, int d_c) {
-  return 256 + 16 * static_cast<size_t>(B) + 2 * static_cast<size_t>(device_sm_count()) * (H <= 16 ? 16 : (H <= 32 ? 32 : 64)) * (d_c + 2) * 4;
+  const Shape s = shape_of(H);
+  return info_bytes(B) + 2 * static_cast<size_t>(s.lines) * s.groups * part_floats(d_c, s.n) * 4;
 }
 
 cudaError_t launch_latent_decode(const LatentArgs& a, cudaStream_t st) {

@@ -80,6 +80,49 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
       : "memory");
 }
 
+// 16 consecutive columns of the lane's row
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      : TQ_R8(r, 0), TQ_R8(r, 8)
+      : "r"(addr)
+      : "memory");
+}
+// Rows of an accumulator of 64 rows: the 16 rows of the warp's quarter lie in its first 16 lanes.  Threads 0 .. 15 get
+// COLS columns of their row from the address on, threads 16 .. 31 those of the same rows COLS columns further.
+template <int COLS>
+__device__ __forceinline__ void tmem_ld_halves(uint32_t addr, uint32_t* r) {
+  static_assert(COLS == 8 || COLS == 16 || COLS == 32, "");
+  if constexpr (COLS == 8) {
+    asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], 8;\n" : TQ_R8(r, 0) : "r"(addr) : "memory");
+  } else if constexpr (COLS == 16) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x32bx2.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16], 16;\n"
+        : TQ_R8(r, 0), TQ_R8(r, 8)
+        : "r"(addr)
+        : "memory");
+  } else {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x32bx2.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+        "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32], 32;\n"
+        : TQ_R8(r, 0), TQ_R8(r, 8), TQ_R8(r, 16), TQ_R8(r, 24)
+        : "r"(addr)
+        : "memory");
+  }
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if one of them is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // ---- descriptors
 // Shared-memory operand in 128-byte rows, 128-byte swizzle (what a tensor map with that swizzle writes): groups of 8
 // rows are 1024 bytes apart.  K-major (rows along M or N): `lead` is not used.  MN-major (rows along K, 64 elements of
@@ -94,6 +137,7 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, int m, int n, bool 
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 constexpr uint32_t kNegateA = 1u << 13;
+constexpr uint32_t kMnMajorA = 1u << 15;  // rows of A run along K
 
 // One lane of a converged warp, the same one in every call: 1 there, 0 in the others.
 __device__ __forceinline__ uint32_t elect_one() {
