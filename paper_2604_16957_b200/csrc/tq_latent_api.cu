@@ -1,4 +1,6 @@
 // extern "C" entry points of latent attention: argument validation and dispatch.  See include/tq.h.
+#include <initializer_list>
+
 #include "tq_latent.cuh"
 
 namespace tq {
@@ -16,7 +18,10 @@ int check_latent(const tq_latent_cache* c) {
 }
 
 int check_heads_of(const tq_heads* x, int64_t width) {
-  return x->row_stride >= width && x->head_stride >= width && x->row_stride % 8 == 0 && x->head_stride % 8 == 0 ? TQ_OK : TQ_ERR_SHAPE;
+  // (2^39: what a tensor map can describe)
+  for (const int64_t s : {x->row_stride, x->head_stride})
+    if (s < width || s % 8 || s >= 1LL << 39) return TQ_ERR_SHAPE;
+  return TQ_OK;
 }
 
 }  // namespace
@@ -91,11 +96,7 @@ int tq_sdpa_latent_prompt(const tq_heads* q_n, const tq_heads* q_r, const tq_hea
   if (int r = check_heads_of(q_r, kRope)) return r;
   if (int r = check_heads_of(k_n, d)) return r;
   if (int r = check_heads_of(v, d)) return r;
-  if (kr_stride < kRope || kr_stride % 8) return TQ_ERR_SHAPE;
-  // (what a tensor map can describe)
-  for (const int64_t s : {q_n->row_stride, q_n->head_stride, q_r->row_stride, q_r->head_stride, k_n->row_stride, k_n->head_stride,
-                          v->row_stride, v->head_stride, kr_stride})
-    if (s >= 1LL << 39) return TQ_ERR_SHAPE;
+  if (kr_stride < kRope || kr_stride % 8 || kr_stride >= 1LL << 39) return TQ_ERR_SHAPE;
   if (!aligned(q_n->data, 16) || !aligned(q_r->data, 16) || !aligned(k_n->data, 16) || !aligned(k_r, 16) || !aligned(v->data, 16) ||
       !aligned(out, 16) || !aligned(q_offsets, 4) || !aligned(kv_offsets, 4) || !aligned(status, 4))
     return TQ_ERR_ALIGN;

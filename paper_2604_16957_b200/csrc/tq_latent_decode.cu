@@ -19,9 +19,15 @@
 // The query of a head is multiplied by a power of two that brings its largest channel into [2^15, 2^16) and held in fp16, for
 // either input type.
 //
-// Roles: four warps of softmax and epilogue (a thread has a token and half of the heads: S^T of 64 rows fills 16 lanes of every
-// quarter of TMEM), eight warps that turn codes into operands (a tile's loads are in registers while the tile before is
-// turned), one that issues the MMAs, one that finds the work, looks up pages and asks for the tiles' blocks to be brought to L2.
+// Roles: four or eight warps of softmax and epilogue (a thread has a token and 8 or 16 heads: S^T of 64 rows fills 16 lanes of
+// every quarter of TMEM), eight warps that turn codes into operands, one that issues the MMAs, one that finds the work, looks
+// up pages, asks for the tiles' blocks to be brought to L2 and loads the queries.
+//
+// What bounds it is shared memory: 128 bytes a cycle for the MMAs' operands, the converted codes and everything else.  So the
+// codes go to shared memory once, as K-major rows for the scores, and from the same registers to TMEM, where their
+// transpose is the left operand of O^T: a lane there is a channel, and the thread of a lane has 4 neighbouring channels of every
+// token (d_c = 512; 2, 1 below), one for each of the four row tiles of O^T.  (With O^T's operand read from shared memory a
+// tile took 1.3 to 1.5 times as long: the operands alone were 2560 cycles of 64 heads instead of 2040.)
 //
 // Work: the tiles of all sequences lie on a line, each sequence with kFixed places for its start in front; every thread block
 // takes an equal share.  Sequences that are cut leave partial results (O^T, ref, sums) and a second kernel joins them.
@@ -30,6 +36,7 @@
 #include "tq_async.cuh"
 #include "tq_latent.cuh"
 #include "tq_tcgen05.cuh"
+#include "tq_tensor_map.cuh"
 
 namespace tq {
 namespace {
@@ -37,12 +44,12 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 64;                       // tokens of a tile
 constexpr int kBatch = 8;                      // tiles whose pages are looked up together: a lane per block
-constexpr int kSoft = 4, kConv = 8;            // warps of softmax, of conversion
-constexpr int kMmaWarp = kSoft + kConv, kFeedWarp = kMmaWarp + 1, kWarps = kFeedWarp + 1, kThreads = 32 * kWarps;
+constexpr int kWarps = 14, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 2;                      // what the start of a sequence costs, in tiles
 constexpr int kMinShare = 4;                   // places on the line that a thread block takes at least
 constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
+constexpr float kFar = 1048576.0f;             // scores from which ref is kept in two parts, see the top
 
 // A part: [N][DC] sums, then [N] scores and offsets of ref, and [N] sums of weights.
 __host__ __device__ constexpr int part_floats(int dc, int n) { return n * (dc + 4); }
@@ -51,25 +58,32 @@ __host__ __device__ constexpr size_t info_bytes(int B) { return (8 * static_cast
 template <int DC, int N_>
 struct Cfg {
   static constexpr int N = N_;                         // columns: heads of a thread block
-  static constexpr int HN = N / 2;                     // heads of a softmax thread
-  static constexpr int UNITS = DC / 128;               // a tile's codes are handed over 128 channels at a time
+  static constexpr int SOFT = N == 64 ? 8 : 4;         // softmax warps: four have every second half of N heads between them
+  static constexpr bool TURNED = N < 64;               // O^T's operand: codes transposed into TMEM; or those in shared memory
+  static constexpr int CONV = 12 - SOFT;               // warps that turn codes into operands: one or two sets of four
+  static constexpr int HN = N / (SOFT / 2);            // heads of a softmax thread
+  static constexpr int UNITS = DC / 128;               // row tiles of O^T (TURNED: and channels of a lane)
+  static constexpr int PARTS = TURNED ? 1 : UNITS + 1; // that a tile's shared memory is given back in
   static constexpr int PANELS = DC / 64 + 1;           // 64 channels each; the last one is the positional part
   static constexpr int TILE = PANELS * kPanel;
   static constexpr int QPANEL = N * 128;
   static constexpr int Q = 0, P = Q + PANELS * QPANEL, RING = P + kPanel;
   static constexpr int SMALL_BYTES = 3072;
   static constexpr int FIT = (232448 - SMALL_BYTES - RING) / TILE;
-  static constexpr int NB = FIT < 4 ? FIT : 4;         // tiles in shared memory
+  static constexpr int NB = FIT < 3 ? FIT : 3;         // tiles in shared memory
   static constexpr int SMALL = RING + NB * TILE;
   static constexpr int SMEM = SMALL + SMALL_BYTES;
-  static constexpr int S_COL = 0, O_COL = 4 * N;       // TMEM: two buffers of scores in two parts, then O^T
-  static constexpr int COLS = 8 * N;
-  static_assert(NB >= 2 && SMEM <= 232448 && O_COL + UNITS * N <= COLS && COLS <= 512, "");
+  // TMEM: O^T, two buffers of scores in two parts, two of transposed codes (two tokens a column)
+  static constexpr int O_COL = 0, S_COL = UNITS * N, V_COL = S_COL + 4 * N;
+  static constexpr int NEED = V_COL + (TURNED ? 64 * UNITS : 0), COLS = NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512);
+  static_assert(NB >= 2 && SMEM <= 232448 && NEED <= 512, "");
   // mbarriers
-  static constexpr int FULL = 0, EMPTY = FULL + NB * UNITS;                     // operands: by buffer and unit
-  static constexpr int SCORES = EMPTY + NB * UNITS, WEIGHTS = SCORES + 2, DONE = WEIGHTS + 1;  // S^T, P^T, and O^T += of a tile
-  static constexpr int QUERY = DONE + 1, QUERY_FREE = QUERY + 1, DRAINED = QUERY_FREE + 1;     // O^T has been read
-  static constexpr int WORK = DRAINED + 1, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
+  static constexpr int FULL = 0, EMPTY = FULL + NB;                             // operands of the scores
+  static constexpr int SCORES = EMPTY + NB * PARTS, READ = SCORES + 2;                  // S^T: made, read
+  static constexpr int VALUES = READ + 2, VALUES_FREE = VALUES + 2;             // transposed codes
+  static constexpr int WEIGHTS = VALUES_FREE + 2, DONE = WEIGHTS + 1, DRAINED = DONE + 1;  // P^T; O^T += of a tile; O^T has been read
+  static constexpr int RAW = DRAINED + 1, QUERY = RAW + 1, QUERY_FREE = QUERY + 1, SCALED = QUERY_FREE + 1;  // queries as they are, as operands; their scales read
+  static constexpr int WORK = SCALED + 1, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
                        BARS = END + 1;
 };
 
@@ -80,11 +94,11 @@ struct Work {
 
 template <int DC, int N>
 struct Small {
-  float ref_z[N], ref_o[N], scale[2][N], tmp[N], red[kSoft][N];  // (scale: two pieces of work in turn)
+  float ref_z[N], ref_o[N], scale[N], tmp[N], red[4][N];
   int pages[2][4 * kBatch];
   Work work[2];
   uint64_t bars[Cfg<DC, N>::BARS];
-  int sums[kWarps], start_b, start_p, total, stop;
+  int sums[kWarps], start_b, start_p, far, stop;
   uint32_t tmem;
 };
 
@@ -94,17 +108,21 @@ struct Hook {
   int wait_cycles, fault_tile;
 };
 
-// pred over the four softmax warps: true for all if true for one
+// pred over the softmax threads: true for all if true for one
+template <int THREADS>
 __device__ __forceinline__ bool any_of_group(bool p) {
   uint32_t r;
   asm volatile(
-      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, 1, 128, p;\nselp.u32 %0, 1, 0, q;\n}\n"
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, 1, %2, p;\nselp.u32 %0, 1, 0, q;\n}\n"
       : "=r"(r)
-      : "r"(static_cast<uint32_t>(p))
+      : "r"(static_cast<uint32_t>(p)), "n"(THREADS)
       : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void group_sync() { asm volatile("barrier.cta.sync 1, 128;\n" ::: "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void group_sync() {
+  asm volatile("barrier.cta.sync 1, %0;\n" ::"n"(THREADS) : "memory");
+}
 
 struct Max {
   __device__ static float of(float a, float b) { return fmaxf(a, b); }
@@ -141,16 +159,31 @@ __device__ __forceinline__ int tiles_of(int len, int window) {
 }
 __device__ __forceinline__ int clamped_len(const LatentArgs& a, int b) { return min(max(a.c.seq_lens[b], 0), a.c.S_cap); }
 
-// four codes as stored -> two words of exact fp16 numbers
-__device__ __forceinline__ uint2 halves_of(uint32_t w) {
+// Which code a lane of TMEM has: channels `channel` .. + UNITS - 1 of every token, from byte `byte` on of its codes.
+template <int UNITS>
+struct Lane {
+  int unit, half, piece, low, first;  // 128 channels, 64 of them, 8 of them, 4 of them; the first of the lane's in those
+  __device__ Lane(int quarter, int lane)
+      : unit(quarter / (4 / UNITS)), half(lane >> 4), piece((lane & 15) >> 1), low(lane & 1), first((quarter % (4 / UNITS)) * UNITS) {}
+  __device__ int channel() const { return 128 * unit + 64 * half + 8 * piece + 4 * low + first; }
+  __device__ int word() const { return 128 * unit + 16 * piece + 8 * half + 4 * low; }  // (byte of the four codes that hold them)
+};
+
+// bytes (low, high) of two codes as stored -> exact fp16 numbers
+__device__ __forceinline__ uint32_t codes16(uint32_t bytes, uint32_t selector) {
   const __half2 k = __half2half2(__ushort_as_half(0x6480));  // 1024 + 128
-  const uint32_t lo = __byte_perm(w, 0x64646464u, 0x4140), hi = __byte_perm(w, 0x64646464u, 0x4342);
-  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&lo), k), y = __hsub2(*reinterpret_cast<const __half2*>(&hi), k);
-  return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  const uint32_t w = __byte_perm(bytes, 0x64646464u, selector);
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&w), k);
+  return *reinterpret_cast<const uint32_t*>(&x);
 }
 
+struct QueryMaps {
+  CUtensorMap c, r;
+};
+
 template <int DC, int N, bool TEST>
-__global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a, int groups, int per_group, const Hook hook) {
+__global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_constant__ QueryMaps maps, const LatentArgs a, int groups,
+                                                                        int per_group, const Hook hook) {
   using C = Cfg<DC, N>;
   extern __shared__ __align__(1024) uint8_t smem[];
   auto& sm = *reinterpret_cast<Small<DC, N>*>(smem + C::SMALL);
@@ -162,26 +195,31 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
   const long long tile_wait = TEST ? hook.wait_cycles : kTileWait;
   const int group = blockIdx.x % groups, line = blockIdx.x / groups, lines = gridDim.x / groups;
   const int h0 = group * per_group, heads = min(per_group, a.H - h0);
+  const bool bf16 = a.q_dtype == TQ_BF16;
 
   if (warp == kMmaWarp) tmem_alloc(smem_addr(&sm.tmem), C::COLS);
   if (tid == 0) {
-    for (int i = 0; i < C::NB * C::UNITS; ++i) {
-      mbar_init(bar(C::FULL + i), kConv);
-      mbar_init(bar(C::EMPTY + i), 1);
+    for (int i = 0; i < C::NB; ++i) {
+      mbar_init(bar(C::FULL + i), C::CONV);
+      for (int k = 0; k < C::PARTS; ++k) mbar_init(bar(C::EMPTY + i * C::PARTS + k), 1);
     }
-    mbar_init(bar(C::SCORES), 1);
-    mbar_init(bar(C::SCORES + 1), 1);
-    mbar_init(bar(C::WEIGHTS), kSoft);
-    mbar_init(bar(C::DONE), 1);
-    mbar_init(bar(C::QUERY), kConv);
-    mbar_init(bar(C::QUERY_FREE), 1);
-    mbar_init(bar(C::DRAINED), kSoft);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(C::SCORES + i), 1);
+      mbar_init(bar(C::READ + i), C::SOFT);
+      mbar_init(bar(C::VALUES + i), C::CONV);
+      mbar_init(bar(C::VALUES_FREE + i), 1);
       mbar_init(bar(C::WORK + i), 1);
-      mbar_init(bar(C::WORK_FREE + i), kSoft + kConv + 1);
+      mbar_init(bar(C::WORK_FREE + i), 13);
       mbar_init(bar(C::PAGES + i), 1);
-      mbar_init(bar(C::PAGES_FREE + i), kSoft + kConv);
+      mbar_init(bar(C::PAGES_FREE + i), 12);
     }
+    mbar_init(bar(C::WEIGHTS), C::SOFT);
+    mbar_init(bar(C::DONE), 1);
+    mbar_init(bar(C::DRAINED), C::SOFT);
+    mbar_init(bar(C::RAW), 1);
+    mbar_init(bar(C::QUERY), C::CONV);
+    mbar_init(bar(C::QUERY_FREE), 1);
+    mbar_init(bar(C::SCALED), C::SOFT);
     mbar_init(bar(C::END), 1);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     sm.stop = 0;
@@ -192,40 +230,47 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
   pdl_wait();
 
   // ---- this thread block's share of the line: [x0, x1), and the sequence it begins in
-  {
-    int sum = 0;
-    for (int b = tid; b < a.c.B; b += kThreads) sum += tiles_of(clamped_len(a, b), a.window) + kFixed;
-    sum = __reduce_add_sync(0xffffffffu, sum);
-    if (lane == 0) sm.sums[warp] = sum;
-  }
+  // (thread i looks at sequences i, i + THREADS, ...; one of so few that a round will do is looked at once)
+  const bool one_round = a.c.B <= kThreads;
+  int cost = tid < a.c.B ? tiles_of(clamped_len(a, tid), a.window) + kFixed : 0;
+  auto scan = [&](int v) {  // over the thread block's threads: up to and with this one
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, v, off);
+      if (lane >= off) v += y;
+    }
+    __syncthreads();
+    if (lane == 31) sm.sums[warp] = v;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) v += sm.sums[i];
+    return v;
+  };
+  auto total = [&] {
+    int v = 0;
+    for (int i = 0; i < kWarps; ++i) v += sm.sums[i];
+    return v;
+  };
+  int sum = cost;
+  if (!one_round)
+    for (int b = tid + kThreads; b < a.c.B; b += kThreads) sum += tiles_of(clamped_len(a, b), a.window) + kFixed;
   tc_fence_before();
-  __syncthreads();
+  int upto = scan(sum);
   tc_fence_after();
-  int length = 0;
-  for (int i = 0; i < kWarps; ++i) length += sm.sums[i];
+  const int length = total();
   const int share = max(kMinShare, (length + lines - 1) / lines);
   const int x0 = min(line * share, length), x1 = min(x0 + share, length);
   for (int b0 = 0, p0 = 0; b0 < a.c.B && p0 <= x0; b0 += kThreads) {
-    __syncthreads();
-    const int b = b0 + tid, cost = b < a.c.B ? tiles_of(clamped_len(a, b), a.window) + kFixed : 0;
-    int upto = cost;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, upto, off);
-      if (lane >= off) upto += y;
+    if (!one_round) {
+      const int b = b0 + tid;
+      cost = b < a.c.B ? tiles_of(clamped_len(a, b), a.window) + kFixed : 0;
+      upto = scan(cost);
     }
-    if (lane == 31) sm.sums[warp] = upto;
-    __syncthreads();
-    int before = p0;
-    for (int i = 0; i < kWarps; ++i) {
-      before += i < warp ? sm.sums[i] : 0;
-      p0 += sm.sums[i];
-    }
-    const int p = before + upto - cost;
+    const int p = p0 + upto - cost;
     if (cost > 0 && p <= x0 && x0 < p + cost) {
-      sm.start_b = b;
+      sm.start_b = b0 + tid;
       sm.start_p = p;
     }
+    p0 += total();
   }
   __syncthreads();
   const uint32_t tmem = sm.tmem;
@@ -239,12 +284,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
     return live;
   };
 
-  if (warp < kSoft) {
+  if (warp < C::SOFT) {
     // =========================================================================================== softmax, epilogue
-    // The four warps meet at named barriers, so none leaves the others: a warp whose wait ran out goes on without waiting
+    // The warps meet at named barriers, so none leaves the others: a warp whose wait ran out goes on without waiting
     // (what it computes means nothing then), and they leave together between pieces of work.
-    const int row = 16 * warp + (lane & 15), hbase = (lane >> 4) * C::HN;
-    const uint32_t quarter = static_cast<uint32_t>(32 * warp) << 16;
+    const int wq = warp & 3, column0 = (warp >> 2) * 2 * C::HN;  // quarter of TMEM, first head of the warp
+    const int row = 16 * wq + (lane & 15), hbase = column0 + (lane >> 4) * C::HN;
+    const uint32_t quarter = static_cast<uint32_t>(32 * wq) << 16;
     uint8_t* const p_row = smem + C::P + row * 128;
     float* const parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + info_bytes(a.c.B));
     bool live = true;
@@ -255,14 +301,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
     Work w;
     for (int it = 0;; ++it) {
       const bool got = next_work(it, w, live);
-      if (any_of_group(!got) || !w.more) break;
-      float l[C::HN];
+      if (any_of_group<32 * C::SOFT>(!got) || !w.more) break;
+      float l[C::HN], ref[C::HN], scale[C::HN];
+      bool far = false;
 #pragma unroll
-      for (int i = 0; i < C::HN; ++i) l[i] = 0.0f;
+      for (int i = 0; i < C::HN; ++i) {
+        l[i] = 0.0f;
+        scale[i] = a.attn_scale * kLog2e;
+      }
       // scales of this thread's token, a tile ahead
       auto scales = [&](int i) {
         if (i % kBatch == 0) wait(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1);
-        const long long blk = sm.pages[batch & 1][4 * (i % kBatch) + warp];
+        const long long blk = sm.pages[batch & 1][4 * (i % kBatch) + wq];
         if (i % kBatch == kBatch - 1 || i == w.n - 1) {
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
@@ -280,15 +330,24 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
         const float unit = seen ? (sc.x > 0.0f ? __fdiv_rn(sc.x, 127.0f) : 0.0f) : 0.0f, pos = seen ? sc.y : 0.0f;
         const float lg = seen ? (sc.x > 0.0f ? __log2f(unit) : -71.0f) : -INFINITY;
         const float inv = seen ? (sc.x > 0.0f ? __fdiv_rn(127.0f, sc.x) : 2.3611832414348226e21f) : 0.0f;
-        const uint32_t s_at = tmem + quarter + C::S_COL + (tile & 1) * 2 * N;
-        // (the operands' barrier shows the queries' scales, too)
-        if (i == 0) wait(bar(C::FULL + (tile % C::NB) * C::UNITS), (tile / C::NB) & 1);
-        wait(bar(C::SCORES + (tile & 1)), (tile >> 1) & 1);
+        const int buf = tile % 2;
+        const uint32_t s_at = tmem + quarter + C::S_COL + buf * 2 * N + column0;
+        if (i == 0 && bf16) {
+          wait(bar(C::QUERY), pieces & 1);
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) scale[x] = sm.scale[hbase + x];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::SCALED));
+        }
+        wait(bar(C::SCORES + buf), (tile / 2) & 1);
         tc_fence_after();
         float z[C::HN], e[C::HN];
         tmem_ld_halves<C::HN>(s_at, reinterpret_cast<uint32_t*>(z));
         tmem_ld_halves<C::HN>(s_at + N, reinterpret_cast<uint32_t*>(e));
         tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::READ + buf));
         if (__any_sync(0xffffffffu, !seen)) {
           // (rows that no token was appended to may hold anything)
 #pragma unroll
@@ -298,11 +357,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
           }
         }
         const uint64_t unit2 = pair(unit, unit), pos2 = pair(pos, pos), lg2 = pair(lg, lg), inv2 = pair(inv, inv);
-        auto consts = [&](const float* c, int x) { return pair(c[hbase + x], c[hbase + x + 1]); };
 #pragma unroll
         for (int x = 0; x < C::HN; x += 2) {
           const uint64_t y = fma2(pair(z[x], z[x + 1]), unit2, mul2(pair(e[x], e[x + 1]), pos2));
-          const float2 v = unpair(mul2(y, consts(sm.scale[pieces & 1], x)));
+          const float2 v = unpair(mul2(y, pair(scale[x], scale[x + 1])));
           z[x] = v.x;
           z[x + 1] = v.y;
         }
@@ -310,8 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
           float top = -INFINITY;
 #pragma unroll
           for (int x = 0; x < C::HN; x += 2) {
-            const float2 r = unpair(consts(sm.ref_z, x)), o = unpair(consts(sm.ref_o, x));
-            const float2 v = unpair(add2(add2(add2(pair(z[x], z[x + 1]), pair(-r.x, -r.y)), lg2), pair(-o.x, -o.y)));
+            float2 v = unpair(add2(add2(pair(z[x], z[x + 1]), pair(-ref[x], -ref[x + 1])), lg2));
+            if (far) v = make_float2(v.x - sm.ref_o[hbase + x], v.y - sm.ref_o[hbase + x + 1]);
             e[x] = v.x;
             e[x + 1] = v.y;
             top = fmaxf(top, fmaxf(v.x, v.y));
@@ -320,38 +378,44 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
         };
         bool raise = i == 0;
         if (i > 0) raise = exponents() > kMost;
-        if (any_of_group(raise)) {
+        if (any_of_group<32 * C::SOFT>(raise)) {
           // ref anew: the largest score, then the largest exponent beside it
           float v[C::HN];
 #pragma unroll
           for (int x = 0; x < C::HN; ++x) v[x] = seen ? z[x] : -INFINITY;
-          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[warp]);
-          group_sync();
+          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[wq]);
+          group_sync<32 * C::SOFT>();
           float new_z = 0.0f;
+          if (tid == 0) sm.far = 0;
           if (tid < N) sm.tmp[tid] = new_z = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid]));
-          group_sync();
+          group_sync<32 * C::SOFT>();
 #pragma unroll
           for (int x = 0; x < C::HN; ++x) v[x] = (z[x] - sm.tmp[hbase + x]) + lg;
-          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[warp]);
-          group_sync();
+          reduce_half<Max, C::HN>(v, lane, hbase, sm.red[wq]);
+          group_sync<32 * C::SOFT>();
           if (tid < N) {
             const float new_o = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid])) - kTop;
             const float up = (new_z - sm.ref_z[tid]) + (new_o - sm.ref_o[tid]);
             const bool take = i == 0 || up > kMost - kTop;  // (by itself: no head's result depends on another's)
             sm.tmp[tid] = take ? ex2(-up) : 1.0f;
             if (take) {
-              sm.ref_z[tid] = new_z;
-              sm.ref_o[tid] = new_o;
+              const bool apart = fabsf(new_z) > kFar;
+              sm.ref_z[tid] = apart ? new_z : new_z + new_o;
+              sm.ref_o[tid] = apart ? new_o : 0.0f;
             }
+            if (sm.ref_o[tid] != 0.0f) sm.far = 1;
           }
-          group_sync();
+          group_sync<32 * C::SOFT>();
+          far = sm.far != 0;
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) ref[x] = sm.ref_z[hbase + x];
           if (i > 0) {
 #pragma unroll
             for (int x = 0; x < C::HN; ++x) l[x] *= sm.tmp[hbase + x];
             wait(bar(C::DONE), (tile - 1) & 1);
             tc_fence_after();
 #pragma unroll 1
-            for (int x = 0; x < C::UNITS * N; x += 16) {
+            for (int x = 16 * (warp >> 2); x < C::UNITS * N; x += 4 * C::SOFT) {
               uint32_t o[16];
               tmem_ld16(tmem + quarter + C::O_COL + x, o);
               tmem_wait_ld();
@@ -381,9 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::WEIGHTS));
       }
-      // ---- epilogue: a thread has a channel of every 128, for all heads
-      reduce_half<Sum, C::HN>(l, lane, hbase, sm.red[warp]);
-      group_sync();
+      // ---- epilogue: a thread has UNITS neighbouring channels, for all heads
+      reduce_half<Sum, C::HN>(l, lane, hbase, sm.red[wq]);
+      group_sync<32 * C::SOFT>();
       if (tid < N) {
         const float sum = (sm.red[0][tid] + sm.red[1][tid]) + (sm.red[2][tid] + sm.red[3][tid]);
         sm.tmp[tid] = w.part < 0 ? (w.n > 0 ? __fdiv_rn(1.0f, sum) : 0.0f) : 1.0f;
@@ -394,33 +458,48 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
           more[2 * N + tid] = sum;
         }
       }
-      group_sync();
+      group_sync<32 * C::SOFT>();
       if (w.n > 0) wait(bar(C::DONE), (tile - 1) & 1);
       tc_fence_after();
+      // TURNED: UNITS neighbouring channels (one of each row tile); otherwise one of every 128
+      constexpr int VEC = C::TURNED ? C::UNITS : 1;
+      const int channel = C::TURNED ? Lane<C::UNITS>(wq, lane).channel() : 32 * wq + lane;
 #pragma unroll 1
-      for (int x = 0; x < C::UNITS * N; x += 16) {
-        uint32_t o[16];
+      for (int h = 8 * (warp >> 2); h < N; h += 2 * C::SOFT) {
+        uint32_t o[C::UNITS][8];
         if (w.n > 0) {
-          tmem_ld16(tmem + quarter + C::O_COL + x, o);
+#pragma unroll
+          for (int m = 0; m < C::UNITS; ++m) tmem_ld8(tmem + quarter + C::O_COL + m * N + h, o[m]);
           tmem_wait_ld();
-        } else {
-#pragma unroll
-          for (int y = 0; y < 16; ++y) o[y] = 0;
         }
-        const int head = x % N, channel = 128 * (x / N) + 32 * warp + lane;
-        if (w.part >= 0) {
-          float* const dst = parts + static_cast<long long>(w.part) * part_floats(DC, N) + head * DC + channel;
+        float* const part = w.part >= 0 ? parts + static_cast<long long>(w.part) * part_floats(DC, N) + channel : nullptr;
 #pragma unroll
-          for (int y = 0; y < 16; ++y) dst[y * DC] = __uint_as_float(o[y]);
-        } else {
-          const long long to = (static_cast<long long>(w.b) * a.H + h0 + head) * DC + channel;
+        for (int y = 0; y < 8; ++y) {
 #pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            if (head + y >= heads) continue;
-            const float v = __uint_as_float(o[y]) * sm.tmp[head + y];
-            if (a.out_dtype == TQ_FP32) static_cast<float*>(a.out)[to + y * DC] = v;
-            else if (a.out_dtype == TQ_BF16) static_cast<__nv_bfloat16*>(a.out)[to + y * DC] = __float2bfloat16_rn(v);
-            else static_cast<__half*>(a.out)[to + y * DC] = __float2half_rn(v);
+          for (int m = 0; m < C::UNITS; m += VEC) {
+            float v[VEC];
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[k] = w.n > 0 ? __uint_as_float(o[m + k][y]) * sm.tmp[h + y] : 0.0f;
+            auto store32 = [&](float* dst) {
+              if constexpr (VEC == 4) *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+              else if constexpr (VEC == 2) *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+              else *dst = v[0];
+            };
+            if (part) {
+              store32(part + (h + y) * DC + 128 * m);
+            } else if (h + y < heads) {
+              const long long to = (static_cast<long long>(w.b) * a.H + h0 + h + y) * DC + channel + 128 * m;
+              if (a.out_dtype == TQ_FP32) {
+                store32(static_cast<float*>(a.out) + to);
+              } else {
+                uint16_t* const dst = static_cast<uint16_t*>(a.out) + to;
+                const uint32_t lo = bf16 ? pack2<TQ_BF16>(v[0], v[VEC > 1 ? 1 : 0]) : pack2<TQ_FP16>(v[0], v[VEC > 1 ? 1 : 0]);
+                if constexpr (VEC == 4)
+                  *reinterpret_cast<uint2*>(dst) = make_uint2(lo, bf16 ? pack2<TQ_BF16>(v[2], v[3]) : pack2<TQ_FP16>(v[2], v[3]));
+                else if constexpr (VEC == 2) *reinterpret_cast<uint32_t*>(dst) = lo;
+                else *dst = static_cast<uint16_t>(lo);
+              }
+            }
           }
         }
       }
@@ -433,139 +512,230 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
     }
   } else if (warp < kMmaWarp) {
     // ================================================================================= queries, codes into operands
-    const int me = tid - 32 * kSoft, cw = warp - kSoft;
-    const int row = me >> 3, piece = me & 7;                   // rows `row` and `row` + 32 of a tile, a 16-byte piece of each
-    const uint32_t to = row * 128 + ((piece ^ (row & 7)) << 4);  // (row + 32 has the same place in its group of 8)
+    // A thread has four neighbouring channels of every token of its set (TURNED and d_c < 512: the lane's ones of those), and
+    // 16 bytes of the positional part of every fourth token of the warp's.
+    constexpr int TOK = C::TURNED ? 32 : 16 * C::UNITS, ROPES = 16 / C::CONV;  // tokens of a set
+    constexpr int UNITS = C::TURNED ? C::UNITS : 4;                              // as far as a lane is concerned
+    const int cw = warp - C::SOFT, set = C::TURNED ? cw >> 2 : cw / C::UNITS;
+    const Lane<UNITS> own(C::TURNED ? cw & 3 : cw % C::UNITS, lane);
+    const uint32_t quarter = static_cast<uint32_t>(32 * (cw & 3)) << 16;
+    const int rope0 = 64 / C::CONV * cw + (lane >> 3), piece = lane & 7;  // positional part: 16 bytes of tokens rope0, rope0 + 4, ...
+    // bytes of a word that are the lane's (d_c < 512): of one word; of two words, neighbours side by side
+    const uint32_t mine = UNITS == 2 ? (own.first ? 0x4342u : 0x4140u) : 0x4440u + own.first;
+    const uint32_t both = UNITS == 2 ? (own.first ? 0x7362u : 0x5140u) : 0x0040u + 0x11u * own.first;
     bool ok = true;
-    uint32_t tile = 0, batch = 0, queries = 0;
+    uint32_t tile = 0, batch = 0, pieces = 0;
     Work w;
-    for (int it = 0; ok && next_work(it, w, true) && w.more; ++it) {
-      if (w.n == 0) continue;
-      uint4 code[C::UNITS][2], rope[2];
-      const uint8_t* src[2];
-      auto find = [&](int i) {  // the two rows of tile i
-        if (i % kBatch == 0 && !warp_wait_on(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1, stop, tile_wait)) return false;
+    uint4 rope[ROPES], ahead[ROPES];  // of the tile that is next, of the last one asked for
+    auto rope_next = [&] {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-          src[x] = a.c.blocks + static_cast<long long>(sm.pages[batch & 1][4 * (i % kBatch) + 2 * x + (row >> 4)]) * latent_block_bytes(DC);
-        if (i % kBatch == kBatch - 1 || i == w.n - 1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
-          ++batch;
-        }
-        return true;
-      };
-      auto load_unit = [&](int u) {
+      for (int x = 0; x < ROPES; ++x) rope[x] = ahead[x];
+    };
+    // asks for the values of tile i of the piece
+    auto load = [&](int i, uint32_t (&code)[TOK]) {
+      if (i % kBatch == 0 && !warp_wait_on(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1, stop, tile_wait)) return false;
+      const int* const pages = sm.pages[batch & 1] + 4 * (i % kBatch);
+      {
+        const uint8_t* const blk = a.c.blocks + static_cast<long long>(pages[rope0 >> 4]) * latent_block_bytes(DC) + latent_rope_offset(DC, rope0 & 15);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) code[u][x] = *reinterpret_cast<const uint4*>(src[x] + DC * (row & 15) + 128 * u + 16 * piece);
-      };
-      auto load_rope = [&] {
+        for (int x = 0; x < ROPES; ++x) ahead[x] = *reinterpret_cast<const uint4*>(blk + 4 * 2 * kRope * x + 16 * piece);
+      }
 #pragma unroll
-        for (int x = 0; x < 2; ++x) rope[x] = *reinterpret_cast<const uint4*>(src[x] + latent_rope_offset(DC, row & 15) + 16 * piece);
-      };
-      ok = find(0);
-      if (!ok) break;
-      load_rope();
+      for (int x = 0; x < TOK; x += 16) {
+        const uint8_t* const blk = a.c.blocks + static_cast<long long>(pages[(set * TOK + x) / 16]) * latent_block_bytes(DC) + own.word();
 #pragma unroll
-      for (int u = 0; u < C::UNITS; ++u) load_unit(u);
-      // ---- the queries of this piece's sequence
-      ok = warp_wait_on(bar(C::QUERY_FREE), (queries++ & 1) ^ 1, stop, kBlockWait);
-      if (!ok) break;
-      for (int h = cw; h < N; h += kConv) {
-        constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32;
-        uint4 v[PER];
-        const uint16_t* qc = static_cast<const uint16_t*>(a.q_c.data) + w.b * a.q_c.row_stride + (h0 + h) * a.q_c.head_stride;
-        const uint16_t* qr = static_cast<const uint16_t*>(a.q_r.data) + w.b * a.q_r.row_stride + (h0 + h) * a.q_r.head_stride;
-        uint32_t top = 0;
+        for (int y = 0; y < 16; ++y) code[x + y] = *reinterpret_cast<const uint32_t*>(blk + DC * y);
+      }
+      if (i % kBatch == kBatch - 1 || i == w.n - 1) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
+        ++batch;
+      }
+      return true;
+    };
+    // codes and positional part of a tile into shared memory
+    auto keys = [&](uint32_t x, const uint32_t (&code)[TOK]) {
+      const int buf = x % C::NB;
+      const uint32_t parity = ((x / C::NB) & 1) ^ 1;
+      if (!warp_wait_on(bar(C::EMPTY + buf * C::PARTS + C::PARTS - 1), parity, stop, tile_wait)) return false;
+      if (!C::TURNED && !warp_wait_on(bar(C::EMPTY + buf * C::PARTS + own.unit), parity, stop, tile_wait)) return false;
+      const uint32_t dst = base + C::RING + buf * C::TILE;
 #pragma unroll
-        for (int x = 0; x < PER; ++x) {
-          const int c = lane + 32 * x;
-          v[x] = make_uint4(0, 0, 0, 0);
-          if (h < heads && c < CHUNKS) v[x] = *reinterpret_cast<const uint4*>(c < DC / 8 ? qc + 8 * c : qr + 8 * c - DC);
-          top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu)),
-                         __vmaxu2(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu));
-        }
-        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-        const bool bf16 = a.q_dtype == TQ_BF16;
-        const bool bad = top >= (bf16 ? 0x7f80u : 0x7c00u);  // an infinity or a NaN: the head gives NaN
-        const float most = bf16 ? unpack2<TQ_BF16>(top).x : unpack2<TQ_FP16>(top).x;
-        const int ex = most > 0.0f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 15, -126) : 0;
-        const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-        if (lane == 0) sm.scale[(queries & 1) ^ 1][h] = h < heads ? (bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + ex) << 23)) : 0.0f;
+      for (int y = 0; y < ROPES; ++y) {
+        const int r = rope0 + 4 * y;
+        *reinterpret_cast<uint4*>(smem + C::RING + buf * C::TILE + (C::PANELS - 1) * kPanel + r * 128 + ((piece ^ (r & 7)) << 4)) = rope[y];
+      }
+      const uint32_t to = dst + (2 * own.unit + own.half) * kPanel + set * (TOK * 128) + 16 * own.piece + 8 * own.low + 2 * own.first;
 #pragma unroll
-        for (int x = 0; x < PER; ++x) {
-          const int c = lane + 32 * x;
-          if (c >= CHUNKS) continue;
-          const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-          uint32_t o[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 f = bf16 ? unpack2<TQ_BF16>(y[k]) : unpack2<TQ_FP16>(y[k]);
-            o[k] = bad ? 0 : pack2<TQ_FP16>(__fmul_rn(f.x, up), __fmul_rn(f.y, up));
-          }
-          *reinterpret_cast<uint4*>(smem + C::Q + (c >> 3) * C::QPANEL + h * 128 + (((c & 7) ^ (h & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-        }
+      for (int y = 0; y < TOK; ++y) {
+        const uint32_t at = (to ^ ((y & 7) << 4)) + y * 128;
+        if constexpr (UNITS == 4)
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(at), "r"(codes16(code[y], 0x4140)), "r"(codes16(code[y], 0x4342)) : "memory");
+        else if constexpr (UNITS == 2)
+          asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(at), "r"(codes16(code[y], mine)) : "memory");
+        else
+          asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at), "h"(static_cast<uint16_t>(codes16(code[y], mine))) : "memory");
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::QUERY));
-      // ---- tiles
-      for (int i = 0; i < w.n && ok; ++i, ++tile) {
-        const bool more = i + 1 < w.n;
-        if (more && !find(i + 1)) {
-          ok = false;
-          break;
+      if (lane == 0 && !(TEST && static_cast<int>(x) == hook.fault_tile)) mbar_arrive(bar(C::FULL + buf));
+      return true;
+    };
+    // the codes' transpose into TMEM
+    auto values = [&](uint32_t x, const uint32_t (&code)[TOK]) {
+      const int buf = x % 2;
+      if (!warp_wait_on(bar(C::VALUES_FREE + buf), ((x / 2) & 1) ^ 1, stop, tile_wait)) return false;
+      tc_fence_after();
+      const uint32_t to = tmem + quarter + C::V_COL + buf * 32 * UNITS + set * (TOK / 2);
+#pragma unroll
+      for (int y = 0; y < TOK; y += 16) {
+        uint32_t v[UNITS][8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t c0 = code[y + 2 * k], c1 = code[y + 2 * k + 1];
+          if constexpr (UNITS == 4) {
+            const uint32_t lo = __byte_perm(c0, c1, 0x5140), hi = __byte_perm(c0, c1, 0x7362);
+            v[0][k] = codes16(lo, 0x4140);
+            v[1][k] = codes16(lo, 0x4342);
+            v[2][k] = codes16(hi, 0x4140);
+            v[3][k] = codes16(hi, 0x4342);
+          } else {
+            const uint32_t lo = __byte_perm(c0, c1, both);
+            v[0][k] = codes16(lo, 0x4140);
+            if constexpr (UNITS == 2) v[1][k] = codes16(lo, 0x4342);
+          }
         }
-        const int buf = tile % C::NB;
-        const uint32_t parity = ((tile / C::NB) & 1) ^ 1;
-        uint8_t* const dst = smem + C::RING + buf * C::TILE + to;
 #pragma unroll
-        for (int u = 0; u < C::UNITS; ++u) {
-          if (ok) ok = warp_wait_on(bar(C::EMPTY + buf * C::UNITS + u), parity, stop, tile_wait);
-          if (!ok) break;
-          if (u == 0) {
+        for (int m = 0; m < UNITS; ++m) tmem_st8(to + 32 * m + y / 2, v[m]);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::VALUES + buf));
+      return true;
+    };
+    for (int it = 0; ok && next_work(it, w, true) && w.more; ++it) {
+      if (w.n == 0) continue;
+      // TURNED: two tiles in registers in turn, so that loads have a tile's time to arrive.  (Of the others, whose 64 tokens take
+      // twice the registers, the next tile's are asked for when this one's are in shared memory.)
+      uint32_t even[TOK], odd[C::TURNED ? TOK : 1];
+      ok = load(0, even);
+      if (!ok) break;
+      if (bf16) {
+        // queries of bf16 as fp16, each head times the power of two that brings its largest into [2^15, 2^16)
+        ok = warp_wait_on(bar(C::RAW), pieces & 1, stop, kBlockWait) && warp_wait_on(bar(C::SCALED), (pieces & 1) ^ 1, stop, kBlockWait);
+        if (!ok) break;
+#pragma unroll 1
+        for (int h = cw; h < N; h += C::CONV) {
+          constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32;
+          uint4 v[PER];
+          uint32_t top = 0;
+          auto at = [&](int c) { return reinterpret_cast<uint4*>(smem + C::Q + (c >> 3) * C::QPANEL + h * 128 + (((c & 7) ^ (h & 7)) << 4)); };
 #pragma unroll
-            for (int x = 0; x < 2; ++x) *reinterpret_cast<uint4*>(dst + (C::PANELS - 1) * kPanel + 4096 * x) = rope[x];
-            if (more) load_rope();
+          for (int x = 0; x < PER; ++x) {
+            const int c = lane + 32 * x;
+            v[x] = c < CHUNKS ? *at(c) : make_uint4(0, 0, 0, 0);
+            top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu)),
+                           __vmaxu2(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu));
           }
+          top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+          const bool bad = top >= 0x7f80u;  // an infinity or a NaN: the head gives NaN
+          const float most = unpack2<TQ_BF16>(top).x;
+          const int ex = most > 0.0f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 15, -126) : 0;
+          const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+          if (lane == 0) sm.scale[h] = bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint4 k = code[u][x];
-            const uint2 f0 = halves_of(k.x), f1 = halves_of(k.y), f2 = halves_of(k.z), f3 = halves_of(k.w);
-            *reinterpret_cast<uint4*>(dst + 2 * u * kPanel + 4096 * x) = make_uint4(f0.x, f0.y, f1.x, f1.y);
-            *reinterpret_cast<uint4*>(dst + (2 * u + 1) * kPanel + 4096 * x) = make_uint4(f2.x, f2.y, f3.x, f3.y);
+          for (int x = 0; x < PER; ++x) {
+            const int c = lane + 32 * x;
+            if (c >= CHUNKS) continue;
+            const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 f = unpack2<TQ_BF16>(y[k]);
+              o[k] = bad ? 0 : pack2<TQ_FP16>(__fmul_rn(f.x, up), __fmul_rn(f.y, up));
+            }
+            *at(c) = make_uint4(o[0], o[1], o[2], o[3]);
           }
-          if (more) load_unit(u);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0 && !(TEST && static_cast<int>(tile) == hook.fault_tile)) mbar_arrive(bar(C::FULL + buf * C::UNITS + u));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::QUERY));
+      }
+      ++pieces;
+      if constexpr (C::TURNED) {
+        rope_next();
+        if (w.n > 1) ok = load(1, odd);
+        for (int i = 0; i < w.n && ok; i += 2) {
+          ok = keys(tile + i, even) && values(tile + i, even);
+          if (ok) rope_next();
+          if (ok && i + 2 < w.n) ok = load(i + 2, even);
+          if (!ok || i + 1 >= w.n) break;
+          ok = keys(tile + i + 1, odd) && values(tile + i + 1, odd);
+          if (ok) rope_next();
+          if (ok && i + 3 < w.n) ok = load(i + 3, odd);
+        }
+      } else {
+        for (int i = 0; i < w.n && ok; ++i) {
+          rope_next();
+          ok = keys(tile + i, even);
+          if (ok && i + 1 < w.n) ok = load(i + 1, even);
         }
       }
+      tile += w.n;
     }
+    tmem_wait_st();
   } else if (warp == kMmaWarp) {
     // ========================================================================================================== MMAs
     // The warp stays together and its control flow is uniform, see mma_ss.
-    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
     const uint32_t leader = elect_one(), tm = uniform(tmem);
-    const uint32_t id_s = instr_desc(false, kTok, N, false), id_o = instr_desc(false, 128, N, true) | kMnMajorA;
-    const uint32_t q_lo = desc_lo(base + C::Q, 0), p_lo = desc_lo(base + C::P, 0), k_lo = desc_lo(base + C::RING, 0),
-                   v_lo = desc_lo(base + C::RING, kPanel);
+    const uint32_t id_s = instr_desc(false, kTok, N, false), id_o = instr_desc(false, 128, N, true);
+    const uint32_t q_lo = desc_lo(base + C::Q, 0), p_lo = desc_lo(base + C::P, 0), k_lo = desc_lo(base + C::RING, 0);
     bool ok = true;
     uint32_t tile = 0, pieces = 0;
-    // O^T += codes^T P^T of tile x
+    auto scores = [&](uint32_t x, bool last) {
+      const uint32_t buf = x % C::NB, sbuf = x % 2;
+      ok = ok && warp_wait_on(bar(C::FULL + buf), (x / C::NB) & 1, stop, tile_wait);
+      ok = ok && warp_wait_on(bar(C::READ + sbuf), ((x / 2) & 1) ^ 1, stop, tile_wait);
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t d = uniform(tm + C::S_COL + sbuf * 2 * N), k = uniform(k_lo + ((buf * C::TILE) >> 4));
+#pragma unroll
+      for (int y = 0; y < DC / 16; ++y)
+        mma_ss(leader, d, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > 0);
+#pragma unroll
+      for (int y = DC / 16; y < (DC + kRope) / 16; ++y)
+        mma_ss(leader, d + N, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > DC / 16);
+      mma_commit(leader, bar(C::SCORES + sbuf));
+      mma_commit(leader, bar(C::EMPTY + buf * C::PARTS + C::PARTS - 1));
+      if (last) mma_commit(leader, bar(C::QUERY_FREE));
+    };
     auto outputs = [&](uint32_t x, bool first) {
+      const uint32_t vbuf = x % 2, buf = x % C::NB;
+      if (C::TURNED) ok = ok && warp_wait_on(bar(C::VALUES + vbuf), (x / 2) & 1, stop, tile_wait);
       ok = ok && warp_wait_on(bar(C::WEIGHTS), x & 1, stop, tile_wait);
       if (ok && first) ok = warp_wait_on(bar(C::DRAINED), (pieces & 1) ^ 1, stop, tile_wait);
       if (!ok) return;
       tc_fence_after();
-      const int buf = x % C::NB;
-      const uint32_t v = v_lo + ((buf * C::TILE) >> 4);
+      const uint32_t add = uniform(!first);
+      if constexpr (C::TURNED) {
+        const uint32_t v = uniform(tm + C::V_COL + vbuf * 32 * C::UNITS);
 #pragma unroll
-      for (int m = 0; m < C::UNITS; ++m) {
+        for (int m = 0; m < C::UNITS; ++m)
 #pragma unroll
-        for (int y = 0; y < kTok / 16; ++y)
-          mma_ss(leader, tm + C::O_COL + m * N, v + ((2 * m * kPanel + y * 2048) >> 4), p_lo + (y * 2048 >> 4), kDescHi, id_o, y > 0 || !first);
-        mma_commit(leader, bar(C::EMPTY + buf * C::UNITS + m));
+          for (int y = 0; y < kTok / 16; ++y)
+            mma_ts(leader, tm + C::O_COL + m * N, v + 32 * m + 8 * y, p_lo + (y * 2048 >> 4), kDescHi, id_o, y > 0 || add);
+        mma_commit(leader, bar(C::VALUES_FREE + vbuf));
+      } else {
+        const uint32_t v = uniform(k_lo + ((buf * C::TILE) >> 4) + ((kPanel >> 4) << 16));
+#pragma unroll
+        for (int m = 0; m < C::UNITS; ++m) {
+#pragma unroll
+          for (int y = 0; y < kTok / 16; ++y)
+            mma_ss(leader, tm + C::O_COL + m * N, v + ((2 * m * kPanel + y * 2048) >> 4), p_lo + (y * 2048 >> 4), kDescHi, id_o | kMnMajorA, y > 0 || add);
+          mma_commit(leader, bar(C::EMPTY + buf * C::PARTS + m));
+        }
       }
       mma_commit(leader, bar(C::DONE));
     };
@@ -574,41 +744,24 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
       const int n = uniform(w.n);
       if (!uniform(w.more)) break;
       if (n == 0) continue;
-      ok = warp_wait_on(bar(C::QUERY), pieces & 1, stop, kBlockWait);
-      for (int i = 0; i < n && ok; ++i, ++tile) {
-        const int buf = tile % C::NB;
-        const uint32_t parity = (tile / C::NB) & 1, d = tm + C::S_COL + (tile & 1) * 2 * N, k = k_lo + ((buf * C::TILE) >> 4);
-#pragma unroll
-        for (int u = 0; u < C::UNITS; ++u) {
-          ok = ok && warp_wait_on(bar(C::FULL + buf * C::UNITS + u), parity, stop, tile_wait);
-          if (!ok) break;
-          tc_fence_after();
-          if (u == 0) {
-#pragma unroll
-            for (int y = 0; y < kRope / 16; ++y)
-              mma_ss(leader, d + N, k + (((C::PANELS - 1) * kPanel + y * 32) >> 4), q_lo + (((C::PANELS - 1) * C::QPANEL + y * 32) >> 4), kDescHi, id_s, y > 0);
-          }
-#pragma unroll
-          for (int y = 8 * u; y < 8 * u + 8; ++y)
-            mma_ss(leader, d, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > 0);
-        }
-        if (!ok) break;
-        mma_commit(leader, bar(C::SCORES + (tile & 1)));
-        if (i + 1 == n) mma_commit(leader, bar(C::QUERY_FREE));
-        if (i > 0) outputs(tile - 1, i == 1);
+      ok = warp_wait_on(bar(bf16 ? C::QUERY : C::RAW), pieces & 1, stop, kBlockWait);
+      for (int i = 0; i < n && ok; ++i) {
+        scores(tile + i, i + 1 == n);
+        if (i > 0) outputs(tile + i - 1, i == 1);
       }
-      if (ok) outputs(tile - 1, n == 1);
+      if (ok) outputs(tile + n - 1, n == 1);
+      tile += n;
       ++pieces;
     }
     // everything issued has completed before the block gives its memory back
     mma_commit(leader, bar(C::END));
     if (!__all_sync(0xffffffffu, wait_stage_inline(bar(C::END), 0, kTileWait))) *stop = 1;
-  } else {
-    // ============================================================================================ the work, and pages
+  } else if (warp == kFeedWarp) {
+    // ============================================================================== the work, pages, loads of queries
     int2* const info = static_cast<int2*>(a.workspace);
     int b = sm.start_b, p = sm.start_p, it = 0, known = 0, first = b;  // lane i holds the length of sequence first + i
     bool ok = true;
-    uint32_t batch = 0;
+    uint32_t batch = 0, pieces = 0;
     auto post = [&](const Work& w) {
       ok = warp_wait_on(bar(C::WORK_FREE + (it & 1)), ((it >> 1) & 1) ^ 1, stop, kBlockWait);
       if (!ok) return;
@@ -656,11 +809,23 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC)), "r"(latent_block_bytes(DC)) : "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES + (batch & 1)));
+          if (i > 0) continue;
+          // the queries: heads beyond the last one are zeros, those beyond the group's are not looked at
+          ok = warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait);
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_expect_tx(bar(C::RAW), C::PANELS * C::QPANEL);
+            for (int x = 0; x < DC / 64; ++x) tma_load_3d(base + C::Q + x * C::QPANEL, &maps.c, 64 * x, h0, b, bar(C::RAW));
+            tma_load_3d(base + C::Q + (DC / 64) * C::QPANEL, &maps.r, 0, h0, b, bar(C::RAW));
+          }
+          ++pieces;
         }
       }
       p += n + kFixed;
     }
     if (ok) post(Work{});
+    // loads on their way land before the block ends (whoever waits for them may have given up)
+    if (pieces > 0) wait_stage_inline(bar(C::RAW), (pieces - 1) & 1, kMaxWaitCycles);
   }
 
   __syncwarp();
@@ -672,16 +837,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const LatentArgs a,
 }
 
 // ---- joining: out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^(ref_i - max ref)
-// A thread has four channels of a head; LANES threads share the parts of such a piece.
-constexpr int kJoin = 256;
+// A thread block takes pieces of a row in turn: 4 kJoin / lanes channels of a head, `lanes` threads to a column of 4.
+constexpr int kJoin = 256, kMaxParts = 256;
 
 template <int DC, int N>
 __global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines, int lanes) {
   __shared__ float4 s_sum[kJoin];
-  __shared__ float s_z[32], s_o[32], s_l[kJoin];
+  __shared__ float s_f[kMaxParts], s_max[2][kJoin / 32], s_l[kJoin / 32];
   pdl_launch_dependents();
   pdl_wait();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int columns = kJoin / lanes, chunks = DC / 4 / columns;
   const float* const parts = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + info_bytes(a.c.B));
   const int2* const info = static_cast<const int2*>(a.workspace);
@@ -690,49 +855,52 @@ __global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, 
     const int b = static_cast<int>(x / (static_cast<long long>(a.H) * chunks)), y = static_cast<int>(x % (static_cast<long long>(a.H) * chunks));
     const int h = y / chunks, chunk = y % chunks;
     const int2 in = info[b];  // first line, number of parts
-    // (the second: what a call that gave up has left behind)
-    if (in.y < 2 || in.x < 0 || in.y > lines - in.x) continue;
+    // (the rest: what a call that gave up has left behind)
+    if (in.y < 2 || in.y > kMaxParts || in.x < 0 || in.y > lines - in.x) continue;
     const int group = h / per_group, head = h % per_group;
     auto part = [&](int i) { return parts + static_cast<long long>((2 * (in.x + i) + (i == 0)) * groups + group) * part_floats(DC, N); };
     // ref of the joined row: the largest score part, and the largest of the rest beside it
-    float z = -INFINITY;
-    for (int i = tid; i < in.y; i += kJoin) z = fmaxf(z, part(i)[N * DC + head]);
+    const bool mine = tid < in.y;
+    const float* const q = part(mine ? tid : 0) + N * DC + head;
+    const float z = mine ? q[0] : -INFINITY, o = mine ? q[N] : 0.0f, l = mine ? q[2 * N] : 0.0f;
     auto block_max = [&](float v, float* s) {
+#pragma unroll
       for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-      if ((tid & 31) == 0) s[tid >> 5] = v;
+      if (lane == 0) s[warp] = v;
       __syncthreads();
       v = s[0];
+#pragma unroll
       for (int i = 1; i < kJoin / 32; ++i) v = fmaxf(v, s[i]);
       return v;
     };
-    z = block_max(z, s_z);
-    float o = -INFINITY;
-    for (int i = tid; i < in.y; i += kJoin) o = fmaxf(o, (part(i)[N * DC + head] - z) + part(i)[N * DC + N + head]);
-    o = block_max(o, s_o);
-    const int column = chunk * columns + tid % columns, first = tid / columns;
+    const float most = block_max(z, s_max[0]);
+    const float rest = mine ? (z - most) + o : -INFINITY;
+    const float f = ex2(rest - block_max(rest, s_max[1]));
+    float total = mine ? f * l : 0.0f;
+    if (mine) s_f[tid] = f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+    if (lane == 0) s_l[warp] = total;
+    __syncthreads();
+    const int column = chunk * columns + tid % columns;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float l = 0.0f;
-#pragma unroll 4
-    for (int i = first; i < in.y; i += lanes) {
-      const float* const q = part(i);
-      const float4 v = *reinterpret_cast<const float4*>(q + head * DC + 4 * column);
-      const float f = ex2((q[N * DC + head] - z) + (q[N * DC + N + head] - o));
-      sum.x = fmaf(f, v.x, sum.x);
-      sum.y = fmaf(f, v.y, sum.y);
-      sum.z = fmaf(f, v.z, sum.z);
-      sum.w = fmaf(f, v.w, sum.w);
-      l = fmaf(f, q[N * DC + 2 * N + head], l);
+#pragma unroll 8
+    for (int i = tid / columns; i < in.y; i += lanes) {
+      const float4 v = *reinterpret_cast<const float4*>(part(i) + head * DC + 4 * column);
+      const float g = s_f[i];
+      sum = make_float4(fmaf(g, v.x, sum.x), fmaf(g, v.y, sum.y), fmaf(g, v.z, sum.z), fmaf(g, v.w, sum.w));
     }
     s_sum[tid] = sum;
-    s_l[tid] = l;
     __syncthreads();
     if (tid < columns) {
       for (int i = 1; i < lanes; ++i) {
         const float4 v = s_sum[tid + i * columns];
         sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
-        l += s_l[tid + i * columns];
       }
-      const float inv = __fdiv_rn(1.0f, l);
+      total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kJoin / 32; ++i) total += s_l[i];
+      const float inv = __fdiv_rn(1.0f, total);
       const long long to = (static_cast<long long>(b) * a.H + h) * DC + 4 * column;
       const float4 v = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
       if (a.out_dtype == TQ_FP32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = v;
@@ -754,7 +922,7 @@ Shape shape_of(int H) {
   s.groups = (H + 63) / 64;
   s.per_group = (H + s.groups - 1) / s.groups;
   s.n = s.per_group <= 16 ? 16 : (s.per_group <= 32 ? 32 : 64);
-  s.lines = device_sm_count() / s.groups;
+  s.lines = (device_sm_count() < kMaxParts ? device_sm_count() : kMaxParts) / s.groups;
   if (s.lines < 1) s.lines = 1;
   return s;
 }
@@ -779,7 +947,13 @@ cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook 
   const long long longest = static_cast<long long>(a.c.B) * ((a.max_len + kTok - 1) / kTok + 1 + kFixed);
   const long long most = (longest + kMinShare - 1) / kMinShare;
   const int lines = most < s.lines ? static_cast<int>(most) : s.lines;
-  if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, a, s.groups, s.per_group, hook)) return e;
+  QueryMaps maps;
+  if (!encode_fn()) return cudaErrorNotSupported;
+  if (!make_map(&maps.c, a.q_c.data, a.q_dtype, DC, a.H, a.c.B, a.q_c.row_stride, a.q_c.head_stride, N, 1) ||
+      !make_map(&maps.r, a.q_r.data, a.q_dtype, kRope, a.H, a.c.B, a.q_r.row_stride, a.q_r.head_stride, N, 1))
+    return cudaErrorInvalidValue;
+  if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, maps, a, s.groups, s.per_group, hook))
+    return e;
   if (lines == 1) return cudaSuccess;  // nothing is cut
   // threads that share a piece's parts: as many as there are parts, about, but pieces enough for the GPU
   int lanes = kJoin / (DC / 4);
