@@ -44,7 +44,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 64;                       // tokens of a tile
 constexpr int kBatch = 8;                      // tiles whose pages are looked up together: a lane per block
-constexpr int kWarps = 14, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion
+constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion, two idle
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 2;                      // what the start of a sequence costs, in tiles
 constexpr int kMinShare = 4;                   // places on the line that a thread block takes at least
@@ -60,7 +60,7 @@ struct Cfg {
   static constexpr int N = N_;                         // columns: heads of a thread block
   static constexpr int SOFT = N == 64 ? 8 : 4;         // softmax warps: four have every second half of N heads between them
   static constexpr bool TURNED = N < 64;               // O^T's operand: codes transposed into TMEM; or those in shared memory
-  static constexpr int CONV = 12 - SOFT;               // warps that turn codes into operands: one or two sets of four
+  static constexpr int CONV = 12 - SOFT;               // warps that turn codes into operands
   static constexpr int HN = N / (SOFT / 2);            // heads of a softmax thread
   static constexpr int UNITS = DC / 128;               // row tiles of O^T (TURNED: and channels of a lane)
   static constexpr int PARTS = TURNED ? 1 : UNITS + 1; // that a tile's shared memory is given back in
@@ -275,6 +275,17 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
   __syncthreads();
   const uint32_t tmem = sm.tmem;
 
+  // 512 threads have 128 registers each; the last four warps leave half of theirs to the softmax warps.  A quarter of an SM
+  // has its own registers, so what is taken there has to be left there: in each one or two softmax warps, two or one of
+  // conversion and one of the last four, 192 + 2 x 128 + 64 = 2 x 160 + 128 + 64 = 4 x 128.
+  static_assert(kWarps == 16 && kMmaWarp == 12 && (C::SOFT == 4 || C::SOFT == 8), "register split");
+  if (warp < C::SOFT) {
+    if constexpr (C::SOFT == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;\n");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 160;\n");
+  } else if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;\n");
+  }
+
   // the it-th piece of work, for every warp but the one that finds it; false: none, or the block winds down
   auto next_work = [&](int it, Work& w, bool live) {
     if (live) live = warp_wait_on(bar(C::WORK + (it & 1)), (it >> 1) & 1, stop, kBlockWait);
@@ -309,21 +320,27 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         l[i] = 0.0f;
         scale[i] = a.attn_scale * kLog2e;
       }
-      // scales of this thread's token, a tile ahead
-      auto scales = [&](int i) {
+      // Scales of this thread's token are asked for a tile ahead, their block is looked up two tiles ahead: while MMAs read
+      // shared memory a look-up takes about as long as they do, and nothing here may wait for one.
+      auto block = [&](int i) {
         if (i % kBatch == 0) wait(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1);
-        const long long blk = sm.pages[batch & 1][4 * (i % kBatch) + wq];
+        const int blk = sm.pages[batch & 1][4 * (i % kBatch) + wq];
         if (i % kBatch == kBatch - 1 || i == w.n - 1) {
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
           ++batch;
         }
-        return *reinterpret_cast<const float2*>(a.c.blocks + (live ? blk : 0) * latent_block_bytes(DC) + latent_scale_offset(DC, row & 15));
+        return live ? blk : 0;
       };
-      float2 next = w.n > 0 ? scales(0) : make_float2(0.0f, 0.0f);
+      auto scales = [&](int blk) {
+        return *reinterpret_cast<const float2*>(a.c.blocks + static_cast<long long>(blk) * latent_block_bytes(DC) + latent_scale_offset(DC, row & 15));
+      };
+      float2 next = w.n > 0 ? scales(block(0)) : make_float2(0.0f, 0.0f);
+      int after = w.n > 1 ? block(1) : 0;
       for (int i = 0; i < w.n; ++i, ++tile) {
         const float2 sc = next;
-        if (i + 1 < w.n) next = scales(i + 1);
+        if (i + 1 < w.n) next = scales(after);
+        if (i + 2 < w.n) after = block(i + 2);
         const int at = w.t0 + kTok * i + row;
         const bool seen = at >= w.lo && at < w.len;
         // (a token without a range has codes of 0 and counts as the smallest: 2^-64 / 127, about 2^-71)
@@ -427,6 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           }
           exponents();
         }
+        const bool free = live && tile > 0 ? mbar_test_wait(bar(C::DONE), (tile - 1) & 1) : true;  // (looked at in time, too)
         uint32_t p[C::HN / 2];
 #pragma unroll
         for (int x = 0; x < C::HN; x += 2) {
@@ -436,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           l[x + 1] = s.y;
           p[x >> 1] = pack2<TQ_FP16>(e0, e1);
         }
-        if (tile > 0) wait(bar(C::DONE), (tile - 1) & 1);
+        if (!__all_sync(0xffffffffu, free)) wait(bar(C::DONE), (tile - 1) & 1);
 #pragma unroll
         for (int x = 0; x < C::HN / 8; ++x)
           *reinterpret_cast<uint4*>(p_row + (((hbase / 8 + x) ^ (row & 7)) << 4)) = make_uint4(p[4 * x], p[4 * x + 1], p[4 * x + 2], p[4 * x + 3]);
@@ -512,12 +530,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     }
   } else if (warp < kMmaWarp) {
     // ================================================================================= queries, codes into operands
-    // A thread has four neighbouring channels of every token of its set (TURNED and d_c < 512: the lane's ones of those), and
-    // 16 bytes of the positional part of every fourth token of the warp's.
-    constexpr int TOK = C::TURNED ? 32 : 16 * C::UNITS, ROPES = 16 / C::CONV;  // tokens of a set
-    constexpr int UNITS = C::TURNED ? C::UNITS : 4;                              // as far as a lane is concerned
-    const int cw = warp - C::SOFT, set = C::TURNED ? cw >> 2 : cw / C::UNITS;
-    const Lane<UNITS> own(C::TURNED ? cw & 3 : cw % C::UNITS, lane);
+    // A warp has the codes of TOK tokens, a thread four neighbouring channels of every 128 (TURNED: of one 128, of those its
+    // lane's; two sets of four warps), and 16 bytes of the positional part of every fourth token of the warp's.
+    constexpr int TOK = C::TURNED ? 32 : 16, ROPES = 16 / C::CONV;
+    constexpr int UNITS = C::TURNED ? C::UNITS : 4;      // as far as a lane is concerned
+    constexpr int TURNS = C::TURNED ? 1 : C::UNITS;      // 128 channels each
+    const int cw = warp - C::SOFT, set = C::TURNED ? cw >> 2 : cw;
+    const Lane<UNITS> own(C::TURNED ? cw & 3 : 0, lane);
     const uint32_t quarter = static_cast<uint32_t>(32 * (cw & 3)) << 16;
     const int rope0 = 64 / C::CONV * cw + (lane >> 3), piece = lane & 7;  // positional part: 16 bytes of tokens rope0, rope0 + 4, ...
     // bytes of a word that are the lane's (d_c < 512): of one word; of two words, neighbours side by side
@@ -532,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       for (int x = 0; x < ROPES; ++x) rope[x] = ahead[x];
     };
     // asks for the values of tile i of the piece
-    auto load = [&](int i, uint32_t (&code)[TOK]) {
+    auto load = [&](int i, uint32_t (&code)[TURNS * TOK]) {
       if (i % kBatch == 0 && !warp_wait_on(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1, stop, tile_wait)) return false;
       const int* const pages = sm.pages[batch & 1] + 4 * (i % kBatch);
       {
@@ -542,9 +561,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       }
 #pragma unroll
       for (int x = 0; x < TOK; x += 16) {
-        const uint8_t* const blk = a.c.blocks + static_cast<long long>(pages[(set * TOK + x) / 16]) * latent_block_bytes(DC) + own.word();
+        const uint8_t* const blk = a.c.blocks + static_cast<long long>(pages[(set * TOK + x) >> 4]) * latent_block_bytes(DC) + own.word();
 #pragma unroll
-        for (int y = 0; y < 16; ++y) code[x + y] = *reinterpret_cast<const uint32_t*>(blk + DC * y);
+        for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+          for (int y = 0; y < 16; ++y) code[u * TOK + x + y] = *reinterpret_cast<const uint32_t*>(blk + 128 * u + DC * y);
       }
       if (i % kBatch == kBatch - 1 || i == w.n - 1) {
         __syncwarp();
@@ -554,27 +575,30 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       return true;
     };
     // codes and positional part of a tile into shared memory
-    auto keys = [&](uint32_t x, const uint32_t (&code)[TOK]) {
+    auto keys = [&](uint32_t x, const uint32_t (&code)[TURNS * TOK]) {
       const int buf = x % C::NB;
       const uint32_t parity = ((x / C::NB) & 1) ^ 1;
       if (!warp_wait_on(bar(C::EMPTY + buf * C::PARTS + C::PARTS - 1), parity, stop, tile_wait)) return false;
-      if (!C::TURNED && !warp_wait_on(bar(C::EMPTY + buf * C::PARTS + own.unit), parity, stop, tile_wait)) return false;
       const uint32_t dst = base + C::RING + buf * C::TILE;
 #pragma unroll
       for (int y = 0; y < ROPES; ++y) {
         const int r = rope0 + 4 * y;
         *reinterpret_cast<uint4*>(smem + C::RING + buf * C::TILE + (C::PANELS - 1) * kPanel + r * 128 + ((piece ^ (r & 7)) << 4)) = rope[y];
       }
-      const uint32_t to = dst + (2 * own.unit + own.half) * kPanel + set * (TOK * 128) + 16 * own.piece + 8 * own.low + 2 * own.first;
 #pragma unroll
-      for (int y = 0; y < TOK; ++y) {
-        const uint32_t at = (to ^ ((y & 7) << 4)) + y * 128;
-        if constexpr (UNITS == 4)
-          asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(at), "r"(codes16(code[y], 0x4140)), "r"(codes16(code[y], 0x4342)) : "memory");
-        else if constexpr (UNITS == 2)
-          asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(at), "r"(codes16(code[y], mine)) : "memory");
-        else
-          asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at), "h"(static_cast<uint16_t>(codes16(code[y], mine))) : "memory");
+      for (int u = 0; u < TURNS; ++u) {
+        if (!C::TURNED && !warp_wait_on(bar(C::EMPTY + buf * C::PARTS + u), parity, stop, tile_wait)) return false;
+        const uint32_t to = dst + (2 * (own.unit + u) + own.half) * kPanel + set * (TOK * 128) + 16 * own.piece + 8 * own.low + 2 * own.first;
+#pragma unroll
+        for (int y = 0; y < TOK; ++y) {
+          const uint32_t at = (to ^ ((y & 7) << 4)) + y * 128, c = code[u * TOK + y];
+          if constexpr (UNITS == 4)
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(at), "r"(codes16(c, 0x4140)), "r"(codes16(c, 0x4342)) : "memory");
+          else if constexpr (UNITS == 2)
+            asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(at), "r"(codes16(c, mine)) : "memory");
+          else
+            asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at), "h"(static_cast<uint16_t>(codes16(c, mine))) : "memory");
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -582,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       return true;
     };
     // the codes' transpose into TMEM
-    auto values = [&](uint32_t x, const uint32_t (&code)[TOK]) {
+    auto values = [&](uint32_t x, const uint32_t (&code)[TURNS * TOK]) {
       const int buf = x % 2;
       if (!warp_wait_on(bar(C::VALUES_FREE + buf), ((x / 2) & 1) ^ 1, stop, tile_wait)) return false;
       tc_fence_after();
@@ -618,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       if (w.n == 0) continue;
       // TURNED: two tiles in registers in turn, so that loads have a tile's time to arrive.  (Of the others, whose 64 tokens take
       // twice the registers, the next tile's are asked for when this one's are in shared memory.)
-      uint32_t even[TOK], odd[C::TURNED ? TOK : 1];
+      uint32_t even[TURNS * TOK], odd[C::TURNED ? TOK : 1];
       ok = load(0, even);
       if (!ok) break;
       if (bf16) {
@@ -696,8 +720,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     uint32_t tile = 0, pieces = 0;
     auto scores = [&](uint32_t x, bool last) {
       const uint32_t buf = x % C::NB, sbuf = x % 2;
-      ok = ok && warp_wait_on(bar(C::FULL + buf), (x / C::NB) & 1, stop, tile_wait);
-      ok = ok && warp_wait_on(bar(C::READ + sbuf), ((x / 2) & 1) ^ 1, stop, tile_wait);
+      ok = warp_wait_on(bar(C::FULL + buf), (x / C::NB) & 1, stop, tile_wait) && warp_wait_on(bar(C::READ + sbuf), ((x / 2) & 1) ^ 1, stop, tile_wait);
       if (!ok) return;
       tc_fence_after();
       const uint32_t d = uniform(tm + C::S_COL + sbuf * 2 * N), k = uniform(k_lo + ((buf * C::TILE) >> 4));
@@ -713,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     };
     auto outputs = [&](uint32_t x, bool first) {
       const uint32_t vbuf = x % 2, buf = x % C::NB;
-      if (C::TURNED) ok = ok && warp_wait_on(bar(C::VALUES + vbuf), (x / 2) & 1, stop, tile_wait);
+      if (C::TURNED) ok = warp_wait_on(bar(C::VALUES + vbuf), (x / 2) & 1, stop, tile_wait);
       ok = ok && warp_wait_on(bar(C::WEIGHTS), x & 1, stop, tile_wait);
       if (ok && first) ok = warp_wait_on(bar(C::DRAINED), (pieces & 1) ^ 1, stop, tile_wait);
       if (!ok) return;
@@ -745,9 +768,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       if (!uniform(w.more)) break;
       if (n == 0) continue;
       ok = warp_wait_on(bar(bf16 ? C::QUERY : C::RAW), pieces & 1, stop, kBlockWait);
+      // The scores of the next tile go before the outputs of this one, whose weights are made meanwhile.
       for (int i = 0; i < n && ok; ++i) {
         scores(tile + i, i + 1 == n);
-        if (i > 0) outputs(tile + i - 1, i == 1);
+        if (i > 0 && ok) outputs(tile + i - 1, i == 1);
       }
       if (ok) outputs(tile + n - 1, n == 1);
       tile += n;
