@@ -861,77 +861,118 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
 }
 
 // ---- joining: out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^(ref_i - max ref)
-// A thread block takes pieces of a row in turn: 4 kJoin / lanes channels of a head, `lanes` threads to a column of 4.
-constexpr int kJoin = 256, kMaxParts = 256;
+// Outputs are on their way before the refs have been looked at.  MANY parts (few sequences): a thread block has 64 channels of a
+// head, 16 threads to a column of four; a thread looks at one part's ref, and the f_i go through shared memory.  Few parts: a
+// thread has four channels of a head and every part, and 16 threads look at the refs for themselves.
+constexpr int kJoin = 256;
 
-template <int DC, int N>
-__global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines, int lanes) {
-  __shared__ float4 s_sum[kJoin];
-  __shared__ float s_f[kMaxParts], s_max[2][kJoin / 32], s_l[kJoin / 32];
+__device__ __forceinline__ void store_joined(const LatentArgs& a, long long to, const float4& sum, float l) {
+  const float inv = __fdiv_rn(1.0f, l);
+  const float4 v = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+  if (a.out_dtype == TQ_FP32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = v;
+  else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) =
+      a.out_dtype == TQ_BF16 ? make_uint2(pack2<TQ_BF16>(v.x, v.y), pack2<TQ_BF16>(v.z, v.w)) : make_uint2(pack2<TQ_FP16>(v.x, v.y), pack2<TQ_FP16>(v.z, v.w));
+}
+__device__ __forceinline__ void add4(float4& sum, float f, const float4& v) {
+  sum = make_float4(fmaf(f, v.x, sum.x), fmaf(f, v.y, sum.y), fmaf(f, v.z, sum.z), fmaf(f, v.w, sum.w));
+}
+
+template <int DC, int N, bool MANY>
+__global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines) {
+  constexpr int COLUMNS = MANY ? 16 : DC / 4, LANES = MANY ? 16 : 1, CHUNKS = DC / 4 / COLUMNS, PER = kJoin / (COLUMNS * LANES), AHEAD = MANY ? 10 : 4;
+  __shared__ float4 s_sum[MANY ? kJoin : 1];
+  __shared__ float s_f[MANY ? kJoin : 1], s_max[2][kJoin / 32], s_l[kJoin / 32];
   pdl_launch_dependents();
   pdl_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int columns = kJoin / lanes, chunks = DC / 4 / columns;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, own = tid / COLUMNS % LANES;
   const float* const parts = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + info_bytes(a.c.B));
   const int2* const info = static_cast<const int2*>(a.workspace);
-  const long long pieces = static_cast<long long>(a.c.B) * a.H * chunks;
-  for (long long x = blockIdx.x; x < pieces; x += gridDim.x) {
-    const int b = static_cast<int>(x / (static_cast<long long>(a.H) * chunks)), y = static_cast<int>(x % (static_cast<long long>(a.H) * chunks));
-    const int h = y / chunks, chunk = y % chunks;
-    const int2 in = info[b];  // first line, number of parts
-    // (the rest: what a call that gave up has left behind)
-    if (in.y < 2 || in.y > kMaxParts || in.x < 0 || in.y > lines - in.x) continue;
+  const unsigned pieces = static_cast<unsigned>(a.c.B) * a.H * CHUNKS;
+  for (unsigned x0 = blockIdx.x * PER; x0 < pieces; x0 += gridDim.x * PER) {
+    const unsigned x = x0 + tid / (COLUMNS * LANES);
+    const bool inside = x < pieces;
+    const unsigned row = (inside ? x : 0) / CHUNKS, b = row / a.H, h = row % a.H;
+    int2 in = inside ? info[b] : make_int2(0, 0);  // first line, number of parts
+    // (the last two: what a call that gave up has left behind)
+    if (in.y < 2 || in.x < 0 || in.y > lines - in.x) in.y = 0;
+    if (MANY && in.y == 0) continue;
     const int group = h / per_group, head = h % per_group;
-    auto part = [&](int i) { return parts + static_cast<long long>((2 * (in.x + i) + (i == 0)) * groups + group) * part_floats(DC, N); };
-    // ref of the joined row: the largest score part, and the largest of the rest beside it
-    const bool mine = tid < in.y;
-    const float* const q = part(mine ? tid : 0) + N * DC + head;
-    const float z = mine ? q[0] : -INFINITY, o = mine ? q[N] : 0.0f, l = mine ? q[2 * N] : 0.0f;
-    auto block_max = [&](float v, float* s) {
+    const int column = (x % CHUNKS) * COLUMNS + tid % COLUMNS;
+    const int stride = 2 * groups * part_floats(DC, N);
+    // of part i > 0; the first one stands a place further
+    const float* const base = parts + static_cast<long long>(2 * in.x * groups + group) * part_floats(DC, N);
+    auto part = [&](int i) { return base + static_cast<long long>(i) * stride + (i == 0 ? groups * part_floats(DC, N) : 0); };
+    auto load = [&](int i) { return *reinterpret_cast<const float4*>(part(i) + head * DC + 4 * column); };
+    float4 first[AHEAD];
 #pragma unroll
-      for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-      if (lane == 0) s[warp] = v;
-      __syncthreads();
-      v = s[0];
-#pragma unroll
-      for (int i = 1; i < kJoin / 32; ++i) v = fmaxf(v, s[i]);
-      return v;
-    };
-    const float most = block_max(z, s_max[0]);
-    const float rest = mine ? (z - most) + o : -INFINITY;
-    const float f = ex2(rest - block_max(rest, s_max[1]));
-    float total = mine ? f * l : 0.0f;
-    if (mine) s_f[tid] = f;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
-    if (lane == 0) s_l[warp] = total;
-    __syncthreads();
-    const int column = chunk * columns + tid % columns;
+    for (int k = 0; k < AHEAD; ++k) first[k] = own + k * LANES < in.y ? load(own + k * LANES) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int i = tid / columns; i < in.y; i += lanes) {
-      const float4 v = *reinterpret_cast<const float4*>(part(i) + head * DC + 4 * column);
-      const float g = s_f[i];
-      sum = make_float4(fmaf(g, v.x, sum.x), fmaf(g, v.y, sum.y), fmaf(g, v.z, sum.z), fmaf(g, v.w, sum.w));
-    }
-    s_sum[tid] = sum;
-    __syncthreads();
-    if (tid < columns) {
-      for (int i = 1; i < lanes; ++i) {
-        const float4 v = s_sum[tid + i * columns];
-        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
-      }
-      total = 0.0f;
+    float l = 0.0f;
+    const long long to = static_cast<long long>(row) * DC + 4 * column;
+    // ref of the joined row: the largest score part, and the largest of the rest beside it
+    if constexpr (MANY) {
+      const bool mine = tid < in.y;  // (there are fewer parts than threads)
+      const float* const q = part(mine ? tid : 0) + N * DC + head;
+      const float z = mine ? q[0] : -INFINITY, o = mine ? q[N] : 0.0f, sums = mine ? q[2 * N] : 0.0f;
+      auto block_max = [&](float v, float* s) {
 #pragma unroll
-      for (int i = 0; i < kJoin / 32; ++i) total += s_l[i];
-      const float inv = __fdiv_rn(1.0f, total);
-      const long long to = (static_cast<long long>(b) * a.H + h) * DC + 4 * column;
-      const float4 v = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-      if (a.out_dtype == TQ_FP32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = v;
-      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) =
-          a.out_dtype == TQ_BF16 ? make_uint2(pack2<TQ_BF16>(v.x, v.y), pack2<TQ_BF16>(v.z, v.w)) : make_uint2(pack2<TQ_FP16>(v.x, v.y), pack2<TQ_FP16>(v.z, v.w));
+        for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+        if (lane == 0) s[warp] = v;
+        __syncthreads();
+        v = s[0];
+#pragma unroll
+        for (int i = 1; i < kJoin / 32; ++i) v = fmaxf(v, s[i]);
+        return v;
+      };
+      const float most = block_max(z, s_max[0]);
+      const float rest = mine ? (z - most) + o : -INFINITY;
+      const float f = ex2(rest - block_max(rest, s_max[1]));
+      float total = mine ? f * sums : 0.0f;
+      if (mine) s_f[tid] = f;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+      if (lane == 0) s_l[warp] = total;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (own + k * LANES < in.y) add4(sum, s_f[own + k * LANES], first[k]);
+      for (int i = own + AHEAD * LANES; i < in.y; i += LANES) add4(sum, s_f[i], load(i));
+      s_sum[tid] = sum;
+      __syncthreads();
+      if (own == 0) {
+#pragma unroll
+        for (int i = 1; i < LANES; ++i) add4(sum, 1.0f, s_sum[tid + i * COLUMNS]);
+#pragma unroll
+        for (int i = 0; i < kJoin / 32; ++i) l += s_l[i];
+        store_joined(a, to, sum, l);
+      }
+      __syncthreads();
+    } else {
+      // (a warp may hold two rows or four, of 16 columns and more)
+      auto score = [&](int i) { return part(i)[N * DC + head]; };
+      auto offset = [&](int i) { return part(i)[N * DC + N + head]; };
+      float z = -INFINITY, o = -INFINITY;
+      for (int i = lane & 15; i < in.y; i += 16) z = fmaxf(z, score(i));
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, off));
+      for (int i = lane & 15; i < in.y; i += 16) o = fmaxf(o, (score(i) - z) + offset(i));
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) o = fmaxf(o, __shfl_xor_sync(0xffffffffu, o, off));
+      auto weight = [&](int i) { return ex2(((score(i) - z) + offset(i)) - o); };
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        if (k >= in.y) continue;
+        const float f = weight(k);
+        l = fmaf(f, part(k)[N * DC + 2 * N + head], l);
+        add4(sum, f, first[k]);
+      }
+      for (int i = AHEAD; i < in.y; ++i) {
+        const float f = weight(i);
+        l = fmaf(f, part(i)[N * DC + 2 * N + head], l);
+        add4(sum, f, load(i));
+      }
+      if (in.y > 0) store_joined(a, to, sum, l);
     }
-    __syncthreads();
   }
 }
 
@@ -946,7 +987,7 @@ Shape shape_of(int H) {
   s.groups = (H + 63) / 64;
   s.per_group = (H + s.groups - 1) / s.groups;
   s.n = s.per_group <= 16 ? 16 : (s.per_group <= 32 ? 32 : 64);
-  s.lines = (device_sm_count() < kMaxParts ? device_sm_count() : kMaxParts) / s.groups;
+  s.lines = device_sm_count() / s.groups;
   if (s.lines < 1) s.lines = 1;
   return s;
 }
@@ -979,13 +1020,13 @@ cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook 
   if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, maps, a, s.groups, s.per_group, hook))
     return e;
   if (lines == 1) return cudaSuccess;  // nothing is cut
-  // threads that share a piece's parts: as many as there are parts, about, but pieces enough for the GPU
-  int lanes = kJoin / (DC / 4);
-  while (lanes < 16 && static_cast<long long>(a.c.B) * a.H * (lanes * DC / 4 / kJoin) < 2 * device_sm_count() && lanes * a.c.B < lines) lanes *= 2;
-  const long long pieces = static_cast<long long>(a.c.B) * a.H * (DC / 4 / (kJoin / lanes));
-  const long long blocks = 8LL * device_sm_count();
-  return launch_kernel(latent_join_kernel<DC, N>, dim3(static_cast<unsigned>(pieces < blocks ? pieces : blocks)), dim3(kJoin), 0, st, a, s.groups,
-                       s.per_group, lines, lanes);
+  // (sequences have about lines / B parts)
+  static_assert(kJoin >= 148, "");
+  const bool many = 4 * a.c.B <= lines && lines <= kJoin;
+  const long long rows = static_cast<long long>(a.c.B) * a.H, want = many ? rows * (DC / 64) : (rows * (DC / 4) + kJoin - 1) / kJoin;
+  const long long most_blocks = 8LL * device_sm_count();
+  return launch_kernel(many ? latent_join_kernel<DC, N, true> : latent_join_kernel<DC, N, false>,
+                       dim3(static_cast<unsigned>(want < most_blocks ? want : most_blocks)), dim3(kJoin), 0, st, a, s.groups, s.per_group, lines);
 }
 
 template <int DC>
