@@ -47,7 +47,7 @@ constexpr int kBatch = 8;                      // tiles whose pages are looked u
 constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion, two idle
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 2;                      // what the start of a sequence costs, in tiles
-constexpr int kMinShare = 4;                   // places on the line that a thread block takes at least
+constexpr int kMinShare = 1;                   // places on the line that a thread block takes at least
 constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
 constexpr float kFar = 1048576.0f;             // scores from which ref is kept in two parts, see the top
 
@@ -157,7 +157,6 @@ __device__ __forceinline__ void reduce_half(float (&v)[HN], int lane, int base, 
 __device__ __forceinline__ int tiles_of(int len, int window) {
   return len > 0 ? (len - (window_begin(len, window) & ~15) + kTok - 1) / kTok : 0;
 }
-__device__ __forceinline__ int clamped_len(const LatentArgs& a, int b) { return min(max(a.c.seq_lens[b], 0), a.c.S_cap); }
 
 // Which code a lane of TMEM has: channels `channel` .. + UNITS - 1 of every token, from byte `byte` on of its codes.
 template <int UNITS>
@@ -230,39 +229,46 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
   pdl_wait();
 
   // ---- this thread block's share of the line: [x0, x1), and the sequence it begins in
-  // (thread i looks at sequences i, i + THREADS, ...; one of so few that a round will do is looked at once)
+  // (thread i looks at sequences i, i + kThreads, ...; of so few that a round will do the lengths are kept for the warp that finds
+  // the work, in the weights' place)
   const bool one_round = a.c.B <= kThreads;
-  int cost = tid < a.c.B ? tiles_of(clamped_len(a, tid), a.window) + kFixed : 0;
-  auto scan = [&](int v) {  // over the thread block's threads: up to and with this one
+  int* const lengths = reinterpret_cast<int*>(smem + C::P);
+  auto cost_of = [&](int raw) { return tiles_of(min(max(raw, 0), a.c.S_cap), a.window) + kFixed; };
+  int cost = 0, total = 0;
+  if (tid < a.c.B) {
+    const int raw = a.c.seq_lens[tid];
+    if (one_round) lengths[tid] = raw;
+    cost = cost_of(raw);
+  }
+  auto scan = [&](int v) {  // over the thread block's threads: up to and with this one; `total` of all
+    auto up = [&](int x) {
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, v, off);
-      if (lane >= off) v += y;
-    }
+      for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+      }
+      return x;
+    };
+    v = up(v);
     __syncthreads();
     if (lane == 31) sm.sums[warp] = v;
     __syncthreads();
-    for (int i = 0; i < warp; ++i) v += sm.sums[i];
-    return v;
-  };
-  auto total = [&] {
-    int v = 0;
-    for (int i = 0; i < kWarps; ++i) v += sm.sums[i];
-    return v;
+    const int w = up(lane < kWarps ? sm.sums[lane] : 0), before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+    total = __shfl_sync(0xffffffffu, w, 31);
+    return warp > 0 ? v + before : v;
   };
   int sum = cost;
   if (!one_round)
-    for (int b = tid + kThreads; b < a.c.B; b += kThreads) sum += tiles_of(clamped_len(a, b), a.window) + kFixed;
+    for (int b = tid + kThreads; b < a.c.B; b += kThreads) sum += cost_of(a.c.seq_lens[b]);
   tc_fence_before();
   int upto = scan(sum);
   tc_fence_after();
-  const int length = total();
-  const int share = max(kMinShare, (length + lines - 1) / lines);
+  const int length = total, share = max(kMinShare, (length + lines - 1) / lines);
   const int x0 = min(line * share, length), x1 = min(x0 + share, length);
   for (int b0 = 0, p0 = 0; b0 < a.c.B && p0 <= x0; b0 += kThreads) {
     if (!one_round) {
       const int b = b0 + tid;
-      cost = b < a.c.B ? tiles_of(clamped_len(a, b), a.window) + kFixed : 0;
+      cost = b < a.c.B ? cost_of(a.c.seq_lens[b]) : 0;
       upto = scan(cost);
     }
     const int p = p0 + upto - cost;
@@ -270,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       sm.start_b = b0 + tid;
       sm.start_p = p;
     }
-    p0 += total();
+    p0 += total;
   }
   __syncthreads();
   const uint32_t tmem = sm.tmem;
@@ -643,43 +649,56 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       // TURNED: two tiles in registers in turn, so that loads have a tile's time to arrive.  (Of the others, whose 64 tokens take
       // twice the registers, the next tile's are asked for when this one's are in shared memory.)
       uint32_t even[TURNS * TOK], odd[C::TURNED ? TOK : 1];
-      ok = load(0, even);
-      if (!ok) break;
       if (bf16) {
         // queries of bf16 as fp16, each head times the power of two that brings its largest into [2^15, 2^16)
         ok = warp_wait_on(bar(C::RAW), pieces & 1, stop, kBlockWait) && warp_wait_on(bar(C::SCALED), (pieces & 1) ^ 1, stop, kBlockWait);
         if (!ok) break;
+        constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32, AT_ONCE = N / C::CONV < 4 ? N / C::CONV : 4;
 #pragma unroll 1
-        for (int h = cw; h < N; h += C::CONV) {
-          constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32;
-          uint4 v[PER];
-          uint32_t top = 0;
-          auto at = [&](int c) { return reinterpret_cast<uint4*>(smem + C::Q + (c >> 3) * C::QPANEL + h * 128 + (((c & 7) ^ (h & 7)) << 4)); };
+        for (int first = cw; first < N; first += AT_ONCE * C::CONV) {
+          uint4 v[AT_ONCE][PER];
+          uint32_t top[AT_ONCE];
+          auto at = [&](int k, int c) {
+            const int h = first + k * C::CONV;
+            return reinterpret_cast<uint4*>(smem + C::Q + (c >> 3) * C::QPANEL + h * 128 + (((c & 7) ^ (h & 7)) << 4));
+          };
 #pragma unroll
-          for (int x = 0; x < PER; ++x) {
-            const int c = lane + 32 * x;
-            v[x] = c < CHUNKS ? *at(c) : make_uint4(0, 0, 0, 0);
-            top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu)),
-                           __vmaxu2(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu));
-          }
-          top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-          const bool bad = top >= 0x7f80u;  // an infinity or a NaN: the head gives NaN
-          const float most = unpack2<TQ_BF16>(top).x;
-          const int ex = most > 0.0f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 15, -126) : 0;
-          const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-          if (lane == 0) sm.scale[h] = bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+          for (int k = 0; k < AT_ONCE; ++k) {
+            top[k] = 0;
 #pragma unroll
-          for (int x = 0; x < PER; ++x) {
-            const int c = lane + 32 * x;
-            if (c >= CHUNKS) continue;
-            const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-            uint32_t o[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float2 f = unpack2<TQ_BF16>(y[k]);
-              o[k] = bad ? 0 : pack2<TQ_FP16>(__fmul_rn(f.x, up), __fmul_rn(f.y, up));
+            for (int x = 0; x < PER; ++x) {
+              const int c = lane + 32 * x;
+              v[k][x] = c < CHUNKS ? *at(k, c) : make_uint4(0, 0, 0, 0);
             }
-            *at(c) = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+#pragma unroll
+          for (int k = 0; k < AT_ONCE; ++k) {
+#pragma unroll
+            for (int x = 0; x < PER; ++x)
+              top[k] = __vmaxu2(__vmaxu2(top[k], __vmaxu2(v[k][x].x & 0x7fff7fffu, v[k][x].y & 0x7fff7fffu)),
+                                __vmaxu2(v[k][x].z & 0x7fff7fffu, v[k][x].w & 0x7fff7fffu));
+            top[k] = __reduce_max_sync(0xffffffffu, max(top[k] & 0xffffu, top[k] >> 16));
+          }
+#pragma unroll
+          for (int k = 0; k < AT_ONCE; ++k) {
+            const bool bad = top[k] >= 0x7f80u;  // an infinity or a NaN: the head gives NaN
+            const float most = unpack2<TQ_BF16>(top[k]).x;
+            const int ex = most > 0.0f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 15, -126) : 0;
+            const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+            if (lane == 0) sm.scale[first + k * C::CONV] = bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+              const int c = lane + 32 * x;
+              if (c >= CHUNKS) continue;
+              const uint32_t y[4] = {v[k][x].x, v[k][x].y, v[k][x].z, v[k][x].w};
+              uint32_t o[4];
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
+                const float2 f = unpack2<TQ_BF16>(y[m]);
+                o[m] = bad ? 0 : pack2<TQ_FP16>(__fmul_rn(f.x, up), __fmul_rn(f.y, up));
+              }
+              *at(k, c) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
           }
         }
         fence_proxy_async_smem();
@@ -687,6 +706,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         if (lane == 0) mbar_arrive(bar(C::QUERY));
       }
       ++pieces;
+      ok = load(0, even);
+      if (!ok) break;
       if constexpr (C::TURNED) {
         rope_next();
         if (w.n > 1) ok = load(1, odd);
@@ -798,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     for (bool fresh = true; b < a.c.B && p < x1 && x0 < x1 && ok; ++b) {
       if (fresh || b - first == 32) {
         first = b;
-        known = b + lane < a.c.B ? a.c.seq_lens[b + lane] : 0;
+        known = b + lane < a.c.B ? (fresh && one_round ? lengths[b + lane] : a.c.seq_lens[b + lane]) : 0;
         fresh = false;
       }
       const int raw = __shfl_sync(0xffffffffu, known, b - first), len = min(max(raw, 0), a.c.S_cap);
@@ -829,20 +850,21 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           const long long blk = latent_block(a.c, b, min(j, last), good);
           if (!good && a.status) atomicOr(a.status, TQ_STATUS_BAD_PAGE);
           sm.pages[batch & 1][lane] = static_cast<int>(blk);
-          if (j <= last && lane < 4 * (w.n - i))
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC)), "r"(latent_block_bytes(DC)) : "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES + (batch & 1)));
-          if (i > 0) continue;
-          // the queries: heads beyond the last one are zeros, those beyond the group's are not looked at
-          ok = warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait);
-          if (!ok) break;
-          if (lane == 0) {
-            mbar_expect_tx(bar(C::RAW), C::PANELS * C::QPANEL);
-            for (int x = 0; x < DC / 64; ++x) tma_load_3d(base + C::Q + x * C::QPANEL, &maps.c, 64 * x, h0, b, bar(C::RAW));
-            tma_load_3d(base + C::Q + (DC / 64) * C::QPANEL, &maps.r, 0, h0, b, bar(C::RAW));
+          if (i == 0) {
+            // the queries: heads beyond the last one are zeros, those beyond the group's are not looked at
+            ok = warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait);
+            if (!ok) break;
+            if (lane == 0) {
+              mbar_expect_tx(bar(C::RAW), C::PANELS * C::QPANEL);
+              for (int x = 0; x < DC / 64; ++x) tma_load_3d(base + C::Q + x * C::QPANEL, &maps.c, 64 * x, h0, b, bar(C::RAW));
+              tma_load_3d(base + C::Q + (DC / 64) * C::QPANEL, &maps.r, 0, h0, b, bar(C::RAW));
+            }
+            ++pieces;
           }
-          ++pieces;
+          if (j <= last && lane < 4 * (w.n - i))
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC)), "r"(latent_block_bytes(DC)) : "memory");
         }
       }
       p += n + kFixed;
