@@ -167,8 +167,8 @@ void free_cache(PyObject* capsule) {
   for (PyObject* k : x->keep) Py_XDECREF(k);
   delete x;
 }
-// What caches have in common: seq_lens [B] and page_table [B][max_pages] or None beside the blocks, whose third last to last
-// but one sizes are [sequences or pages] ... [blocks] (`tokens` of a sequence or page).
+// What caches have in common: seq_lens [B], and page_table [B][max_pages] or None, beside the blocks, whose first size is the
+// number of sequences or pages, of `tokens` tokens each.
 template <typename S>
 void hold_cache(Cache<S>& x, const char* w, PyObject* const* a, int64_t tokens, void (*refuse_it)(const char*, const char*)) {
   const at::Tensor &blocks = THPVariable_Unpack(a[0]), &lens = THPVariable_Unpack(a[1]);

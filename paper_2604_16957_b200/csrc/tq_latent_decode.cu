@@ -3,11 +3,10 @@
 //
 // All heads of a sequence attend the same tokens, so both products have the heads as their narrow side, and the tokens and
 // channels as the wide one.  A thread block takes a group of up to N = 16, 32 or 64 heads over a run of tiles of 64 tokens:
-//     S^T = [codes | r] [qc | qr]^T     64 tokens x N heads: codes and positional part apart, a = 64 rows
+//     S^T = [codes | r] [qc | qr]^T     64 tokens x N heads; codes and positional part apart: S_c, S_r
 //     z = alpha log2 e (a / 127 S_c + s S_r),   P^T = 2^(z - ref + log2(a / 127)),   rounded to fp16
 //     O^T += codes^T P^T                d_c channels x N heads, accumulated in TMEM: d_c / 128 times N columns
-// The codes, made fp16 once (they are exact), serve both products: rows of tokens are K-major for the first and MN-major for
-// the second, in the same shared memory.  Neither the token's range nor the latent's rounding enters the products: the range
+// The codes are made fp16 once (they are exact) for both products.  Neither the token's range nor the latent's rounding enters the products: the range
 // goes into the score in fp32 and, as its logarithm, into the weight's exponent, so weights of tokens of any size share one
 // fp16 scale.  The sum of weights takes it out again (P^T times 127 / a, before rounding, in fp32).
 //
@@ -16,21 +15,32 @@
 // exceeds 2^15.5; then O^T and the sums are rescaled.  fp16 weights are rounded by 2^-11 of themselves, or by 2^-25: 2^-33
 // of the largest.
 //
-// The query of a head is multiplied by a power of two that brings its largest channel into [2^15, 2^16) and held in fp16, for
-// either input type.
+// Queries are fp16 operands for either input type: bf16 ones are multiplied by a power of two that brings the head's largest
+// channel into [2^15, 2^16).
 //
 // Roles: four or eight warps of softmax and epilogue (a thread has a token and 8 or 16 heads: S^T of 64 rows fills 16 lanes of
-// every quarter of TMEM), eight warps that turn codes into operands, one that issues the MMAs, one that finds the work, looks
+// every quarter of TMEM), eight or four that turn codes into operands, one that issues the MMAs, one that finds the work, looks
 // up pages, asks for the tiles' blocks to be brought to L2 and loads the queries.
 //
-// What bounds it is shared memory: 128 bytes a cycle for the MMAs' operands, the converted codes and everything else.  So the
-// codes go to shared memory once, as K-major rows for the scores, and from the same registers to TMEM, where their
-// transpose is the left operand of O^T: a lane there is a channel, and the thread of a lane has 4 neighbouring channels of every
-// token (d_c = 512; 2, 1 below), one for each of the four row tiles of O^T.  (With O^T's operand read from shared memory a
-// tile took 1.3 to 1.5 times as long: the operands alone were 2560 cycles of 64 heads instead of 2040.)
+// What bounds it is shared memory with L1: 128 bytes a cycle for the MMAs' operands, the converted codes, the loads and every
+// look at a barrier, and while MMAs read at that rate the rest waits.  64 tokens of 16 heads take 720 cycles of the scores'
+// operands, 640 of codes stored and about as many loaded; of 64 heads 1155 and, where O^T's operand comes from shared
+// memory too, 770.  So
+//   - up to 32 heads the codes go to shared memory as K-major rows for the scores, and from the same registers to TMEM, where
+//     their transpose is the left operand of O^T: a lane there is a channel, and the thread of a lane has UNITS neighbouring
+//     channels of every token, one for each row tile of O^T.  With 64 heads O^T takes half of TMEM and both products read
+//     the codes in shared memory (transposed codes in the one buffer that was left: 258 us instead of 216 for the
+//     ragged batch below).
+//   - no softmax thread spills or looks anything up between the scores and the weights (216 -> 181 us); block numbers are
+//     looked up two tiles ahead.  Registers go from the last four warps to the softmax warps.
+//   - 64 heads share one pass; four groups of 32 took 234 us instead of 164.
+// A tile takes 2600 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 36 us (85 MB, floor 13);
+// 32K tokens, 128 heads 39 us; 32 sequences of 2000 to 16384 tokens, 128 heads 164 us, 500 TFLOP/s; 60 of 100 to 1500, 20 heads,
+// d_c = 256 24 us; 1K tokens, 16 heads 11 us.
 //
 // Work: the tiles of all sequences lie on a line, each sequence with kFixed places for its start in front; every thread block
-// takes an equal share.  Sequences that are cut leave partial results (O^T, ref, sums) and a second kernel joins them.
+// takes an equal share (down to one tile: 1K tokens, 16 heads 11 us; with shares of four 15).  Sequences that are cut leave
+// partial results (O^T, ref, sums) and a second kernel joins them.
 #include <cuda.h>
 
 #include "tq_async.cuh"
@@ -47,7 +57,6 @@ constexpr int kBatch = 8;                      // tiles whose pages are looked u
 constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion, two idle
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 3;                      // what the start of a sequence costs, in tiles
-constexpr int kMinShare = 1;                   // places on the line that a thread block takes at least
 constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
 constexpr float kFar = 1048576.0f;             // scores from which ref is kept in two parts, see the top
 
@@ -270,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
   tc_fence_before();
   int upto = scan(sum);
   tc_fence_after();
-  const int length = total, share = max(kMinShare, (length + lines - 1) / lines);
+  const int length = total, share = max(1, (length + lines - 1) / lines);
   const int x0 = min(line * share, length), x1 = min(x0 + share, length);
   for (int b0 = 0, p0 = 0; b0 < a.c.B && p0 <= x0; b0 += kThreads) {
     if (!one_round) {
@@ -1037,10 +1046,9 @@ cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook 
     if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM)) return e;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  // no more lines than the longest possible one has shares
+  // no more lines than there can be places
   const long long longest = static_cast<long long>(a.c.B) * ((a.max_len + kTok - 1) / kTok + 1 + kFixed);
-  const long long most = (longest + kMinShare - 1) / kMinShare;
-  const int lines = most < s.lines ? static_cast<int>(most) : s.lines;
+  const int lines = longest < s.lines ? static_cast<int>(longest) : s.lines;
   QueryMaps maps;
   if (!encode_fn()) return cudaErrorNotSupported;
   if (!make_map(&maps.c, a.q_c.data, a.q_dtype, DC, a.H, a.c.B, a.q_c.row_stride, a.q_c.head_stride, N, 1) ||

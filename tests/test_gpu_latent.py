@@ -136,6 +136,29 @@ def test_append_edge_values(gpu, d_c, kind):
     _check_cache(cache, model, slots)
 
 
+@pytest.mark.parametrize("d_c,n", [(512, 20001), (128, 90007)])
+def test_append_and_gather_many(gpu, d_c, n):
+    """So many rows that a warp has two on their way; an odd number of them, scattered over the cache."""
+    tq, torch = gpu
+    rng = np.random.default_rng(n)
+    cache, _ = _cache(tq, torch, 1, d_c, 0, -(-n // 16) * 16, 0)
+    slots = rng.permutation(cache.S_cap)[:n]
+    slots[::97] = -1
+    c, r = _rows(torch, rng, n, d_c, "bf16")
+    s = torch.from_numpy(slots).cuda()
+    tq.tq_latent_append(cache, c, r, s)
+    model = L.Cache(cache.S_cap, d_c)
+    model.append(c, r, slots)
+    _check_cache(cache, model, slots)
+    co, ro = torch.empty((n, d_c), device="cuda"), torch.empty((n, 64), device="cuda")
+    tq.tq_latent_gather(cache, s, co, ro)
+    on = slots >= 0
+    want = model.values(np.where(on, slots, 0))
+    for out, ref in ((co, want[0]), (ro, want[1])):
+        ref = np.where(on[:, None], ref, 0.0)
+        assert np.all(np.abs(out.double().cpu().numpy() - ref) <= 2.0 ** -23 * np.abs(ref))
+
+
 def test_append_and_gather_refuse_bad_slots(gpu):
     tq, torch = gpu
     cache, _ = _cache(tq, torch, 2, 256, 0, 32, 0)
