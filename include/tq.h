@@ -624,8 +624,9 @@ int tq_latent_gather(const tq_latent_cache* cache /* host */, const int64_t* slo
  * out_h = sum_t p_ht c_t,  p_h = softmax_t(attn_scale (qc_h . c_t + qr_h . r_t)),  one query token per sequence over its
  * cached tokens [max(0, seq_lens[b] - window), seq_lens[b]) (window = 0: all of them), all heads on the same tokens.
  *   q_c, q_r    : fp16 or bf16 (q_dtype): rows are sequences; d_c channels a head (the query multiplied by the head's key
- *                 expansion) and 64.  A head whose query holds an infinity or a NaN gives NaN, and only that head.  bf16 queries
- *                 keep their digits but for channels below 2^-32 of the head's largest (of both parts), off by 2^-40 of it.
+ *                 expansion) and 64.  A head whose query holds an infinity or a NaN gives NaN, and only that head.  Up to 16
+ *                 heads, q_c is held to 2^-26 of the head's largest channel; more heads keep fp16 queries as they are, and bf16
+ *                 ones but for channels below 2^-32 of the head's largest (of both parts), off by 2^-40 of it.
  *   H           : query heads, 1 .. 1024
  *   max_seq_len : 0, or an upper bound on the lengths that the host knows; it only limits the launch
  *   workspace   : tq_latent_workspace_bytes(B, H, d_c) bytes or more, 16-byte aligned, contents destroyed.  Calls that may

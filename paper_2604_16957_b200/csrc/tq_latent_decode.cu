@@ -6,9 +6,9 @@
 //     S^T = [codes | r] [qc | qr]^T     64 tokens x N heads; codes and positional part apart: S_c, S_r
 //     z = alpha log2 e (a / 127 S_c + s S_r),   P^T = 2^(z - ref + log2(a / 127)),   rounded to fp16
 //     O^T += codes^T P^T                d_c channels x N heads, accumulated in TMEM: d_c / 128 times N columns
-// The codes are made fp16 once (they are exact) for both products.  Neither the token's range nor the latent's rounding enters the products: the range
-// goes into the score in fp32 and, as its logarithm, into the weight's exponent, so weights of tokens of any size share one
-// fp16 scale.  The sum of weights takes it out again (P^T times 127 / a, before rounding, in fp32).
+// The codes are made fp16 once (they are exact) for both products (BYTES: for O^T).  Neither the token's range nor the latent's
+// rounding enters the products: the range goes into the score in fp32 and, as its logarithm, into the weight's exponent, so
+// weights of tokens of any size share one fp16 scale.  The sum of weights takes it out again (P^T times 127 / a, before rounding, in fp32).
 //
 // ref is per head, in two parts that add up to ref: a score (subtracted first, which is exact where it matters: equal scores of
 // any size give equal weights) and an offset.  It is set so that the largest weight of the first tile is 2^8, and raised when one
@@ -17,24 +17,31 @@
 //
 // Queries are fp16 operands for either input type: bf16 ones are multiplied by a power of two that brings the head's largest
 // channel into [2^15, 2^16).
+// Up to 16 heads (BYTES) the scores take the codes as they are, unsigned bytes c + 128, and the queries as four signed digits to
+// the base 128, 64 columns for 16 heads: whole numbers, exact but for the query's rounding by 2^-26 of the largest of a head's
+// d_c.  The codes' offset is taken out again as 128 times the sum of the digits.
 //
 // Roles: four or eight warps of softmax and epilogue (a thread has a token and 8 or 16 heads: S^T of 64 rows fills 16 lanes of
 // every quarter of TMEM), eight or four that turn codes into operands, one that issues the MMAs, one that finds the work, looks
-// up pages, asks for the tiles' blocks to be brought to L2 and loads the queries.
+// up pages, asks for the tiles' blocks to be brought to L2 and loads the queries (BYTES: loads the tiles); up to 32 heads two
+// more that make tokens' factors of their scales.
 //
 // What bounds it is shared memory with L1: 128 bytes a cycle for the MMAs' operands, the converted codes, the loads and every
-// look at a barrier, and while MMAs read at that rate the rest waits.  64 tokens of 16 heads take 720 cycles of the scores'
+// look at a barrier, and while MMAs read at that rate the rest waits.  64 tokens of 32 heads take 790 cycles of the scores'
 // operands, 640 of codes stored and about as many loaded; of 64 heads 1155 and, where O^T's operand comes from shared
 // memory too, 770.  So
-//   - up to 32 heads the codes go to shared memory as K-major rows for the scores, and from the same registers to TMEM, where
-//     their transpose is the left operand of O^T: a lane there is a channel, and the thread of a lane has UNITS neighbouring
-//     channels of every token, one for each row tile of O^T.  With 64 heads O^T takes half of TMEM and both products read
+//   - up to 16 heads codes come by TMA and are not stored a second time: 600 cycles of the scores' operands, 320 to write a
+//     tile and 256 to read it for O^T (128K tokens, 16 heads 36 -> 33 us).
+//   - up to 32 heads the codes go to shared memory as K-major rows for the scores (BYTES: they are there), and from registers
+//     to TMEM, where their transpose is the left operand of O^T: a lane there is a channel, and the thread of a lane has UNITS
+//     neighbouring channels of every token, one for each row tile of O^T.  With 64 heads O^T takes half of TMEM and both products read
 //     the codes in shared memory (transposed codes in the one buffer that was left: 258 us instead of 216 for the
 //     ragged batch below).
 //   - no softmax thread spills or looks anything up between the scores and the weights (216 -> 181 us); block numbers are
-//     looked up two tiles ahead.  Registers go from the last four warps to the softmax warps.
+//     looked up two tiles ahead; up to 32 heads other warps divide and take logarithms (33 -> 31 us).  Registers go from the
+//     last four warps to the softmax warps.
 //   - 64 heads share one pass; four groups of 32 took 234 us instead of 164.
-// A tile takes 2600 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 36 us (85 MB, floor 13);
+// A tile takes 2100 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 31 us (85 MB, floor 13);
 // 32K tokens, 128 heads 39 us; 32 sequences of 2000 to 16384 tokens, 128 heads 164 us, 500 TFLOP/s; 60 of 100 to 1500, 20 heads,
 // d_c = 256 24 us; 1K tokens, 16 heads 11 us.
 //
@@ -54,10 +61,12 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 64;                       // tokens of a tile
 constexpr int kBatch = 8;                      // tiles whose pages are looked up together: a lane per block
-constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion, two idle
+constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 3;                      // what the start of a sequence costs, in tiles
 constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
+constexpr int kFactorWarp = 14, kSlots = 4;    // two warps that make tokens' factors, tiles of them in shared memory (TURNED)
+constexpr int kDigits = 4;                     // of a query, to the base 128: 26 bits and a sign
 constexpr float kFar = 1048576.0f;             // scores from which ref is kept in two parts, see the top
 
 // A part: [N][DC] sums, then [N] scores and offsets of ref, and [N] sums of weights.
@@ -73,17 +82,19 @@ struct Cfg {
   static constexpr int HN = N / (SOFT / 2);            // heads of a softmax thread
   static constexpr int UNITS = DC / 128;               // row tiles of O^T (TURNED: and channels of a lane)
   static constexpr int PARTS = TURNED ? 1 : UNITS + 1; // that a tile's shared memory is given back in
-  static constexpr int PANELS = DC / 64 + 1;           // 64 channels each; the last one is the positional part
+  static constexpr bool BYTES = N == 16;               // scores from the codes as they are, queries in kDigits digits
+  static constexpr int PANELS = (BYTES ? UNITS : DC / 64) + 1;  // rows of 128 bytes each; the last one is the positional part
   static constexpr int TILE = PANELS * kPanel;
-  static constexpr int QPANEL = N * 128;
-  static constexpr int Q = 0, P = Q + PANELS * QPANEL, RING = P + kPanel;
-  static constexpr int SMALL_BYTES = 3072;
+  static constexpr int QPANEL = (BYTES ? kDigits : 1) * N * 128;
+  static constexpr int Q = 0, Q_POS = Q + (PANELS - 1) * QPANEL, P = Q_POS + N * 128, RING = (P + kPanel + 1023) & ~1023;
+  static constexpr int SN = (BYTES ? kDigits + 1 : 2) * N;  // columns of a buffer of scores; the last N are the positional part's
+  static constexpr int SMALL_BYTES = TURNED ? 8192 : 3072;
   static constexpr int FIT = (232448 - SMALL_BYTES - RING) / TILE;
-  static constexpr int NB = FIT < 3 ? FIT : 3;         // tiles in shared memory
+  static constexpr int MOST = BYTES ? 4 : 3, NB = FIT < MOST ? FIT : MOST;  // tiles in shared memory
   static constexpr int SMALL = RING + NB * TILE;
   static constexpr int SMEM = SMALL + SMALL_BYTES;
   // TMEM: O^T, two buffers of scores in two parts, two of transposed codes (two tokens a column)
-  static constexpr int O_COL = 0, S_COL = UNITS * N, V_COL = S_COL + 4 * N;
+  static constexpr int O_COL = 0, S_COL = UNITS * N, V_COL = S_COL + 2 * SN;
   static constexpr int NEED = V_COL + (TURNED ? 64 * UNITS : 0), COLS = NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512);
   static_assert(NB >= 2 && SMEM <= 232448 && NEED <= 512, "");
   // mbarriers
@@ -92,7 +103,8 @@ struct Cfg {
   static constexpr int VALUES = READ + 2, VALUES_FREE = VALUES + 2;             // transposed codes
   static constexpr int WEIGHTS = VALUES_FREE + 2, DONE = WEIGHTS + 1, DRAINED = DONE + 1;  // P^T; O^T += of a tile; O^T has been read
   static constexpr int RAW = DRAINED + 1, QUERY = RAW + 1, QUERY_FREE = QUERY + 1, SCALED = QUERY_FREE + 1;  // queries as they are, as operands; their scales read
-  static constexpr int WORK = SCALED + 1, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
+  static constexpr int FACTORS = SCALED + 1, FACTORS_FREE = FACTORS + kSlots;
+  static constexpr int WORK = FACTORS_FREE + kSlots, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
                        BARS = END + 1;
 };
 
@@ -103,8 +115,10 @@ struct Work {
 
 template <int DC, int N>
 struct Small {
-  float ref_z[N], ref_o[N], scale[N], tmp[N], red[4][N];
+  float ref_z[N], ref_o[N], scale[N], scale_r[Cfg<DC, N>::BYTES ? N : 1], tmp[N], red[4][N];
+  int bias[kDigits][Cfg<DC, N>::BYTES ? N : 1];
   int pages[2][4 * kBatch];
+  float4 factors[Cfg<DC, N>::TURNED ? kSlots : 1][Cfg<DC, N>::TURNED ? kTok : 1];
   Work work[2];
   uint64_t bars[Cfg<DC, N>::BARS];
   int sums[kWarps], start_b, start_p, far, stop;
@@ -192,12 +206,24 @@ __device__ __forceinline__ uint32_t load_once(const uint8_t* p) {
   return v;
 }
 
-struct QueryMaps {
+// BYTES: the cache's codes and positional parts; otherwise the queries' two parts
+struct LatentMaps {
   CUtensorMap c, r;
 };
 
+// What a token's scales are used as: {a / 127, s, log2(a / 127), 127 / a}; {0, 0, -inf, 0} of one that is not seen.
+// (One without a range has codes of 0 and counts as the smallest: 2^-64 / 127, about 2^-71.)
+__device__ __forceinline__ float4 token_factors(float2 sc, bool seen) {
+  const float unit = sc.x > 0.0f ? __fdiv_rn(sc.x, 127.0f) : 0.0f;
+  const float lg = sc.x > 0.0f ? __log2f(unit) : -71.0f, inv = sc.x > 0.0f ? __fdiv_rn(127.0f, sc.x) : 2.3611832414348226e21f;
+  return seen ? make_float4(unit, sc.y, lg, inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+}
+__device__ __forceinline__ float2 token_scales(const uint8_t* blocks, int blk, int d_c, int t) {
+  return *reinterpret_cast<const float2*>(blocks + static_cast<long long>(blk) * latent_block_bytes(d_c) + latent_scale_offset(d_c, t & 15));
+}
+
 template <int DC, int N, bool TEST>
-__global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_constant__ QueryMaps maps, const LatentArgs a, int groups,
+__global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_constant__ LatentMaps maps, const LatentArgs a, int groups,
                                                                         int per_group, const Hook hook) {
   using C = Cfg<DC, N>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -215,18 +241,22 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
   if (warp == kMmaWarp) tmem_alloc(smem_addr(&sm.tmem), C::COLS);
   if (tid == 0) {
     for (int i = 0; i < C::NB; ++i) {
-      mbar_init(bar(C::FULL + i), C::CONV);
-      for (int k = 0; k < C::PARTS; ++k) mbar_init(bar(C::EMPTY + i * C::PARTS + k), 1);
+      mbar_init(bar(C::FULL + i), C::BYTES ? 1 : C::CONV);
+      for (int k = 0; k < C::PARTS; ++k) mbar_init(bar(C::EMPTY + i * C::PARTS + k), C::BYTES ? C::CONV + 1 : 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(C::SCORES + i), 1);
+      mbar_init(bar(C::SCORES + i), C::TURNED ? 2 : 1);
       mbar_init(bar(C::READ + i), C::SOFT);
       mbar_init(bar(C::VALUES + i), C::CONV);
       mbar_init(bar(C::VALUES_FREE + i), 1);
       mbar_init(bar(C::WORK + i), 1);
-      mbar_init(bar(C::WORK_FREE + i), 13);
+      mbar_init(bar(C::WORK_FREE + i), C::TURNED ? 15 : 13);
       mbar_init(bar(C::PAGES + i), 1);
-      mbar_init(bar(C::PAGES_FREE + i), 12);
+      mbar_init(bar(C::PAGES_FREE + i), C::BYTES ? 2 : (C::TURNED ? C::CONV + 2 : 12));
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(bar(C::FACTORS + i), 2);
+      mbar_init(bar(C::FACTORS_FREE + i), C::SOFT);
     }
     mbar_init(bar(C::WEIGHTS), C::SOFT);
     mbar_init(bar(C::DONE), 1);
@@ -335,15 +365,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     for (int it = 0;; ++it) {
       const bool got = next_work(it, w, live);
       if (any_of_group<32 * C::SOFT>(!got) || !w.more) break;
-      float l[C::HN], ref[C::HN], scale[C::HN];
+      float l[C::HN], ref[C::HN], scale[C::HN], scale_r[C::BYTES ? C::HN : 1];
       bool far = false;
+      int bias[C::BYTES ? kDigits : 1][C::HN];
 #pragma unroll
       for (int i = 0; i < C::HN; ++i) {
         l[i] = 0.0f;
         scale[i] = a.attn_scale * kLog2e;
       }
-      // Scales of this thread's token are asked for a tile ahead, their block is looked up two tiles ahead: while MMAs read
-      // shared memory a look-up takes about as long as they do, and nothing here may wait for one.
+      // Factors of this thread's token.  TURNED: another warp's, announced with the scores.  Otherwise scales are asked for a tile
+      // ahead, their block is looked up two tiles ahead: while MMAs read shared memory a look-up takes about as long as they do,
+      // and nothing here may wait for one.
+      float4 own;
       auto block = [&](int i) {
         if (i % kBatch == 0) wait(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1);
         const int blk = sm.pages[batch & 1][4 * (i % kBatch) + wq];
@@ -354,39 +387,64 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         }
         return live ? blk : 0;
       };
-      auto scales = [&](int blk) {
-        return *reinterpret_cast<const float2*>(a.c.blocks + static_cast<long long>(blk) * latent_block_bytes(DC) + latent_scale_offset(DC, row & 15));
-      };
-      float2 next = w.n > 0 ? scales(block(0)) : make_float2(0.0f, 0.0f);
-      int after = w.n > 1 ? block(1) : 0;
+      float2 next;
+      int after = 0;
+      if constexpr (!C::TURNED) {
+        if (w.n > 0) next = token_scales(a.c.blocks, block(0), DC, row);
+        if (w.n > 1) after = block(1);
+      }
       for (int i = 0; i < w.n; ++i, ++tile) {
-        const float2 sc = next;
-        if (i + 1 < w.n) next = scales(after);
-        if (i + 2 < w.n) after = block(i + 2);
-        const int at = w.t0 + kTok * i + row;
-        const bool seen = at >= w.lo && at < w.len;
-        // (a token without a range has codes of 0 and counts as the smallest: 2^-64 / 127, about 2^-71)
-        const float unit = seen ? (sc.x > 0.0f ? __fdiv_rn(sc.x, 127.0f) : 0.0f) : 0.0f, pos = seen ? sc.y : 0.0f;
-        const float lg = seen ? (sc.x > 0.0f ? __log2f(unit) : -71.0f) : -INFINITY;
-        const float inv = seen ? (sc.x > 0.0f ? __fdiv_rn(127.0f, sc.x) : 2.3611832414348226e21f) : 0.0f;
+        if constexpr (!C::TURNED) {
+          const int at = w.t0 + kTok * i + row;
+          own = token_factors(next, at >= w.lo && at < w.len);
+          if (i + 1 < w.n) next = token_scales(a.c.blocks, after, DC, row);
+          if (i + 2 < w.n) after = block(i + 2);
+        }
         const int buf = tile % 2;
-        const uint32_t s_at = tmem + quarter + C::S_COL + buf * 2 * N + column0;
-        if (i == 0 && bf16) {
+        const uint32_t s_at = tmem + quarter + C::S_COL + buf * C::SN + column0;
+        if (i == 0 && (bf16 || C::BYTES)) {
           wait(bar(C::QUERY), pieces & 1);
 #pragma unroll
-          for (int x = 0; x < C::HN; ++x) scale[x] = sm.scale[hbase + x];
+          for (int x = 0; x < C::HN; ++x) {
+            scale[x] = sm.scale[hbase + x];
+            if constexpr (C::BYTES) {
+              scale_r[x] = sm.scale_r[hbase + x];
+#pragma unroll
+              for (int d = 0; d < kDigits; ++d) bias[d][x] = sm.bias[d][hbase + x];
+            }
+          }
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::SCALED));
         }
         wait(bar(C::SCORES + buf), (tile / 2) & 1);
         tc_fence_after();
         float z[C::HN], e[C::HN];
-        tmem_ld_halves<C::HN>(s_at, reinterpret_cast<uint32_t*>(z));
-        tmem_ld_halves<C::HN>(s_at + N, reinterpret_cast<uint32_t*>(e));
-        tmem_wait_ld();
+        tmem_ld_halves<C::HN>(s_at + C::SN - N, reinterpret_cast<uint32_t*>(e));
+        if constexpr (C::TURNED) own = sm.factors[tile % kSlots][row];
+        if constexpr (C::BYTES) {
+          uint32_t d[kDigits][C::HN];
+          tmem_ld_halves<kDigits * C::HN>(s_at, d[0]);
+          tmem_wait_ld();
+          // whole numbers of 22 bits, without what the codes' offset of 128 adds: exact in fp32 (1.5 2^23 + x), and put together
+#pragma unroll
+          for (int x = 0; x < C::HN; ++x) {
+            auto digit = [&](int k) { return __uint_as_float(d[k][x] + static_cast<uint32_t>(bias[k][x])) - 12582912.0f; };
+            z[x] = digit(kDigits - 1);
+#pragma unroll
+            for (int k = kDigits - 2; k >= 0; --k) z[x] = fmaf(z[x], 128.0f, digit(k));
+          }
+        } else {
+          tmem_ld_halves<C::HN>(s_at, reinterpret_cast<uint32_t*>(z));
+          tmem_wait_ld();
+        }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::READ + buf));
+        if (lane == 0) {
+          mbar_arrive(bar(C::READ + buf));
+          if (C::TURNED) mbar_arrive(bar(C::FACTORS_FREE + tile % kSlots));
+        }
+        const float unit = own.x, pos = own.y, lg = own.z, inv = own.w;
+        const bool seen = lg > -INFINITY;
         if (__any_sync(0xffffffffu, !seen)) {
           // (rows that no token was appended to may hold anything)
 #pragma unroll
@@ -398,8 +456,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         const uint64_t unit2 = pair(unit, unit), pos2 = pair(pos, pos), lg2 = pair(lg, lg), inv2 = pair(inv, inv);
 #pragma unroll
         for (int x = 0; x < C::HN; x += 2) {
-          const uint64_t y = fma2(pair(z[x], z[x + 1]), unit2, mul2(pair(e[x], e[x + 1]), pos2));
-          const float2 v = unpair(mul2(y, pair(scale[x], scale[x + 1])));
+          const uint64_t sum_r = mul2(pair(e[x], e[x + 1]), pos2), by = pair(scale[x], scale[x + 1]);
+          float2 v;
+          if constexpr (C::BYTES) v = unpair(fma2(mul2(pair(z[x], z[x + 1]), unit2), by, mul2(sum_r, pair(scale_r[x], scale_r[x + 1]))));
+          else v = unpair(mul2(fma2(pair(z[x], z[x + 1]), unit2, sum_r), by));
           z[x] = v.x;
           z[x + 1] = v.y;
         }
@@ -660,8 +720,127 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       if (lane == 0) mbar_arrive(bar(C::VALUES + buf));
       return true;
     };
+    // BYTES: the queries of sequence b as digits, t = round(2^(25 - E) q) = sum_k 128^k t_k with the largest magnitude in
+    // [2^E, 2^(E + 1)) (|t| < 2^26, -64 <= t_k < 64), in the order of the codes' bytes; their sums, times the codes' offset; and the
+    // positional part as fp16 numbers, times a power of two of its own.  Digits of HN heads stand together, as a thread reads them.
+    auto digits = [&](int b, auto type) {
+      constexpr int T = decltype(type)::value;
+      constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32, HEADS = N / C::CONV;
+      uint4 v[HEADS][PER];
+#pragma unroll
+      for (int k = 0; k < HEADS; ++k) {
+        const int h = cw + k * C::CONV;
+        const uint16_t* qc = static_cast<const uint16_t*>(a.q_c.data) + b * a.q_c.row_stride + (h0 + h) * a.q_c.head_stride;
+        const uint16_t* qr = static_cast<const uint16_t*>(a.q_r.data) + b * a.q_r.row_stride + (h0 + h) * a.q_r.head_stride;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int c = lane + 32 * x;
+          v[k][x] = make_uint4(0, 0, 0, 0);
+          if (h < heads && c < CHUNKS) v[k][x] = *reinterpret_cast<const uint4*>(c < DC / 8 ? qc + 8 * c : qr + 8 * c - DC);
+        }
+      }
+      if (!warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait)) return false;
+      if (!warp_wait_on(bar(C::SCALED), (pieces & 1) ^ 1, stop, kBlockWait)) return false;
+#pragma unroll
+      for (int k = 0; k < HEADS; ++k) {
+        const int h = cw + k * C::CONV;
+        uint32_t top = 0, top_r = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const uint32_t most = __vmaxu2(__vmaxu2(v[k][x].x & 0x7fff7fffu, v[k][x].y & 0x7fff7fffu),
+                                         __vmaxu2(v[k][x].z & 0x7fff7fffu, v[k][x].w & 0x7fff7fffu));
+          if (lane + 32 * x < DC / 8) top = __vmaxu2(top, most);
+          else top_r = __vmaxu2(top_r, most);
+        }
+        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+        top_r = __reduce_max_sync(0xffffffffu, max(top_r & 0xffffu, top_r >> 16));
+        const bool bad = max(top, top_r) >= (T == TQ_BF16 ? 0x7f80u : 0x7c00u);  // an infinity or a NaN: the head gives NaN
+        auto exponent = [&](uint32_t most) {  // (of 2^-100 at least)
+          const float f = unpack2<T>(most).x;
+          return f > 0.0f && !bad ? max(static_cast<int>(__float_as_uint(f) >> 23) - 127, -100) : 0;
+        };
+        auto power = [](int x) { return __uint_as_float(static_cast<uint32_t>(127 + x) << 23); };
+        const int ex = exponent(top), ex_r = exponent(top_r);
+        if (lane == 0) {
+          const float factor = bad ? __uint_as_float(0x7fc00000u) : a.attn_scale * kLog2e;
+          sm.scale[h] = h >= heads ? 0.0f : factor * power(ex - 15);  // (2^10 of it are in the tokens' factors)
+          sm.scale_r[h] = h >= heads ? 0.0f : factor * power(ex_r - 15);
+        }
+        const float up = power(25 - ex), up_r = power(15 - ex_r);
+        int sums[kDigits] = {};
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int c = lane + 32 * x;
+          if (c >= CHUNKS) continue;
+          const uint32_t y[4] = {v[k][x].x, v[k][x].y, v[k][x].z, v[k][x].w};
+          const bool pos = c >= DC / 8;
+          const float by = pos ? up_r : up;
+          float f[8];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const float2 g = unpack2<T>(y[m]);
+            f[2 * m] = g.x * by;
+            f[2 * m + 1] = g.y * by;
+          }
+          if (pos) {
+            *reinterpret_cast<uint4*>(smem + C::Q_POS + h * 128 + (((c - DC / 8) ^ (h & 7)) << 4)) =
+                make_uint4(pack2<TQ_FP16>(f[0], f[1]), pack2<TQ_FP16>(f[2], f[3]), pack2<TQ_FP16>(f[4], f[5]), pack2<TQ_FP16>(f[6], f[7]));
+            continue;
+          }
+          // t + 64 (1 + 128 + 128^2 + 128^3) has the digits + 64 as its own: 7 bits each, spread to bytes, 64 taken off again
+          uint32_t w[8], word[kDigits][2];
+#pragma unroll
+          for (int m = 0; m < 8; ++m) {
+            const uint32_t u = static_cast<uint32_t>(__float2int_rn(f[m])) + 0x08102040u;
+            const uint32_t two = (u & 0x3fffu) | ((u << 2) & 0x3fff0000u), four = (two & 0x007f007fu) | ((two << 1) & 0x7f007f00u);
+            w[m] = (four + 0x40404040u) ^ 0x80808080u;
+          }
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const uint32_t lo0 = __byte_perm(w[4 * m], w[4 * m + 1], 0x5140), lo1 = __byte_perm(w[4 * m + 2], w[4 * m + 3], 0x5140);
+            const uint32_t hi0 = __byte_perm(w[4 * m], w[4 * m + 1], 0x7362), hi1 = __byte_perm(w[4 * m + 2], w[4 * m + 3], 0x7362);
+            word[0][m] = __byte_perm(lo0, lo1, 0x5410);
+            word[1][m] = __byte_perm(lo0, lo1, 0x7632);
+            word[2][m] = __byte_perm(hi0, hi1, 0x5410);
+            word[3][m] = __byte_perm(hi0, hi1, 0x7632);
+          }
+          // channels 8 c ..: 128 channels c / 16, piece c % 8, half c % 16 / 8
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d) {
+            const int row = (h / C::HN * kDigits + d) * C::HN + h % C::HN;
+            sums[d] = __dp4a(static_cast<int>(word[d][1]), 0x01010101, __dp4a(static_cast<int>(word[d][0]), 0x01010101, sums[d]));
+            *reinterpret_cast<uint2*>(smem + C::Q + (c >> 4) * C::QPANEL + row * 128 + (((c & 7) ^ (row & 7)) << 4) + (c & 8)) = make_uint2(word[d][0], word[d][1]);
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < kDigits; ++d) {
+          const int sum = __reduce_add_sync(0xffffffffu, sums[d]);
+          if (lane == 0) sm.bias[d][h] = 0x4b400000 - 128 * sum;  // (with the bits of 1.5 2^23)
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::QUERY));
+      return true;
+    };
     for (int it = 0; ok && next_work(it, w, true) && w.more; ++it) {
       if (w.n == 0) continue;
+      if constexpr (C::BYTES) {
+        ok = bf16 ? digits(w.b, std::integral_constant<int, TQ_BF16>{}) : digits(w.b, std::integral_constant<int, TQ_FP16>{});
+        for (int i = 0; i < w.n && ok; ++i, ++tile) {
+          const int buf = tile % C::NB;
+          ok = warp_wait_on(bar(C::FULL + buf), (tile / C::NB) & 1, stop, tile_wait);
+          if (!ok) break;
+          uint32_t code[TOK];
+          const uint32_t from = base + C::RING + buf * C::TILE + own.unit * kPanel + set * (TOK * 128) + 16 * own.piece + 8 * own.half + 4 * own.low;
+#pragma unroll
+          for (int y = 0; y < TOK; ++y) asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(code[y]) : "r"((from ^ ((y & 7) << 4)) + y * 128) : "memory");
+          ok = values(tile, code);
+          if (lane == 0) mbar_arrive(bar(C::EMPTY + buf));
+        }
+        ++pieces;
+        continue;
+      }
       // TURNED: two tiles in registers in turn, so that loads have a tile's time to arrive.  (Of the others, whose 64 tokens take
       // twice the registers, the next tile's are asked for when this one's are in shared memory.)
       uint32_t even[TURNS * TOK], odd[C::TURNED ? TOK : 1];
@@ -758,16 +937,22 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     auto scores = [&](uint32_t x, bool last) {
       const uint32_t buf = x % C::NB, sbuf = x % 2;
       ok = warp_wait_on(bar(C::FULL + buf), (x / C::NB) & 1, stop, tile_wait) && warp_wait_on(bar(C::READ + sbuf), ((x / 2) & 1) ^ 1, stop, tile_wait);
+      if (C::TURNED && ok) ok = warp_wait_on(bar(C::FACTORS + x % kSlots), (x / kSlots) & 1, stop, tile_wait);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t d = uniform(tm + C::S_COL + sbuf * 2 * N), k = uniform(k_lo + ((buf * C::TILE) >> 4));
+      const uint32_t d = uniform(tm + C::S_COL + sbuf * C::SN), k = uniform(k_lo + ((buf * C::TILE) >> 4));
+      constexpr int STEPS = (C::PANELS - 1) * 4;  // of 32 bytes
 #pragma unroll
-      for (int y = 0; y < DC / 16; ++y)
-        mma_ss(leader, d, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > 0);
+      for (int y = 0; y < STEPS; ++y) {
+        const uint32_t ka = k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), qa = q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4);
+        if constexpr (C::BYTES) mma_ss_bytes(leader, d, ka, qa, kDescHi, instr_desc_bytes(kTok, kDigits * N), y > 0);
+        else mma_ss(leader, d, ka, qa, kDescHi, id_s, y > 0);
+      }
 #pragma unroll
-      for (int y = DC / 16; y < (DC + kRope) / 16; ++y)
-        mma_ss(leader, d + N, k + (((y >> 2) * kPanel + (y & 3) * 32) >> 4), q_lo + (((y >> 2) * C::QPANEL + (y & 3) * 32) >> 4), kDescHi, id_s, y > DC / 16);
+      for (int y = 0; y < kRope / 16; ++y)
+        mma_ss(leader, d + C::SN - N, k + (((C::PANELS - 1) * kPanel + y * 32) >> 4), q_lo + ((C::Q_POS - C::Q + y * 32) >> 4), kDescHi, id_s, y > 0);
       mma_commit(leader, bar(C::SCORES + sbuf));
+      if (C::TURNED && leader) mbar_arrive(bar(C::SCORES + sbuf));  // (the tokens' factors)
       mma_commit(leader, bar(C::EMPTY + buf * C::PARTS + C::PARTS - 1));
       if (last) mma_commit(leader, bar(C::QUERY_FREE));
     };
@@ -804,7 +989,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       const int n = uniform(w.n);
       if (!uniform(w.more)) break;
       if (n == 0) continue;
-      ok = warp_wait_on(bar(bf16 ? C::QUERY : C::RAW), pieces & 1, stop, kBlockWait);
+      ok = warp_wait_on(bar(bf16 || C::BYTES ? C::QUERY : C::RAW), pieces & 1, stop, kBlockWait);
       // The scores of the next tile go before the outputs of this one, whose weights are made meanwhile.
       for (int i = 0; i < n && ok; ++i) {
         scores(tile + i, i + 1 == n);
@@ -822,7 +1007,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     int2* const info = static_cast<int2*>(a.workspace);
     int b = sm.start_b, p = sm.start_p, it = 0, known = 0, first = b;  // lane i holds the length of sequence first + i
     bool ok = true;
-    uint32_t batch = 0, pieces = 0;
+    uint32_t batch = 0, pieces = 0, tile = 0;
     auto post = [&](const Work& w) {
       ok = warp_wait_on(bar(C::WORK_FREE + (it & 1)), ((it >> 1) & 1) ^ 1, stop, kBlockWait);
       if (!ok) return;
@@ -868,6 +1053,24 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           sm.pages[batch & 1][lane] = static_cast<int>(blk);
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES + (batch & 1)));
+          if constexpr (C::BYTES) {
+            // (the softmax warps ask for the scales themselves)
+            if (j <= last && lane < 4 * (w.n - i))
+              asm volatile("prefetch.global.L2 [%0];\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC) + latent_scale_offset(DC, 0)) : "memory");
+            // the tiles' values: a lane per block of 16 tokens and 128 channels, or positional part
+            for (int x = 0; x < kBatch && i + x < w.n && ok; ++x, ++tile) {
+              const int buf = tile % C::NB;
+              ok = warp_wait_on(bar(C::EMPTY + buf), ((tile / C::NB) & 1) ^ 1, stop, kBlockWait);
+              const int from = __shfl_sync(0xffffffffu, static_cast<int>(blk), 4 * x + (lane & 3)), unit = lane >> 2;
+              if (!ok) break;
+              if (lane == 0) mbar_expect_tx(bar(C::FULL + buf), C::TILE + (TEST && static_cast<int>(tile) == hook.fault_tile ? 16 : 0));
+              __syncwarp();
+              const uint32_t to = base + C::RING + buf * C::TILE + unit * kPanel + (lane & 3) * 2048;
+              if (unit < C::UNITS) tma_load_4d(to, &maps.c, 0, 0, unit, from, bar(C::FULL + buf));
+              else if (unit == C::UNITS) tma_load_3d(to, &maps.r, 0, 0, from, bar(C::FULL + buf));
+            }
+            continue;
+          }
           if (i == 0) {
             // the queries: heads beyond the last one are zeros, those beyond the group's are not looked at
             ok = warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait);
@@ -888,6 +1091,42 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     if (ok) post(Work{});
     // loads on their way land before the block ends (whoever waits for them may have given up)
     if (pieces > 0) wait_stage_inline(bar(C::RAW), (pieces - 1) & 1, kMaxWaitCycles);
+    for (uint32_t x = 0; C::BYTES && x < C::NB && x < tile; ++x) {
+      const uint32_t n = tile - 1 - x;
+      wait_stage_inline(bar(C::FULL + n % C::NB), (n / C::NB) & 1, kMaxWaitCycles);
+    }
+  } else if (C::TURNED) {
+    // ============================================================================================ factors of tokens
+    const int row = 32 * (warp - kFactorWarp) + lane;
+    bool ok = true;
+    uint32_t tile = 0, batch = 0;
+    Work w;
+    for (int it = 0; ok && next_work(it, w, true) && w.more; ++it) {
+      auto scales = [&](int i) {
+        if (i % kBatch == 0) ok = ok && warp_wait_on(bar(C::PAGES + (batch & 1)), (batch >> 1) & 1, stop, kBlockWait);
+        if (!ok) return make_float2(0.0f, 0.0f);
+        const int blk = sm.pages[batch & 1][4 * (i % kBatch) + (row >> 4)];
+        if (i % kBatch == kBatch - 1 || i == w.n - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::PAGES_FREE + (batch & 1)));
+          ++batch;
+        }
+        return token_scales(a.c.blocks, blk, DC, row);
+      };
+      float2 next = w.n > 0 ? scales(0) : make_float2(0.0f, 0.0f);
+      for (int i = 0; i < w.n && ok; ++i, ++tile) {
+        const float2 sc = next;
+        if (i + 1 < w.n) next = scales(i + 1);
+        const int at = w.t0 + kTok * i + row, slot = tile % kSlots;
+        float4 f = token_factors(sc, at >= w.lo && at < w.len);
+        if (C::BYTES) f.x *= 9.765625e-4f;  // 2^-10, see digits
+        ok = ok && warp_wait_on(bar(C::FACTORS_FREE + slot), ((tile / kSlots) & 1) ^ 1, stop, kBlockWait);
+        if (!ok) break;
+        sm.factors[slot][row] = f;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::FACTORS + slot));
+      }
+    }
   }
 
   __syncwarp();
@@ -1030,6 +1269,19 @@ Shape shape_of(int H) {
   return s;
 }
 
+// The cache's blocks: codes as [blocks][128 channels][token][128 bytes], positional parts as [blocks][token][64].
+bool make_cache_maps(LatentMaps* maps, const tq_latent_cache& c) {
+  const cuuint64_t bytes = static_cast<cuuint64_t>(latent_block_bytes(c.d_c)), blocks = static_cast<cuuint64_t>(latent_slots(c) / 16);
+  const cuuint64_t dims[4] = {128, 16, static_cast<cuuint64_t>(c.d_c / 128), blocks}, strides[3] = {static_cast<cuuint64_t>(c.d_c), 128, bytes};
+  const cuuint64_t rope_dims[3] = {kRope, 16, blocks}, rope_strides[2] = {2 * kRope, bytes};
+  const cuuint32_t box[4] = {128, 16, 1, 1}, rope_box[3] = {kRope, 16, 1}, ones[4] = {1, 1, 1, 1};
+  return encode_fn()(&maps->c, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c.blocks, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
+         encode_fn()(&maps->r, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, c.blocks + latent_rope_offset(c.d_c, 0), rope_dims, rope_strides, rope_box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DC, int N, bool TEST = false>
 cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook hook = {}) {
   using C = Cfg<DC, N>;
@@ -1049,11 +1301,12 @@ cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook 
   // no more lines than there can be places
   const long long longest = static_cast<long long>(a.c.B) * ((a.max_len + kTok - 1) / kTok + 1 + kFixed);
   const int lines = longest < s.lines ? static_cast<int>(longest) : s.lines;
-  QueryMaps maps;
+  LatentMaps maps;
   if (!encode_fn()) return cudaErrorNotSupported;
-  if (!make_map(&maps.c, a.q_c.data, a.q_dtype, DC, a.H, a.c.B, a.q_c.row_stride, a.q_c.head_stride, N, 1) ||
-      !make_map(&maps.r, a.q_r.data, a.q_dtype, kRope, a.H, a.c.B, a.q_r.row_stride, a.q_r.head_stride, N, 1))
-    return cudaErrorInvalidValue;
+  const bool made = C::BYTES ? make_cache_maps(&maps, a.c)
+                             : make_map(&maps.c, a.q_c.data, a.q_dtype, DC, a.H, a.c.B, a.q_c.row_stride, a.q_c.head_stride, N, 1) &&
+                                   make_map(&maps.r, a.q_r.data, a.q_dtype, kRope, a.H, a.c.B, a.q_r.row_stride, a.q_r.head_stride, N, 1);
+  if (!made) return cudaErrorInvalidValue;
   if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, maps, a, s.groups, s.per_group, hook))
     return e;
   if (lines == 1) return cudaSuccess;  // nothing is cut

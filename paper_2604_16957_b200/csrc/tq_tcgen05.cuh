@@ -17,6 +17,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+               : "memory");
+}
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];\n" ::"l"(map), "r"(x), "r"(y), "r"(z),
                "r"(src)
@@ -145,6 +150,10 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, int m, int n, bool 
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((mn_major_b ? 1u : 0u) << 16) |
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
+// kind::i8, both operands K-major: A of unsigned bytes, B of signed ones
+__host__ __device__ constexpr uint32_t instr_desc_bytes(int m, int n) {
+  return (2u << 4) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
 constexpr uint32_t kNegateA = 1u << 13;
 constexpr uint32_t kMnMajorA = 1u << 15;  // rows of A run along K
 
@@ -162,6 +171,14 @@ __device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a_l
   asm volatile(
       "{\n.reg .pred p, q;\n.reg .b64 x, y;\nsetp.ne.u32 p, %5, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\n"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add)), "r"(leader)
+      : "memory");
+}
+// the same for bytes (kind::i8, 32-bit whole numbers; see instr_desc_bytes)
+__device__ __forceinline__ void mma_ss_bytes(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p, q;\n.reg .b64 x, y;\nsetp.ne.u32 p, %5, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::i8 [%0], x, y, %4, p;\n}\n" ::"r"(d),
       "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(static_cast<uint32_t>(add)), "r"(leader)
       : "memory");
 }
