@@ -41,7 +41,7 @@
 //     looked up two tiles ahead; up to 32 heads other warps divide and take logarithms (33 -> 31 us).  Registers go from the
 //     last four warps to the softmax warps.
 //   - 64 heads share one pass; four groups of 32 took 234 us instead of 164.
-// A tile takes 2100 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 31 us (85 MB, floor 13);
+// A tile takes 2000 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 31 us (85 MB, floor 13);
 // 32K tokens, 128 heads 39 us; 32 sequences of 2000 to 16384 tokens, 128 heads 164 us, 500 TFLOP/s; 60 of 100 to 1500, 20 heads,
 // d_c = 256 24 us; 1K tokens, 16 heads 11 us.
 //
@@ -934,12 +934,19 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     const uint32_t q_lo = desc_lo(base + C::Q, 0), p_lo = desc_lo(base + C::P, 0), k_lo = desc_lo(base + C::RING, 0);
     bool ok = true;
     uint32_t tile = 0, pieces = 0;
+    // for the scores of tile x (TURNED: its tokens' factors, too), and for the outputs of tile y, the first of its piece or not
+    auto can_score = [&](uint32_t x) {
+      if (C::TURNED && !warp_wait_on(bar(C::FACTORS + x % kSlots), (x / kSlots) & 1, stop, tile_wait)) return false;
+      return warp_wait_on(bar(C::FULL + x % C::NB), (x / C::NB) & 1, stop, tile_wait) && warp_wait_on(bar(C::READ + x % 2), ((x / 2) & 1) ^ 1, stop, tile_wait);
+    };
+    auto can_output = [&](uint32_t y, bool first) {
+      if (C::TURNED && !warp_wait_on(bar(C::VALUES + y % 2), (y / 2) & 1, stop, tile_wait)) return false;
+      if (first && !warp_wait_on(bar(C::DRAINED), (pieces & 1) ^ 1, stop, tile_wait)) return false;
+      return warp_wait_on(bar(C::WEIGHTS), y & 1, stop, tile_wait);
+    };
     auto scores = [&](uint32_t x, bool last) {
-      const uint32_t buf = x % C::NB, sbuf = x % 2;
-      ok = warp_wait_on(bar(C::FULL + buf), (x / C::NB) & 1, stop, tile_wait) && warp_wait_on(bar(C::READ + sbuf), ((x / 2) & 1) ^ 1, stop, tile_wait);
-      if (C::TURNED && ok) ok = warp_wait_on(bar(C::FACTORS + x % kSlots), (x / kSlots) & 1, stop, tile_wait);
-      if (!ok) return;
       tc_fence_after();
+      const uint32_t buf = x % C::NB, sbuf = x % 2;
       const uint32_t d = uniform(tm + C::S_COL + sbuf * C::SN), k = uniform(k_lo + ((buf * C::TILE) >> 4));
       constexpr int STEPS = (C::PANELS - 1) * 4;  // of 32 bytes
 #pragma unroll
@@ -957,12 +964,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       if (last) mma_commit(leader, bar(C::QUERY_FREE));
     };
     auto outputs = [&](uint32_t x, bool first) {
-      const uint32_t vbuf = x % 2, buf = x % C::NB;
-      if (C::TURNED) ok = warp_wait_on(bar(C::VALUES + vbuf), (x / 2) & 1, stop, tile_wait);
-      ok = ok && warp_wait_on(bar(C::WEIGHTS), x & 1, stop, tile_wait);
-      if (ok && first) ok = warp_wait_on(bar(C::DRAINED), (pieces & 1) ^ 1, stop, tile_wait);
-      if (!ok) return;
       tc_fence_after();
+      const uint32_t vbuf = x % 2, buf = x % C::NB;
       const uint32_t add = uniform(!first);
       if constexpr (C::TURNED) {
         const uint32_t v = uniform(tm + C::V_COL + vbuf * 32 * C::UNITS);
@@ -990,12 +993,33 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
       if (!uniform(w.more)) break;
       if (n == 0) continue;
       ok = warp_wait_on(bar(bf16 || C::BYTES ? C::QUERY : C::RAW), pieces & 1, stop, kBlockWait);
-      // The scores of the next tile go before the outputs of this one, whose weights are made meanwhile.
-      for (int i = 0; i < n && ok; ++i) {
-        scores(tile + i, i + 1 == n);
-        if (i > 0 && ok) outputs(tile + i - 1, i == 1);
+      if constexpr (C::TURNED) {
+        // Scores are two tiles ahead, issued behind the outputs: while they read shared memory nobody else does much, so all
+        // barriers are looked at before.
+        for (int i = 0; i < 2 && i < n && ok; ++i) {
+          ok = can_score(tile + i);
+          if (ok) scores(tile + i, i + 1 == n);
+        }
+        for (int i = 0; i < n && ok; ++i) {
+          const bool more = i + 2 < n;
+          ok = (!more || can_score(tile + i + 2)) && can_output(tile + i, i == 0);
+          if (!ok) break;
+          outputs(tile + i, i == 0);
+          if (more) scores(tile + i + 2, i + 3 == n);
+        }
+      } else {
+        // The scores of the next tile go before the outputs of this one, whose weights are made meanwhile.
+        for (int i = 0; i <= n && ok; ++i) {
+          if (i < n) {
+            ok = can_score(tile + i);
+            if (ok) scores(tile + i, i + 1 == n);
+          }
+          if (i > 0 && ok) {
+            ok = can_output(tile + i - 1, i == 1);
+            if (ok) outputs(tile + i - 1, i == 1);
+          }
+        }
       }
-      if (ok) outputs(tile + n - 1, n == 1);
       tile += n;
       ++pieces;
     }
