@@ -726,29 +726,31 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
     auto digits = [&](int b, auto type) {
       constexpr int T = decltype(type)::value;
       constexpr int CHUNKS = (DC + kRope) / 8, PER = (CHUNKS + 31) / 32, HEADS = N / C::CONV;
-      uint4 v[HEADS][PER];
-#pragma unroll
-      for (int k = 0; k < HEADS; ++k) {
-        const int h = cw + k * C::CONV;
+      uint4 v[PER], following[PER];
+      auto load = [&](int h) {
         const uint16_t* qc = static_cast<const uint16_t*>(a.q_c.data) + b * a.q_c.row_stride + (h0 + h) * a.q_c.head_stride;
         const uint16_t* qr = static_cast<const uint16_t*>(a.q_r.data) + b * a.q_r.row_stride + (h0 + h) * a.q_r.head_stride;
 #pragma unroll
         for (int x = 0; x < PER; ++x) {
           const int c = lane + 32 * x;
-          v[k][x] = make_uint4(0, 0, 0, 0);
-          if (h < heads && c < CHUNKS) v[k][x] = *reinterpret_cast<const uint4*>(c < DC / 8 ? qc + 8 * c : qr + 8 * c - DC);
+          following[x] = make_uint4(0, 0, 0, 0);
+          if (h < heads && c < CHUNKS) following[x] = *reinterpret_cast<const uint4*>(c < DC / 8 ? qc + 8 * c : qr + 8 * c - DC);
         }
-      }
+      };
+      load(cw);
       if (!warp_wait_on(bar(C::QUERY_FREE), (pieces & 1) ^ 1, stop, kBlockWait)) return false;
       if (!warp_wait_on(bar(C::SCALED), (pieces & 1) ^ 1, stop, kBlockWait)) return false;
-#pragma unroll
+#pragma unroll 1  // (code that is met for the first time takes longer than what it does)
       for (int k = 0; k < HEADS; ++k) {
         const int h = cw + k * C::CONV;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) v[x] = following[x];
+        if (k + 1 < HEADS) load(h + C::CONV);
         uint32_t top = 0, top_r = 0;
 #pragma unroll
         for (int x = 0; x < PER; ++x) {
-          const uint32_t most = __vmaxu2(__vmaxu2(v[k][x].x & 0x7fff7fffu, v[k][x].y & 0x7fff7fffu),
-                                         __vmaxu2(v[k][x].z & 0x7fff7fffu, v[k][x].w & 0x7fff7fffu));
+          const uint32_t most = __vmaxu2(__vmaxu2(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu),
+                                         __vmaxu2(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu));
           if (lane + 32 * x < DC / 8) top = __vmaxu2(top, most);
           else top_r = __vmaxu2(top_r, most);
         }
@@ -772,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         for (int x = 0; x < PER; ++x) {
           const int c = lane + 32 * x;
           if (c >= CHUNKS) continue;
-          const uint32_t y[4] = {v[k][x].x, v[k][x].y, v[k][x].z, v[k][x].w};
+          const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
           const bool pos = c >= DC / 8;
           const float by = pos ? up_r : up;
           float f[8];
