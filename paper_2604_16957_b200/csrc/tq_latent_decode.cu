@@ -43,11 +43,11 @@
 //   - 64 heads share one pass; four groups of 32 took 234 us instead of 164.
 // A tile takes 2000 cycles with 16 heads and 4200 with 64.  Measured (B200, graphs): 128K tokens, 16 heads 31 us (85 MB, floor 13);
 // 32K tokens, 128 heads 39 us; 32 sequences of 2000 to 16384 tokens, 128 heads 164 us, 500 TFLOP/s; 60 of 100 to 1500, 20 heads,
-// d_c = 256 24 us; 1K tokens, 16 heads 11 us.
+// d_c = 256 24 us; 1K tokens, 16 heads 12 us.
 //
 // Work: the tiles of all sequences lie on a line, each sequence with kFixed places for its start in front; every thread block
-// takes an equal share (down to one tile: 1K tokens, 16 heads 11 us; with shares of four 15).  Sequences that are cut leave
-// partial results (O^T, ref, sums) and a second kernel joins them.
+// takes an equal share (down to one tile: calls on 1K tokens, 16 heads 11.6 us; with shares of four 15).  Sequences that are
+// cut leave partial results (O^T, ref, sums) and a second kernel joins them.
 #include <cuda.h>
 
 #include "tq_async.cuh"
@@ -103,7 +103,7 @@ struct Cfg {
   static constexpr int VALUES = READ + 2, VALUES_FREE = VALUES + 2;             // transposed codes
   static constexpr int WEIGHTS = VALUES_FREE + 2, DONE = WEIGHTS + 1, DRAINED = DONE + 1;  // P^T; O^T += of a tile; O^T has been read
   static constexpr int RAW = DRAINED + 1, QUERY = RAW + 1, QUERY_FREE = QUERY + 1, SCALED = QUERY_FREE + 1;  // queries as they are, as operands; their scales read
-  static constexpr int FACTORS = SCALED + 1, FACTORS_FREE = FACTORS + kSlots;
+  static constexpr int FACTORS = SCALED + 1, FACTORS_FREE = FACTORS + kSlots;  // of a tile's tokens: made, read
   static constexpr int WORK = FACTORS_FREE + kSlots, WORK_FREE = WORK + 2, PAGES = WORK_FREE + 2, PAGES_FREE = PAGES + 2, END = PAGES_FREE + 2,
                        BARS = END + 1;
 };

@@ -399,6 +399,54 @@ def test_latent_decode_of_scores_far_from_zero(gpu, n, H, size):
     assert torch.all((out[0].double().cpu() - c.mean(0)).abs() <= tol)
 
 
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("n,H,d_c", [(70, 16, 512), (3000, 16, 256), (500, 9, 128), (3000, 20, 512)])
+def test_latent_decode_of_queries_at_the_limits(gpu, n, H, d_c, kind):
+    """Heads whose channels are all as large as the largest, of either sign; whose two parts, or whose channels, differ by
+    2^10; with one channel, or none; over rows of which all channels are as large.  Queries times 2^8 with a scale times
+    2^-8 give the same bits."""
+    tq, torch = gpu
+    top = 2.0 - 2 * torch.finfo(_types(torch)[kind]).eps
+    rng = np.random.default_rng(n + H)
+    x = rng.standard_normal((n, d_c + 64))
+    x[0, :d_c], x[1, :d_c], x[2, :d_c] = 1.0, -1.0, np.where(np.arange(d_c) % 2, 1.0, -1.0)
+    x[:, 0] = 0.0
+    x = torch.from_numpy(x).to(_types(torch)[kind]).cuda()
+    cache, table = _cache(tq, torch, 1, d_c, 16, -(-n // 16) * 16, 3)
+    slots = R.slots_of([0], [n], table, 16, cache.S_cap)
+    tq.tq_latent_append(cache, x[:, :d_c], x[:, d_c:], torch.from_numpy(slots).cuda())
+    cache.seq_lens.fill_(n)
+    model = L.Cache(cache.blocks.numel() // (d_c + 136), d_c)
+    model.append(x[:, :d_c], x[:, d_c:], slots)
+    c, r = model.values(slots)
+    q_c, q_r = torch.from_numpy(rng.standard_normal((1, H, d_c))), torch.from_numpy(rng.standard_normal((1, H, 64)))
+    q_c[0, 0], q_c[0, 1] = top, -top
+    q_c[0, 2] = torch.tensor([top, -top]).repeat(d_c // 2)
+    q_r[0, 0], q_r[0, 1] = top, -top
+    q_r[0, 3] *= 2.0 ** -10
+    q_c[0, 4] *= 2.0 ** -10
+    q_c[0, 5] = 0.0
+    q_c[0, 5, 7] = top
+    q_c[0, 6] *= 2.0 ** -10                                        # (the largest channel meets zeros)
+    q_c[0, 6, 0] = top
+    q_r[0, 6] *= 2.0 ** -10
+    q_c[0, 7], q_c[0, 8], q_r[0, 8] = 0.0, 0.0, 0.0
+    q_c, q_r = q_c.to(_types(torch)[kind]).cuda(), q_r.to(_types(torch)[kind]).cuda()
+    work = tq.alloc_latent_workspace(1, H, d_c)
+    out, same = torch.empty((1, H, d_c), device="cuda"), torch.empty((1, H, d_c), device="cuda")
+    for alpha, rows in (((d_c + 64) ** -0.5, range(H)), (64.0, [6])):
+        tq.tq_sdpa_latent_decode(cache, q_c, q_r, alpha, 0, 0, work, out)
+        tq.tq_sdpa_latent_decode(cache, q_c * 256, q_r * 256, alpha / 256, 0, 0, work, same)
+        assert torch.equal(out, same)
+        for h in rows:
+            ref, weighed, p, mag = L.attention(q_c[0, h:h + 1].double().cpu(), q_r[0, h:h + 1].double().cpu(), c, r, alpha)
+            # a score is off by the query's rounding, 2^-26 of its largest channel; twice that, numerator and denominator
+            delta = alpha * 2.0 ** -26 * float(q_c[0, h].abs().max()) * float(np.abs(c).sum(1).max())
+            tol = L.bound(ref, weighed, p, mag, n, d_c, c, 0.0) + weighed * 2.0 * np.expm1(delta)
+            err = (out[0, h:h + 1].double().cpu() - ref).abs()
+            assert torch.all(err <= tol), (h, alpha, float((err / tol).max()))
+
+
 def test_latent_decode_status_bits(gpu):
     tq, torch = gpu
     cache, values = _filled(tq, torch, [64, 64], 256, 16, "fp16", 8)
