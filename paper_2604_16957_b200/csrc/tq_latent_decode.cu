@@ -9,9 +9,13 @@
 // The codes are made fp16 once (they are exact) for both products (BYTES: for O^T).  Neither the token's range nor the latent's
 // rounding enters the products: the range goes into the score in fp32 and, as its logarithm, into the weight's exponent, so
 // weights of tokens of any size share one fp16 scale.  The sum of weights takes it out again (P^T times 127 / a, before rounding, in fp32).
+// Ranges may lie 2^128 apart (2^64 to 2^-64, zeros among the smallest): a token of small range has no part in O^T beside a large
+// one, but all of its weight in the sum.  So the exponentials are made 2^48 times as large (they are normal numbers in fp32
+// down to 2^-174 then, where the weight is less than 2^-53 of the head's largest), which P^T loses again before it is rounded and the sum in
+// 127 / a; and where sums are rescaled or joined their factor, down to 2^-128, is taken in two halves.
 //
 // ref is per head, in two parts that add up to ref: a score (subtracted first, which is exact where it matters: equal scores of
-// any size give equal weights) and an offset.  It is set so that the largest weight of the first tile is 2^8, and raised when one
+// any size give equal weights) and an offset, less 48.  It is set so that the largest weight of the first tile is 2^8, and raised when one
 // exceeds 2^15.5; then O^T and the sums are rescaled.  fp16 weights are rounded by 2^-11 of themselves, or by 2^-25: 2^-33
 // of the largest.
 //
@@ -64,7 +68,8 @@ constexpr int kBatch = 8;                      // tiles whose pages are looked u
 constexpr int kWarps = 16, kThreads = 32 * kWarps, kMmaWarp = 12, kFeedWarp = 13;  // 12 of softmax and conversion
 constexpr int kPanel = kTok * 128;             // bytes of 64 tokens x 64 channels
 constexpr int kFixed = 3;                      // what the start of a sequence costs, in tiles
-constexpr float kTop = 8.0f, kMost = 15.5f;    // log2 of the largest weight when ref is set; when it is raised
+// log2 of the largest exponential when ref is set; when it is raised.  Weights are 2^-48 of them (see the top).
+constexpr float kTop = 8.0f + 48.0f, kMost = 15.5f + 48.0f, kDown = 1.0f / 281474976710656.0f;
 constexpr int kFactorWarp = 14, kSlots = 4;    // two warps that make tokens' factors, tiles of them in shared memory (TURNED)
 constexpr int kDigits = 4;                     // of a query, to the base 128: 26 bits and a sign
 constexpr float kFar = 1048576.0f;             // scores from which ref is kept in two parts, see the top
@@ -211,11 +216,11 @@ struct LatentMaps {
   CUtensorMap c, r;
 };
 
-// What a token's scales are used as: {a / 127, s, log2(a / 127), 127 / a}; {0, 0, -inf, 0} of one that is not seen.
+// What a token's scales are used as: {a / 127, s, log2(a / 127), 2^-48 127 / a}; {0, 0, -inf, 0} of one that is not seen.
 // (One without a range has codes of 0 and counts as the smallest: 2^-64 / 127, about 2^-71.)
 __device__ __forceinline__ float4 token_factors(float2 sc, bool seen) {
   const float unit = sc.x > 0.0f ? __fdiv_rn(sc.x, 127.0f) : 0.0f;
-  const float lg = sc.x > 0.0f ? __log2f(unit) : -71.0f, inv = sc.x > 0.0f ? __fdiv_rn(127.0f, sc.x) : 2.3611832414348226e21f;
+  const float lg = sc.x > 0.0f ? __log2f(unit) : -71.0f, inv = sc.x > 0.0f ? __fdiv_rn(127.0f * kDown, sc.x) : 2.3611832414348226e21f * kDown;
   return seen ? make_float4(unit, sc.y, lg, inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
 }
 __device__ __forceinline__ float2 token_scales(const uint8_t* blocks, int blk, int d_c, int t) {
@@ -496,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
             const float new_o = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid])) - kTop;
             const float up = (new_z - sm.ref_z[tid]) + (new_o - sm.ref_o[tid]);
             const bool take = i == 0 || up > kMost - kTop;  // (by itself: no head's result depends on another's)
-            sm.tmp[tid] = take ? ex2(-up) : 1.0f;
+            sm.tmp[tid] = take ? ex2(-0.5f * up) : 1.0f;  // (half of it: sums may need a factor of 2^-128)
             if (take) {
               const bool apart = fabsf(new_z) > kFar;
               sm.ref_z[tid] = apart ? new_z : new_z + new_o;
@@ -510,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           for (int x = 0; x < C::HN; ++x) ref[x] = sm.ref_z[hbase + x];
           if (i > 0) {
 #pragma unroll
-            for (int x = 0; x < C::HN; ++x) l[x] *= sm.tmp[hbase + x];
+            for (int x = 0; x < C::HN; ++x) l[x] = l[x] * sm.tmp[hbase + x] * sm.tmp[hbase + x];
             wait(bar(C::DONE), (tile - 1) & 1);
             tc_fence_after();
 #pragma unroll 1
@@ -519,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
               tmem_ld16(tmem + quarter + C::O_COL + x, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * sm.tmp[(x + y) % N]);
+              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * sm.tmp[(x + y) % N] * sm.tmp[(x + y) % N]);
               tmem_st16(tmem + quarter + C::O_COL + x, o);
             }
             tmem_wait_st();
@@ -534,7 +539,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           const float2 s = unpair(fma2(pair(e0, e1), inv2, pair(l[x], l[x + 1])));
           l[x] = s.x;
           l[x + 1] = s.y;
-          p[x >> 1] = pack2<TQ_FP16>(e0, e1);
+          const float2 weight = unpair(mul2(pair(e0, e1), pair(kDown, kDown)));
+          p[x >> 1] = pack2<TQ_FP16>(weight.x, weight.y);
         }
         if (!__all_sync(0xffffffffu, free)) wait(bar(C::DONE), (tile - 1) & 1);
 #pragma unroll
@@ -1163,7 +1169,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
   if (tid == 0 && sm.stop && a.status) atomicOr(a.status, TQ_STATUS_TIMEOUT);
 }
 
-// ---- joining: out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^(ref_i - max ref)
+// ---- joining: out = sum_i f_i^2 O_i / sum_i f_i^2 l_i,  f_i = 2^((ref_i - max ref) / 2): halves, as sums are largest where ref is smallest
 // Outputs are on their way before the refs have been looked at.  MANY parts (few sequences): a thread block has 64 channels of a
 // head, 16 threads to a column of four; a thread looks at one part's ref, and the f_i go through shared memory.  Few parts: a
 // thread has four channels of a head and every part, and 16 threads look at the refs for themselves.
@@ -1229,9 +1235,9 @@ __global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, 
       };
       const float most = block_max(z, s_max[0]);
       const float rest = mine ? (z - most) + o : -INFINITY;
-      const float f = ex2(rest - block_max(rest, s_max[1]));
-      float total = mine ? f * sums : 0.0f;
-      if (mine) s_f[tid] = f;
+      const float f = ex2(0.5f * (rest - block_max(rest, s_max[1])));
+      float total = mine ? f * sums * f : 0.0f;
+      if (mine) s_f[tid] = f * f;
 #pragma unroll
       for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
       if (lane == 0) s_l[warp] = total;
@@ -1261,18 +1267,18 @@ __global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, 
       for (int i = lane & 15; i < in.y; i += 16) o = fmaxf(o, (score(i) - z) + offset(i));
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) o = fmaxf(o, __shfl_xor_sync(0xffffffffu, o, off));
-      auto weight = [&](int i) { return ex2(((score(i) - z) + offset(i)) - o); };
+      auto weight = [&](int i) { return ex2(0.5f * (((score(i) - z) + offset(i)) - o)); };
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
         if (k >= in.y) continue;
         const float f = weight(k);
-        l = fmaf(f, part(k)[N * DC + 2 * N + head], l);
-        add4(sum, f, first[k]);
+        l = fmaf(f * part(k)[N * DC + 2 * N + head], f, l);
+        add4(sum, f * f, first[k]);
       }
       for (int i = AHEAD; i < in.y; ++i) {
         const float f = weight(i);
-        l = fmaf(f, part(i)[N * DC + 2 * N + head], l);
-        add4(sum, f, load(i));
+        l = fmaf(f * part(i)[N * DC + 2 * N + head], f, l);
+        add4(sum, f * f, load(i));
       }
       if (in.y > 0) store_joined(a, to, sum, l);
     }
