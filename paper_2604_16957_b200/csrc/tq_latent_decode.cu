@@ -127,6 +127,7 @@ struct Small {
   Work work[2];
   uint64_t bars[Cfg<DC, N>::BARS];
   int sums[kWarps], start_b, start_p, far, stop;
+  uint32_t over[Cfg<DC, N>::SOFT];  // heads of each softmax warp whose exponentials exceed 2^kMost
   uint32_t tmem;
 };
 
@@ -483,7 +484,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
         bool raise = i == 0;
         if (i > 0) raise = exponents() > kMost;
         if (any_of_group<32 * C::SOFT>(raise)) {
-          // ref anew: the largest score, then the largest exponent beside it
+          // ref anew: the largest score, then the largest exponent beside it; but for the first tile only of heads that asked for
+          // it themselves (no head's result depends on another's)
+          if (i > 0) {
+            uint32_t over = 0;
+#pragma unroll
+            for (int x = 0; x < C::HN; ++x) over |= static_cast<uint32_t>(e[x] > kMost) << x;
+            over = __reduce_or_sync(0xffffffffu, over << (lane & 16 ? C::HN : 0));
+            if (lane == 0) sm.over[warp] = over;
+          }
           float v[C::HN];
 #pragma unroll
           for (int x = 0; x < C::HN; ++x) v[x] = seen ? z[x] : -INFINITY;
@@ -500,7 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           if (tid < N) {
             const float new_o = fmaxf(fmaxf(sm.red[0][tid], sm.red[1][tid]), fmaxf(sm.red[2][tid], sm.red[3][tid])) - kTop;
             const float up = (new_z - sm.ref_z[tid]) + (new_o - sm.ref_o[tid]);
-            const bool take = i == 0 || up > kMost - kTop;  // (by itself: no head's result depends on another's)
+            const uint32_t* const asked = sm.over + 4 * (tid / (2 * C::HN));
+            const bool take = i == 0 || ((asked[0] | asked[1] | asked[2] | asked[3]) >> (tid % (2 * C::HN)) & 1);
             sm.tmp[tid] = take ? ex2(-0.5f * up) : 1.0f;  // (half of it: sums may need a factor of 2^-128)
             if (take) {
               const bool apart = fabsf(new_z) > kFar;
