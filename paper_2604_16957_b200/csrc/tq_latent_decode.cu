@@ -54,6 +54,8 @@
 // cut leave partial results (O^T, ref, sums) and a second kernel joins them.
 #include <cuda.h>
 
+#include <algorithm>
+
 #include "tq_async.cuh"
 #include "tq_latent.cuh"
 #include "tq_tcgen05.cuh"
@@ -1180,10 +1182,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
 }
 
 // ---- joining: out = sum_i f_i^2 O_i / sum_i f_i^2 l_i,  f_i = 2^((ref_i - max ref) / 2): halves, as sums are largest where ref is smallest
-// Outputs are on their way before the refs have been looked at.  MANY parts (few sequences): a thread block has 64 channels of a
-// head, 16 threads to a column of four; a thread looks at one part's ref, and the f_i go through shared memory.  Few parts: a
-// thread has four channels of a head and every part, and 16 threads look at the refs for themselves.
-constexpr int kJoin = 256;
+// How many parts a sequence has depends on its length and on all others', which are known here only.  Every thread block lists the
+// sequences that were cut and takes its share of their rows; refs and outputs are asked for together.
+//   More than kFew parts: a thread block has 64 channels of a head, 16 threads to a column of four; a thread looks at one
+//   part's ref, and the f_i go through shared memory.
+//   Fewer: a thread has four channels of a head and every part, and a warp looks at the refs for itself.
+// Measured (whole calls in a graph): 8 sequences of 16K tokens, 32 heads, 18 parts each: 52 us in the first form, 48 in the second; 4
+// of 32K, 128 heads, 19 parts: 94 and 83; 4 of 32K, 32 heads, 37 parts (first form): 47.  One of 128K among 63 of one token, 16
+// heads: 33 us (71 when the form went by the number of sequences).
+// A single sequence (ONE) is not listed and takes the first form: 128K tokens, 16 heads 28.2 us instead of 29.8.
+constexpr int kJoin = 256, kFew = 24;
 
 __device__ __forceinline__ void store_joined(const LatentArgs& a, long long to, const float4& sum, float l) {
   const float inv = __fdiv_rn(1.0f, l);
@@ -1196,43 +1204,80 @@ __device__ __forceinline__ void add4(float4& sum, float f, const float4& v) {
   sum = make_float4(fmaf(f, v.x, sum.x), fmaf(f, v.y, sum.y), fmaf(f, v.z, sum.z), fmaf(f, v.w, sum.w));
 }
 
-template <int DC, int N, bool MANY>
-__global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines) {
-  constexpr int COLUMNS = MANY ? 16 : DC / 4, LANES = MANY ? 16 : 1, CHUNKS = DC / 4 / COLUMNS, PER = kJoin / (COLUMNS * LANES), AHEAD = MANY ? 10 : 4;
-  __shared__ float4 s_sum[MANY ? kJoin : 1];
-  __shared__ float s_f[MANY ? kJoin : 1], s_max[2][kJoin / 32], s_l[kJoin / 32];
+template <int DC, int N, bool ONE>
+__global__ void __launch_bounds__(kJoin, 4) latent_join_kernel(const LatentArgs a, int groups, int per_group, int lines) {
+  __shared__ int4 s_seq[kJoin];  // sequences that were cut: number, first line, parts; from the front those of many parts
+  __shared__ int2 s_first[kJoin];
+  __shared__ int s_many[kJoin / 32], s_few[kJoin / 32];
   pdl_launch_dependents();
-  pdl_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, own = tid / COLUMNS % LANES;
-  const float* const parts = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + info_bytes(a.c.B));
-  const int2* const info = static_cast<const int2*>(a.workspace);
-  const unsigned pieces = static_cast<unsigned>(a.c.B) * a.H * CHUNKS;
-  for (unsigned x0 = blockIdx.x * PER; x0 < pieces; x0 += gridDim.x * PER) {
-    const unsigned x = x0 + tid / (COLUMNS * LANES);
-    const bool inside = x < pieces;
-    const unsigned row = (inside ? x : 0) / CHUNKS, b = row / a.H, h = row % a.H;
-    int2 in = inside ? info[b] : make_int2(0, 0);  // first line, number of parts
-    // (the last two: what a call that gave up has left behind)
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // first line of sequence b and its number of parts; 0: it was not cut.  (The last two conditions: what a call that gave up has
+  // left behind.)
+  auto cut_of = [&](int b) {
+    int2 in = static_cast<const int2*>(a.workspace)[b];
     if (in.y < 2 || in.x < 0 || in.y > lines - in.x) in.y = 0;
-    if (MANY && in.y == 0) continue;
-    const int group = h / per_group, head = h % per_group;
-    const int column = (x % CHUNKS) * COLUMNS + tid % COLUMNS;
-    const int stride = 2 * groups * part_floats(DC, N);
-    // of part i > 0; the first one stands a place further
-    const float* const base = parts + static_cast<long long>(2 * in.x * groups + group) * part_floats(DC, N);
-    auto part = [&](int i) { return base + static_cast<long long>(i) * stride + (i == 0 ? groups * part_floats(DC, N) : 0); };
-    auto load = [&](int i) { return *reinterpret_cast<const float4*>(part(i) + head * DC + 4 * column); };
-    float4 first[AHEAD];
+    return in;
+  };
+  unsigned n_many = 0, n_few = 0;
+  int4 only;
+  if constexpr (ONE) {
+    pdl_wait();
+    const int2 in = cut_of(0);
+    n_many = in.y > 0;
+    only = make_int4(0, in.x, in.y, 0);
+  } else {
+    // at most one of those that begin in a line goes on into the next: by first line they have an order, the same in every
+    // thread block
+    s_first[tid] = make_int2(0, 0);
+    __syncthreads();
+    pdl_wait();
+    for (int b = tid; b < a.c.B; b += kJoin) {
+      const int2 in = cut_of(b);
+      if (in.y > 0) s_first[in.x] = make_int2(b, in.y);
+    }
+    __syncthreads();
+    const int2 cut = s_first[tid];
+    const unsigned many = __ballot_sync(0xffffffffu, cut.y > kFew), few = __ballot_sync(0xffffffffu, cut.y > 0 && cut.y <= kFew);
+    s_many[warp] = __popc(many);
+    s_few[warp] = __popc(few);
+    __syncthreads();
+    int many_before = 0, few_before = 0;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) first[k] = own + k * LANES < in.y ? load(own + k * LANES) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float l = 0.0f;
-    const long long to = static_cast<long long>(row) * DC + 4 * column;
-    // ref of the joined row: the largest score part, and the largest of the rest beside it
-    if constexpr (MANY) {
-      const bool mine = tid < in.y;  // (there are fewer parts than threads)
-      const float* const q = part(mine ? tid : 0) + N * DC + head;
+    for (int i = 0; i < kJoin / 32; ++i) {
+      if (i == warp) many_before = n_many, few_before = n_few;
+      n_many += s_many[i];
+      n_few += s_few[i];
+    }
+    const unsigned below = (1u << lane) - 1;
+    if (cut.y > 0)
+      s_seq[cut.y > kFew ? many_before + __popc(many & below) : kJoin - 1 - few_before - __popc(few & below)] = make_int4(cut.x, tid, cut.y, 0);
+    __syncthreads();
+  }
+
+  const float* const parts = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + info_bytes(a.c.B));
+  const int stride = 2 * groups * part_floats(DC, N);
+  // part i of head h (the first one stands a place further than the line would say)
+  auto part_of = [&](const int4& in, int h, int i) {
+    return parts + static_cast<long long>(2 * in.y * groups + h / per_group) * part_floats(DC, N) + static_cast<long long>(i) * stride +
+           (i == 0 ? groups * part_floats(DC, N) : 0);
+  };
+  {
+    constexpr int LANES = 16, WIDE = kJoin / LANES, CHUNKS = DC / 4 / WIDE, AHEAD = ONE ? 10 : 8;  // (148 parts; 8 leave registers for the rest)
+    __shared__ float4 s_sum[kJoin / 32][WIDE];
+    __shared__ float s_f[kJoin], s_max[2][kJoin / 32], s_l[kJoin / 32];
+    const int own = tid / WIDE;
+    for (unsigned x = blockIdx.x; x < n_many * a.H * CHUNKS; x += gridDim.x) {
+      const int h = ONE ? x / CHUNKS : x / CHUNKS % a.H, head = h % per_group, column = (x % CHUNKS) * WIDE + tid % WIDE;
+      const int4 in = ONE ? only : s_seq[x / CHUNKS / a.H];
+      const int n = in.z;
+      auto load = [&](int i) { return *reinterpret_cast<const float4*>(part_of(in, h, i) + head * DC + 4 * column); };
+      // ref of the joined row: the largest score part, and the largest of the rest beside it
+      const bool mine = tid < n;  // (there are fewer parts than threads)
+      const float* const q = part_of(in, h, mine ? tid : 0) + N * DC + head;
       const float z = mine ? q[0] : -INFINITY, o = mine ? q[N] : 0.0f, sums = mine ? q[2 * N] : 0.0f;
+      float4 first[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) first[k] = own + k * LANES < n ? load(own + k * LANES) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       auto block_max = [&](float v, float* s) {
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
@@ -1252,45 +1297,72 @@ __global__ void __launch_bounds__(kJoin) latent_join_kernel(const LatentArgs a, 
       for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
       if (lane == 0) s_l[warp] = total;
       __syncthreads();
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
-        if (own + k * LANES < in.y) add4(sum, s_f[own + k * LANES], first[k]);
-      for (int i = own + AHEAD * LANES; i < in.y; i += LANES) add4(sum, s_f[i], load(i));
-      s_sum[tid] = sum;
+        if (own + k * LANES < n) add4(sum, s_f[own + k * LANES], first[k]);
+      for (int i = own + AHEAD * LANES; i < n; i += LANES) add4(sum, s_f[i], load(i));
+      // a warp's threads of a column, then the warps
+#pragma unroll
+      for (int off = WIDE; off < 32; off *= 2)
+        add4(sum, 1.0f, make_float4(__shfl_xor_sync(0xffffffffu, sum.x, off), __shfl_xor_sync(0xffffffffu, sum.y, off),
+                                    __shfl_xor_sync(0xffffffffu, sum.z, off), __shfl_xor_sync(0xffffffffu, sum.w, off)));
+      if (lane < WIDE) s_sum[warp][lane] = sum;
       __syncthreads();
       if (own == 0) {
+        float l = s_l[0];
 #pragma unroll
-        for (int i = 1; i < LANES; ++i) add4(sum, 1.0f, s_sum[tid + i * COLUMNS]);
-#pragma unroll
-        for (int i = 0; i < kJoin / 32; ++i) l += s_l[i];
-        store_joined(a, to, sum, l);
+        for (int i = 1; i < kJoin / 32; ++i) {
+          add4(sum, 1.0f, s_sum[i][tid]);
+          l += s_l[i];
+        }
+        store_joined(a, (static_cast<long long>(in.x) * a.H + h) * DC + 4 * column, sum, l);
       }
       __syncthreads();
-    } else {
-      // (a warp may hold two rows or four, of 16 columns and more)
-      auto score = [&](int i) { return part(i)[N * DC + head]; };
-      auto offset = [&](int i) { return part(i)[N * DC + N + head]; };
-      float z = -INFINITY, o = -INFINITY;
-      for (int i = lane & 15; i < in.y; i += 16) z = fmaxf(z, score(i));
+    }
+  }
+  if constexpr (!ONE) {
+    constexpr int COLUMNS = DC / 4, PER = kJoin / COLUMNS, AHEAD = 4;
+    static_assert(COLUMNS % 32 == 0 && kFew <= 32, "a warp has one row, and a lane for each part");
+    const int column = tid % COLUMNS;
+    for (unsigned x = (gridDim.x - 1 - blockIdx.x) * PER + tid / COLUMNS; x < n_few * a.H; x += gridDim.x * PER) {
+      const int h = x % a.H, head = h % per_group;
+      const int4 in = s_seq[kJoin - 1 - x / a.H];
+      const int n = in.z;
+      auto load = [&](int i) { return *reinterpret_cast<const float4*>(part_of(in, h, i) + head * DC + 4 * column); };
+      const bool mine = lane < n;
+      const float* const q = part_of(in, h, mine ? lane : 0) + N * DC + head;
+      const float z = mine ? q[0] : -INFINITY, o = mine ? q[N] : 0.0f, sums = mine ? q[2 * N] : 0.0f;
+      float4 first[AHEAD];
 #pragma unroll
-      for (int off = 8; off > 0; off >>= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, off));
-      for (int i = lane & 15; i < in.y; i += 16) o = fmaxf(o, (score(i) - z) + offset(i));
+      for (int k = 0; k < AHEAD; ++k) first[k] = k < n ? load(k) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      auto warp_max = [](float v) {
 #pragma unroll
-      for (int off = 8; off > 0; off >>= 1) o = fmaxf(o, __shfl_xor_sync(0xffffffffu, o, off));
-      auto weight = [&](int i) { return ex2(0.5f * (((score(i) - z) + offset(i)) - o)); };
+        for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+        return v;
+      };
+      const float most = warp_max(z), rest = mine ? (z - most) + o : -INFINITY;
+      const float f = ex2(0.5f * (rest - warp_max(rest)));
+      float l = mine ? f * sums * f : 0.0f;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        if (k >= in.y) continue;
-        const float f = weight(k);
-        l = fmaf(f * part(k)[N * DC + 2 * N + head], f, l);
-        add4(sum, f * f, first[k]);
+        const float fk = __shfl_sync(0xffffffffu, f * f, k);
+        if (k < n) add4(sum, fk, first[k]);
       }
-      for (int i = AHEAD; i < in.y; ++i) {
-        const float f = weight(i);
-        l = fmaf(f * part(i)[N * DC + 2 * N + head], f, l);
-        add4(sum, f * f, load(i));
+      for (int i = AHEAD; i < n; i += 4) {
+        float4 next[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) next[k] = i + k < n ? load(i + k) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float fk = __shfl_sync(0xffffffffu, f * f, i + k);
+          if (i + k < n) add4(sum, fk, next[k]);
+        }
       }
-      if (in.y > 0) store_joined(a, to, sum, l);
+      store_joined(a, (static_cast<long long>(in.x) * a.H + h) * DC + 4 * column, sum, l);
     }
   }
 }
@@ -1306,7 +1378,7 @@ Shape shape_of(int H) {
   s.groups = (H + 63) / 64;
   s.per_group = (H + s.groups - 1) / s.groups;
   s.n = s.per_group <= 16 ? 16 : (s.per_group <= 32 ? 32 : 64);
-  s.lines = device_sm_count() / s.groups;
+  s.lines = std::min(device_sm_count() / s.groups, kJoin);  // (joining has a thread for each)
   if (s.lines < 1) s.lines = 1;
   return s;
 }
@@ -1352,13 +1424,12 @@ cudaError_t launch_n(const LatentArgs& a, const Shape& s, cudaStream_t st, Hook 
   if (cudaError_t e = launch_kernel(kernel, dim3(static_cast<unsigned>(lines * s.groups)), dim3(kThreads), C::SMEM, st, maps, a, s.groups, s.per_group, hook))
     return e;
   if (lines == 1) return cudaSuccess;  // nothing is cut
-  // (sequences have about lines / B parts)
-  static_assert(kJoin >= 148, "");
-  const bool many = 4 * a.c.B <= lines && lines <= kJoin;
-  const long long rows = static_cast<long long>(a.c.B) * a.H, want = many ? rows * (DC / 64) : (rows * (DC / 4) + kJoin - 1) / kJoin;
-  const long long most_blocks = 8LL * device_sm_count();
-  return launch_kernel(many ? latent_join_kernel<DC, N, true> : latent_join_kernel<DC, N, false>,
-                       dim3(static_cast<unsigned>(want < most_blocks ? want : most_blocks)), dim3(kJoin), 0, st, a, s.groups, s.per_group, lines);
+  // (lines cut lines - 1 sequences at most, and (lines - 1) / kFew into more than kFew parts)
+  const bool one = a.c.B == 1;
+  const long long cut = std::min<long long>(a.c.B, lines - 1), many = one ? 1 : std::min<long long>(cut, (lines - 1) / kFew);
+  const long long want = many * a.H * (DC / 64) + (one ? 0 : (cut * a.H * (DC / 4) + kJoin - 1) / kJoin);
+  return launch_kernel(one ? latent_join_kernel<DC, N, true> : latent_join_kernel<DC, N, false>,
+                       dim3(static_cast<unsigned>(std::min<long long>(want, (one ? 8LL : 4LL) * device_sm_count()))), dim3(kJoin), 0, st, a, s.groups, s.per_group, lines);
 }
 
 template <int DC>
