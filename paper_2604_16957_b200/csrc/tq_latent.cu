@@ -7,8 +7,9 @@
 //
 // The codes are exact roundings of the true quotients (the division by the range is that of the 8-bit cache, see
 // tq_kv8.cuh).  Bound by HBM for prompts: 74 K tokens of d_c = 512 are 133 MB each way, 20 us at the copy rate; append and gather
-// take 51 us together.  A decode step's is two dependent memory latencies.  The positional key keeps its digits: multiplied by a power of two that brings the largest magnitude into
-// [2^15, 2^16) it is exact in fp16 but for bf16 channels below 2^-32 of the largest, which are off by 2^-40 of it.
+// take 51 us together.  A decode step's is two dependent memory latencies.  The positional key keeps its digits: multiplied by
+// a power of two that brings the largest magnitude into [2^15, 2^16) it is exact in fp16 but for bf16 channels below 2^-32 of the
+// largest, which are off by 2^-40 of it.
 #include "tq_latent.cuh"
 
 namespace tq {

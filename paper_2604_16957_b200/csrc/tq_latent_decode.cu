@@ -1098,7 +1098,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_kernel(const __grid_consta
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C::PAGES + (batch & 1)));
           if constexpr (C::BYTES) {
-            // (the softmax warps ask for the scales themselves)
+            // (the tiles come by TMA; the scales are asked for by the warps that make factors of them)
             if (j <= last && lane < 4 * (w.n - i))
               asm volatile("prefetch.global.L2 [%0];\n" ::"l"(a.c.blocks + blk * latent_block_bytes(DC) + latent_scale_offset(DC, 0)) : "memory");
             // the tiles' values: a lane per block of 16 tokens and 128 channels, or positional part

@@ -85,9 +85,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
       : "memory");
 }
 
-__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
-}
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"r"(addr), TQ_W8(r, 0) : "memory");
 }
