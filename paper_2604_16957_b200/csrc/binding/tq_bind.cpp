@@ -79,23 +79,23 @@ class Call {
   }
   // packed [n][heads][d] whose heads stand side by side; returns the distance of its rows
   int64_t rows(const at::Tensor& t, const char* name, int64_t n, int64_t heads, int64_t d) {
-    if (t.dim() != 3 || t.size(0) != n || t.size(1) != heads || t.size(2) != d || t.stride(2) != 1 ||
-        (heads > 1 && t.stride(1) != d))
+    if (t.dim() != 3 || t.size(0) != n || t.size(1) != heads || t.size(2) != d ||
+        (n > 0 && (t.stride(2) != 1 || (heads > 1 && t.stride(1) != d))))
       refuse(where_, (std::string(name) + " must be [" + std::to_string(n) + "][" + std::to_string(heads) + "][" +
                       std::to_string(d) + "] with its heads side by side").c_str());
-    return n > 1 ? t.stride(0) : heads * d;  // the stride of a single row means nothing
+    return n > 1 ? t.stride(0) : heads * d;  // the stride of a single row means nothing, nor does any without rows
   }
   // [n][heads][d] with its channels side by side, rows and heads anywhere
   tq_heads heads(const at::Tensor& t, const char* name, int64_t n, int64_t heads, int64_t d) {
-    if (t.dim() != 3 || t.size(0) != n || t.size(1) != heads || t.size(2) != d || t.stride(2) != 1)
+    if (t.dim() != 3 || t.size(0) != n || t.size(1) != heads || t.size(2) != d || (n > 0 && t.stride(2) != 1))
       refuse(where_, (std::string(name) + " must be [" + std::to_string(n) + "][" + std::to_string(heads) + "][" +
                       std::to_string(d) + "] with its channels side by side").c_str());
-    // (the stride of a single row or head means nothing)
-    return {t.data_ptr(), n > 1 ? t.stride(0) : d, heads > 1 ? t.stride(1) : d};
+    // (the stride of a single row or head means nothing, nor does any without rows)
+    return {t.data_ptr(), n > 1 ? t.stride(0) : d, n > 0 && heads > 1 ? t.stride(1) : d};
   }
   // [n][d] with its channels side by side; returns the distance of its rows
   int64_t flat_rows(const at::Tensor& t, const char* name, int64_t n, int64_t d) {
-    if (t.dim() != 2 || t.size(0) != n || t.size(1) != d || t.stride(1) != 1)
+    if (t.dim() != 2 || t.size(0) != n || t.size(1) != d || (n > 0 && t.stride(1) != 1))
       refuse(where_, (std::string(name) + " must be [" + std::to_string(n) + "][" + std::to_string(d) + "] with its channels side by side").c_str());
     return n > 1 ? t.stride(0) : d;
   }

@@ -86,3 +86,21 @@ def test_a_third_tile_without_operands(gpu, lens, H, reached):
     if reached:
         tq.tq_sdpa_latent_decode(cache, q_c, q_r, 0.05, 0, 0, work, out)
     _check_decode(torch, out, q_c, q_r, values, 0.05, 0, rows=range(min(B, 6)))
+
+
+def test_tensors_without_rows_have_no_strides(gpu):
+    """What has no elements may come with any strides (those of an empty numpy array are all zero)."""
+    tq, torch = gpu
+    none = lambda *s: torch.zeros((0, *s), dtype=torch.float16, device="cuda").as_strided((0, *s), (0,) * (1 + len(s)))  # noqa: E731
+    out, at = torch.full((5, 3, 128), 7.0, dtype=torch.float16, device="cuda"), [_dev(torch, [0, n]) for n in (0, 5)]
+    q = torch.randn((5, 3, 192), device="cuda").half()
+    tq.tq_sdpa_latent_prompt(q[..., :128], q[..., 128:], none(3, 128), none(64), none(3, 128), at[1], at[0], 0.1, out)
+    assert torch.all(out == 0)
+    tq.tq_sdpa_latent_prompt(none(3, 128), none(3, 64), q[..., :128], q[:, 0, :64], q[..., :128], at[0], at[1], 0.1, out[:0])
+    out.fill_(7.0)
+    tq.tq_sdpa_prompt(q[..., :128].contiguous(), none(3, 128), none(3, 128), at[1], at[0], 0.1, out)
+    assert torch.all(out == 0)
+    slots = torch.zeros((0,), dtype=torch.int64, device="cuda")
+    tq.tq_latent_append(tq.LatentCache(1, 16, 128), none(128), none(64), slots)
+    tq.tq_kv8_append(tq.KV8Cache(1, 2, 16, 64), none(2, 64), none(2, 64), slots)
+    torch.cuda.synchronize()
